@@ -227,6 +227,16 @@ def lib() -> C.CDLL:
         l.bm_row_scatter.argtypes = [i32, vp, vp, vp, i32, i32, vp]
         for name in ("bm_cp_conversion_plan", "bm_cp_encoder_unit_size", "bm_row_gather", "bm_row_scatter"):
             getattr(l, name).restype = C.c_int
+        f32 = C.c_float
+        l.bm_embedding_forward.argtypes = [i32] * 3 + [vp, i32, vp, i32, f32, vp, i32, vp]
+        l.bm_embedding_backward_scratch_bytes.argtypes = [i32] * 2
+        l.bm_embedding_backward_scratch_bytes.restype = sz
+        l.bm_embedding_backward.argtypes = [i32] * 3 + [vp, i32, vp, i32, f32, vp, i32, vp, sz, vp]
+        l.bm_cross_entropy_scratch_bytes.argtypes = [i32] * 3
+        l.bm_cross_entropy_scratch_bytes.restype = sz
+        l.bm_cross_entropy.argtypes = [i32] * 3 + [vp, i32, vp, vp, vp, vp, i32, vp, sz, vp]
+        for name in ("bm_embedding_forward", "bm_embedding_backward", "bm_cross_entropy"):
+            getattr(l, name).restype = C.c_int
         _lib = l
     return _lib
 
@@ -472,6 +482,30 @@ def row_gather(dtype, src, rows_dev, dst, n, width, stream=None):
 def row_scatter(dtype, src, rows_dev, dst, n, width, stream=None):
     _check(lib().bm_row_scatter(dtype, _ptr(src), _ptr(rows_dev), _ptr(dst), n, width,
                                 _stream() if stream is None else stream))
+
+
+def embedding_forward(dtype, V, d, table, ld_table, ids, T, scale, y, ld_y, stream=None):
+    _check(lib().bm_embedding_forward(dtype, V, d, _ptr(table), ld_table, _ptr(ids), T, scale, _ptr(y), ld_y,
+                                      _stream() if stream is None else stream))
+
+
+def embedding_backward_scratch_bytes(T, d) -> int:
+    return lib().bm_embedding_backward_scratch_bytes(T, d)
+
+
+def embedding_backward(dtype, V, d, dy, ld_dy, ids, T, scale, dtable, ld_dtable, scratch, scratch_bytes, stream=None):
+    _check(lib().bm_embedding_backward(dtype, V, d, _ptr(dy), ld_dy, _ptr(ids), T, scale, _ptr(dtable), ld_dtable,
+                                       _ptr(scratch), scratch_bytes, _stream() if stream is None else stream))
+
+
+def cross_entropy_scratch_bytes(dtype, T, V) -> int:
+    return lib().bm_cross_entropy_scratch_bytes(dtype, T, V)
+
+
+def cross_entropy(dtype, T, V, logits, ld, labels, weight, loss, dlogits, ld_d, scratch=None, scratch_bytes=0,
+                  stream=None):
+    _check(lib().bm_cross_entropy(dtype, T, V, _ptr(logits), ld, _ptr(labels), _ptr(weight), _ptr(loss), _ptr(dlogits),
+                                  ld_d, _ptr(scratch), scratch_bytes, _stream() if stream is None else stream))
 
 
 def probe_mfma(blocks, iters, out, stream=None):

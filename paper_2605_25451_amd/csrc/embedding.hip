@@ -1,0 +1,435 @@
+// Token embeddings: the scaled lookup and the gradient of the table.
+//
+// The lookup is a copy of rows: bound by HBM (the rows written, and the distinct rows read).
+//
+// The gradient sums the rows of dy that belong to the same word.  Three launches, none of them with
+// floating-point atomics:
+//   group    the text tokens, word by word, each word's in the order of the pack.  256 workgroups, one
+//            for the ids with the same low 8 bits: words are drawn by frequency, and neighbouring ids
+//            are about equally frequent, so low bits share a pack far better than ranges of ids would.
+//            A workgroup reads all ids (they lie in L2), counts those of the buckets before its own --
+//            where its tokens go -- and collects its own; a stable counting sort by the other bits in
+//            LDS puts them into order.
+//   sum      chunks of equally many grouped rows, whatever words they are, so that a word with a tenth
+//            of the pack costs no more than as many rows of rare ones.  A word that lies inside a chunk
+//            is added to the table at once, its pieces in several chunks go to the workspace.
+//   fold     adds up the pieces of those words, in order.
+// Bound by HBM: dy once, the rows of distinct words read and written in fp32.
+#include "train.h"
+
+namespace bm {
+
+namespace {
+
+// ---- lookup ---------------------------------------------------------------------------------
+
+// lanes: threads of a row, a power of two up to 64; VEC: whole 16 bytes
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void embed_kernel(const T* __restrict__ table, long ld_table, const int32_t* __restrict__ ids,
+                                                    int n, int V, int d, float scale, T* __restrict__ y, long ld_y, int log_lanes) {
+  constexpr int W = VEC ? Elt<T>::VEC : 1;
+  const long row = ((long)blockIdx.x * 256 + threadIdx.x) >> log_lanes;
+  if (row >= n) return;
+  const int id = ids[row];
+  if (id < 0) return;
+  const bool known = id < V;
+  const T* src = table + (size_t)(known ? id : 0) * ld_table;
+  T* dst = y + (size_t)row * ld_y;
+  const int step = W << log_lanes;
+  const float nan = __builtin_nanf("");
+#pragma unroll 8
+  for (int c = (threadIdx.x & ((1 << log_lanes) - 1)) * W; c < d; c += step) {
+    if constexpr (VEC) {
+      float v[W];
+      load16(src + c, v);
+#pragma unroll
+      for (int e = 0; e < W; ++e) v[e] = known ? v[e] * scale : nan;
+      store16(dst + c, v);
+    } else {
+      dst[c] = Elt<T>::from_f(known ? Elt<T>::to_f(src[c]) * scale : nan);
+    }
+  }
+}
+
+// ---- group ----------------------------------------------------------------------------------
+
+constexpr int BUCKET_BITS = 8, BUCKETS = 1 << BUCKET_BITS;
+constexpr int DIGIT_BITS = 10, DIGITS = 1 << DIGIT_BITS;
+constexpr int GROUP_THREADS = 1024, GROUP_WAVES = GROUP_THREADS / WAVE;
+
+// a wavefront's share of n tokens, in whole 64
+__device__ inline int share(int n) { return (n + GROUP_WAVES * WAVE - 1) / (GROUP_WAVES * WAVE) * WAVE; }
+
+// word[i], pos[i]: the id and the row of the i-th grouped token; *count: how many there are
+struct Grouped { int32_t *word, *pos, *word2, *pos2, *count; };
+
+__global__ __launch_bounds__(GROUP_THREADS) void group_kernel(const int32_t* __restrict__ ids, int n, int V, int digit_passes, Grouped g) {
+  __shared__ int below[GROUP_WAVES], mine[GROUP_WAVES], wave_total[GROUP_WAVES];
+  __shared__ int counts[GROUP_WAVES][DIGITS];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int bucket = blockIdx.x;
+  // every wavefront has a contiguous range of whole 64 tokens
+  const int per = share(n);
+  const int first = min(n, wave * per), last = min(n, first + per);
+  int lower = 0, own = 0;
+#pragma unroll 8
+  for (int i = first + lane; i - lane < last; i += WAVE) {
+    const int id = i < last ? ids[min(i, n - 1)] : -1;
+    const int b = (uint32_t)id < (uint32_t)V ? id & (BUCKETS - 1) : BUCKETS;
+    lower += __popcll(__ballot(b < bucket));
+    own += __popcll(__ballot(b == bucket));
+  }
+  if (lane == 0) { below[wave] = lower; mine[wave] = own; }
+  __syncthreads();
+  int base = 0, total = 0, at = 0;
+#pragma unroll
+  for (int w = 0; w < GROUP_WAVES; ++w) {
+    base += below[w];
+    if (w == wave) at = total;
+    total += mine[w];
+  }
+  if (bucket == BUCKETS - 1 && threadIdx.x == 0) *g.count = base + total;
+  if (total == 0) return;
+  // an odd number of passes ends in the other pair of arrays: start so that the last one ends in word/pos
+  int32_t *word = (digit_passes & 1 ? g.word2 : g.word) + base, *pos = (digit_passes & 1 ? g.pos2 : g.pos) + base;
+  int32_t *word_to = (digit_passes & 1 ? g.word : g.word2) + base, *pos_to = (digit_passes & 1 ? g.pos : g.pos2) + base;
+  for (int i = first + lane; i - lane < last; i += WAVE) {
+    const int id = i < last ? ids[i] : -1;
+    const bool in = (uint32_t)id < (uint32_t)V && (id & (BUCKETS - 1)) == bucket;
+    const uint64_t m = __ballot(in);
+    if (in) {
+      const int to = at + __popcll(m & ((1ull << lane) - 1));
+      word[to] = id;
+      pos[to] = i;
+    }
+    at += __popcll(m);
+  }
+  // stable counting sorts by the bits above the bucket's, DIGIT_BITS at a time
+  const int per_own = share(total);
+  const int own_first = min(total, wave * per_own), own_last = min(total, own_first + per_own);
+  for (int pass = 0; pass < digit_passes; ++pass) {
+    const int shift = BUCKET_BITS + pass * DIGIT_BITS;
+    for (int i = threadIdx.x; i < GROUP_WAVES * DIGITS; i += GROUP_THREADS) (&counts[0][0])[i] = 0;
+    __syncthreads();                                       // (the tokens written above are visible behind it, too)
+    // the lanes with the same digit, by its bits; the first of them counts for all
+    auto same = [&](bool in, int digit) {
+      uint64_t m = __ballot(in);
+#pragma unroll
+      for (int b = 0; b < DIGIT_BITS; ++b) {
+        const uint64_t v = __ballot((digit >> b) & 1);
+        m &= (digit >> b) & 1 ? v : ~v;
+      }
+      return m;
+    };
+    for (int i = own_first + lane; i - lane < own_last; i += WAVE) {
+      const bool in = i < own_last;
+      const int digit = in ? (word[i] >> shift) & (DIGITS - 1) : 0;
+      const uint64_t m = same(in, digit);
+      if (in && (m & ((1ull << lane) - 1)) == 0) counts[wave][digit] += __popcll(m);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    __syncthreads();
+    // counts -> first places: over the digits, and within one over the wavefronts
+    static_assert(DIGITS == GROUP_THREADS, "a thread per digit");
+    int sum = 0;
+#pragma unroll
+    for (int w = 0; w < GROUP_WAVES; ++w) sum += counts[w][threadIdx.x];
+    int scan = sum;
+#pragma unroll
+    for (int off = 1; off < WAVE; off <<= 1) {
+      const int v = __shfl_up(scan, off, WAVE);
+      if (lane >= off) scan += v;
+    }
+    if (lane == 63) wave_total[wave] = scan;
+    __syncthreads();
+    int run = scan - sum;
+    for (int w = 0; w < wave; ++w) run += wave_total[w];
+#pragma unroll
+    for (int w = 0; w < GROUP_WAVES; ++w) {
+      const int c = counts[w][threadIdx.x];
+      counts[w][threadIdx.x] = run;
+      run += c;
+    }
+    __syncthreads();
+    for (int i = own_first + lane; i - lane < own_last; i += WAVE) {
+      const bool in = i < own_last;
+      const int id = in ? word[i] : 0, p = in ? pos[i] : 0;
+      const int digit = (id >> shift) & (DIGITS - 1);
+      const uint64_t m = same(in, digit);
+      const int before = __popcll(m & ((1ull << lane) - 1));
+      if (in) {
+        const int to = counts[wave][digit] + before;
+        word_to[to] = id;
+        pos_to[to] = p;
+      }
+      // the lanes of a wavefront have all read the place before the first of them moves it on
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (in && before == 0) counts[wave][digit] += __popcll(m);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    __syncthreads();
+    int32_t* t = word; word = word_to; word_to = t;
+    t = pos; pos = pos_to; pos_to = t;
+  }
+}
+
+// ---- sum and fold ---------------------------------------------------------------------------
+
+constexpr int COLS = 8;                       // of a lane
+constexpr int SLICE = COLS * WAVE;            // of a wavefront
+constexpr int AHEAD = 4;                      // rows in flight
+
+template <typename T, bool VEC>
+__device__ inline void load_cols(const T* p, int left, float (&v)[COLS]) {
+  if constexpr (VEC) {
+    constexpr int W = Elt<T>::VEC;
+#pragma unroll
+    for (int q = 0; q < COLS / W; ++q) {
+      float t[W];
+      if (q * W < left) load16(p + q * W, t);
+#pragma unroll
+      for (int e = 0; e < W; ++e) v[q * W + e] = q * W < left ? t[e] : 0.f;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) v[e] = e < left ? Elt<T>::to_f(p[e]) : 0.f;
+  }
+}
+template <bool VEC>
+__device__ inline void store_cols(float* p, int left, const float (&v)[COLS]) {
+#pragma unroll
+  for (int q = 0; q < COLS; q += 4) {
+    if constexpr (VEC) {
+      if (q < left) *reinterpret_cast<float4*>(p + q) = float4{v[q], v[q + 1], v[q + 2], v[q + 3]};
+    } else {
+#pragma unroll
+      for (int e = q; e < q + 4; ++e)
+        if (e < left) p[e] = v[e];
+    }
+  }
+}
+
+// What happens behind the last row of a word in a chunk: added to the table, or kept as a piece of a word that lies in
+// several chunks -- piece[2 c] where chunk c starts inside the word, piece[2 c + 1] where it only ends inside it.
+enum { GOES_ON = 0, ADD, HEAD, TAIL };
+
+// A wavefront: one chunk of grouped rows, one slice of columns.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void sum_kernel(const T* __restrict__ dy, long ld_dy, Grouped g, int d, int chunk, int chunks,
+                                                  int slices, float scale, float* __restrict__ dtable, long ld_dtable,
+                                                  float* __restrict__ piece, long ld_piece) {
+  const int lane = threadIdx.x & 63;
+  const long job = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = (int)(job / slices), slice = (int)(job % slices);
+  const int total = *g.count;
+  if (c >= chunks || (long)c * chunk >= total) return;
+  const int first = c * chunk, last = (int)min((long)total, (long)first + chunk);
+  const int col = slice * SLICE + lane * COLS, left = d - col;
+  bool inside = first > 0 && g.word[first - 1] == g.word[first];     // the current word began in an earlier chunk
+  float acc[COLS] = {};
+  for (int r0 = first; r0 < last; r0 += AHEAD) {
+    float v[AHEAD][COLS], old[AHEAD][COLS];
+    int word[AHEAD], then[AHEAD];
+    // what the next rows need of dy and of the table is requested together
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      const int r = r0 + a;
+      then[a] = GOES_ON;
+      if (r >= last) continue;
+      word[a] = g.word[r];
+      if (left > 0) load_cols<T, VEC>(dy + (size_t)g.pos[r] * ld_dy + col, left, v[a]);
+      const bool ends = r + 1 == total || g.word[r + 1] != word[a];
+      if (ends) then[a] = inside ? HEAD : ADD;
+      else if (r + 1 == last) then[a] = inside ? HEAD : TAIL;
+      if (ends) inside = false;
+      if (then[a] == ADD && left > 0) load_cols<float, VEC>(dtable + (size_t)word[a] * ld_dtable + col, left, old[a]);
+    }
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      if (r0 + a >= last || left <= 0) continue;
+#pragma unroll
+      for (int e = 0; e < COLS; ++e) acc[e] += v[a][e];
+      if (then[a] == GOES_ON) continue;
+      if (then[a] == ADD) {
+#pragma unroll
+        for (int e = 0; e < COLS; ++e) old[a][e] = fmaf(scale, acc[e], old[a][e]);
+        store_cols<VEC>(dtable + (size_t)word[a] * ld_dtable + col, left, old[a]);
+      } else {
+        store_cols<true>(piece + (2l * c + (then[a] == TAIL)) * ld_piece + col, COLS, acc);
+      }
+#pragma unroll
+      for (int e = 0; e < COLS; ++e) acc[e] = 0.f;
+    }
+  }
+}
+
+// A workgroup: the chunk in which a word begins that later chunks go on with, one slice of columns.  Its wavefronts share the
+// pieces of the later chunks.
+constexpr int FOLD_WAVES = 8;
+template <bool VEC>
+__global__ __launch_bounds__(FOLD_WAVES * 64) void fold_kernel(Grouped g, int d, int chunk, int chunks, int slices, float scale,
+                                                               float* __restrict__ dtable, long ld_dtable,
+                                                               const float* __restrict__ piece, long ld_piece) {
+  __shared__ float part[FOLD_WAVES][COLS][WAVE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = blockIdx.x / slices, slice = blockIdx.x % slices;
+  const int total = *g.count;
+  const long end = (long)(c + 1) * chunk;                    // first row of the next chunk
+  if (end >= total) return;
+  const int first = c * chunk, word = g.word[end - 1];
+  if (g.word[end] != word) return;
+  if (first > 0 && g.word[first - 1] == word && g.word[first] == word) return;
+  // chunks c + 1 .. c + more hold pieces: the last row of all of them but the last is followed by the same word
+  int more = 1;
+  for (;; more += WAVE) {
+    const long next = (long)(c + 1 + more + lane) * chunk;   // first row behind chunk c + more + lane
+    const bool on = next < total && g.word[next] == word;
+    const uint64_t m = ~__ballot(on);
+    if (m) { more += __ffsll((unsigned long long)m) - 1; break; }
+  }
+  const int col = slice * SLICE + lane * COLS, left = d - col;
+  const int per = (more + FOLD_WAVES - 1) / FOLD_WAVES;
+  const int from = c + 1 + wave * per, to = min(c + 1 + more, from + per);
+  float acc[COLS] = {};
+  if (left > 0) {
+    if (wave == 0) load_cols<float, true>(piece + (2l * c + 1) * ld_piece + col, COLS, acc);
+#pragma unroll 4
+    for (int k = from; k < to; ++k) {
+      float v[COLS];
+      load_cols<float, true>(piece + 2l * k * ld_piece + col, COLS, v);
+#pragma unroll
+      for (int e = 0; e < COLS; ++e) acc[e] += v[e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < COLS; ++e) part[wave][e][lane] = acc[e];
+  __syncthreads();
+  if (wave || left <= 0) return;
+#pragma unroll
+  for (int w = 1; w < FOLD_WAVES; ++w)
+#pragma unroll
+    for (int e = 0; e < COLS; ++e) acc[e] += part[w][e][lane];
+  float old[COLS];
+  float* to_row = dtable + (size_t)word * ld_dtable + col;
+  load_cols<float, VEC>(to_row, left, old);
+#pragma unroll
+  for (int e = 0; e < COLS; ++e) old[e] = fmaf(scale, acc[e], old[e]);
+  store_cols<VEC>(to_row, left, old);
+}
+
+// ---- host -------------------------------------------------------------------------------------
+
+// rows of a chunk: few tokens are cut into short ones, so that there are wavefronts enough
+int chunk_rows(int T) { return T <= 2048 ? 4 : T <= 8192 ? 8 : T <= 32768 ? 16 : 32; }
+
+constexpr int MAX_TOKENS = 1 << 30;
+
+struct Workspace {
+  Grouped g;
+  float* piece;
+  long ld_piece;
+  size_t bytes;
+  Workspace(void* scratch, int T, int d) {
+    Arena a(scratch);
+    const size_t ids = (size_t)T * sizeof(int32_t);
+    g.word = a.take<int32_t>(ids); g.pos = a.take<int32_t>(ids);
+    g.word2 = a.take<int32_t>(ids); g.pos2 = a.take<int32_t>(ids);
+    g.count = a.take<int32_t>(sizeof(int32_t));
+    ld_piece = (long)align_up((size_t)d, COLS);
+    piece = a.take<float>(2 * (size_t)cdiv(T, chunk_rows(T)) * ld_piece * sizeof(float));
+    bytes = a.off;
+  }
+};
+
+template <typename T>
+void launch_embed(const void* table, int ld_table, const int32_t* ids, int n, int V, int d, float scale, void* y, int ld_y,
+                  hipStream_t st) {
+  constexpr int W = Elt<T>::VEC;
+  const bool vec = d % W == 0 && ld_table % W == 0 && ld_y % W == 0;
+  const int chunks = vec ? d / W : d;
+  int log_lanes = 0;
+  while (log_lanes < 6 && (1 << log_lanes) < chunks) ++log_lanes;
+  const unsigned blocks = (unsigned)((((long)n << log_lanes) + 255) / 256);
+  if (vec)
+    hipLaunchKernelGGL((embed_kernel<T, true>), dim3(blocks), dim3(256), 0, st, (const T*)table, (long)ld_table, ids, n, V, d, scale,
+                       (T*)y, (long)ld_y, log_lanes);
+  else
+    hipLaunchKernelGGL((embed_kernel<T, false>), dim3(blocks), dim3(256), 0, st, (const T*)table, (long)ld_table, ids, n, V, d, scale,
+                       (T*)y, (long)ld_y, log_lanes);
+}
+
+template <typename T, bool VEC>
+bm_status launch_sums(const void* dy, int ld_dy, const Workspace& w, int n, int d, float scale, float* dtable, int ld_dtable,
+                      hipStream_t st) {
+  const int chunk = chunk_rows(n), chunks = cdiv(n, chunk), slices = cdiv(d, SLICE);
+  const long jobs = (long)chunks * slices;
+  hipLaunchKernelGGL((sum_kernel<T, VEC>), dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, st, (const T*)dy, (long)ld_dy, w.g, d,
+                     chunk, chunks, slices, scale, dtable, (long)ld_dtable, w.piece, w.ld_piece);
+  BM_CHECK_LAUNCH("embedding sums");
+  if (chunks > 1) {
+    hipLaunchKernelGGL((fold_kernel<VEC>), dim3((unsigned)((long)(chunks - 1) * slices)), dim3(FOLD_WAVES * 64), 0, st, w.g, d, chunk,
+                       chunks, slices, scale, dtable, (long)ld_dtable, w.piece, w.ld_piece);
+    BM_CHECK_LAUNCH("embedding fold");
+  }
+  return BM_OK;
+}
+
+bm_status check(const char* name, int32_t dtype, int32_t V, int32_t d, int32_t T, int32_t ld0, int32_t ld1) {
+  BM_ARG_CHECK(good_dtype(dtype), "%s: dtype %d", name, dtype);
+  BM_ARG_CHECK(V > 0 && d > 0, "%s: V and d must be positive", name);
+  BM_ARG_CHECK(T >= 0 && T <= MAX_TOKENS, "%s: %d tokens", name, T);
+  BM_ARG_CHECK(ld0 >= d && ld1 >= d, "%s: leading dimension too small", name);
+  // workgroups of a grid
+  BM_ARG_CHECK((long)T * cdiv(d, SLICE) < (1l << 31), "%s: %d tokens of %d columns are too many", name, T, d);
+  return BM_OK;
+}
+
+}  // namespace
+}  // namespace bm
+
+using namespace bm;
+
+extern "C" bm_status bm_embedding_forward(int32_t dtype, int32_t V, int32_t d, const void* table, int32_t ld_table,
+                                          const int32_t* ids, int32_t T, float scale, void* y, int32_t ld_y, void* hip_stream) {
+  BM_RETURN_IF(check("bm_embedding_forward", dtype, V, d, T, ld_table, ld_y));
+  if (T == 0) return BM_OK;
+  BM_ARG_CHECK(table && ids && y && aligned16(table) && aligned16(ids) && aligned16(y), "bm_embedding_forward: NULL or misaligned tensor");
+  hipStream_t st = (hipStream_t)hip_stream;
+  ProfScope prof(PROF_ELEMENTWISE, 2.0 * T * d * elt_size(dtype), st);
+  if (dtype == BM_DTYPE_BF16) launch_embed<bf16_t>(table, ld_table, ids, T, V, d, scale, y, ld_y, st);
+  else launch_embed<float>(table, ld_table, ids, T, V, d, scale, y, ld_y, st);
+  BM_CHECK_LAUNCH("embedding lookup");
+  return BM_OK;
+}
+
+extern "C" size_t bm_embedding_backward_scratch_bytes(int32_t T, int32_t d) {
+  if (T <= 0 || T > MAX_TOKENS || d <= 0) return 0;
+  return Workspace(nullptr, T, d).bytes;
+}
+
+extern "C" bm_status bm_embedding_backward(int32_t dtype, int32_t V, int32_t d, const void* dy, int32_t ld_dy, const int32_t* ids,
+                                           int32_t T, float scale, float* dtable, int32_t ld_dtable, void* scratch,
+                                           size_t scratch_bytes, void* hip_stream) {
+  BM_RETURN_IF(check("bm_embedding_backward", dtype, V, d, T, ld_dy, ld_dtable));
+  if (T == 0) return BM_OK;
+  BM_ARG_CHECK(dy && ids && dtable && aligned16(dy) && aligned16(ids) && aligned16(dtable) && aligned16(scratch),
+               "bm_embedding_backward: NULL or misaligned tensor");
+  const Workspace w(scratch, T, d);
+  if (!scratch || scratch_bytes < w.bytes) {
+    set_error("bm_embedding_backward needs %zu scratch bytes, got %zu", w.bytes, scratch_bytes);
+    return BM_ERR_WORKSPACE_TOO_SMALL;
+  }
+  hipStream_t st = (hipStream_t)hip_stream;
+  ProfScope prof(PROF_ELEMENTWISE, (double)T * d * (elt_size(dtype) + 8.0), st);
+  int bits = 0;                                             // of the ids, above those of the bucket
+  while (bits < 31 - BUCKET_BITS && ((V - 1) >> (BUCKET_BITS + bits))) ++bits;
+  hipLaunchKernelGGL(group_kernel, dim3(BUCKETS), dim3(GROUP_THREADS), 0, st, ids, T, V, cdiv(bits, DIGIT_BITS), w.g);
+  BM_CHECK_LAUNCH("embedding group");
+  const int W = dtype == BM_DTYPE_BF16 ? 8 : 4;
+  const bool vec = d % W == 0 && ld_dy % W == 0 && ld_dtable % 4 == 0;
+  if (dtype == BM_DTYPE_BF16)
+    return vec ? launch_sums<bf16_t, true>(dy, ld_dy, w, T, d, scale, dtable, ld_dtable, st)
+               : launch_sums<bf16_t, false>(dy, ld_dy, w, T, d, scale, dtable, ld_dtable, st);
+  return vec ? launch_sums<float, true>(dy, ld_dy, w, T, d, scale, dtable, ld_dtable, st)
+             : launch_sums<float, false>(dy, ld_dy, w, T, d, scale, dtable, ld_dtable, st);
+}

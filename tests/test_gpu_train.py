@@ -1,0 +1,318 @@
+"""Parity of the training-step operators with the fp64 oracle (needs a GPU).
+
+U: half a step of the storage type, relative.  F: the same of fp32, in which everything is computed.
+"""
+import numpy as np
+import pytest
+
+from oracle import train_oracle as to
+from paper_2605_25451_amd import binding as bm
+
+pytestmark = pytest.mark.gpu
+
+F = 2.0 ** -24
+U = {0: 2.0 ** -8, 1: F}
+TYPES = [0, 1]
+NAMES = ["bf16", "fp32"]
+
+
+def torch_type(dtype):
+    import torch
+    return torch.float32 if dtype else torch.bfloat16
+
+
+def device(a, dtype):
+    """[rows, cols] values in the storage type, and what they are in fp64."""
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(a, np.float32)).cuda().to(torch_type(dtype))
+    return t, t.double().cpu().numpy()
+
+
+def strided(a, dtype, ld, fill=7.0):
+    """The same with rows of ld elements, `fill` behind them."""
+    import torch
+    t = torch.full((len(a), ld), fill, dtype=torch_type(dtype), device="cuda")
+    t[:, :a.shape[1]] = torch.from_numpy(np.ascontiguousarray(a, np.float32)).cuda().to(t.dtype)
+    return t, t[:, :a.shape[1]].double().cpu().numpy()
+
+
+def ints(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a, np.int32)).cuda()
+
+
+def scratch_of(n):
+    """A workspace of n bytes full of NaN, and bytes behind it that nobody writes."""
+    import torch
+    return torch.full((n + 256,), 255, dtype=torch.uint8, device="cuda")
+
+
+# ---- embeddings ------------------------------------------------------------------------------------
+
+IDS = {
+    "one": lambda rng, T, V: np.full(T, V - 1),
+    "any": lambda rng, T, V: rng.integers(0, V, T),
+    "few": lambda rng, T, V: rng.integers(0, max(1, V // 50), T) * (V // max(1, V // 50)),
+    "images": lambda rng, T, V: np.where(rng.random(T) < 0.5, -1, rng.integers(0, V, T)),
+    "none": lambda rng, T, V: np.full(T, -2 ** 31),
+    "past": lambda rng, T, V: np.where(rng.random(T) < 0.3, rng.choice([V, V + 256, 2 ** 31 - 1], T), rng.integers(0, V, T)),
+    "ranked": lambda rng, T, V: np.minimum(V - 1, np.exp(rng.random(T) * np.log(V + 1)) - 1).astype(np.int64),
+}
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
+@pytest.mark.parametrize("T,V,d,pad,kind", [
+    (1, 1, 1, 0, "one"), (1, 50, 4096, 0, "any"), (3, 7, 8, 8, "any"), (64, 300, 24, 0, "images"), (65, 300, 100, 3, "past"),
+    (257, 1000, 1152, 16, "images"), (33, 100, 1028, 0, "any"), (19, 100, 1001, 0, "past"), (70, 10, 513, 7, "none")])
+def test_lookup(T, V, d, pad, kind, dtype):
+    rng = np.random.default_rng(T + V + d)
+    ids = IDS[kind](rng, T, V)
+    table, table64 = strided(rng.standard_normal((V, d)), dtype, d + pad)
+    y, y64 = strided(rng.standard_normal((T, d)), dtype, d + 2 * pad, fill=3.0)
+    scale = float(np.float32(d ** 0.5))
+    bm.embedding_forward(dtype, V, d, table, d + pad, ints(ids), T, scale, y, d + 2 * pad)
+    want = to.embedding_forward(table64, ids, scale, y64)
+    got = y.double().cpu().numpy()
+    assert (got[:, d:] == 3.0).all()
+    got = got[:, :d]
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    live = ~np.isnan(want)
+    # the product in fp32, rounded to the storage type
+    assert (np.abs(got - want)[live] <= (U[dtype] + 2 * F) * np.abs(want)[live]).all()
+    assert np.array_equal(got[ids < 0], y64[ids < 0])
+
+
+def embedding_backward(dtype, V, d, dy, ld_dy, ids, T, scale, dtable, ld):
+    n = bm.embedding_backward_scratch_bytes(T, d)
+    scratch = scratch_of(n)
+    bm.embedding_backward(dtype, V, d, dy, ld_dy, ids, T, scale, dtable, ld, scratch, n)
+    assert (scratch[n:] == 255).all()
+
+
+CASES = [(1, 1, 1, 0, "one"), (2, 3, 5, 0, "one"), (5, 300, 8, 8, "any"), (64, 256, 24, 0, "images"), (65, 257, 100, 3, "past"),
+         (777, 1000, 1152, 16, "ranked"), (2048, 3000, 72, 0, "any"), (2049, 500, 520, 0, "few"), (4099, 9, 1028, 4, "one"),
+         (8193, 70000, 36, 0, "ranked"), (9000, 300000, 8, 0, "ranked"), (33000, 400, 17, 1, "images"), (33000, 50, 64, 0, "one"),
+         (130, 40, 513, 0, "none"), (1500, 4, 2048, 0, "any")]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
+@pytest.mark.parametrize("T,V,d,pad,kind", CASES)
+def test_embedding_gradient(T, V, d, pad, kind, dtype):
+    import torch
+    rng = np.random.default_rng(T + V + d)
+    ids = IDS[kind](rng, T, V)
+    dy, dy64 = strided(rng.standard_normal((T, d)), dtype, d + pad)
+    start, start64 = strided(0.5 * rng.standard_normal((V, d)), 1, d + 2 * pad, fill=3.0)
+    scale = 0.75
+    runs = []
+    for _ in range(2):
+        dtable = start.clone()
+        embedding_backward(dtype, V, d, dy, d + pad, ints(ids), T, scale, dtable, d + 2 * pad)
+        runs.append(dtable)
+    assert torch.equal(runs[0], runs[1])
+    got = runs[0].double().cpu().numpy()
+    assert (got[:, d:] == 3.0).all()
+    got = got[:, :d]
+    live = (ids >= 0) & (ids < V)
+    count = np.bincount(ids[live], minlength=V)[:, None]
+    assert np.array_equal(got[count[:, 0] == 0], start64[count[:, 0] == 0])
+    want = to.embedding_backward(dy64, ids, scale, start64)
+    size = to.embedding_backward(np.abs(dy64), ids, scale, np.abs(start64))
+    # one rounding for each row that is added, one for the table's own, and the scale (a power of two apart from 3/4) in the last
+    assert (np.abs(got - want) <= (count + 2) * F * size).all()
+
+
+def test_gradient_of_a_vocabulary_of_more_than_28_bits():
+    """Three digits behind the bucket's, rows past 4 GiB from the table's first."""
+    import torch
+    V, T, d, ld = (1 << 28) + 77, 3000, 3, 5
+    rng = np.random.default_rng(3)
+    words = np.concatenate([rng.integers(0, V, 40), [0, V - 1, 1 << 28, (1 << 28) - 1]])
+    ids = rng.choice(words, T)
+    dy, dy64 = device(rng.standard_normal((T, d)), 1)
+    dtable = torch.zeros((V, ld), device="cuda")
+    embedding_backward(1, V, d, dy, d, ints(ids), T, 1.0, dtable, ld)
+    u, inverse = np.unique(ids, return_inverse=True)
+    got = dtable[torch.from_numpy(u).cuda()].double().cpu().numpy()
+    want = to.embedding_backward(dy64, inverse, 1.0, np.zeros((len(u), d)))
+    size = to.embedding_backward(np.abs(dy64), inverse, 1.0, np.zeros((len(u), d)))
+    assert (got[:, d:] == 0).all()
+    assert (np.abs(got[:, :d] - want) <= (np.bincount(inverse)[:, None] + 2) * F * size).all()
+    assert int((dtable != 0).sum()) == int((got != 0).sum())
+
+
+# ---- cross-entropy -----------------------------------------------------------------------------------
+
+def cross_entropy(dtype, T, V, logits, ld, labels, weight, dlogits, ld_d, loss=True):
+    import torch
+    n = bm.cross_entropy_scratch_bytes(dtype, T, V)
+    scratch = scratch_of(n)
+    out = torch.full((T,), 5.0, device="cuda") if loss else None
+    bm.cross_entropy(dtype, T, V, logits, ld, labels, weight, out, dlogits, ld_d, scratch, n)
+    assert (scratch[n:] == 255).all()
+    return out
+
+
+def check_loss(loss, grad, z64, labels, weight, dtype):
+    T, V = z64.shape
+    want, dwant = to.cross_entropy(z64, labels, weight)
+    w = np.ones(T) if weight is None else np.abs(weight).astype(np.float64)
+    finite = np.where(np.isfinite(z64), z64, np.nan)
+    reach = np.zeros(T)
+    some = np.isfinite(z64).any(axis=1)
+    reach[some] = np.nanmax(finite[some], axis=1) - np.nanmin(finite[some], axis=1)
+    reach = np.minimum(reach, 110.0)                          # exp of less than that is under fp32's range
+    # exp(z - m): the difference, the factor log2 e and the function are a rounding or two each; a thread adds at most V/256 of them and
+    # scales its sum as often, 32 more joins
+    term = (3 * reach + 6) * F
+    total = term + (3 * -(-V // 256) + 64) * F
+    if loss is not None:
+        nan = np.isnan(want)
+        assert np.array_equal(np.isnan(loss), nan)
+        inf = np.isinf(want)
+        assert np.array_equal(loss[inf], want[inf])
+        ok = ~nan & ~inf & (np.asarray(labels) >= 0)
+        at = np.zeros(T)
+        at[ok] = np.abs(z64[ok, np.asarray(labels)[ok]])
+        top = np.where(some, np.abs(np.nan_to_num(z64.max(axis=1), posinf=0, neginf=0)), 0)
+        assert (np.abs(loss - want)[ok] <= (w * (total + 4 * F * (at + top + np.log(V) + 1)))[ok]).all()
+        assert (loss[np.asarray(labels) < 0] == 0).all()
+    if grad is not None:
+        assert np.array_equal(np.isnan(grad), np.isnan(dwant))
+        p = np.abs(dwant)
+        rows = np.asarray(labels) >= 0
+        lab = np.zeros((T, V))
+        for t in np.nonzero(rows & (np.asarray(labels) < V))[0]:
+            lab[t, labels[t]] = w[t]                          # p - 1 keeps the rounding of p
+        bound = (p + lab) * (total + term + 4 * F)[:, None] + U[dtype] * p + 1e-37
+        ok = ~np.isnan(dwant)
+        assert (np.abs(grad - dwant)[ok] <= bound[ok]).all()
+        assert (grad[~rows] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
+@pytest.mark.parametrize("T,V,pad", [(1, 1, 0), (1, 2, 0), (3, 7, 0), (2, 8, 8), (5, 9, 1), (64, 300, 20), (17, 1001, 0), (300, 520, 0),
+                                     (9, 4096, 0), (7, 8191, 2), (4, 33000, 0), (3, 50257, 0), (2, 65537, 7), (2, 128000, 0),
+                                     (2, 131075, 0), (1, 200003, 0), (1100, 2050, 0)])
+def test_cross_entropy(T, V, pad, dtype):
+    rng = np.random.default_rng(T + V)
+    z = rng.standard_normal((T, V)) * rng.choice([0.1, 2.0, 12.0], (T, 1)) + rng.choice([0.0, 30.0, -100.0], (T, 1))
+    labels = rng.integers(0, V, T)
+    if T > 2:
+        labels[rng.random(T) < 0.4] = -1
+    weight = rng.random(T).astype(np.float32)
+    logits, z64 = strided(z, dtype, V + pad)
+    dlogits, _ = strided(z, dtype, V + pad)
+    loss = cross_entropy(dtype, T, V, logits, V + pad, ints(labels), device(weight, 1)[0], dlogits, V + pad)
+    got = dlogits.double().cpu().numpy()
+    assert (got[:, V:] == 7.0).all()
+    check_loss(loss.double().cpu().numpy(), got[:, :V], z64, labels, weight, dtype)
+    assert np.array_equal(logits[:, :V].double().cpu().numpy(), z64)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
+@pytest.mark.parametrize("T,V,ld,ld_d", [(6, 1000, 1000, 1003), (5, 1001, 1003, 1004), (3, 40001, 40001, 40004), (2, 140000, 140001, 140002)])
+def test_gradient_rows_that_start_elsewhere(T, V, ld, ld_d, dtype):
+    rng = np.random.default_rng(V)
+    labels = rng.integers(0, V, T)
+    logits, z64 = strided(3 * rng.standard_normal((T, V)), dtype, ld)
+    dlogits, _ = strided(np.zeros((T, V)), dtype, ld_d)
+    loss = cross_entropy(dtype, T, V, logits, ld, ints(labels), None, dlogits, ld_d)
+    got = dlogits.double().cpu().numpy()
+    assert (got[:, V:] == 7.0).all()
+    check_loss(loss.double().cpu().numpy(), got[:, :V], z64, labels, None, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
+@pytest.mark.parametrize("T,V", [(2, 900), (300, 901), (3, 32000), (2, 70001), (2, 180000)])
+def test_loss_alone_gradient_alone_and_in_place(T, V, dtype):
+    import torch
+    rng = np.random.default_rng(V)
+    labels = rng.integers(0, V, T)
+    labels[0] = -5
+    z = 3 * rng.standard_normal((T, V))
+    z[0] = np.nan                                             # never read
+    logits, z64 = device(z, dtype)
+    both = torch.full_like(logits, 9.0)
+    loss = cross_entropy(dtype, T, V, logits, V, ints(labels), None, both, V)
+    check_loss(loss.double().cpu().numpy(), both.double().cpu().numpy(), z64, labels, None, dtype)
+    alone = cross_entropy(dtype, T, V, logits, V, ints(labels), None, None, V)
+    assert torch.equal(alone, loss)
+    grad = torch.full_like(logits, 9.0)
+    assert cross_entropy(dtype, T, V, logits, V, ints(labels), None, grad, V, loss=False) is None
+    assert torch.equal(grad, both)
+    again = cross_entropy(dtype, T, V, logits, V, ints(labels), None, logits, V)
+    assert torch.equal(again, loss) and torch.equal(logits, both)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
+@pytest.mark.parametrize("V", [11, 2100, 33001, 140000])
+def test_masks_infinities_and_labels_that_are_none(V, dtype):
+    rng = np.random.default_rng(V)
+    z = rng.standard_normal((9, V))
+    low = -3.3e38
+    z[0, 1:] = -np.inf                                        # one word is left, the label: loss 0
+    z[1, 5:] = -np.inf                                        # a label that is masked: loss inf
+    z[2] = -np.inf                                            # nothing is left
+    z[3] = low                                                # the lowest value everywhere: uniform
+    z[4, ::2] = low
+    z[5, 3] = np.inf
+    z[6, 3] = np.nan
+    z[7, 0] = 3.0e38                                          # differences past fp32
+    z[7, 1] = -3.0e38
+    labels = np.array([0, 7, 2, 1, 1, 2, 2, 0, V])
+    logits, z64 = device(z, dtype)
+    dlogits = logits.clone()
+    loss = cross_entropy(dtype, 9, V, logits, V, ints(labels), None, dlogits, V).double().cpu().numpy()
+    grad = dlogits.double().cpu().numpy()
+    for t in (2, 5, 6, 8):
+        assert np.isnan(loss[t])
+        assert np.isnan(grad[t]).any()
+    assert loss[1] == np.inf
+    keep = [0, 3, 4, 7]
+    check_loss(loss[keep], grad[keep], z64[keep], labels[keep], None, dtype)
+    check_loss(None, grad[1:2], z64[1:2], labels[1:2], None, dtype)
+
+
+# ---- as a program calls them ---------------------------------------------------------------------------
+
+def test_another_stream_and_replays_of_a_captured_step():
+    """Lookup, loss and both gradients captured on a stream of their own, and replayed over changing inputs."""
+    import torch
+    T, V, d = 700, 5000, 256
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    table = torch.randn((V, d), device="cuda", generator=g)
+    ids = torch.randint(-1, V, (T,), device="cuda", generator=g, dtype=torch.int32)
+    y, dtable = torch.zeros((T, d), device="cuda"), torch.zeros((V, d), device="cuda")
+    logits, dlogits = torch.randn((T, V), device="cuda", generator=g), torch.zeros((T, V), device="cuda")
+    loss = torch.zeros(T, device="cuda")
+    n, m = bm.embedding_backward_scratch_bytes(T, d), bm.cross_entropy_scratch_bytes(1, T, V)
+    s1, s2 = torch.zeros(n, dtype=torch.uint8, device="cuda"), torch.zeros(max(m, 16), dtype=torch.uint8, device="cuda")
+
+    def step():
+        bm.embedding_forward(1, V, d, table, d, ids, T, 2.0, y, d)
+        bm.cross_entropy(1, T, V, logits, V, ids, None, loss, dlogits, V, s2, m)
+        bm.embedding_backward(1, V, d, y, d, ids, T, 0.5, dtable, d, s1, n)
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step()
+    for k in range(4):
+        ids.copy_(torch.randint(-1, V, (T,), device="cuda", generator=g, dtype=torch.int32))
+        logits.copy_(torch.randn((T, V), device="cuda", generator=g))
+        for t in (y, dtable, loss, dlogits):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (y, dtable, loss, dlogits)]
+        for t in (y, dtable, loss, dlogits):
+            t.zero_()
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (y, dtable, loss, dlogits))), k
