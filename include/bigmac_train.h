@@ -61,6 +61,28 @@ bm_status bm_cross_entropy(int32_t dtype, int32_t T, int32_t V, const void* logi
                            const int32_t* labels, const float* weight, float* loss, void* dlogits, int32_t ld_d,
                            void* scratch, size_t scratch_bytes, void* hip_stream);
 
+/* ---- orthogonalised update ----------------------------------------------------------------
+ * For every matrix b of a batch, with G_b [M, N] and m = min(M, N):
+ *   X = G_b / (|G_b|_F + eps),  then `steps` times  X <- a X + (b A + c A^2) X  with A = X X^T
+ *   (X^T X for a matrix that is taller than wide), and O_b = X.
+ * The iteration moves every singular value of G_b towards the fixed points of
+ * a s + b s^3 + c s^5; with (3.4445, -4.7750, 2.0315) and 5 steps all but the smallest end between 0.7 and 1.2.
+ *   grad dev  fp32, matrix b at grad + b*stride_g, rows of ld_g >= N elements
+ *   out  dev  dtype, matrix b at out + b*stride_o, rows of ld_o >= N elements; overwritten
+ *   coefficients host [3]: a, b, c.  steps 1..64.  eps >= 0; with eps = 0 a matrix of zeros gives NaN.
+ * Strides are in elements and not negative; stride_g may be 0; matrices of `out` lie one behind the other or side by
+ * side, and may take the place of grad (all of which is read before any of them is written).
+ * The products run on the matrix cores in 11-bit significands (fp16, scaled; X itself is kept in 22 bits until the
+ * last two steps, in which only singular values near the fixed points are still moved) for dtype BM_DTYPE_BF16, and in
+ * 22 bits for BM_DTYPE_FP32; sums are fp32, the norm fp64.
+ * BM_ERR_UNSUPPORTED for coefficients under which a singular value of [0, 1] exceeds 8 within `steps` steps.
+ * A matrix that holds an infinity or a NaN gives NaN; other matrices of the batch are not affected.
+ * scratch: bm_orthogonalize_scratch_bytes(dtype, batch, M, N) bytes.  batch may be 0. */
+size_t    bm_orthogonalize_scratch_bytes(int32_t dtype, int32_t batch, int32_t M, int32_t N);
+bm_status bm_orthogonalize(int32_t dtype, int32_t batch, int32_t M, int32_t N, const float* grad, int32_t ld_g,
+                           int64_t stride_g, void* out, int32_t ld_o, int64_t stride_o, const float* coefficients,
+                           int32_t steps, float eps, void* scratch, size_t scratch_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

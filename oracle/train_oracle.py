@@ -42,3 +42,18 @@ def cross_entropy(logits, labels, weight=None):
         p[labels[t]] -= 1.0
         grad[t] = w * p
     return loss, grad
+
+
+def orthogonalize(G, coefficients, steps, eps):
+    """Every step's X as well, the result last: [X0, X1, ...] with as many rows as G's smaller side."""
+    a, b, c = (float(np.float32(v)) for v in coefficients)
+    X = np.asarray(G, np.float64)
+    if X.shape[0] > X.shape[1]:
+        X = X.T
+    X = X / (np.sqrt((X * X).sum()) + float(np.float32(eps)))
+    out = [X]
+    for _ in range(steps):
+        A = X @ X.T
+        X = a * X + (b * A + c * A @ A) @ X
+        out.append(X)
+    return out

@@ -235,7 +235,10 @@ def lib() -> C.CDLL:
         l.bm_cross_entropy_scratch_bytes.argtypes = [i32] * 3
         l.bm_cross_entropy_scratch_bytes.restype = sz
         l.bm_cross_entropy.argtypes = [i32] * 3 + [vp, i32, vp, vp, vp, vp, i32, vp, sz, vp]
-        for name in ("bm_embedding_forward", "bm_embedding_backward", "bm_cross_entropy"):
+        l.bm_orthogonalize_scratch_bytes.argtypes = [i32] * 4
+        l.bm_orthogonalize_scratch_bytes.restype = sz
+        l.bm_orthogonalize.argtypes = [i32] * 4 + [vp, i32, i64, vp, i32, i64, C.POINTER(f32), i32, f32, vp, sz, vp]
+        for name in ("bm_embedding_forward", "bm_embedding_backward", "bm_cross_entropy", "bm_orthogonalize"):
             getattr(l, name).restype = C.c_int
         _lib = l
     return _lib
@@ -506,6 +509,18 @@ def cross_entropy(dtype, T, V, logits, ld, labels, weight, loss, dlogits, ld_d, 
                   stream=None):
     _check(lib().bm_cross_entropy(dtype, T, V, _ptr(logits), ld, _ptr(labels), _ptr(weight), _ptr(loss), _ptr(dlogits),
                                   ld_d, _ptr(scratch), scratch_bytes, _stream() if stream is None else stream))
+
+
+def orthogonalize_scratch_bytes(dtype, batch, M, N) -> int:
+    return lib().bm_orthogonalize_scratch_bytes(dtype, batch, M, N)
+
+
+def orthogonalize(dtype, batch, M, N, grad, ld_g, stride_g, out, ld_o, stride_o, coefficients, steps, eps, scratch,
+                  scratch_bytes, stream=None):
+    """coefficients: the three of the iteration's polynomial, or None for a NULL pointer."""
+    c = None if coefficients is None else (C.c_float * 3)(*coefficients)
+    _check(lib().bm_orthogonalize(dtype, batch, M, N, _ptr(grad), ld_g, stride_g, _ptr(out), ld_o, stride_o, c, steps,
+                                  eps, _ptr(scratch), scratch_bytes, _stream() if stream is None else stream))
 
 
 def probe_mfma(blocks, iters, out, stream=None):

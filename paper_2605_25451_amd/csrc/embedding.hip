@@ -72,9 +72,8 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_kernel(const int32_t* __r
   const int per = share(n);
   const int first = min(n, wave * per), last = min(n, first + per);
   int lower = 0, own = 0;
-#pragma unroll 8
   for (int i = first + lane; i - lane < last; i += WAVE) {
-    const int id = i < last ? ids[min(i, n - 1)] : -1;
+    const int id = i < last ? ids[i] : -1;
     const int b = (uint32_t)id < (uint32_t)V ? id & (BUCKETS - 1) : BUCKETS;
     lower += __popcll(__ballot(b < bucket));
     own += __popcll(__ballot(b == bucket));

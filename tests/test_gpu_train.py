@@ -316,3 +316,179 @@ def test_another_stream_and_replays_of_a_captured_step():
         step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, (y, dtable, loss, dlogits))), k
+
+
+# ---- orthogonalised updates ----------------------------------------------------------------------------
+
+MUON = (3.4445, -4.7750, 2.0315)
+
+
+def orthogonalize(dtype, grad, ld_g, stride_g, B, M, N, ld_o, stride_o, coefficients=MUON, steps=5, eps=1e-7, size=None):
+    import torch
+    n = bm.orthogonalize_scratch_bytes(dtype, B, M, N)
+    scratch = scratch_of(n)
+    out = torch.full((size or (B - 1) * stride_o + (M - 1) * ld_o + N,), 9.0, dtype=torch_type(dtype), device="cuda")
+    bm.orthogonalize(dtype, B, M, N, grad, ld_g, stride_g, out, ld_o, stride_o, coefficients, steps, eps, scratch, n)
+    assert (scratch[n:] == 255).all()
+    return out
+
+
+def worst_case(Xs, coefficients, dtype):
+    """Bound of the 2-norm of all entries' errors: every rounding at its largest, every step with the Lipschitz constant of
+    its polynomial on the singular values that occur.  The error of the steps before moves the factors of these terms
+    in second order only, for which half as much again stands at the end; fed back into the factors it would make the bound grow
+    doubly exponentially (past fp64 within nine steps of a polynomial that spreads neighbouring values fourfold)."""
+    a, b, c = (abs(float(v)) for v in coefficients)
+    norm, top = np.linalg.norm, lambda x: np.linalg.norm(x, 2)
+    steps, m, n = len(Xs) - 1, *Xs[0].shape
+    h = 2.0 ** -11 if dtype == 0 else 2.0 ** -20              # of an operand; for three products the two parts and what they leave out
+    full = 2.0 ** -21                                         # of X in two parts, with its fp32 arithmetic
+    sums = lambda k: (k / 32 + 40) * F
+    E = full * norm(Xs[0])
+    for i, X in enumerate(Xs[:-1]):
+        s, f = top(X), norm(X)
+        grid = np.linspace(0, s, 500)[1:]
+        lip = max(np.abs(coefficients[0] + 3 * coefficients[1] * grid ** 2 + 5 * coefficients[2] * grid ** 4).max(),
+                  np.abs(coefficients[0] + coefficients[1] * grid ** 2 + coefficients[2] * grid ** 4).max())
+        A = X @ X.T
+        dA = (2 * h + h) * s * f + sums(n) * f * f
+        dB = b * dA + c * (2 * s * s * dA + 2 * h * s * s * norm(A) + sums(m) * norm(A) ** 2) + h * (b * norm(A) + c * norm(A @ A)) * 2
+        B2 = b * s * s + c * s ** 4
+        local = dB * s + B2 * h * f + sums(m) * B2 * np.sqrt(m) * f
+        rounds = full if dtype or i + 1 + 2 < steps else 2.0 ** -11
+        E = lip * E + local + (rounds + 4 * F) * norm(Xs[i + 1])
+    return 1.5 * E + U[dtype] * norm(Xs[-1])
+
+
+def spectrum(rng, M, N, kind):
+    G = rng.standard_normal((M, N))
+    if kind == "falls":
+        m = min(M, N)
+        q = lambda n: np.linalg.qr(rng.standard_normal((n, m)))[0]
+        G = (q(M) * np.logspace(0, -3, m)) @ q(N).T
+    if kind == "one":
+        G = np.outer(G[:, 0], G[0])
+    return G
+
+
+SHAPES = [(1, 1, 1, "noise"), (1, 1, 40, "noise"), (1, 40, 1, "noise"), (1, 5, 3, "one"), (1, 64, 64, "noise"), (1, 65, 63, "noise"),
+          (3, 20, 200, "falls"), (2, 200, 20, "falls"), (1, 130, 130, "falls"), (1, 192, 64, "noise"), (2, 257, 129, "noise"),
+          (1, 256, 256, "falls"), (1, 300, 700, "noise"), (2, 513, 320, "noise"), (1, 640, 520, "falls"), (17, 33, 70, "noise"),
+          (1, 16, 3000, "noise"), (1, 3000, 100, "falls"), (1, 96, 96, "one"), (2, 768, 1000, "noise"), (1, 1030, 1100, "noise")]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
+@pytest.mark.parametrize("B,M,N,kind", SHAPES)
+def test_orthogonalize(B, M, N, kind, dtype):
+    import torch
+    rng = np.random.default_rng(M * N + B)
+    ld_g, ld_o = N + 3, N + 5
+    sg, so = M * ld_g + 7, M * ld_o + 9
+    G = np.stack([spectrum(rng, M, N, kind) * 10.0 ** rng.integers(-12, 12) for _ in range(B)]).astype(np.float32)
+    buf = np.full((B, sg), 1e30, np.float32)
+    for b in range(B):
+        for r in range(M):
+            buf[b, r * ld_g:r * ld_g + N] = G[b, r]
+    grad = torch.from_numpy(buf).cuda()
+    eps = 1e-20
+    out = orthogonalize(dtype, grad, ld_g, sg, B, M, N, ld_o, so, eps=eps, size=B * so)
+    assert torch.equal(out, orthogonalize(dtype, grad, ld_g, sg, B, M, N, ld_o, so, eps=eps, size=B * so))
+    out = out.double().cpu().numpy().reshape(B, so)
+    for b in range(B):
+        Xs = to.orthogonalize(G[b], MUON, 5, eps)
+        want = Xs[-1].T if M > N else Xs[-1]
+        rows = out[b][:M * ld_o].reshape(M, ld_o)
+        assert (rows[:, N:] == 9).all() and (out[b][M * ld_o:] == 9).all()
+        assert np.linalg.norm(rows[:, :N] - want) <= worst_case(Xs, MUON, dtype)
+
+
+def emulate(G, coefficients, steps, eps):
+    """The iteration with the roundings that a bf16 result is computed with."""
+    half = lambda x, s=1.0: (x * s).astype(np.float16).astype(np.float64) / s
+    a, b, c = (float(np.float32(v)) for v in coefficients)
+    X = to.orthogonalize(G, coefficients, 0, eps)[0]
+    s = 2.0 ** np.floor(np.log2(np.sqrt(X.size)))
+    for i in range(steps):
+        hi = half(X, s)
+        if i + 2 >= steps:
+            X = hi
+        A = half(hi @ hi.T, 2.0 ** 14)
+        X = a * X + half(b * A + c * A @ A, 2.0 ** 11) @ hi
+    return X
+
+
+@pytest.mark.parametrize("M,N,kind", [(256, 256, "noise"), (300, 700, "falls"), (640, 520, "noise"), (512, 512, "falls"), (128, 2000, "falls")])
+def test_orthogonalize_is_as_exact_as_its_roundings(M, N, kind):
+    import torch
+    G = spectrum(np.random.default_rng(M), M, N, kind).astype(np.float32)
+    grad = torch.from_numpy(G).cuda()
+    want = to.orthogonalize(G, MUON, 5, 1e-7)[-1]
+    got = orthogonalize(0, grad, N, M * N, 1, M, N, N, M * N).double().cpu().numpy().reshape(M, N)
+    size = np.linalg.norm(want)
+    inner = np.linalg.norm(emulate(G, MUON, 5, 1e-7) - want) / size
+    # independent roundings add up in squares; one of bf16 is uniform over a step of up to 2^-8 relative: at most 2^-8 / sqrt 3
+    assert np.linalg.norm((got.T if M > N else got) - want) / size <= 1.5 * np.hypot(inner, 2.0 ** -8 / 3 ** 0.5)
+    got = orthogonalize(1, grad, N, M * N, 1, M, N, N, M * N).double().cpu().numpy().reshape(M, N)
+    assert np.linalg.norm((got.T if M > N else got) - want) / size <= 1e-5
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
+@pytest.mark.parametrize("coefficients,steps", [(MUON, 1), (MUON, 2), (MUON, 9), ((1.5, -0.5, 0.0), 12), ((1.875, -1.25, 0.375), 6),
+                                                ((1.0, 0.0, 0.0), 3), ((0.5, 0.25, 0.125), 4)])
+def test_other_polynomials(coefficients, steps, dtype):
+    import torch
+    M, N = 100, 150
+    G = np.random.default_rng(steps).standard_normal((M, N)).astype(np.float32)
+    Xs = to.orthogonalize(G, coefficients, steps, 1e-7)
+    got = orthogonalize(dtype, torch.from_numpy(G).cuda(), N, 0, 1, M, N, N, M * N, coefficients, steps).double().cpu().numpy().reshape(M, N)
+    assert np.linalg.norm(got - Xs[-1]) <= worst_case(Xs, coefficients, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
+def test_matrices_of_a_batch_side_by_side_and_in_place(dtype):
+    """Matrices that share rows; one matrix read three times; zeros, NaN and infinities beside ordinary ones."""
+    import torch
+    rng = np.random.default_rng(5)
+    B, M, N = 5, 70, 40
+    G = rng.standard_normal((M, B * N)).astype(np.float32)
+    G[:, N:2 * N] = 0
+    G[3, 2 * N + 1] = np.nan
+    G[4, 3 * N + 1] = np.inf
+    grad = torch.from_numpy(G).cuda()
+    out = orthogonalize(dtype, grad, B * N, N, B, M, N, B * N, N, size=M * B * N).double().cpu().numpy().reshape(M, B * N)
+    assert (out[:, N:2 * N] == 0).all() and np.isnan(out[:, 2 * N:4 * N]).all()
+    for b in (0, 4):
+        Xs = to.orthogonalize(G[:, b * N:(b + 1) * N], MUON, 5, 1e-7)
+        assert np.linalg.norm(out[:, b * N:(b + 1) * N] - Xs[-1].T) <= worst_case(Xs, MUON, dtype)
+    same = orthogonalize(dtype, grad, B * N, 0, 3, M, N, N, M * N).double().cpu().numpy().reshape(3, M, N)
+    assert all(np.array_equal(m, out[:, :N]) for m in same)
+    if dtype == 1:
+        n = bm.orthogonalize_scratch_bytes(1, B, M, N)
+        bm.orthogonalize(1, B, M, N, grad, B * N, N, grad, B * N, N, MUON, 5, 1e-7, scratch_of(n), n)
+        assert np.array_equal(grad.double().cpu().numpy(), out, equal_nan=True)
+
+
+def test_orthogonalize_replayed():
+    import torch
+    B, M, N = 2, 300, 200
+    n = bm.orthogonalize_scratch_bytes(0, B, M, N)
+    scratch = torch.empty(n, dtype=torch.uint8, device="cuda")
+    grad, out = torch.randn((B, M, N), device="cuda"), torch.zeros((B, M, N), dtype=torch.bfloat16, device="cuda")
+    step = lambda: bm.orthogonalize(0, B, M, N, grad, N, M * N, out, N, M * N, MUON, 5, 1e-7, scratch, n)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step()
+    for _ in range(3):
+        grad.copy_(torch.randn((B, M, N), device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        out.zero_()
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(got, out)

@@ -72,3 +72,32 @@ def test_no_tokens_is_nothing_to_do():
     bm.embedding_forward(0, 100, 16, None, 16, None, 0, 1.0, None, 16, stream=0)
     bm.embedding_backward(0, 100, 16, None, 16, None, 0, 1.0, None, 16, None, 0, stream=0)
     bm.cross_entropy(0, 0, 100, None, 100, None, None, None, None, 100, stream=0)
+
+
+ORTHO = dict(dtype=0, batch=3, M=20, N=30, grad=P, ld_g=30, stride_g=600, out=Q, ld_o=30, stride_o=600,
+             coefficients=(3.4445, -4.7750, 2.0315), steps=5, eps=1e-7, scratch=R, scratch_bytes=1 << 30)
+
+
+@pytest.mark.parametrize("bad", [dict(dtype=2), dict(batch=-1), dict(M=0), dict(N=-1), dict(ld_g=29), dict(ld_o=29),
+                                 dict(stride_g=-1), dict(stride_o=-600), dict(stride_o=599), dict(stride_o=30, ld_o=89),
+                                 dict(steps=0), dict(steps=65), dict(eps=-1.0), dict(eps=float("inf")), dict(eps=float("nan")),
+                                 dict(coefficients=None), dict(grad=None), dict(out=None), dict(grad=P + 4), dict(out=Q + 2),
+                                 dict(scratch=R + 8), dict(M=(1 << 20) + 1), dict(M=1 << 20, N=1 << 20, ld_g=1 << 20, ld_o=1 << 20)])
+def test_orthogonalize_refusals(bad):
+    refused(bm.BM_ERR_INVALID_ARG, bm.orthogonalize, *{**ORTHO, **bad}.values())
+
+
+@pytest.mark.parametrize("c", [(9.0, 0.0, 0.0), (1.6, 0.0, 0.0), (float("nan"), 0.0, 0.0), (1.0, float("inf"), 0.0), (3.0, 4.0, 5.0)])
+def test_orthogonalize_refuses_coefficients_that_diverge(c):
+    refused(bm.BM_ERR_UNSUPPORTED, bm.orthogonalize, *{**ORTHO, "coefficients": c}.values())
+
+
+def test_orthogonalize_workspace():
+    for dtype in (0, 1):
+        need = bm.orthogonalize_scratch_bytes(dtype, 3, 20, 30)
+        assert need > 0
+        for bad in (dict(scratch_bytes=need - 1), dict(scratch=None)):
+            refused(bm.BM_ERR_WORKSPACE_TOO_SMALL, bm.orthogonalize, *{**ORTHO, "dtype": dtype, **bad}.values())
+    for args in ((2, 1, 8, 8), (0, 0, 8, 8), (0, 1, 0, 8), (0, 1, 8, (1 << 20) + 1), (0, 1, 1 << 20, 1 << 20)):
+        assert bm.orthogonalize_scratch_bytes(*args) == 0
+    bm.orthogonalize(0, 0, 8, 8, None, 8, 64, None, 8, 64, (1.0, 0.0, 0.0), 1, 0.0, None, 0, stream=0)

@@ -47,3 +47,23 @@ def test_cross_entropy_closed_forms():
     loss, grad = to.cross_entropy(z, [1])
     assert abs(loss[0] - np.log(2)) < 1e-15 and grad[0, 0] == 0
     assert np.isnan(to.cross_entropy(z, [3])[0][0])
+
+
+def test_orthogonalize_moves_singular_values_by_the_polynomial():
+    rng = np.random.default_rng(2)
+    for shape in ((5, 9), (9, 5), (1, 4), (6, 6)):
+        G = rng.standard_normal(shape)
+        u, s, v = np.linalg.svd(G, full_matrices=False)
+        s = s / (np.sqrt((s * s).sum()) + np.float32(1e-7))
+        a, b, c = (float(np.float32(x)) for x in (3.4445, -4.775, 2.0315))
+        for _ in range(4):
+            s = a * s + b * s ** 3 + c * s ** 5
+        X = to.orthogonalize(G, (3.4445, -4.775, 2.0315), 4, 1e-7)[-1]
+        want = (u * s) @ v
+        assert np.abs((X.T if shape[0] > shape[1] else X) - want).max() < 1e-12
+
+
+def test_orthogonalize_converges_to_an_orthogonal_matrix():
+    G = np.random.default_rng(3).standard_normal((6, 11))
+    X = to.orthogonalize(G, (1.875, -1.25, 0.375), 30, 0.0)[-1]
+    assert np.abs(X @ X.T - np.eye(6)).max() < 1e-12
