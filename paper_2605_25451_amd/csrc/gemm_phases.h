@@ -32,6 +32,9 @@ __device__ inline int source_row(const int32_t* source, int row, int src_rows) {
 // LDS layouts of a region of R rows x 64 k (the swizzles keep fragment reads free of bank conflicts):
 //   k-contiguous operand  [row][64 k]: 16-byte chunk c of row r sits at c ^ ((r >> 1) & 7)
 //   transposed operand    [k][R rows]: chunk c of k-row k sits at c ^ ((k & 3) << 2) ^ (((k >> 3) & 1) << 1)
+//                         R = 64: c ^ (k & 2) ^ (((k >> 3) & 1) << 2)
+// (a transpose read of 32 lanes takes 32 bytes of 8 k rows: k .. k + 3 and 8 rows further on.  Rows of 256 bytes all start in the same
+// bank, rows of 128 in two that are half of the banks apart)
 // A region is filled in LOADS loads per wavefront of WAVES; load i of wavefront w writes the 1 KiB run i*WAVES + w.
 template <int R, bool TR, int WAVES = 8>
 struct Region {
@@ -44,7 +47,7 @@ struct Region {
   static __device__ inline void place(int i, int wave, int lane, int* row, int* chunk) {
     const int r = (i * WAVES + wave) * RPL + lane / CPR;
     *row = r;
-    *chunk = (lane % CPR) ^ (TR ? ((r & 3) << 2) ^ (((r >> 3) & 1) << 1) : (r >> 1) & 7);
+    *chunk = (lane % CPR) ^ (TR ? (R == 64 ? (r & 2) ^ (((r >> 3) & 1) << 2) : ((r & 3) << 2) ^ (((r >> 3) & 1) << 1)) : (r >> 1) & 7);
   }
   // row0: this region's first row in the tile; rows past rows_left (counted from the tile's first row)
   // are clamped into the matrix: their products are never stored.
@@ -102,7 +105,8 @@ struct Fragments {
         // the 16 lanes of group gi read a 4(k) x 16(row) block, 8 bytes each; the transpose read
         // hands lane s row s with 4 consecutive k; two reads give 8 k
         const int k = gi * 8 + (s >> 2);
-        const int c = (row0 / 8 + q * 2 + ((s & 3) >> 1)) ^ ((s >> 2) << 2) ^ ((gi & 1) << 1);
+        const int c = R == 64 ? (row0 / 8 + q * 2 + ((s & 3) >> 1)) ^ ((s >> 2) & 2) ^ ((gi & 1) << 2)
+                              : (row0 / 8 + q * 2 + ((s & 3) >> 1)) ^ ((s >> 2) << 2) ^ ((gi & 1) << 1);
         addr[q] = k * (R * 2) + c * 16 + (s & 1) * 8;
       } else {
         addr[q] = (row0 + s) * (BK * 2) + ((q * 4 + gi) ^ (s >> 1)) * 16;

@@ -13,9 +13,11 @@
 // fall over three decades (hi alone all the time: 0.14 and 0.4-0.7 %).  For fp32 results all of X, A and B are hi + lo and every
 // product is three, hi hi + hi lo + lo hi: 3e-7 to 1.3e-6 off.
 // fp16's range: with powers of two s, t and u the buffers hold s X, t A and u B (see Scales).
+#include "gemm_phases.h"
 #include "train.h"
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 namespace bm {
@@ -24,7 +26,6 @@ namespace {
 
 typedef _Float16 half_t;
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int PAD = 64;                        // rows and columns of the buffers are whole 64, the rest zeros
 
@@ -35,7 +36,6 @@ __device__ inline void put(const Split& d, size_t i, float v) {
   d.hi[i] = h;
   if (d.lo) d.lo[i] = (half_t)(v - (float)h);
 }
-__device__ inline float get(const Split& d, size_t i) { return (float)d.hi[i] + (d.lo ? (float)d.lo[i] : 0.f); }
 
 enum { GRAM = 0, POLY, STEP, LAST };
 
@@ -48,6 +48,32 @@ struct Product {
   void* out; long ld_o, stride_o;              // LAST: [rows, cols] or, transposed, [cols, rows]
   int rows, cols, transposed, out_fp32;
 };
+
+__device__ inline half8 as_half(const bf16x8& v) { return __builtin_bit_cast(half8, v); }
+
+// up to 8 values of a row of the result
+__device__ inline void store_result(const Product& p, long at, int count, const float (&v)[8]) {
+  if (p.out_fp32) {
+    float* o = (float*)p.out + at;
+    if (count == 8 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+      *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<f32x4*>(o + 4) = f32x4{v[4], v[5], v[6], v[7]};
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < count) o[e] = v[e];
+  } else {
+    bf16_t* o = (bf16_t*)p.out + at;
+    if (count == 8 && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+      store16(o, v);
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < count) o[e] = (bf16_t)v[e];
+  }
+}
 
 // ---- norm and conversion ----------------------------------------------------------------------
 
@@ -111,82 +137,312 @@ __device__ inline void triangle_tile(int id, int n, int* tm, int* tn) {
   *tn = r + id - (r * n - r * (r - 1) / 2);
 }
 
-// One 64 x 64 tile: four wavefronts of 32 x 32.  NN: B lies [K, N], else [N, K].
-template <int KIND>
-__global__ __launch_bounds__(256) void small_product_kernel(Product p, int tiles, int tiles_n) {
-  constexpr bool NN = KIND == STEP || KIND == LAST, SYMMETRIC = !NN;
-  constexpr int LD = 72;                       // halves of an LDS row: 144 bytes, so that rows differ in their banks
-  __shared__ __attribute__((aligned(16))) half_t sa[64 * LD], sb[64 * LD];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int b = blockIdx.x / tiles, t = blockIdx.x % tiles;
-  int tm, tn;
-  if (SYMMETRIC) triangle_tile(t, tiles_n, &tm, &tn);
-  else { tm = t / tiles_n; tn = t % tiles_n; }
-  const int m0 = tm * 64, n0 = tn * 64;
-  f32x4 acc[2][2] = {};
-  for (int term = 0; term < p.terms; ++term) {
-    const half_t* A = (term == 2 ? p.A.lo : p.A.hi) + b * p.stride_a;
-    const half_t* B = (term == 1 ? p.B.lo : p.B.hi) + b * p.stride_b;
-    for (int k0 = 0; k0 < p.K; k0 += 64) {
-      half8 ra[2], rb[2];
+// v of a block behind alpha and beta; 16-byte pieces of rows as hi and lo
+struct Halves { half8 hi, lo; };
+__device__ inline void split8(const float (&v)[8], half8* hi, half8* lo) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int id = threadIdx.x + i * 256, r = id >> 3, c = (id & 7) * 8;
-        ra[i] = *reinterpret_cast<const half8*>(A + (size_t)(m0 + r) * p.lda + k0 + c);
-        rb[i] = *reinterpret_cast<const half8*>(NN ? B + (size_t)(k0 + r) * p.ldb + n0 + c : B + (size_t)(n0 + r) * p.ldb + k0 + c);
+  for (int e = 0; e < 8; ++e) {
+    (*hi)[e] = (half_t)v[e];
+    (*lo)[e] = (half_t)(v[e] - (float)(*hi)[e]);
+  }
+}
+
+// ---- epilogue of one wavefront: FM x FN blocks of 16 x 16, in strips of 16 rows.  The MFMAs run with swapped operands: of
+// block (i, j) a lane holds row l % 16 and 4 columns from 4 (l / 16) on.  A strip goes through the wavefront's own LDS, so that
+// rows are read and written 16 bytes per lane; a tile above the diagonal, or a result that is transposed, is read
+// back by columns from there.  Sizes are whole 64, so a strip lies inside the matrix or outside.
+//   row_of(i)  first row of strip i;  col0  first column;  mirror  the tile lies above the diagonal
+//   stage      16 x (16 FN + 4) floats of LDS, free once `last` has returned
+// `old` is requested two strips ahead, the first two strips before the tile's last MFMAs (`last`).
+template <int KIND, int FM, int FN, typename RowOf, typename Last>
+__device__ inline void finish(const Product& p, int b, f32x4 (&acc)[FM][FN], float* stage, int lane, int col0, bool mirror,
+                              RowOf row_of, Last last) {
+  constexpr int W = FN * 16, SLD = W + 4;
+  constexpr int LPR = W / 8, RPI = 64 / LPR, TPS = 16 / RPI;            // lanes of a row, rows of an access, accesses of a strip
+  constexpr int DOWN = 16 * W / 64;                                     // rows of a lane in a column
+  const int m_in = lane & 15, q4 = (lane >> 4) * 4;
+  const int rcol = (lane % LPR) * 8, rrow = lane / LPR;
+  const int down_col = lane % W, down_row = lane / W * DOWN;
+  const size_t at0 = b * p.stride_c;
+  Halves pre[2][TPS];
+  auto request = [&](auto i_t) {
+    constexpr int i = decltype(i_t)::value;
+    if (KIND == GRAM || i >= FM) return;
+    if (row_of(i) >= p.M || col0 >= p.N) return;
+#pragma unroll
+    for (int t = 0; t < TPS; ++t) {
+      const size_t at = at0 + (size_t)(row_of(i) + t * RPI + rrow) * p.ldc + col0 + rcol;
+      pre[i & 1][t].hi = *reinterpret_cast<const half8*>(p.old.hi + at);
+      if (p.old.lo) pre[i & 1][t].lo = *reinterpret_cast<const half8*>(p.old.lo + at);
+      else pre[i & 1][t].lo = half8{};
+    }
+  };
+  request(std::integral_constant<int, 0>{});
+  request(std::integral_constant<int, 1>{});
+  last();
+  if (col0 >= p.N) return;
+  const bool down = mirror || (KIND == LAST && p.transposed);
+  const long out0 = b * p.stride_o;
+  static_for<FM>([&](auto i_t) {
+    constexpr int i = decltype(i_t)::value;
+    if (row_of(i) >= p.M) return;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) *reinterpret_cast<f32x4*>(stage + m_in * SLD + j * 16 + q4) = acc[i][j];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int t = 0; t < TPS; ++t) {
+      const int row = t * RPI + rrow, r = row_of(i) + row, c = col0 + rcol;
+      float* piece = stage + row * SLD + rcol;
+      const f32x4 x0 = *reinterpret_cast<const f32x4*>(piece), x1 = *reinterpret_cast<const f32x4*>(piece + 4);
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[e] = p.alpha * (e < 4 ? x0[e] : x1[e - 4]);
+        if (KIND != GRAM) v[e] += p.beta * ((float)pre[i & 1][t].hi[e] + (float)pre[i & 1][t].lo[e]);
       }
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int id = threadIdx.x + i * 256, r = id >> 3, c = (id & 7) * 8;
-        *reinterpret_cast<half8*>(sa + r * LD + c) = ra[i];
-        if (NN) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sb[(c + e) * LD + r] = rb[i][e];
-        } else {
-          *reinterpret_cast<half8*>(sb + r * LD + c) = rb[i];
-        }
+      if (down) {
+        *reinterpret_cast<f32x4*>(piece) = f32x4{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f32x4*>(piece + 4) = f32x4{v[4], v[5], v[6], v[7]};
       }
-      __syncthreads();
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        half8 fa[2], fb[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          fa[i] = *reinterpret_cast<const half8*>(sa + ((wave >> 1) * 32 + i * 16 + (lane & 15)) * LD + ks * 32 + (lane >> 4) * 8);
-          fb[i] = *reinterpret_cast<const half8*>(sb + ((wave & 1) * 32 + i * 16 + (lane & 15)) * LD + ks * 32 + (lane >> 4) * 8);
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+      if constexpr (KIND == LAST) {
+        if (!p.transposed && r < p.rows) store_result(p, out0 + r * p.ld_o + c, min(8, p.cols - c), v);
+      } else {
+        half8 hi, lo;
+        split8(v, &hi, &lo);
+        const size_t at = at0 + (size_t)r * p.ldc + c;
+        *reinterpret_cast<half8*>(p.C.hi + at) = hi;
+        if (p.C.lo) *reinterpret_cast<half8*>(p.C.lo + at) = lo;
       }
     }
-  }
-  Split C = p.C, old = p.old;
-  if (KIND != LAST) { C.hi += b * p.stride_c; if (C.lo) C.lo += b * p.stride_c; }
-  if (KIND != GRAM) { old.hi += b * p.stride_c; if (old.lo) old.lo += b * p.stride_c; }
+    if (down) {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      const int r = col0 + down_col, c0 = row_of(i) + down_row;           // of the transposed matrix
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+      for (int q = 0; q < DOWN; q += 8) {
+        float v[8];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = m0 + (wave >> 1) * 32 + i * 16 + (lane >> 4) * 4 + e, c = n0 + (wave & 1) * 32 + j * 16 + (lane & 15);
-        const size_t at = (size_t)r * p.ldc + c;
-        float v = p.alpha * acc[i][j][e];
-        if (KIND != GRAM) v += p.beta * get(old, at);
-        if (KIND == LAST) {
-          if (r < p.rows && c < p.cols) {
-            const long o = b * p.stride_o + (p.transposed ? c * p.ld_o + r : r * p.ld_o + c);
-            if (p.out_fp32) ((float*)p.out)[o] = v;
-            else ((bf16_t*)p.out)[o] = (bf16_t)v;
-          }
+        for (int e = 0; e < 8; ++e) v[e] = stage[(down_row + q + e) * SLD + down_col];
+        if constexpr (KIND == LAST) {
+          if (r < p.cols) store_result(p, out0 + r * p.ld_o + c0 + q, min(8, p.rows - c0 - q), v);
         } else {
-          put(C, at, v);
-          if (SYMMETRIC && tm != tn) put(C, (size_t)c * p.ldc + r, v);
+          half8 hi, lo;
+          split8(v, &hi, &lo);
+          const size_t at = at0 + (size_t)r * p.ldc + c0 + q;
+          *reinterpret_cast<half8*>(p.C.hi + at) = hi;
+          if (p.C.lo) *reinterpret_cast<half8*>(p.C.lo + at) = lo;
         }
       }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    request(std::integral_constant<int, i + 2>{});
+  });
+}
+
+// Where a workgroup's tile lies.  Workgroups of one XCD have neighbouring tiles.
+struct Place { int b, tm, tn; };
+template <bool SYMMETRIC>
+__device__ inline Place place(int tiles_m, int tiles_n, int tiles) {
+  const int id = xcd_run(blockIdx.x, gridDim.x), t = id % tiles;
+  Place q;
+  q.b = id / tiles;
+  if (SYMMETRIC) triangle_tile(t, tiles_n, &q.tm, &q.tn);
+  else grouped_tile<4>(t, tiles_m, tiles_n, &q.tm, &q.tn);
+  q.tm = __builtin_amdgcn_readfirstlane(q.tm);              // (the root is taken in vector registers)
+  q.tn = __builtin_amdgcn_readfirstlane(q.tn);
+  return q;
+}
+
+// A slice's operands: terms of K / 64 slices each, hi hi, hi lo, lo hi.
+template <bool B_TR>
+struct Operands {
+  const bf16_t *a[2], *b[2];
+  int slices;                                  // of a term
+  size_t b_step;
+  __device__ inline Operands(const Product& p, const Place& q, int m0, int n0) {
+    const size_t ao = q.b * p.stride_a + (size_t)m0 * p.lda, bo = q.b * p.stride_b + (B_TR ? (size_t)n0 : (size_t)n0 * p.ldb);
+    a[0] = reinterpret_cast<const bf16_t*>(p.A.hi + ao);
+    b[0] = reinterpret_cast<const bf16_t*>(p.B.hi + bo);
+    a[1] = p.terms > 1 ? reinterpret_cast<const bf16_t*>(p.A.lo + ao) : a[0];
+    b[1] = p.terms > 1 ? reinterpret_cast<const bf16_t*>(p.B.lo + bo) : b[0];
+    slices = p.K / BK;
+    b_step = B_TR ? (size_t)BK * p.ldb : (size_t)BK;
+  }
+  __device__ inline const bf16_t* a_at(int j) const {
+    const int t = (j >= slices) + (j >= 2 * slices);
+    return (t == 2 ? a[1] : a[0]) + (size_t)(j - t * slices) * BK;
+  }
+  __device__ inline const bf16_t* b_at(int j) const {
+    const int t = (j >= slices) + (j >= 2 * slices);
+    return (t == 1 ? b[1] : b[0]) + (size_t)(j - t * slices) * b_step;
+  }
+};
+
+// ---- TILE x TILE (64 or 128), four wavefronts of a quarter each.  DEPTH slices of LDS: DEPTH - 1 are on their way while one is
+// multiplied, with one barrier a slice.
+template <int KIND, int TILE, int DEPTH>
+__global__ __launch_bounds__(256) void small_product_kernel(Product p, int tiles_m, int tiles_n, int tiles) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  constexpr bool NN = KIND == STEP || KIND == LAST;
+  using RegA = Region<TILE, false, 4>;
+  using RegB = Region<TILE, NN, 4>;
+  constexpr uint32_t B0 = RegA::BYTES, BUF = B0 + RegB::BYTES;
+  constexpr int LOADS = RegA::LOADS + RegB::LOADS, F = TILE / 32, HALF = TILE / 2;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  const Place q = place<!NN>(tiles_m, tiles_n, tiles);
+  const int m0 = q.tm * TILE, n0 = q.tn * TILE;
+  const Operands<NN> op(p, q, m0, n0);
+  const int n = op.slices * p.terms;
+  RegA ra;
+  RegB rb;
+  ra.init(p.lda, 0, p.M - m0, wave, lane);
+  rb.init(p.ldb, 0, p.N - n0, wave, lane);
+  auto load = [&](int j, uint32_t buf) {
+    rb.template load<false>(op.b_at(j), p.ldb, BK, buf + B0, wave, lane);
+    ra.template load<false>(op.a_at(j), p.lda, BK, buf, wave, lane);
+  };
+  Fragments<TILE, false, F> fa;
+  Fragments<TILE, NN, F> fb;
+  fa.init(wm * HALF, lane);
+  fb.init(wn * HALF, lane);
+  f32x4 acc[F][F] = {};
+#pragma unroll
+  for (int s = 0; s < DEPTH - 1; ++s)
+    if (s < n) load(s, s * BUF);
+  uint32_t cur = 0, free = (DEPTH - 1) * BUF;
+  for (int j = 0; j < n; ++j) {
+    // slice j has landed; later ones need not have
+    const int later = n - 1 - j;
+    if (later >= DEPTH - 2) wait_loads<(DEPTH - 2) * LOADS>();
+    else if (DEPTH > 3 && later == 1) wait_loads<LOADS>();
+    else wait_loads<0>();
+    end_phase();                                             // for all; and all have read slice j - 1
+    if (j + DEPTH - 1 < n) load(j + DEPTH - 1, free);
+    bf16x8 a[2][F], bb[2][F];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int f = 0; f < F; ++f) {
+        bb[ks][f] = fb.read(smem, f, ks, cur + B0);
+        a[ks][f] = fa.read(smem, f, ks, cur);
+      }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int c = 0; c < F; ++c)
+          acc[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half(bb[ks][c]), as_half(a[ks][i]), acc[i][c], 0, 0, 0);
+    wait_fragments();
+    free = cur;
+    cur = cur == (DEPTH - 1) * BUF ? 0 : cur + BUF;
+  }
+  end_phase();                                               // the strips overlay the slices
+  finish<KIND, F, F>(p, q.b, acc, reinterpret_cast<float*>(smem) + wave * 16 * (F * 16 + 4), lane, n0 + wn * HALF, !NN && q.tm != q.tn,
+                     [&](int i) { return m0 + wm * HALF + i * 16; }, [] {});
+}
+
+// ---- 256 x 256: two groups of four wavefronts that take turns between MFMAs and everything else, as in the bf16 kernels.
+__device__ inline void mfma16_half(f32x4& acc, const bf16x8& a, const bf16x8& b) {
+  asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+}
+
+template <int KIND>
+__global__ __launch_bounds__(512, 2) void large_product_kernel(Product p, int tiles_m, int tiles_n, int tiles) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  constexpr bool NN = KIND == STEP || KIND == LAST;
+  using RegA = Region<128, false>;
+  using RegB = Region<256, NN>;
+  constexpr uint32_t A1 = RegA::BYTES, B0 = 2 * RegA::BYTES, BUF = B0 + RegB::BYTES;
+  constexpr int LATE = RegA::LOADS, EARLY = RegA::LOADS + RegB::LOADS;   // loads of a slice's two parts
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 2, wn = wave & 3;                                 // wm is the group
+  const Place q = place<!NN>(tiles_m, tiles_n, tiles);
+  const int m0 = q.tm * 256, n0 = q.tn * 256;
+  const Operands<NN> op(p, q, m0, n0);
+  const int n = op.slices * p.terms;
+  RegA ra0, ra1;
+  RegB rb;
+  ra0.init(p.lda, 0, p.M - m0, wave, lane);
+  ra1.init(p.lda, 128, p.M - m0, wave, lane);
+  rb.init(p.ldb, 0, p.N - n0, wave, lane);
+  auto load_early = [&](int j, uint32_t buf) {
+    rb.template load<false>(op.b_at(j), p.ldb, BK, buf + B0, wave, lane);
+    ra0.template load<false>(op.a_at(j), p.lda, BK, buf, wave, lane);
+  };
+  auto load_late = [&](int j, uint32_t buf) { ra1.template load<false>(op.a_at(j), p.lda, BK, buf + A1, wave, lane); };
+  Fragments<128, false, 4> fa;
+  Fragments<256, NN, 4> fb;
+  fa.init(wm * 64, lane);
+  fb.init(wn * 64, lane);
+  bf16x8 af[2][4], bf[2][4];
+  f32x4 acc[8][4];
+  auto multiply = [&](auto half_t_) {
+    constexpr int H = decltype(half_t_)::value * 4;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mfma16_half(acc[H + i][j], bf[ks][j], af[ks][i]);
+  };
+  // COME: slices that follow this one (2: two or more, 0: this is the last)
+  auto slice = [&](auto come_t, int j) {
+    constexpr int COME = decltype(come_t)::value;
+    const uint32_t buf = (j & 1) * BUF;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+      for (int f = 0; f < 4; ++f) bf[ks][f] = fb.read(smem, f, ks, buf + B0);
+#pragma unroll
+      for (int f = 0; f < 4; ++f) af[ks][f] = fa.read(smem, f, ks, buf);
+    }
+    if (COME >= 1) load_late(j + 1, buf ^ BUF);
+    wait_fragments();
+    // the second half of A of this slice is read next: everything older than the next slice's two parts must have landed
+    wait_loads<COME >= 1 ? EARLY + LATE : 0>();
+    end_phase();
+    multiply(Int<0>{});
+    wait_loads<COME >= 1 ? EARLY + LATE : 0>();
+    end_phase();
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int f = 0; f < 4; ++f) af[ks][f] = fa.read(smem, f, ks, buf + A1);
+    if (COME >= 2) load_early(j + 2, buf);
+    wait_fragments();
+    if (COME == 0) { end_phase(); return; }                 // the last MFMAs belong to the epilogue
+    wait_loads<COME >= 2 ? EARLY + LATE : LATE>();
+    end_phase();
+    multiply(Int<1>{});
+    wait_loads<COME >= 2 ? EARLY + LATE : LATE>();
+    end_phase();
+  };
+  load_early(0, 0);
+  load_late(0, 0);
+  if (n > 1) load_early(1, BUF);
+  {
+    bf16x8 z = {};
+    asm volatile("s_nop 7" : "+v"(z));
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) mfma16_first(acc[i][j], z, z);
+  }
+  if (n > 1) wait_loads<EARLY + LATE>();
+  else wait_loads<0>();
+  end_phase();
+  if (wm == 1) end_phase();                                 // group 1 stays one phase behind
+  for (int j = 0; j < n - 2; ++j) slice(Int<2>{}, j);
+  if (n > 1) slice(Int<1>{}, n - 2);
+  slice(Int<0>{}, n - 1);
+  finish<KIND, 8, 4>(p, q.b, acc, reinterpret_cast<float*>(smem) + wave * 16 * 68, lane, n0 + wn * 64, !NN && q.tm != q.tn,
+                     [&](int i) { return m0 + (i >> 2) * 128 + wm * 64 + (i & 3) * 16; },
+                     [&] {
+                       multiply(Int<1>{});
+                       if (wm == 0) end_phase();            // its strips overlay what group 1 has just read
+                       settle(acc);
+                     });
 }
 
 // ---- host -----------------------------------------------------------------------------------------
@@ -250,14 +506,41 @@ struct Workspace {
   }
 };
 
-template <int KIND>
-bm_status launch(const Product& p, int batch, hipStream_t st) {
-  const int tm = p.M / 64, tn = p.N / 64;
-  const int tiles = KIND == GRAM || KIND == POLY ? tm * (tm + 1) / 2 : tm * tn;
-  ProfScope prof(KIND == GRAM || KIND == POLY ? PROF_GEMM_NT : PROF_GEMM_NN, 2.0 * batch * p.M * p.N * p.K, st);
-  hipLaunchKernelGGL(small_product_kernel<KIND>, dim3((unsigned)((long)tiles * batch)), dim3(256), 0, st, p, tiles, tn);
+// dynamic LDS beyond 64 KiB, allowed once on each device
+template <typename Kernel>
+bm_status allow_lds(Kernel kern, size_t lds, std::atomic<uint64_t>* done) {
+  int dev = 0;
+  BM_CHECK_HIP(hipGetDevice(&dev));
+  const uint64_t bit = 1ull << (dev & 63);
+  if (done->load(std::memory_order_relaxed) & bit) return BM_OK;
+  BM_CHECK_HIP(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+  if (dev < 64) done->fetch_or(bit, std::memory_order_relaxed);
+  return BM_OK;
+}
+
+template <int KIND, int TILE>
+bm_status launch_tile(const Product& p, int batch, hipStream_t st) {
+  constexpr bool SYMMETRIC = KIND == GRAM || KIND == POLY;
+  constexpr int DEPTH = TILE == 256 ? 2 : TILE == 128 ? 2 : 4;
+  constexpr size_t lds = (size_t)DEPTH * 2 * TILE * BK * sizeof(half_t);
+  void (*kern)(Product, int, int, int);
+  if constexpr (TILE == 256) kern = large_product_kernel<KIND>;
+  else kern = small_product_kernel<KIND, TILE, DEPTH>;
+  static std::atomic<uint64_t> done{0};
+  BM_RETURN_IF(allow_lds(kern, lds, &done));
+  const int tm = cdiv(p.M, TILE), tn = cdiv(p.N, TILE), tiles = SYMMETRIC ? tm * (tm + 1) / 2 : tm * tn;
+  ProfScope prof(SYMMETRIC ? PROF_GEMM_NT : PROF_GEMM_NN, (SYMMETRIC ? 1.0 : 2.0) * batch * p.terms * p.M * p.N * p.K, st);
+  hipLaunchKernelGGL(kern, dim3((unsigned)((long)tiles * batch)), dim3(TILE == 256 ? 512 : 256), lds, st, p, tm, tn, tiles);
   BM_CHECK_LAUNCH("orthogonalize product");
   return BM_OK;
+}
+
+template <int KIND>
+bm_status launch(const Product& p, int batch, hipStream_t st) {
+  const long t256 = (long)cdiv(p.M, 256) * cdiv(p.N, 256) * batch, t128 = (long)cdiv(p.M, 128) * cdiv(p.N, 128) * batch;
+  if (t256 >= 128) return launch_tile<KIND, 256>(p, batch, st);
+  if (t128 >= 256) return launch_tile<KIND, 128>(p, batch, st);
+  return launch_tile<KIND, 64>(p, batch, st);
 }
 
 bool sizes_ok(int dtype, int batch, int M, int N) {
