@@ -274,6 +274,33 @@ def test_masks_infinities_and_labels_that_are_none(V, dtype):
     check_loss(None, grad[1:2], z64[1:2], labels[1:2], None, dtype)
 
 
+@pytest.mark.parametrize("ignored", ["none", "all", "most", "first", "last"])
+@pytest.mark.parametrize("T,V", [(2100, 2049), (9000, 130), (530000, 16), (700, 33000), (1100, 20000), (300, 66000)])
+def test_more_rows_than_workgroups(T, V, ignored):
+    """Every row is written once, wherever the ignored ones stand; compared with the formula in fp32 on the GPU."""
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(T)
+    z = 2 * torch.randn((T, V), device="cuda", generator=g)
+    labels = torch.randint(0, V, (T,), device="cuda", generator=g, dtype=torch.int32)
+    at = torch.arange(T, device="cuda")
+    out = {"none": at < 0, "all": at >= 0, "most": torch.rand(T, device="cuda", generator=g) < 0.9, "first": at < T // 2,
+           "last": at >= T // 2}[ignored]
+    labels[out] = -1
+    z[out] = float("nan")
+    grad = torch.full_like(z, 9.0)
+    loss = cross_entropy(1, T, V, z, V, labels, None, grad, V)
+    live = ~out
+    assert (loss[out] == 0).all() and (grad[out] == 0).all()
+    x, lab = z[live].double(), labels[live].long()
+    p = torch.softmax(x, 1)
+    want = torch.logsumexp(x, 1) - x.gather(1, lab[:, None])[:, 0]
+    p.scatter_add_(1, lab[:, None], -torch.ones_like(lab, dtype=torch.float64)[:, None])
+    # logits within 12 of one another: 3 * 24 + 6 roundings of a term, V/256 + 64 of their sum, and of the loss's own parts
+    assert ((loss[live] - want).abs() <= (3 * 24 + 200 + 3 * V / 256 + 60) * F).all()
+    assert ((grad[live] - p).abs() <= (2 * (3 * 24 + 6) + 70 + 3 * V / 256) * F * (p.abs() + 1)).all()
+
+
 # ---- as a program calls them ---------------------------------------------------------------------------
 
 def test_another_stream_and_replays_of_a_captured_step():
