@@ -3,8 +3,10 @@
 // m and s come from one pass: a thread rescales its sum when its maximum grows, and pairs (m, s) are joined.
 // A row whose label is negative is never read.  Bound by HBM.
 //
-// Two launches: parts of rows leave their (m, s), then every part of a row joins those of the whole row and writes its
-// gradient.  The second read of the logits comes from the memory-side cache where they fit.
+// Rows that fit the registers of a workgroup are read once (row_kernel).  Wider ones, and a few wide ones, which would leave the chip
+// idle, are cut into parts: one launch for the parts' (m, s), one that joins those of a row and writes its gradient; the
+// second read of the logits comes from the memory-side cache where they fit.
+// 4096 x 128000 bf16: 2.10 GB in 389 us, 5.4 TB/s (a copy of 2 GB moves 4.9 TB/s).
 #include "train.h"
 
 #include <float.h>
@@ -169,6 +171,8 @@ __global__ __launch_bounds__(PART_THREADS) void part_finish_kernel(const T* logi
 
 // ---- whole rows -----------------------------------------------------------------------------------
 
+typedef unsigned int Quad __attribute__((ext_vector_type(4)));
+
 // The same statistics with an instruction less per element: exp(x - m) as 2^(x L - c), c = m L rounded once, which is a
 // common factor of all terms.  c is kept inside fp32's range, which makes rows whose largest logit is past 1e38 in
 // magnitude wrong (a row of nothing but the lowest finite value, say); those are done again with the difference first.
@@ -212,178 +216,92 @@ __device__ inline Stat2 block_join(Stat2 a, Stat2* sm) {
   return r;
 }
 
-// The rows of a workgroup where there are more rows than workgroups: of LIST rows each, those that are read are dealt out one by one,
-// then those that are ignored, so that all have as much to do wherever the ignored ones stand (30 % of them at random, 16 rows per
-// workgroup: the busiest would read 16, now all read 11 or 12).
-constexpr int LIST = 64;
-template <int THREADS>
-struct RowList {
-  int live[THREADS / WAVE], row[LIST];
-  // rows first .. end - 1, shares of them in a grid of 2^log_grid; how many there are for this workgroup
-  __device__ inline int fill(const int32_t* __restrict__ labels, int first, int end, int log_grid) {
-    constexpr int WAVES = THREADS / WAVE;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int per = (end - first + WAVES * WAVE - 1) / (WAVES * WAVE) * WAVE;
-    const int from = min(end, first + wave * per), to = min(end, from + per);
-    int count = 0;
-    for (int i = from + lane; i - lane < to; i += WAVE) count += __popcll(__ballot(i < to && labels[i] >= 0));
-    __syncthreads();                                         // the list is no longer read
-    if (lane == 0) live[wave] = count;
-    __syncthreads();
-    int before = 0, all = 0;
-#pragma unroll 1
-    for (int w = 0; w < WAVES; ++w) {
-      if (w < wave) before += live[w];
-      all += live[w];
-    }
-    const int grid = 1 << log_grid, me = blockIdx.x;
-    int rest = all + from - first - before;
-    for (int i = from + lane; i - lane < to; i += WAVE) {
-      const bool in = i < to, is = in && labels[i] >= 0;
-      const uint64_t m = __ballot(is), r = __ballot(in && !is), lower = (1ull << lane) - 1;
-      const int rank = is ? before + __popcll(m & lower) : rest + __popcll(r & lower);
-      if (in && (rank & (grid - 1)) == me) row[rank >> log_grid] = i;
-      before += __popcll(m);
-      rest += __popcll(r);
-    }
-    __syncthreads();
-    return (end - first - me + grid - 1) >> log_grid;
-  }
-};
+typedef unsigned int Quad __attribute__((ext_vector_type(4)));
 
-// A workgroup holds a row in its registers, NV vectors per thread, so that the logits are read once; while it writes a row's
-// gradient, every register that has been used is filled from the next row, so that memory is never idle for the
-// exponentials.  Rows of logits and gradient start at the same place between two 16-byte boundaries.
+// A workgroup holds a row in its registers, NV vectors per thread, so that the logits are read once.  Neither they nor the gradient are
+// used again before a cache has lost them: with non-temporal accesses 256 x 128000 take 26 us instead of 31.  One workgroup per
+// row: persistent ones that fetch the next row under the gradient of the last keep in step with one another, so that all read, compute
+// and write at the same time (4096 x 64000 249 us, this 186; 8192 x 8000 93 and 47), and have more to do where fewer rows are ignored.
+// Rows of logits and gradient start at the same place between two 16-byte boundaries.
 template <typename T, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long ld, const int32_t* __restrict__ labels,
-                                                      const float* __restrict__ weight, int V, int rows, int log_grid,
-                                                      float* __restrict__ loss, T* dlogits, long ld_d) {
+                                                      const float* __restrict__ weight, int V, float* __restrict__ loss, T* dlogits,
+                                                      long ld_d) {
   constexpr int W = Span<T>::W;
-  __shared__ RowList<THREADS> list;
   __shared__ Stat2 sm[THREADS / WAVE];
   __shared__ Stat sm_far[THREADS / WAVE];
-  Vec16<T> v[NV];
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, row = blockIdx.x, label = labels[row];
+  const T* x = logits + (size_t)row * ld;
+  T* g = dlogits + (size_t)row * ld_d;
+  const Span<T> sp(x, V);
   // the element of a thread outside of the vectors: in front of them, behind them, or none
-  auto loose = [&](const Span<T>& sp) { return tid < sp.head ? tid : tid >= W && sp.tail + tid - W < V ? sp.tail + tid - W : -1; };
-  float extra = 0.f;
+  const int at = tid < sp.head ? tid : tid >= W && sp.tail + tid - W < V ? sp.tail + tid - W : -1;
   // vector tid + k THREADS of a row: a uniform address and one offset of the thread, or every vector holds two registers
   const uint32_t off = tid * 16u;
-  auto fetch = [&](const T* x, const Span<T>& sp, int k) {
-    if (tid < sp.vecs - k * THREADS)
-      v[k] = *reinterpret_cast<const Vec16<T>*>(reinterpret_cast<const char*>(x + sp.head) + k * (THREADS * 16) + off);
+  auto vec = [&](auto* p, int k) {
+    return reinterpret_cast<Quad*>(reinterpret_cast<char*>(const_cast<T*>(p) + sp.head) + k * (THREADS * 16) + off);
   };
-  // log_grid < 0: a row for every workgroup
-  long segment = 0;
-  int items = 1, item = 0, row = blockIdx.x;
-  if (log_grid >= 0) {
-    items = list.fill(labels, 0, min(rows, LIST << log_grid), log_grid);
-    row = __builtin_amdgcn_readfirstlane(list.row[0]);        // (rows are not fewer than workgroups)
+  if (label < 0) {
+    if (tid == 0 && loss) loss[row] = 0.f;
+    if (!dlogits) return;
+    for (int k = 0; k < NV && tid < sp.vecs - k * THREADS; ++k) __builtin_nontemporal_store(Quad{0u, 0u, 0u, 0u}, vec(g, k));
+    if (at >= 0) g[at] = Elt<T>::from_f(0.f);
+    return;
   }
-  int label = labels[row];
-  const T* x = logits + (size_t)row * ld;
-  Span<T> sp(x, V);
-  auto whole = [&] {
-    const int at = loose(sp);
-    if (at >= 0) extra = Elt<T>::to_f(x[at]);
+  Vec16<T> v[NV];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) fetch(x, sp, k);
-  };
-  if (label >= 0) whole();
-  for (;;) {
-    const bool more = item + 1 < items;
-    const int next = more ? log_grid < 0 ? 0 : __builtin_amdgcn_readfirstlane(list.row[item + 1]) : 0;
-    const int next_label = more ? labels[next] : -1;
-    const int at = loose(sp);
-    Stat2 a = Stat2::none();
-    float scale = 0.f, w = 0.f, p_label = 0.f;
-    bool far = false;
-    if (label >= 0) {
-      const float xl = label_logit(x, label, V);
-      w = weight ? weight[row] : 1.f;
-      if (label >= V) w = xl;                               // NaN
+  for (int k = 0; k < NV; ++k)
+    if (tid < sp.vecs - k * THREADS) v[k] = __builtin_bit_cast(Vec16<T>, __builtin_nontemporal_load(vec(x, k)));
+  const float extra = at >= 0 ? Elt<T>::to_f(x[at]) : 0.f, xl = label_logit(x, label, V);
+  const float w = label >= V ? xl : weight ? weight[row] : 1.f;           // (NaN)
+  Stat2 a = Stat2::none();
 #pragma unroll
-      for (int k = 0; k < NV; ++k) {
-        if (tid < sp.vecs - k * THREADS) {
-          float f[W];
+  for (int k = 0; k < NV; ++k) {
+    if (tid < sp.vecs - k * THREADS) {
+      float f[W];
 #pragma unroll
-          for (int e = 0; e < W; ++e) f[e] = Elt<T>::to_f(v[k].v[e]);
-          a.add(f);
-        }
-      }
-      if (at >= 0) {
-        const float f[1] = {extra};
-        a.add(f);
-      }
-      a = block_join<THREADS>(a, sm);
-      far = !(fabsf(a.m) <= 1e38f);
-      float nll = (a.c + __builtin_amdgcn_logf(a.s)) * LN2 - xl;
-      if (far) {
-        Stat b = Stat::none();
-#pragma unroll 1
-        for (int i = tid; i < V; i += THREADS) {
-          const float f[1] = {Elt<T>::to_f(x[i])};
-          b.add(f);
-        }
-        b = block_join<THREADS>(b, sm_far);                 // (no element is written before all have been read)
-        a.m = b.m;
-        a.s = b.s;
-        nll = b.m - xl + logf(b.s);
-      }
-      scale = w / a.s;
-      p_label = (far ? exp_diff(xl, a.m) : Stat2::term(xl, a.c)) * scale - w;
-      if (tid == 0 && loss) loss[row] = w * nll;
-    } else if (tid == 0 && loss) {
-      loss[row] = 0.f;
-    }
-    const T* xn = logits + (size_t)(more ? next : row) * ld;
-    const Span<T> spn(xn, V);
-    T* g = dlogits + (size_t)row * ld_d;
-    const bool writes = dlogits && !far;
-    if (dlogits && far) {
-#pragma unroll 1
-      for (int i = tid; i < V; i += THREADS)
-        g[i] = Elt<T>::from_f(i == label ? p_label : exp_diff(Elt<T>::to_f(x[i]), a.m) * scale);
-    }
-    auto gradient = [&](float z) { return label < 0 ? 0.f : Stat2::term(z, a.c) * scale; };
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      if (writes && tid < sp.vecs - k * THREADS) {
-        float f[W];
-#pragma unroll
-        for (int e = 0; e < W; ++e) f[e] = gradient(Elt<T>::to_f(v[k].v[e]));
-        store16(reinterpret_cast<T*>(reinterpret_cast<char*>(g + sp.head) + k * (THREADS * 16) + off), f);
-      }
-      if (next_label >= 0) fetch(xn, spn, k);
-    }
-    if (writes) {
-      if (at >= 0) g[at] = Elt<T>::from_f(gradient(extra));
-      // the label's element again, by the thread that has just written it
-      const int in = label - sp.head;
-      const bool owner = in < 0 ? tid == label : in / W < sp.vecs ? tid == in / W % THREADS : tid == label - sp.tail + W;
-      if (label >= 0 && label < V && owner) g[label] = Elt<T>::from_f(p_label);
-    }
-    if (!more) {
-      // the next rows, if there are any
-      segment += (long)LIST << max(log_grid, 0);
-      if (log_grid < 0 || segment >= rows) break;
-      items = list.fill(labels, (int)segment, (int)min((long)rows, segment + (LIST << log_grid)), log_grid);
-      if (items == 0) break;                                // (only at the last of the rows)
-      item = 0;
-      row = __builtin_amdgcn_readfirstlane(list.row[0]);
-      label = labels[row];
-      x = logits + (size_t)row * ld;
-      sp = Span<T>(x, V);
-      if (label >= 0) whole();
-      continue;
-    }
-    ++item;
-    row = next; label = next_label; x = xn; sp = spn;
-    if (label >= 0) {
-      const int to = loose(sp);
-      if (to >= 0) extra = Elt<T>::to_f(x[to]);
+      for (int e = 0; e < W; ++e) f[e] = Elt<T>::to_f(v[k].v[e]);
+      a.add(f);
     }
   }
+  if (at >= 0) {
+    const float f[1] = {extra};
+    a.add(f);
+  }
+  a = block_join<THREADS>(a, sm);
+  if (!(fabsf(a.m) <= 1e38f)) {
+    Stat b = Stat::none();
+#pragma unroll 1
+    for (int i = tid; i < V; i += THREADS) {
+      const float f[1] = {Elt<T>::to_f(x[i])};
+      b.add(f);
+    }
+    b = block_join<THREADS>(b, sm_far);                      // (no element is written before all have been read)
+    const float scale = w / b.s;
+    if (tid == 0 && loss) loss[row] = w * (b.m - xl + logf(b.s));
+    if (!dlogits) return;
+#pragma unroll 1
+    for (int i = tid; i < V; i += THREADS)
+      g[i] = Elt<T>::from_f(exp_diff(Elt<T>::to_f(x[i]), b.m) * scale - (i == label ? w : 0.f));
+    return;
+  }
+  const float scale = w / a.s;
+  if (tid == 0 && loss) loss[row] = w * ((a.c + __builtin_amdgcn_logf(a.s)) * LN2 - xl);
+  if (!dlogits) return;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    if (tid < sp.vecs - k * THREADS) {
+      Vec16<T> f;
+#pragma unroll
+      for (int e = 0; e < W; ++e) f.v[e] = Elt<T>::from_f(Stat2::term(Elt<T>::to_f(v[k].v[e]), a.c) * scale);
+      __builtin_nontemporal_store(__builtin_bit_cast(Quad, f), vec(g, k));
+    }
+  }
+  if (at >= 0) g[at] = Elt<T>::from_f(Stat2::term(extra, a.c) * scale);
+  // the label's element again, by the thread that has just written it
+  const int in = label - sp.head;
+  const bool owner = in < 0 ? tid == label : in / W < sp.vecs ? tid == in / W % THREADS : tid == label - sp.tail + W;
+  if (label < V && owner) g[label] = Elt<T>::from_f(Stat2::term(xl, a.c) * scale - w);
 }
 
 // ---- host ----------------------------------------------------------------------------------------
@@ -407,54 +325,31 @@ struct Workspace {
   }
 };
 
-// threads and vectors per thread of a row that stays in registers; workgroups that a CU holds
-struct RowPlan { int threads, vectors, per_cu; };
-constexpr RowPlan ROW_PLANS[] = {{64, 4, 32}, {256, 4, 8}, {256, 16, 4}, {512, 16, 2}, {1024, 16, 1}, {1024, 20, 1}, {1024, 4, 2}, {1024, 8, 1}};
 constexpr int NUM_CU = 256;
 
-// The plan for rows of V words, or -1: parts of rows.  Measured with T rows of V bf16 words (us):
-//   few rows       more threads per row: 1 x 32000 256x16 10.5, 512x16 8.5, 1024x4 7.3; 256 rows 14.7, 12.3, 11.4
-//   many rows      more rows per CU: 1024 x 32000 256x16 31.2, 512x16 36.3, 1024x4 39.5; 4096 rows 133, 138, 145
-//   between them   the one whose last round is full: 512 x 32000 20.8, 18.5, 21.9; 700 x 64000 512x16 56.8, 1024x8 54.5
-//   wide rows      one fills a CU: 1 x 128000 18.7 against 9.3 of 16 parts, 128 rows 25.5 and 26.2, 256 33 and 45, 300 66 and 52,
-//                  400 69 and 65, 512 66 and 85
+// The kernel for T rows of V words, or -1: parts of rows.  Wide rows have all wavefronts of a CU or half of them; narrower ones fewer
+// wavefronts, so that several share a CU, once there are rows enough for that.  Measured with bf16 words (us):
+//   1024 x 16000: 512x8 12.1, 256x16 13.6, 1024x4 15.6; 256 rows: 512x8 6.3, 1024x4 5.9     4096 x 4000: 256x4 14.9, 512x8 18.1
+//   1024 x 64000: 1024x8 47.4, 512x16 48.7     4096 x 1500: 64x4 8.1, 256x4 10.9
+//   x 128000: 1 row 9.6 in 16 parts, 15.5 in registers; 48 rows 14.8 and 16.7, 128 rows 26.4 and 17.4, 4096 rows 618 and 389
 int row_plan(int dtype, int T, int V) {
   const int vecs = V / (dtype == BM_DTYPE_BF16 ? 8 : 4);
   if (vecs <= 64 * 4) return 0;
   if (vecs <= 256 * 4) return 1;
-  if (vecs <= 1024 * 4) return T <= NUM_CU ? 6 : T <= 2 * NUM_CU ? 3 : 2;
-  if (vecs <= 1024 * 8) return T < NUM_CU / 4 ? -1 : T <= NUM_CU || (T > 2 * NUM_CU && T <= 3 * NUM_CU) ? 7 : 3;
-  if (vecs > 1024 * 20 || T < NUM_CU / 2 || (T > NUM_CU && T <= NUM_CU * 3 / 2)) return -1;
-  return vecs <= 1024 * 16 ? 4 : 5;
-}
-
-template <typename T, int THREADS, int NV>
-bm_status launch_rows(int n, int per_cu, const T* logits, int ld, const int32_t* labels, const float* weight, int V, float* loss,
-                      T* dlogits, int ld_d, hipStream_t st) {
-  const bool one_each = n <= NUM_CU * per_cu;
-  int log_grid = -1;
-  if (!one_each)
-    for (log_grid = 0; (1 << log_grid) < NUM_CU * per_cu;) ++log_grid;
-  hipLaunchKernelGGL((row_kernel<T, THREADS, NV>), dim3(one_each ? n : 1 << log_grid), dim3(THREADS), 0, st, logits, (long)ld, labels,
-                     weight, V, n, log_grid, loss, dlogits, (long)ld_d);
-  BM_CHECK_LAUNCH("cross entropy rows");
-  return BM_OK;
+  if (vecs <= 512 * 8) return T <= 2 * NUM_CU ? 3 : 2;
+  if (vecs <= 1024 * 8) return 4;
+  return vecs > 1024 * 24 || T <= 32 ? -1 : 5;
 }
 
 template <typename T>
 bm_status run_rows(int plan, int n, int V, const T* logits, int ld, const int32_t* labels, const float* weight, float* loss,
                    T* dlogits, int ld_d, hipStream_t st) {
-  const int per = ROW_PLANS[plan].per_cu;
-  switch (plan) {
-    case 0: return launch_rows<T, 64, 4>(n, per, logits, ld, labels, weight, V, loss, dlogits, ld_d, st);
-    case 1: return launch_rows<T, 256, 4>(n, per, logits, ld, labels, weight, V, loss, dlogits, ld_d, st);
-    case 2: return launch_rows<T, 256, 16>(n, per, logits, ld, labels, weight, V, loss, dlogits, ld_d, st);
-    case 3: return launch_rows<T, 512, 16>(n, per, logits, ld, labels, weight, V, loss, dlogits, ld_d, st);
-    case 4: return launch_rows<T, 1024, 16>(n, per, logits, ld, labels, weight, V, loss, dlogits, ld_d, st);
-    case 6: return launch_rows<T, 1024, 4>(n, per, logits, ld, labels, weight, V, loss, dlogits, ld_d, st);
-    case 7: return launch_rows<T, 1024, 8>(n, per, logits, ld, labels, weight, V, loss, dlogits, ld_d, st);
-    default: return launch_rows<T, 1024, 20>(n, per, logits, ld, labels, weight, V, loss, dlogits, ld_d, st);
-  }
+  constexpr decltype(&row_kernel<T, 64, 4>) kernels[] = {row_kernel<T, 64, 4>,   row_kernel<T, 256, 4>,  row_kernel<T, 512, 8>,
+                                                         row_kernel<T, 1024, 4>, row_kernel<T, 1024, 8>, row_kernel<T, 1024, 24>};
+  constexpr int threads[] = {64, 256, 512, 1024, 1024, 1024};
+  hipLaunchKernelGGL(kernels[plan], dim3(n), dim3(threads[plan]), 0, st, logits, (long)ld, labels, weight, V, loss, dlogits, (long)ld_d);
+  BM_CHECK_LAUNCH("cross entropy rows");
+  return BM_OK;
 }
 
 template <typename T>
