@@ -17,6 +17,8 @@
 // Bound by HBM: dy once, the rows of distinct words read and written in fp32.
 #include "train.h"
 
+#include <algorithm>
+
 namespace bm {
 
 namespace {
@@ -56,6 +58,9 @@ __global__ __launch_bounds__(256) void embed_kernel(const T* __restrict__ table,
 constexpr int BUCKET_BITS = 8, BUCKETS = 1 << BUCKET_BITS;
 constexpr int DIGIT_BITS = 10, DIGITS = 1 << DIGIT_BITS;
 constexpr int GROUP_THREADS = 1024, GROUP_WAVES = GROUP_THREADS / WAVE;
+constexpr int RANKED = 256;                    // tokens of a bucket that are ordered by comparing all with all ...
+constexpr int HELD = 8192;                     // ... and that are kept in LDS
+constexpr int BATCH = 8;                       // loads of ids in flight
 
 // a wavefront's share of n tokens, in whole 64
 __device__ inline int share(int n) { return (n + GROUP_WAVES * WAVE - 1) / (GROUP_WAVES * WAVE) * WAVE; }
@@ -63,21 +68,57 @@ __device__ inline int share(int n) { return (n + GROUP_WAVES * WAVE - 1) / (GROU
 // word[i], pos[i]: the id and the row of the i-th grouped token; *count: how many there are
 struct Grouped { int32_t *word, *pos, *word2, *pos2, *count; };
 
-__global__ __launch_bounds__(GROUP_THREADS) void group_kernel(const int32_t* __restrict__ ids, int n, int V, int digit_passes, Grouped g) {
+// f(index, id) for first <= index < last, 64 at a time and all lanes together (id -1 past the end); the ids are loaded in batches
+template <typename F>
+__device__ inline void for_ids(const int32_t* __restrict__ ids, int first, int last, int lane, F f) {
+  for (int i0 = first; i0 < last; i0 += BATCH * WAVE) {
+    int id[BATCH];
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) id[k] = ids[min(i0 + k * WAVE + lane, last - 1)];
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const int i = i0 + k * WAVE + lane;
+      if (i0 + k * WAVE < last) f(i, i < last ? id[k] : -1);
+    }
+  }
+}
+
+// digit_bits: of a pass, so that `digit_passes` of them hold the bits above the bucket's
+__global__ __launch_bounds__(GROUP_THREADS) void group_kernel(const int32_t* __restrict__ ids, int n, int V, int digit_passes, int digit_bits,
+                                                              Grouped g) {
   __shared__ int below[GROUP_WAVES], mine[GROUP_WAVES], wave_total[GROUP_WAVES];
   __shared__ int counts[GROUP_WAVES][DIGITS];
+  __shared__ int2 tokens[HELD];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int bucket = blockIdx.x;
-  // every wavefront has a contiguous range of whole 64 tokens
+  const uint64_t lower_lanes = (1ull << lane) - 1;
+  // every wavefront has a contiguous range
   const int per = share(n);
   const int first = min(n, wave * per), last = min(n, first + per);
+  auto bucket_of = [&](int id) { return (uint32_t)id < (uint32_t)V ? id & (BUCKETS - 1) : BUCKETS; };
+  // Where a lane has up to 64 ids, bit k of `hits` says that the k-th is one of the bucket's: the tokens are then collected without a
+  // second look at all ids.
+  const int steps = (last - first + WAVE - 1) / WAVE;
+  const bool marked = per <= 64 * WAVE;
   int lower = 0, own = 0;
-  for (int i = first + lane; i - lane < last; i += WAVE) {
-    const int id = i < last ? ids[i] : -1;
-    const int b = (uint32_t)id < (uint32_t)V ? id & (BUCKETS - 1) : BUCKETS;
-    lower += __popcll(__ballot(b < bucket));
-    own += __popcll(__ballot(b == bucket));
+  uint64_t hits = 0;
+  if (marked) {
+    int k = 0;
+    for_ids(ids, first, last, lane, [&](int, int id) {
+      const int b = bucket_of(id);
+      lower += b < bucket;
+      hits |= (uint64_t)(b == bucket) << k++;
+    });
+    own = __popcll(hits);
+  } else {
+    for_ids(ids, first, last, lane, [&](int, int id) {
+      const int b = bucket_of(id);
+      lower += b < bucket;
+      own += b == bucket;
+    });
   }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) { lower += __shfl_xor(lower, off, WAVE); own += __shfl_xor(own, off, WAVE); }
   if (lane == 0) { below[wave] = lower; mine[wave] = own; }
   __syncthreads();
   int base = 0, total = 0, at = 0;
@@ -89,32 +130,76 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_kernel(const int32_t* __r
   }
   if (bucket == BUCKETS - 1 && threadIdx.x == 0) *g.count = base + total;
   if (total == 0) return;
+  // f(place, index) for the marked ones, in order
+  auto collect = [&](auto f) {
+    int to = at;
+    for (int k = 0; k < steps; ++k) {
+      const bool hit = (hits >> k) & 1;
+      const uint64_t m = __ballot(hit);
+      if (hit) f(to + __popcll(m & lower_lanes), first + k * WAVE + lane);
+      to += __popcll(m);
+    }
+  };
+  const bool held = marked && total <= HELD;
+  if (held) {
+    collect([&](int to, int i) { tokens[to] = int2{ids[i], i}; });
+    if (total <= RANKED) {
+      // every token counts those that stand before it, the ones of lower words and the earlier ones of its own;
+      // GROUP_THREADS / RANKED threads a token
+      int* ranks = &counts[0][0];
+      if (threadIdx.x < total) ranks[threadIdx.x] = 0;
+      __syncthreads();
+      const int t = threadIdx.x % RANKED;
+      int2 me = int2{0, 0};
+      if (t < total) {
+        me = tokens[t];
+        int rank = 0;
+#pragma unroll 4
+        for (int j = threadIdx.x / RANKED; j < total; j += GROUP_THREADS / RANKED) {
+          const int other = tokens[j].x;
+          rank += other < me.x || (other == me.x && j < t);
+        }
+        atomicAdd(ranks + t, rank);
+      }
+      __syncthreads();
+      if (threadIdx.x < total) {
+        g.word[base + ranks[t]] = me.x;
+        g.pos[base + ranks[t]] = me.y;
+      }
+      return;
+    }
+  }
   // an odd number of passes ends in the other pair of arrays: start so that the last one ends in word/pos
   int32_t *word = (digit_passes & 1 ? g.word2 : g.word) + base, *pos = (digit_passes & 1 ? g.pos2 : g.pos) + base;
   int32_t *word_to = (digit_passes & 1 ? g.word : g.word2) + base, *pos_to = (digit_passes & 1 ? g.pos : g.pos2) + base;
-  for (int i = first + lane; i - lane < last; i += WAVE) {
-    const int id = i < last ? ids[i] : -1;
-    const bool in = (uint32_t)id < (uint32_t)V && (id & (BUCKETS - 1)) == bucket;
-    const uint64_t m = __ballot(in);
-    if (in) {
-      const int to = at + __popcll(m & ((1ull << lane) - 1));
-      word[to] = id;
-      pos[to] = i;
-    }
-    at += __popcll(m);
+  if (!marked) {
+    for_ids(ids, first, last, lane, [&](int i, int id) {
+      const bool in = bucket_of(id) == bucket;
+      const uint64_t m = __ballot(in);
+      if (m == 0) return;
+      if (in) {
+        const int to = at + __popcll(m & lower_lanes);
+        word[to] = id;
+        pos[to] = i;
+      }
+      at += __popcll(m);
+    });
+  } else if (!held || digit_passes == 0) {
+    collect([&](int to, int i) { word[to] = ids[i]; pos[to] = i; });
   }
-  // stable counting sorts by the bits above the bucket's, DIGIT_BITS at a time
+  // stable counting sorts by the bits above the bucket's, digit_bits at a time
   const int per_own = share(total);
   const int own_first = min(total, wave * per_own), own_last = min(total, own_first + per_own);
   for (int pass = 0; pass < digit_passes; ++pass) {
-    const int shift = BUCKET_BITS + pass * DIGIT_BITS;
-    for (int i = threadIdx.x; i < GROUP_WAVES * DIGITS; i += GROUP_THREADS) (&counts[0][0])[i] = 0;
+    const int shift = BUCKET_BITS + pass * digit_bits, mask = (1 << digit_bits) - 1;
+    if ((int)threadIdx.x <= mask)
+      for (int w = 0; w < GROUP_WAVES; ++w) counts[w][threadIdx.x] = 0;
     __syncthreads();                                       // (the tokens written above are visible behind it, too)
+    const bool from_lds = held && pass == 0;
     // the lanes with the same digit, by its bits; the first of them counts for all
     auto same = [&](bool in, int digit) {
       uint64_t m = __ballot(in);
-#pragma unroll
-      for (int b = 0; b < DIGIT_BITS; ++b) {
+      for (int b = 0; b < digit_bits; ++b) {
         const uint64_t v = __ballot((digit >> b) & 1);
         m &= (digit >> b) & 1 ? v : ~v;
       }
@@ -122,17 +207,20 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_kernel(const int32_t* __r
     };
     for (int i = own_first + lane; i - lane < own_last; i += WAVE) {
       const bool in = i < own_last;
-      const int digit = in ? (word[i] >> shift) & (DIGITS - 1) : 0;
+      const int digit = in ? ((from_lds ? tokens[i].x : word[i]) >> shift) & mask : 0;
       const uint64_t m = same(in, digit);
-      if (in && (m & ((1ull << lane) - 1)) == 0) counts[wave][digit] += __popcll(m);
+      if (in && (m & lower_lanes) == 0) counts[wave][digit] += __popcll(m);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
     __syncthreads();
     // counts -> first places: over the digits, and within one over the wavefronts
     static_assert(DIGITS == GROUP_THREADS, "a thread per digit");
+    const bool digit_here = (int)threadIdx.x <= mask;
     int sum = 0;
+    if (digit_here) {
 #pragma unroll
-    for (int w = 0; w < GROUP_WAVES; ++w) sum += counts[w][threadIdx.x];
+      for (int w = 0; w < GROUP_WAVES; ++w) sum += counts[w][threadIdx.x];
+    }
     int scan = sum;
 #pragma unroll
     for (int off = 1; off < WAVE; off <<= 1) {
@@ -143,19 +231,23 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_kernel(const int32_t* __r
     __syncthreads();
     int run = scan - sum;
     for (int w = 0; w < wave; ++w) run += wave_total[w];
+    if (digit_here) {
 #pragma unroll
-    for (int w = 0; w < GROUP_WAVES; ++w) {
-      const int c = counts[w][threadIdx.x];
-      counts[w][threadIdx.x] = run;
-      run += c;
+      for (int w = 0; w < GROUP_WAVES; ++w) {
+        const int c = counts[w][threadIdx.x];
+        counts[w][threadIdx.x] = run;
+        run += c;
+      }
     }
     __syncthreads();
     for (int i = own_first + lane; i - lane < own_last; i += WAVE) {
       const bool in = i < own_last;
-      const int id = in ? word[i] : 0, p = in ? pos[i] : 0;
-      const int digit = (id >> shift) & (DIGITS - 1);
+      int2 token = int2{0, 0};
+      if (in) token = from_lds ? tokens[i] : int2{word[i], pos[i]};
+      const int id = token.x, p = token.y;
+      const int digit = (id >> shift) & mask;
       const uint64_t m = same(in, digit);
-      const int before = __popcll(m & ((1ull << lane) - 1));
+      const int before = __popcll(m & lower_lanes);
       if (in) {
         const int to = counts[wave][digit] + before;
         word_to[to] = id;
@@ -177,6 +269,25 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_kernel(const int32_t* __r
 constexpr int COLS = 8;                       // of a lane
 constexpr int SLICE = COLS * WAVE;            // of a wavefront
 constexpr int AHEAD = 4;                      // rows in flight
+
+// the columns of a lane as they lie in memory
+template <typename T>
+struct Cols {
+  alignas(16) T v[COLS];
+  template <bool VEC> __device__ inline void load(const T* p, int left) {
+    if constexpr (VEC) {
+      constexpr int W = Elt<T>::VEC;
+#pragma unroll
+      for (int q = 0; q < COLS; q += W)
+        if (q < left) *reinterpret_cast<Vec16<T>*>(v + q) = *reinterpret_cast<const Vec16<T>*>(p + q);
+    } else {
+#pragma unroll
+      for (int e = 0; e < COLS; ++e)
+        if (e < left) v[e] = p[e];
+    }
+  }
+  __device__ inline float get(int e) const { return Elt<T>::to_f(v[e]); }
+};
 
 template <typename T, bool VEC>
 __device__ inline void load_cols(const T* p, int left, float (&v)[COLS]) {
@@ -208,51 +319,66 @@ __device__ inline void store_cols(float* p, int left, const float (&v)[COLS]) {
   }
 }
 
+constexpr int CHUNK_MIN = 4, CHUNK_MAX = 60;
+
 // What happens behind the last row of a word in a chunk: added to the table, or kept as a piece of a word that lies in
 // several chunks -- piece[2 c] where chunk c starts inside the word, piece[2 c + 1] where it only ends inside it.
 enum { GOES_ON = 0, ADD, HEAD, TAIL };
 
+
 // A wavefront: one chunk of grouped rows, one slice of columns.
 template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void sum_kernel(const T* __restrict__ dy, long ld_dy, Grouped g, int d, int chunk, int chunks,
+__global__ __launch_bounds__(256) void sum_kernel(const T* __restrict__ dy, long ld_dy, Grouped g, int n, int d, int chunk, int chunks,
                                                   int slices, float scale, float* __restrict__ dtable, long ld_dtable,
                                                   float* __restrict__ piece, long ld_piece) {
   const int lane = threadIdx.x & 63;
   const long job = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = (int)(job / slices), slice = (int)(job % slices);
+  if (c >= chunks) return;
+  const int first = c * chunk, col = slice * SLICE + lane * COLS, left = d - col;
+  // lane l holds the word and the place of row first + l, lane 63 the word in front of the chunk; the one behind it is row `rows`.
+  // (Read next to the number of rows, not behind it.)
+  static_assert(CHUNK_MAX + 2 <= WAVE, "a chunk and the rows next to it");
+  const int mine = lane == 63 ? first - 1 : first + lane, in = max(0, min(mine, n - 1));
+  int my_word = g.word[in], my_pos = g.pos[in];
   const int total = *g.count;
-  if (c >= chunks || (long)c * chunk >= total) return;
-  const int first = c * chunk, last = (int)min((long)total, (long)first + chunk);
-  const int col = slice * SLICE + lane * COLS, left = d - col;
-  bool inside = first > 0 && g.word[first - 1] == g.word[first];     // the current word began in an earlier chunk
+  if (first >= total) return;
+  const int rows = min(chunk, total - first);
+  if (mine < 0 || mine >= total) my_word = -1;
+  const int after = __shfl_down(my_word, 1, WAVE);
+  // of the row in this lane: its word ends with it
+  const uint64_t ends = __ballot(after != my_word);
+  bool inside = __builtin_amdgcn_readlane(my_word, 63) == __builtin_amdgcn_readlane(my_word, 0);   // the current word began in an earlier chunk
   float acc[COLS] = {};
-  for (int r0 = first; r0 < last; r0 += AHEAD) {
-    float v[AHEAD][COLS], old[AHEAD][COLS];
-    int word[AHEAD], then[AHEAD];
+  for (int r0 = 0; r0 < rows; r0 += AHEAD) {
+    Cols<T> v[AHEAD];
+    float old[AHEAD][COLS];
+    int then[AHEAD];
     // what the next rows need of dy and of the table is requested together
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
       const int r = r0 + a;
       then[a] = GOES_ON;
-      if (r >= last) continue;
-      word[a] = g.word[r];
-      if (left > 0) load_cols<T, VEC>(dy + (size_t)g.pos[r] * ld_dy + col, left, v[a]);
-      const bool ends = r + 1 == total || g.word[r + 1] != word[a];
-      if (ends) then[a] = inside ? HEAD : ADD;
-      else if (r + 1 == last) then[a] = inside ? HEAD : TAIL;
-      if (ends) inside = false;
-      if (then[a] == ADD && left > 0) load_cols<float, VEC>(dtable + (size_t)word[a] * ld_dtable + col, left, old[a]);
+      if (r >= rows) continue;
+      const bool end = (ends >> r) & 1;
+      if (end) then[a] = inside ? HEAD : ADD;
+      else if (r + 1 == rows) then[a] = inside ? HEAD : TAIL;
+      if (end) inside = false;
+      if (left <= 0) continue;
+      v[a].template load<VEC>(dy + (size_t)__builtin_amdgcn_readlane(my_pos, r) * ld_dy + col, left);
+      if (then[a] == ADD) load_cols<float, VEC>(dtable + (size_t)__builtin_amdgcn_readlane(my_word, r) * ld_dtable + col, left, old[a]);
     }
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
-      if (r0 + a >= last || left <= 0) continue;
+      const int r = r0 + a;
+      if (r >= rows || left <= 0) continue;
 #pragma unroll
-      for (int e = 0; e < COLS; ++e) acc[e] += v[a][e];
+      for (int e = 0; e < COLS; ++e) acc[e] += v[a].get(e);
       if (then[a] == GOES_ON) continue;
       if (then[a] == ADD) {
 #pragma unroll
         for (int e = 0; e < COLS; ++e) old[a][e] = fmaf(scale, acc[e], old[a][e]);
-        store_cols<VEC>(dtable + (size_t)word[a] * ld_dtable + col, left, old[a]);
+        store_cols<VEC>(dtable + (size_t)__builtin_amdgcn_readlane(my_word, r) * ld_dtable + col, left, old[a]);
       } else {
         store_cols<true>(piece + (2l * c + (then[a] == TAIL)) * ld_piece + col, COLS, acc);
       }
@@ -262,64 +388,80 @@ __global__ __launch_bounds__(256) void sum_kernel(const T* __restrict__ dy, long
   }
 }
 
-// A workgroup: the chunk in which a word begins that later chunks go on with, one slice of columns.  Its wavefronts share the
-// pieces of the later chunks.
-constexpr int FOLD_WAVES = 8;
+// A wavefront: the chunk in which a word begins that later chunks go on with, 256 columns.
+constexpr int FOLD_COLS = 4 * WAVE;
 template <bool VEC>
-__global__ __launch_bounds__(FOLD_WAVES * 64) void fold_kernel(Grouped g, int d, int chunk, int chunks, int slices, float scale,
-                                                               float* __restrict__ dtable, long ld_dtable,
-                                                               const float* __restrict__ piece, long ld_piece) {
-  __shared__ float part[FOLD_WAVES][COLS][WAVE];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = blockIdx.x / slices, slice = blockIdx.x % slices;
+__global__ __launch_bounds__(256) void fold_kernel(Grouped g, int n, int d, int chunk, int chunks, int slices, float scale,
+                                                   float* __restrict__ dtable, long ld_dtable, const float* __restrict__ piece,
+                                                   long ld_piece) {
+  const int lane = threadIdx.x & 63;
+  const long job = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = (int)(job / slices), slice = (int)(job % slices);
+  if (c + 1 >= chunks) return;
+  const int first = c * chunk, end = first + chunk;          // (end < n: c is not the last chunk)
+  // the first word of this lane's chunk, c + 1 + lane; read next to the others, not behind them
+  long next = end + (long)lane * chunk;
+  int at_next = g.word[min(next, (long)n - 1)];
+  const int word = g.word[end - 1], at_first = g.word[first], before = g.word[max(first - 1, 0)];
   const int total = *g.count;
-  const long end = (long)(c + 1) * chunk;                    // first row of the next chunk
-  if (end >= total) return;
-  const int first = c * chunk, word = g.word[end - 1];
-  if (g.word[end] != word) return;
-  if (first > 0 && g.word[first - 1] == word && g.word[first] == word) return;
-  // chunks c + 1 .. c + more hold pieces: the last row of all of them but the last is followed by the same word
-  int more = 1;
-  for (;; more += WAVE) {
-    const long next = (long)(c + 1 + more + lane) * chunk;   // first row behind chunk c + more + lane
-    const bool on = next < total && g.word[next] == word;
-    const uint64_t m = ~__ballot(on);
-    if (m) { more += __ffsll((unsigned long long)m) - 1; break; }
+  if (end >= total || (first > 0 && before == word && at_first == word)) return;
+  // chunks c + 1 .. c + more hold pieces
+  int more = 0;
+  for (;;) {
+    const uint64_t off = ~__ballot(next < total && at_next == word);
+    if (off) { more += __ffsll((unsigned long long)off) - 1; break; }
+    more += WAVE;
+    next += (long)WAVE * chunk;
+    at_next = g.word[min(next, (long)n - 1)];
   }
-  const int col = slice * SLICE + lane * COLS, left = d - col;
-  const int per = (more + FOLD_WAVES - 1) / FOLD_WAVES;
-  const int from = c + 1 + wave * per, to = min(c + 1 + more, from + per);
-  float acc[COLS] = {};
-  if (left > 0) {
-    if (wave == 0) load_cols<float, true>(piece + (2l * c + 1) * ld_piece + col, COLS, acc);
-#pragma unroll 4
-    for (int k = from; k < to; ++k) {
-      float v[COLS];
-      load_cols<float, true>(piece + 2l * k * ld_piece + col, COLS, v);
-#pragma unroll
-      for (int e = 0; e < COLS; ++e) acc[e] += v[e];
-    }
-  }
-#pragma unroll
-  for (int e = 0; e < COLS; ++e) part[wave][e][lane] = acc[e];
-  __syncthreads();
-  if (wave || left <= 0) return;
-#pragma unroll
-  for (int w = 1; w < FOLD_WAVES; ++w)
-#pragma unroll
-    for (int e = 0; e < COLS; ++e) acc[e] += part[w][e][lane];
-  float old[COLS];
+  const int col = slice * FOLD_COLS + lane * 4, left = d - col;
+  if (more == 0 || left <= 0) return;
   float* to_row = dtable + (size_t)word * ld_dtable + col;
-  load_cols<float, VEC>(to_row, left, old);
+  float old[4];
+  if constexpr (VEC) {
+    const float4 v = *reinterpret_cast<const float4*>(to_row);
+    old[0] = v.x; old[1] = v.y; old[2] = v.z; old[3] = v.w;
+  } else {
 #pragma unroll
-  for (int e = 0; e < COLS; ++e) old[e] = fmaf(scale, acc[e], old[e]);
-  store_cols<VEC>(to_row, left, old);
+    for (int e = 0; e < 4; ++e) old[e] = e < left ? to_row[e] : 0.f;
+  }
+  float4 acc = *reinterpret_cast<const float4*>(piece + (2l * c + 1) * ld_piece + col);
+  constexpr int FLIGHT = 16;
+  for (int k0 = 1; k0 <= more; k0 += FLIGHT) {
+    float4 v[FLIGHT];
+#pragma unroll
+    for (int k = 0; k < FLIGHT; ++k)
+      if (k0 + k <= more) v[k] = *reinterpret_cast<const float4*>(piece + 2l * (c + k0 + k) * ld_piece + col);
+#pragma unroll
+    for (int k = 0; k < FLIGHT; ++k)
+      if (k0 + k <= more) { acc.x += v[k].x; acc.y += v[k].y; acc.z += v[k].z; acc.w += v[k].w; }
+  }
+  const float sum[4] = {acc.x, acc.y, acc.z, acc.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) old[e] = fmaf(scale, sum[e], old[e]);
+  if constexpr (VEC) {
+    *reinterpret_cast<float4*>(to_row) = float4{old[0], old[1], old[2], old[3]};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < left) to_row[e] = old[e];
+  }
 }
 
 // ---- host -------------------------------------------------------------------------------------
 
-// rows of a chunk: few tokens are cut into short ones, so that there are wavefronts enough
-int chunk_rows(int T) { return T <= 2048 ? 4 : T <= 8192 ? 8 : T <= 32768 ? 16 : 32; }
+// Rows of a chunk: as many as leave 32 wavefronts for every CU.  Longer chunks leave fewer pieces to the words that occur often
+// (32768 tokens of 4096 columns, one word in eleven the same: folding chunks of 16 rows 25 us, of 60 rows FOLD60).
+constexpr int SUM_WAVES = 8192;
+int chunk_rows(int T, int d) {
+  const long rows = (long)T * cdiv(d, SLICE) / SUM_WAVES;
+  return (int)std::max((long)CHUNK_MIN, std::min((long)CHUNK_MAX, rows));
+}
+// chunks of any number of tokens up to T: a step from k to k + 1 rows makes them fewer, and is at its widest behind the shortest
+size_t max_chunks(int T, int d) {
+  const size_t before = (size_t)(CHUNK_MIN + 1) * SUM_WAVES / cdiv(d, SLICE) / CHUNK_MIN + 2;
+  return std::max((size_t)cdiv(T, CHUNK_MAX), std::min((size_t)cdiv(T, CHUNK_MIN), before));
+}
 
 constexpr int MAX_TOKENS = 1 << 30;
 
@@ -335,7 +477,7 @@ struct Workspace {
     g.word2 = a.take<int32_t>(ids); g.pos2 = a.take<int32_t>(ids);
     g.count = a.take<int32_t>(sizeof(int32_t));
     ld_piece = (long)align_up((size_t)d, COLS);
-    piece = a.take<float>(2 * (size_t)cdiv(T, chunk_rows(T)) * ld_piece * sizeof(float));
+    piece = a.take<float>(2 * max_chunks(T, d) * ld_piece * sizeof(float));
     bytes = a.off;
   }
 };
@@ -360,14 +502,15 @@ void launch_embed(const void* table, int ld_table, const int32_t* ids, int n, in
 template <typename T, bool VEC>
 bm_status launch_sums(const void* dy, int ld_dy, const Workspace& w, int n, int d, float scale, float* dtable, int ld_dtable,
                       hipStream_t st) {
-  const int chunk = chunk_rows(n), chunks = cdiv(n, chunk), slices = cdiv(d, SLICE);
+  const int chunk = chunk_rows(n, d), chunks = cdiv(n, chunk), slices = cdiv(d, SLICE);
   const long jobs = (long)chunks * slices;
-  hipLaunchKernelGGL((sum_kernel<T, VEC>), dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, st, (const T*)dy, (long)ld_dy, w.g, d,
+  hipLaunchKernelGGL((sum_kernel<T, VEC>), dim3((unsigned)((jobs + 3) / 4)), dim3(256), 0, st, (const T*)dy, (long)ld_dy, w.g, n, d,
                      chunk, chunks, slices, scale, dtable, (long)ld_dtable, w.piece, w.ld_piece);
   BM_CHECK_LAUNCH("embedding sums");
   if (chunks > 1) {
-    hipLaunchKernelGGL((fold_kernel<VEC>), dim3((unsigned)((long)(chunks - 1) * slices)), dim3(FOLD_WAVES * 64), 0, st, w.g, d, chunk,
-                       chunks, slices, scale, dtable, (long)ld_dtable, w.piece, w.ld_piece);
+    const int parts = cdiv(d, FOLD_COLS);
+    hipLaunchKernelGGL((fold_kernel<VEC>), dim3((unsigned)(((long)(chunks - 1) * parts + 3) / 4)), dim3(256), 0, st, w.g, n, d, chunk, chunks,
+                       parts, scale, dtable, (long)ld_dtable, w.piece, w.ld_piece);
     BM_CHECK_LAUNCH("embedding fold");
   }
   return BM_OK;
@@ -422,7 +565,8 @@ extern "C" bm_status bm_embedding_backward(int32_t dtype, int32_t V, int32_t d, 
   ProfScope prof(PROF_ELEMENTWISE, (double)T * d * (elt_size(dtype) + 8.0), st);
   int bits = 0;                                             // of the ids, above those of the bucket
   while (bits < 31 - BUCKET_BITS && ((V - 1) >> (BUCKET_BITS + bits))) ++bits;
-  hipLaunchKernelGGL(group_kernel, dim3(BUCKETS), dim3(GROUP_THREADS), 0, st, ids, T, V, cdiv(bits, DIGIT_BITS), w.g);
+  const int passes = cdiv(bits, DIGIT_BITS);
+  hipLaunchKernelGGL(group_kernel, dim3(BUCKETS), dim3(GROUP_THREADS), 0, st, ids, T, V, passes, passes ? cdiv(bits, passes) : 0, w.g);
   BM_CHECK_LAUNCH("embedding group");
   const int W = dtype == BM_DTYPE_BF16 ? 8 : 4;
   const bool vec = d % W == 0 && ld_dy % W == 0 && ld_dtable % 4 == 0;

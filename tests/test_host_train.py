@@ -42,6 +42,7 @@ def test_embedding_gradient_workspace(bad):
 def test_embedding_workspace_grows_with_tokens_and_columns():
     sizes = [bm.embedding_backward_scratch_bytes(T, 64) for T in (1, 2, 777, 2048, 2049, 8192, 8193, 32768, 32769, 1 << 20)]
     assert all(b > 0 for b in sizes)
+    assert all(b >= a for a, b in zip(sizes, sizes[1:]))
     assert bm.embedding_backward_scratch_bytes(777, 65) >= bm.embedding_backward_scratch_bytes(777, 64)
     for T, d in ((0, 8), (8, 0), (-1, 8), ((1 << 30) + 1, 8)):
         assert bm.embedding_backward_scratch_bytes(T, d) == 0
