@@ -88,7 +88,7 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_kernel(const int32_t* __r
                                                               Grouped g) {
   __shared__ int below[GROUP_WAVES], mine[GROUP_WAVES], wave_total[GROUP_WAVES];
   __shared__ int counts[GROUP_WAVES][DIGITS];
-  __shared__ int2 tokens[HELD];
+  __shared__ int keys[HELD], rows[HELD];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int bucket = blockIdx.x;
   const uint64_t lower_lanes = (1ull << lane) - 1;
@@ -142,7 +142,10 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_kernel(const int32_t* __r
   };
   const bool held = marked && total <= HELD;
   if (held) {
-    collect([&](int to, int i) { tokens[to] = int2{ids[i], i}; });
+    collect([&](int to, int i) { rows[to] = i; });
+    __syncthreads();
+    // (fetched where they are collected, a wavefront would wait for every 64 of them)
+    for (int t = threadIdx.x; t < total; t += GROUP_THREADS) keys[t] = ids[rows[t]];
     if (total <= RANKED) {
       // every token counts those that stand before it, the ones of lower words and the earlier ones of its own;
       // GROUP_THREADS / RANKED threads a token
@@ -150,21 +153,20 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_kernel(const int32_t* __r
       if (threadIdx.x < total) ranks[threadIdx.x] = 0;
       __syncthreads();
       const int t = threadIdx.x % RANKED;
-      int2 me = int2{0, 0};
       if (t < total) {
-        me = tokens[t];
+        const int key = keys[t];
         int rank = 0;
 #pragma unroll 4
         for (int j = threadIdx.x / RANKED; j < total; j += GROUP_THREADS / RANKED) {
-          const int other = tokens[j].x;
-          rank += other < me.x || (other == me.x && j < t);
+          const int other = keys[j];
+          rank += other < key || (other == key && j < t);
         }
         atomicAdd(ranks + t, rank);
       }
       __syncthreads();
       if (threadIdx.x < total) {
-        g.word[base + ranks[t]] = me.x;
-        g.pos[base + ranks[t]] = me.y;
+        g.word[base + ranks[t]] = keys[t];
+        g.pos[base + ranks[t]] = rows[t];
       }
       return;
     }
@@ -185,7 +187,9 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_kernel(const int32_t* __r
       at += __popcll(m);
     });
   } else if (!held || digit_passes == 0) {
-    collect([&](int to, int i) { word[to] = ids[i]; pos[to] = i; });
+    collect([&](int to, int i) { pos[to] = i; });
+    __syncthreads();
+    for (int t = threadIdx.x; t < total; t += GROUP_THREADS) word[t] = ids[pos[t]];
   }
   // stable counting sorts by the bits above the bucket's, digit_bits at a time
   const int per_own = share(total);
@@ -207,7 +211,7 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_kernel(const int32_t* __r
     };
     for (int i = own_first + lane; i - lane < own_last; i += WAVE) {
       const bool in = i < own_last;
-      const int digit = in ? ((from_lds ? tokens[i].x : word[i]) >> shift) & mask : 0;
+      const int digit = in ? ((from_lds ? keys[i] : word[i]) >> shift) & mask : 0;
       const uint64_t m = same(in, digit);
       if (in && (m & lower_lanes) == 0) counts[wave][digit] += __popcll(m);
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -242,9 +246,7 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_kernel(const int32_t* __r
     __syncthreads();
     for (int i = own_first + lane; i - lane < own_last; i += WAVE) {
       const bool in = i < own_last;
-      int2 token = int2{0, 0};
-      if (in) token = from_lds ? tokens[i] : int2{word[i], pos[i]};
-      const int id = token.x, p = token.y;
+      const int id = !in ? 0 : from_lds ? keys[i] : word[i], p = !in ? 0 : from_lds ? rows[i] : pos[i];
       const int digit = (id >> shift) & mask;
       const uint64_t m = same(in, digit);
       const int before = __popcll(m & lower_lanes);
