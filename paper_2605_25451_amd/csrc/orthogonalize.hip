@@ -75,22 +75,41 @@ __device__ inline void store_result(const Product& p, long at, int count, const 
   }
 }
 
+// 8 values of a row as hi and lo
+struct Halves { half8 hi, lo; };
+__device__ inline void split8(const float (&v)[8], half8* hi, half8* lo) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    (*hi)[e] = (half_t)v[e];
+    (*lo)[e] = (half_t)(v[e] - (float)(*hi)[e]);
+  }
+}
+
 // ---- norm and conversion ----------------------------------------------------------------------
 
-constexpr int NORM_PARTS = 64;
+constexpr int NORM_PARTS = 256;                // at most
 
-// sums of squares of parts of every matrix, in fp64: squares of fp32 values neither overflow nor vanish there
-__global__ __launch_bounds__(256) void norm_kernel(const float* __restrict__ g, long ld, long stride, int M, int N, int parts,
-                                                   double* __restrict__ sums) {
+// sums of squares of parts of every matrix, in fp64: squares of fp32 values neither overflow nor vanish there.  A row is `per_row`
+// pieces of VEC elements.
+template <int VEC>
+__global__ __launch_bounds__(256) void norm_kernel(const float* __restrict__ g, long ld, long stride, uint32_t per_row, uint32_t pieces,
+                                                   int parts, double* __restrict__ sums) {
   __shared__ double sm[4];
   const int b = blockIdx.x / parts, part = blockIdx.x % parts;
   const float* x = g + b * stride;
   double s = 0.0;
-  for (int r = part; r < M; r += parts)
-    for (int c = threadIdx.x; c < N; c += 256) {
+  const uint32_t step = parts * 256u;
+#pragma unroll 4
+  for (uint32_t i = part * 256u + threadIdx.x; i < pieces; i += step) {
+    const uint32_t r = i / per_row, c = (i - r * per_row) * VEC;
+    if constexpr (VEC == 4) {
+      const float4 v = *reinterpret_cast<const float4*>(x + r * ld + c);
+      s += (double)v.x * v.x + (double)v.y * v.y + (double)v.z * v.z + (double)v.w * v.w;
+    } else {
       const double v = x[r * ld + c];
       s += v * v;
     }
+  }
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off, WAVE);
   if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = s;
@@ -98,29 +117,76 @@ __global__ __launch_bounds__(256) void norm_kernel(const float* __restrict__ g, 
   if (threadIdx.x == 0) sums[blockIdx.x] = sm[0] + sm[1] + sm[2] + sm[3];
 }
 
-// x[m, n] = s G / (|G| + eps), transposed where the rows of G are the columns of x.  A workgroup: 64 x 64 of x.
-__global__ __launch_bounds__(256) void convert_kernel(const float* __restrict__ g, long ld, long stride, int M, int N, int transposed,
-                                                      const double* __restrict__ sums, int parts, float eps, float s, Split x,
-                                                      int ldx, size_t stride_x, int tiles_n, int tiles) {
-  __shared__ float tile[PAD][PAD + 1];
-  const int b = blockIdx.x / tiles, t = blockIdx.x % tiles;
-  const int r0 = (t / tiles_n) * PAD, c0 = (t % tiles_n) * PAD;          // of x
-  double sum = 0.0;
-  for (int p = 0; p < parts; ++p) sum += sums[(size_t)b * parts + p];
-  const double scale = (double)s / (sqrt(sum) + (double)eps);
-  const int gr0 = transposed ? c0 : r0, gc0 = transposed ? r0 : c0;
-  for (int i = threadIdx.x; i < PAD * PAD; i += 256) {
-    const int r = i / PAD, c = i % PAD;
-    float v = 0.f;
-    if (gr0 + r < M && gc0 + c < N) v = (float)((double)g[b * stride + (gr0 + r) * ld + gc0 + c] * scale);
-    if (transposed) tile[c][r] = v; else tile[r][c] = v;
-  }
+// The sum of a matrix's parts, in every thread: four wavefronts, one part per lane.
+__device__ inline double sum_parts(const double* __restrict__ sums, int parts, double* sm) {
+  static_assert(NORM_PARTS <= 256, "a part for each of four wavefronts' lanes");
+  double s = (int)threadIdx.x < parts ? sums[threadIdx.x] : 0.0;
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off, WAVE);
+  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = s;
   __syncthreads();
+  return sm[0] + sm[1] + sm[2] + sm[3];
+}
+
+// x[m, n] = s G / (|G| + eps), transposed where the rows of G are the columns of x.  A workgroup: `across` runs of 64 x 64 of x.
+// VEC: rows of G start on 16 bytes
+template <bool TRANSPOSED, bool VEC>
+__global__ __launch_bounds__(256) void convert_kernel(const float* __restrict__ g, long ld, long stride, int M, int N,
+                                                      const double* __restrict__ sums, int parts, float eps, float s, Split x,
+                                                      int ldx, size_t stride_x, int tiles_n, int runs_n, int across, int runs) {
+  __shared__ float tile[TRANSPOSED ? PAD : 1][PAD + 4];
+  __shared__ double sm[4];
+  const int b = blockIdx.x / runs, t = blockIdx.x % runs;
+  const int r0 = t / runs_n * PAD, first = t % runs_n * across, last = min(tiles_n, first + across);
+  const double scale = (double)s / (sqrt(sum_parts(sums + (size_t)b * parts, parts, sm)) + (double)eps);
+  g += b * stride;
   x.hi += b * stride_x;
   if (x.lo) x.lo += b * stride_x;
-  for (int i = threadIdx.x; i < PAD * PAD; i += 256) {
-    const int r = i / PAD, c = i % PAD;
-    put(x, (size_t)(r0 + r) * ldx + c0 + c, tile[r][c]);
+  // four elements of a row of G
+  auto fetch = [&](int r, int c, float (&v)[4]) {
+    if (VEC && r < M && c + 4 <= N) {
+      const float4 q = *reinterpret_cast<const float4*>(g + r * ld + c);
+      v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = r < M && c + e < N ? g[r * ld + c + e] : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (float)((double)v[e] * scale);
+  };
+  for (int ct = first; ct < last; ++ct) {
+    const int c0 = ct * PAD;
+    if (TRANSPOSED) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = threadIdx.x / 16 + i * 16, c = threadIdx.x % 16 * 4;   // of G: its rows are columns of x
+        float v[4];
+        fetch(c0 + r, r0 + c, v);
+        *reinterpret_cast<float4*>(&tile[r][c]) = float4{v[0], v[1], v[2], v[3]};
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = threadIdx.x / 8 + i * 32, c = threadIdx.x % 8 * 8;       // of x
+      float v[8];
+      if (TRANSPOSED) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = tile[c + e][r];
+      } else {
+        float lo[4], hi[4];
+        fetch(r0 + r, c0 + c, lo);
+        fetch(r0 + r, c0 + c + 4, hi);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[e] = lo[e]; v[4 + e] = hi[e]; }
+      }
+      half8 h, l;
+      split8(v, &h, &l);
+      const size_t at = (size_t)(r0 + r) * ldx + c0 + c;
+      *reinterpret_cast<half8*>(x.hi + at) = h;
+      if (x.lo) *reinterpret_cast<half8*>(x.lo + at) = l;
+    }
   }
 }
 
@@ -135,16 +201,6 @@ __device__ inline void triangle_tile(int id, int n, int* tm, int* tn) {
   while ((r + 1) * n - (r + 1) * r / 2 <= id) ++r;
   *tm = r;
   *tn = r + id - (r * n - r * (r - 1) / 2);
-}
-
-// v of a block behind alpha and beta; 16-byte pieces of rows as hi and lo
-struct Halves { half8 hi, lo; };
-__device__ inline void split8(const float (&v)[8], half8* hi, half8* lo) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    (*hi)[e] = (half_t)v[e];
-    (*lo)[e] = (half_t)(v[e] - (float)(*hi)[e]);
-  }
 }
 
 // ---- epilogue of one wavefront: FM x FN blocks of 16 x 16, in strips of 16 rows.  The MFMAs run with swapped operands: of
@@ -277,29 +333,34 @@ struct Operands {
   }
 };
 
-// ---- TILE x TILE (64 or 128), four wavefronts of a quarter each.  DEPTH slices of LDS: DEPTH - 1 are on their way while one is
+// ---- TILE x TILE (64 or 128), GROUPS times four wavefronts of a quarter each: group g multiplies the slices g, g + GROUPS, ...
+// of the contraction, and group 0 adds up their sums.  Each has DEPTH slices of LDS: DEPTH - 1 are on their way while one is
 // multiplied, with one barrier a slice.
-template <int KIND, int TILE, int DEPTH>
-__global__ __launch_bounds__(256) void small_product_kernel(Product p, int tiles_m, int tiles_n, int tiles) {
+constexpr int small_lds(int tile, int depth, int groups) { return groups * depth * 2 * tile * BK * 2; }
+
+template <int KIND, int TILE, int DEPTH, int GROUPS>
+__global__ __launch_bounds__(256 * GROUPS) void small_product_kernel(Product p, int tiles_m, int tiles_n, int tiles) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr bool NN = KIND == STEP || KIND == LAST;
   using RegA = Region<TILE, false, 4>;
   using RegB = Region<TILE, NN, 4>;
   constexpr uint32_t B0 = RegA::BYTES, BUF = B0 + RegB::BYTES;
   constexpr int LOADS = RegA::LOADS + RegB::LOADS, F = TILE / 32, HALF = TILE / 2;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) & 3);
+  const int group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
   const int wm = wave >> 1, wn = wave & 1;
   const Place q = place<!NN>(tiles_m, tiles_n, tiles);
   const int m0 = q.tm * TILE, n0 = q.tn * TILE;
   const Operands<NN> op(p, q, m0, n0);
-  const int n = op.slices * p.terms;
+  const int all = op.slices * p.terms, n = (all - group + GROUPS - 1) / GROUPS;
   RegA ra;
   RegB rb;
   ra.init(p.lda, 0, p.M - m0, wave, lane);
   rb.init(p.ldb, 0, p.N - n0, wave, lane);
+  const uint32_t base = group * (DEPTH * BUF);
   auto load = [&](int j, uint32_t buf) {
-    rb.template load<false>(op.b_at(j), p.ldb, BK, buf + B0, wave, lane);
-    ra.template load<false>(op.a_at(j), p.lda, BK, buf, wave, lane);
+    rb.template load<false>(op.b_at(group + j * GROUPS), p.ldb, BK, base + buf + B0, wave, lane);
+    ra.template load<false>(op.a_at(group + j * GROUPS), p.lda, BK, base + buf, wave, lane);
   };
   Fragments<TILE, false, F> fa;
   Fragments<TILE, NN, F> fb;
@@ -310,21 +371,22 @@ __global__ __launch_bounds__(256) void small_product_kernel(Product p, int tiles
   for (int s = 0; s < DEPTH - 1; ++s)
     if (s < n) load(s, s * BUF);
   uint32_t cur = 0, free = (DEPTH - 1) * BUF;
-  for (int j = 0; j < n; ++j) {
+  for (int j = 0; j * GROUPS < all; ++j) {
     // slice j has landed; later ones need not have
     const int later = n - 1 - j;
     if (later >= DEPTH - 2) wait_loads<(DEPTH - 2) * LOADS>();
     else if (DEPTH > 3 && later == 1) wait_loads<LOADS>();
     else wait_loads<0>();
     end_phase();                                             // for all; and all have read slice j - 1
+    if (j >= n) break;                                       // (only in the last round)
     if (j + DEPTH - 1 < n) load(j + DEPTH - 1, free);
     bf16x8 a[2][F], bb[2][F];
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
       for (int f = 0; f < F; ++f) {
-        bb[ks][f] = fb.read(smem, f, ks, cur + B0);
-        a[ks][f] = fa.read(smem, f, ks, cur);
+        bb[ks][f] = fb.read(smem, f, ks, base + cur + B0);
+        a[ks][f] = fa.read(smem, f, ks, base + cur);
       }
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
@@ -337,8 +399,30 @@ __global__ __launch_bounds__(256) void small_product_kernel(Product p, int tiles
     free = cur;
     cur = cur == (DEPTH - 1) * BUF ? 0 : cur + BUF;
   }
-  end_phase();                                               // the strips overlay the slices
-  finish<KIND, F, F>(p, q.b, acc, reinterpret_cast<float*>(smem) + wave * 16 * (F * 16 + 4), lane, n0 + wn * HALF, !NN && q.tm != q.tn,
+  end_phase();                                               // sums and strips overlay the slices
+  constexpr int SUM = TILE * TILE;                           // floats of a group's sums
+  float* sums = reinterpret_cast<float*>(smem);
+  if constexpr (GROUPS > 1) {
+    static_assert(((GROUPS - 1) * SUM + 4 * 16 * (F * 16 + 4)) * 4 <= small_lds(TILE, DEPTH, GROUPS), "the sums of the groups fit");
+    auto at = [&](int g, int i, int c) {
+      return reinterpret_cast<f32x4*>(sums + (g - 1) * SUM + (((wave * F + i) * F + c) * 64 + lane) * 4);
+    };
+    if (group > 0) {
+#pragma unroll
+      for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int c = 0; c < F; ++c) *at(group, i, c) = acc[i][c];
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g)
+#pragma unroll
+      for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int c = 0; c < F; ++c) acc[i][c] += *at(g, i, c);
+  }
+  finish<KIND, F, F>(p, q.b, acc, sums + (GROUPS - 1) * SUM + wave * 16 * (F * 16 + 4), lane, n0 + wn * HALF, !NN && q.tm != q.tn,
                      [&](int i) { return m0 + wm * HALF + i * 16; }, [] {});
 }
 
@@ -518,29 +602,39 @@ bm_status allow_lds(Kernel kern, size_t lds, std::atomic<uint64_t>* done) {
   return BM_OK;
 }
 
-template <int KIND, int TILE>
+// GROUPS = 0: the kernel of two groups that take turns
+template <int KIND, int TILE, int DEPTH, int GROUPS>
 bm_status launch_tile(const Product& p, int batch, hipStream_t st) {
   constexpr bool SYMMETRIC = KIND == GRAM || KIND == POLY;
-  constexpr int DEPTH = TILE == 256 ? 2 : TILE == 128 ? 2 : 4;
-  constexpr size_t lds = (size_t)DEPTH * 2 * TILE * BK * sizeof(half_t);
+  constexpr size_t lds = GROUPS ? small_lds(TILE, DEPTH, GROUPS) : 2 * 2 * TILE * BK * sizeof(half_t);
   void (*kern)(Product, int, int, int);
-  if constexpr (TILE == 256) kern = large_product_kernel<KIND>;
-  else kern = small_product_kernel<KIND, TILE, DEPTH>;
+  if constexpr (GROUPS == 0) kern = large_product_kernel<KIND>;
+  else kern = small_product_kernel<KIND, TILE, DEPTH, GROUPS>;
   static std::atomic<uint64_t> done{0};
   BM_RETURN_IF(allow_lds(kern, lds, &done));
   const int tm = cdiv(p.M, TILE), tn = cdiv(p.N, TILE), tiles = SYMMETRIC ? tm * (tm + 1) / 2 : tm * tn;
   ProfScope prof(SYMMETRIC ? PROF_GEMM_NT : PROF_GEMM_NN, (SYMMETRIC ? 1.0 : 2.0) * batch * p.terms * p.M * p.N * p.K, st);
-  hipLaunchKernelGGL(kern, dim3((unsigned)((long)tiles * batch)), dim3(TILE == 256 ? 512 : 256), lds, st, p, tm, tn, tiles);
+  hipLaunchKernelGGL(kern, dim3((unsigned)((long)tiles * batch)), dim3(GROUPS ? 256 * GROUPS : 512), lds, st, p, tm, tn, tiles);
   BM_CHECK_LAUNCH("orthogonalize product");
   return BM_OK;
 }
 
+// Operands come from L2 at 50-60 bytes per ns and CU whatever the kernel (deeper prefetch, fragments read ahead, wavefronts with whole
+// tiles of their own and a compact order of the tiles in an XCD changed nothing), so tiles are as large as leaves one for every CU.
+// A whole update in us, 256x256 / 128x128 / 64x64 two workgroups a CU / 64x64 two groups:
+//   1024 x 1024 420, 243, 160, 149     1536 x 1536 555, 325, 282, 335     2048 x 2048 704, 424, 499, 575     16 of 1024 x 1024 598, 757, 805, 1060
 template <int KIND>
 bm_status launch(const Product& p, int batch, hipStream_t st) {
-  const long t256 = (long)cdiv(p.M, 256) * cdiv(p.N, 256) * batch, t128 = (long)cdiv(p.M, 128) * cdiv(p.N, 128) * batch;
-  if (t256 >= 128) return launch_tile<KIND, 256>(p, batch, st);
-  if (t128 >= 256) return launch_tile<KIND, 128>(p, batch, st);
-  return launch_tile<KIND, 64>(p, batch, st);
+  constexpr bool SYMMETRIC = KIND == GRAM || KIND == POLY;
+  auto tiles = [&](int size) {
+    const long tm = cdiv(p.M, size), tn = cdiv(p.N, size);
+    return (SYMMETRIC ? tm * (tm + 1) / 2 : tm * tn) * batch;
+  };
+  constexpr int NUM_CU = 256;
+  if (tiles(256) >= NUM_CU / 2) return launch_tile<KIND, 256, 2, 0>(p, batch, st);
+  if (tiles(64) <= NUM_CU) return launch_tile<KIND, 64, 4, 2>(p, batch, st);
+  if (tiles(128) <= NUM_CU / 2) return launch_tile<KIND, 64, 4, 1>(p, batch, st);
+  return launch_tile<KIND, 128, 2, 2>(p, batch, st);
 }
 
 bool sizes_ok(int dtype, int batch, int M, int N) {
@@ -594,11 +688,21 @@ extern "C" bm_status bm_orthogonalize(int32_t dtype, int32_t batch, int32_t M, i
   auto in_full = [&](int i) { return full || i + 2 < steps; };
   auto view = [](Split x, bool lo) { if (!lo) x.lo = nullptr; return x; };
 
-  hipLaunchKernelGGL(norm_kernel, dim3(batch * NORM_PARTS), dim3(256), 0, st, grad, (long)ld_g, (long)stride_g, M, N, NORM_PARTS, w.sums);
+  // rows of G that start on 16 bytes are read four elements at a time; rows without a gap are one long row
+  const bool vec = ld_g % 4 == 0 && N % 4 == 0 && (batch == 1 || stride_g % 4 == 0);
+  const uint32_t pieces = (uint32_t)((size_t)M * N / (vec ? 4 : 1)), per_row = ld_g == N ? pieces : (uint32_t)(vec ? N / 4 : N);
+  // enough parts for 8 workgroups a CU, none without 4 pieces a thread
+  const int parts = std::max(1, std::min({NORM_PARTS, cdiv(2048, batch), cdiv(pieces, 1024)}));
+  hipLaunchKernelGGL((vec ? norm_kernel<4> : norm_kernel<1>), dim3((unsigned)batch * parts), dim3(256), 0, st, grad, (long)ld_g,
+                     (long)stride_g, per_row, pieces, parts, w.sums);
   BM_CHECK_LAUNCH("orthogonalize norm");
-  const int tiles_n = q.np / PAD, tiles = q.mp / PAD * tiles_n;
-  hipLaunchKernelGGL(convert_kernel, dim3((unsigned)((long)batch * tiles)), dim3(256), 0, st, grad, (long)ld_g, (long)stride_g, M, N,
-                     (int)q.tall, w.sums, NORM_PARTS, eps, k.s, view(w.X[0], in_full(0)), q.np, q.x, tiles_n, tiles);
+  const int tiles_n = q.np / PAD, across = std::max(1, std::min(4, (int)((long)tiles_n * (q.mp / PAD) * batch / 2048)));
+  const int runs_n = cdiv(tiles_n, across), runs = q.mp / PAD * runs_n;
+  const bool rows_vec = ld_g % 4 == 0 && (batch == 1 || stride_g % 4 == 0);
+  const auto convert = q.tall ? (rows_vec ? convert_kernel<true, true> : convert_kernel<true, false>)
+                              : (rows_vec ? convert_kernel<false, true> : convert_kernel<false, false>);
+  hipLaunchKernelGGL(convert, dim3((unsigned)((long)batch * runs)), dim3(256), 0, st, grad, (long)ld_g, (long)stride_g, M, N, w.sums, parts,
+                     eps, k.s, view(w.X[0], in_full(0)), q.np, q.x, tiles_n, runs_n, across, runs);
   BM_CHECK_LAUNCH("orthogonalize convert");
   for (int i = 0; i < steps; ++i) {
     const Split x = view(w.X[i & 1], in_full(i)), next = view(w.X[(i + 1) & 1], in_full(i + 1));
