@@ -31,12 +31,6 @@ constexpr int PAD = 64;                        // rows and columns of the buffer
 
 struct Split { half_t *hi, *lo; };             // lo may be null: hi alone
 
-__device__ inline void put(const Split& d, size_t i, float v) {
-  const half_t h = (half_t)v;
-  d.hi[i] = h;
-  if (d.lo) d.lo[i] = (half_t)(v - (float)h);
-}
-
 enum { GRAM = 0, POLY, STEP, LAST };
 
 struct Product {
@@ -529,6 +523,271 @@ __global__ __launch_bounds__(512, 2) void large_product_kernel(Product p, int ti
                      });
 }
 
+// ---- few rows: 64 or 128 of X at most ----------------------------------------------------------------
+//
+// A and B fit the LDS of a workgroup, so that a whole step is one launch: a workgroup holds a chunk of X's columns, has A from the sums
+// of all chunks, computes B for itself, moves its chunk on and adds up the chunk's share of the next A.  Where X is one
+// chunk (64 x 512, 128 x 128), all steps are one launch.  The products of the tiled kernels would be three launches a step of one to a few workgroups:
+// 192 x 64 59 us, here TINY192; 29 x 2350 93 and TINY29; 100 x 4096 127 and TINY100.
+//
+// LDS: X and then A or B in blocks of MP rows x 64 columns, 128 bytes a row, 16-byte chunk c of row r at c ^ ((r >> 1) & 7); hi, and lo
+// behind it.  A chunk lies in the workspace as it does in LDS.
+constexpr int TINY_THREADS = 512, TINY_WAVES = TINY_THREADS / WAVE;
+enum { SOLO = 0, FIRST, NEXT };                // all steps; conversion and the first sums; one step
+
+struct Tiny {
+  const float* g; long ld_g, stride_g;
+  int M, N, tall;
+  const double* norms; int parts;
+  float eps, s, t, u;                          // Scales
+  float a, b, c;
+  int steps, step, full_from;                  // X entering step i has a lo part while i < full_from
+  int blocks, chunks;                          // 64-column blocks of a chunk, chunks of a matrix
+  unsigned char* image;                        // [batch, chunks] chunks
+  float4 *sums, *sums_next;                    // [batch, chunks, blocks of A, 64]
+  void* out; long ld_o, stride_o;
+};
+
+// blocks of 16 x 16 on and above the diagonal of A
+constexpr int tiny_gram_blocks(int mp) { return (mp / 16) * (mp / 16 + 1) / 2; }
+constexpr size_t tiny_x_bytes(int mp, int blocks) { return (size_t)blocks * mp * 64 * 2 * 2; }
+constexpr size_t tiny_lds(int mp, int blocks, bool full) { return tiny_x_bytes(mp, blocks) + (size_t)mp * mp * 2 * (full ? 2 : 1) + 64; }
+
+template <int MP, bool FULL, int MODE>
+__global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  constexpr int MB = MP / 16, GB = tiny_gram_blocks(MP), PER_WAVE = (GB + TINY_WAVES - 1) / TINY_WAVES;
+  constexpr int TASKS = MP * 8 / TINY_THREADS, MAX_BLOCKS = MODE == SOLO ? (MP == 64 ? 8 : 2) : MP == 64 ? 4 : 2;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int b = blockIdx.x / t.chunks, chunk = blockIdx.x % t.chunks;
+  const uint32_t x_half = t.blocks * (MP * 128), ab0 = 2 * x_half, ab_half = MP / 64 * (MP * 128);
+  double* sm = reinterpret_cast<double*>(smem + ab0 + ab_half * (FULL ? 2 : 1));
+  const int m_in = lane & 15, q4 = (lane >> 4) * 4;
+  auto at = [](int block, int row, int c) { return (uint32_t)((block * MP + row) * 128 + ((c ^ ((row >> 1) & 7)) << 4)); };
+  // 16 rows x 32 k of an operand whose k is contiguous; k step ks of 32
+  auto rows16 = [&](uint32_t base, int row0, int ks) {
+    return *reinterpret_cast<const half8*>(smem + base + at(ks >> 1, row0 + m_in, (ks & 1) * 4 + (lane >> 4)));
+  };
+  // 16 columns x 32 k of X, whose k are the rows
+  auto cols16 = [&](uint32_t base, int col0, int ks) {
+    const int s = lane & 15, k = ks * 32 + (lane >> 4) * 8 + (s >> 2), c = (col0 & 63) / 8 + ((s & 3) >> 1);
+    const unsigned char* p0 = smem + base + at(col0 >> 6, k, c) + (s & 1) * 8;
+    const unsigned char* p1 = smem + base + at(col0 >> 6, k + 4, c) + (s & 1) * 8;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)p0);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 __attribute__((address_space(3)))*)p1);
+    union { struct { s16x4 a, b; } h; half8 v; } u;
+    u.h.a = lo; u.h.b = hi;
+    return u.v;
+  };
+  auto mfma = [](const half8& x, const half8& y, f32x4& acc) { acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, acc, 0, 0, 0); };
+  // a lane's four neighbours of a row
+  auto four = [&](uint32_t base, int row, int col) {
+    return reinterpret_cast<half_t*>(smem + base + at(col >> 6, row, (col & 63) >> 3) + (col & 4) * 2);
+  };
+  typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+  // block i of this wavefront: its place among the GB, and its first row and column
+  auto block_of = [&](int i, int* r, int* c) {
+    const int id = wave + i * TINY_WAVES;
+    int tm = 0, left = min(id, GB - 1);
+    while (left >= MB - tm) { left -= MB - tm; ++tm; }
+    *r = tm * 16;
+    *c = (tm + left) * 16;
+    return id;
+  };
+  // the symmetric product of the rows at `base`, over `steps` k steps
+  auto gram = [&](uint32_t base, uint32_t half, int steps, f32x4 (&acc)[PER_WAVE]) {
+#pragma unroll
+    for (int i = 0; i < PER_WAVE; ++i) {
+      acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      int r, c;
+      if (block_of(i, &r, &c) >= GB) continue;
+#pragma unroll 2
+      for (int ks = 0; ks < steps; ++ks) {
+        const half8 x = rows16(base, r, ks), y = rows16(base, c, ks);
+        mfma(y, x, acc[i]);
+        if (FULL) {
+          mfma(rows16(base + half, c, ks), x, acc[i]);
+          mfma(y, rows16(base + half, r, ks), acc[i]);
+        }
+      }
+    }
+  };
+  // a symmetric matrix into the place of A and B
+  auto put_symmetric = [&](const f32x4 (&v)[PER_WAVE]) {
+#pragma unroll
+    for (int i = 0; i < PER_WAVE; ++i) {
+      int r, c;
+      if (block_of(i, &r, &c) >= GB) continue;
+      half4 hi, lo;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { hi[e] = (half_t)v[i][e]; lo[e] = (half_t)(v[i][e] - (float)hi[e]); }
+      *reinterpret_cast<half4*>(four(ab0, r + m_in, c + q4)) = hi;
+      if (FULL) *reinterpret_cast<half4*>(four(ab0 + ab_half, r + m_in, c + q4)) = lo;
+      if (r == c) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int row = c + q4 + e, col = r + m_in;
+        const uint32_t o = ab0 + at(col >> 6, row, (col & 63) >> 3) + (col & 7) * 2;
+        *reinterpret_cast<half_t*>(smem + o) = hi[e];
+        if (FULL) *reinterpret_cast<half_t*>(smem + o + ab_half) = lo[e];
+      }
+    }
+  };
+
+  // ---- X: converted from the gradient, or as the last step has left it
+  unsigned char* image = t.image + (size_t)blockIdx.x * tiny_x_bytes(MP, t.blocks);
+  if (MODE == NEXT) {
+    for (uint32_t o = tid * 16; o < 2 * x_half; o += TINY_THREADS * 16)
+      *reinterpret_cast<u32x4*>(smem + o) = *reinterpret_cast<const u32x4*>(image + o);
+  } else {
+    // a thread: 8 columns of a row of X in every block; neighbouring threads read neighbours of a row of the gradient
+    const float* g = t.g + b * t.stride_g;
+    const int m = t.tall ? t.N : t.M, n = t.tall ? t.M : t.N;
+    float v[MAX_BLOCKS * TASKS][8];
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < MAX_BLOCKS * TASKS; ++i) {
+      const int task = tid + i % TASKS * TINY_THREADS, block = i / TASKS;
+      const int r = t.tall ? task % MP : task / 8, c8 = t.tall ? task / MP : task % 8;
+      const int col = (chunk * t.blocks + block) * 64 + c8 * 8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const bool in = block < t.blocks && r < m && col + e < n;
+        v[i][e] = in ? (t.tall ? g[(col + e) * t.ld_g + r] : g[r * t.ld_g + col + e]) : 0.f;
+        if (MODE == SOLO) sum += (double)v[i][e] * v[i][e];
+      }
+    }
+    if (MODE == SOLO) {
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, WAVE);
+      if (lane == 0) sm[wave] = sum;
+      __syncthreads();
+      sum = 0.0;
+      for (int w = 0; w < TINY_WAVES; ++w) sum += sm[w];
+    } else {
+      for (int p = lane; p < t.parts; p += WAVE) sum += t.norms[(size_t)b * t.parts + p];
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, WAVE);
+    }
+    const double scale = (double)t.s / (sqrt(sum) + (double)t.eps);
+#pragma unroll
+    for (int i = 0; i < MAX_BLOCKS * TASKS; ++i) {
+      const int task = tid + i % TASKS * TINY_THREADS, block = i / TASKS;
+      if (block >= t.blocks) continue;
+      const int r = t.tall ? task % MP : task / 8, c8 = t.tall ? task / MP : task % 8;
+      const int col = (chunk * t.blocks + block) * 64 + c8 * 8;
+      float x[8];
+      // (what lies outside of the matrix stays 0 whatever the scale is)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = r < m && col + e < n ? (float)((double)v[i][e] * scale) : 0.f;
+      half8 hi, lo;
+      split8(x, &hi, &lo);
+      *reinterpret_cast<half8*>(smem + at(block, r, c8)) = hi;
+      *reinterpret_cast<half8*>(smem + x_half + at(block, r, c8)) = lo;
+    }
+  }
+  __syncthreads();
+
+  const int k_steps = t.blocks * 2;
+  const size_t sums_of = (size_t)GB * WAVE;    // float4 of a chunk
+  f32x4 acc[PER_WAVE];
+  const int first = MODE == NEXT ? t.step : 0, last = MODE == SOLO ? t.steps : MODE == NEXT ? t.step + 1 : 0;
+  for (int step = first; step < last; ++step) {
+    // A
+    if (MODE == SOLO) {
+      gram(0, x_half, k_steps, acc);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER_WAVE; ++i) {
+        acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const int id = wave + i * TINY_WAVES;
+        if (id >= GB) continue;
+        const float4* from = t.sums + (size_t)b * t.chunks * sums_of + id * WAVE + lane;
+#pragma unroll 8
+        for (int k = 0; k < t.chunks; ++k) {
+          const float4 v = from[k * sums_of];
+          acc[i][0] += v.x; acc[i][1] += v.y; acc[i][2] += v.z; acc[i][3] += v.w;
+        }
+      }
+    }
+    const float alpha = t.t / (t.s * t.s);
+#pragma unroll
+    for (int i = 0; i < PER_WAVE; ++i) acc[i] *= alpha;
+    put_symmetric(acc);
+    __syncthreads();
+    // B in its place
+    f32x4 square[PER_WAVE];
+    gram(ab0, ab_half, MP / 32, square);
+    const float cs = t.c * (t.u / t.t) / t.t, bs = t.b * (t.u / t.t);
+#pragma unroll
+    for (int i = 0; i < PER_WAVE; ++i) square[i] = cs * square[i] + bs * acc[i];
+    __syncthreads();
+    put_symmetric(square);
+    __syncthreads();
+    // X, 16 columns at a time; no other wavefront reads them
+    const bool old_lo = step < t.full_from, new_lo = step + 1 < t.full_from, end = step + 1 == t.steps;
+    const float as = end ? t.a / t.s : t.a, us = (end ? 1.f / t.s : 1.f) / t.u;
+    for (int strip = wave; strip < t.blocks * 4; strip += TINY_WAVES) {
+      const int col0 = strip * 16;
+      f32x4 y[MB] = {};
+#pragma unroll
+      for (int ks = 0; ks < MP / 32; ++ks) {
+        const half8 x = cols16(0, col0, ks);
+        half8 xl;
+        if (FULL) xl = cols16(x_half, col0, ks);
+#pragma unroll
+        for (int i = 0; i < MB; ++i) {
+          const half8 w = rows16(ab0, i * 16, ks);
+          mfma(x, w, y[i]);
+          if (FULL) {
+            mfma(xl, w, y[i]);
+            mfma(x, rows16(ab0 + ab_half, i * 16, ks), y[i]);
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        const int r = i * 16 + m_in, c = col0 + q4;
+        half4* hi_at = reinterpret_cast<half4*>(four(0, r, c));
+        half4* lo_at = reinterpret_cast<half4*>(four(x_half, r, c));
+        half4 hi = *hi_at, lo = {};
+        if (old_lo) lo = *lo_at;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = as * ((float)hi[e] + (float)lo[e]) + us * y[i][e];
+        if (!end) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { hi[e] = (half_t)v[e]; lo[e] = (half_t)(v[e] - (float)hi[e]); }
+          *hi_at = hi;
+          if (new_lo) *lo_at = lo;
+          continue;
+        }
+        const int gc = chunk * t.blocks * 64 + c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int row = t.tall ? gc + e : r, col = t.tall ? r : gc + e;
+          if (row >= t.M || col >= t.N) continue;
+          const long o = b * t.stride_o + row * t.ld_o + col;
+          if (FULL) ((float*)t.out)[o] = v[e];
+          else ((bf16_t*)t.out)[o] = (bf16_t)v[e];
+        }
+      }
+    }
+    __syncthreads();
+  }
+  if (MODE == SOLO || (MODE == NEXT && t.step + 1 == t.steps)) return;
+  // the chunk's share of the next A, and the chunk
+  gram(0, x_half, k_steps, acc);
+#pragma unroll
+  for (int i = 0; i < PER_WAVE; ++i) {
+    const int id = wave + i * TINY_WAVES;
+    if (id >= GB) continue;
+    t.sums_next[(size_t)blockIdx.x * sums_of + id * WAVE + lane] = float4{acc[i][0], acc[i][1], acc[i][2], acc[i][3]};
+  }
+  for (uint32_t o = tid * 16; o < 2 * x_half; o += TINY_THREADS * 16)
+    *reinterpret_cast<u32x4*>(image + o) = *reinterpret_cast<const u32x4*>(smem + o);
+}
+
 // ---- host -----------------------------------------------------------------------------------------
 
 struct Shape {
@@ -570,23 +829,45 @@ struct Scales {
 
 constexpr size_t MAX_ELEMENTS = (size_t)1 << 31;
 
+// How few rows are cut: 64-column blocks of a chunk, and chunks; none where X has too many rows.
+struct TinyPlan {
+  int mp = 0, blocks = 0, chunks = 0;
+  TinyPlan(const Shape& q) {
+    if (q.m > 128) return;
+    mp = q.m <= 64 ? 64 : 128;
+    const int all = cdiv(q.n, 64), solo = mp == 64 ? 8 : 2;
+    blocks = all <= solo ? all : mp == 64 ? 4 : 2;
+    chunks = cdiv(all, blocks);
+  }
+};
+
 struct Workspace {
-  double* sums;
+  double* sums = nullptr;
   Split X[2], A, B;
+  unsigned char* image = nullptr;
+  float4* partial[2] = {nullptr, nullptr};
   size_t bytes;
-  Workspace(void* scratch, int dtype, int batch, const Shape& q) {
+  Workspace(void* scratch, int dtype, int batch, const Shape& q, const TinyPlan& tiny) {
     Arena w(scratch);
     const bool full = dtype == BM_DTYPE_FP32;
-    sums = w.take<double>((size_t)batch * NORM_PARTS * sizeof(double));
-    for (Split& x : X) {
-      x.hi = w.take<half_t>(batch * q.x * sizeof(half_t));
-      x.lo = w.take<half_t>(batch * q.x * sizeof(half_t));
+    if (tiny.chunks != 1) sums = w.take<double>((size_t)batch * NORM_PARTS * sizeof(double));
+    if (tiny.chunks) {
+      if (tiny.chunks > 1) {
+        const size_t chunks = (size_t)batch * tiny.chunks;
+        image = w.take<unsigned char>(chunks * tiny_x_bytes(tiny.mp, tiny.blocks));
+        for (float4*& s : partial) s = w.take<float4>(chunks * tiny_gram_blocks(tiny.mp) * WAVE * sizeof(float4));
+      }
+    } else {
+      for (Split& x : X) {
+        x.hi = w.take<half_t>(batch * q.x * sizeof(half_t));
+        x.lo = w.take<half_t>(batch * q.x * sizeof(half_t));
+      }
+      for (Split* x : {&A, &B}) {
+        x->hi = w.take<half_t>(batch * q.a * sizeof(half_t));
+        x->lo = full ? w.take<half_t>(batch * q.a * sizeof(half_t)) : nullptr;
+      }
     }
-    for (Split* x : {&A, &B}) {
-      x->hi = w.take<half_t>(batch * q.a * sizeof(half_t));
-      x->lo = full ? w.take<half_t>(batch * q.a * sizeof(half_t)) : nullptr;
-    }
-    bytes = w.off;
+    bytes = std::max(w.off, (size_t)256);
   }
 };
 
@@ -637,6 +918,31 @@ bm_status launch(const Product& p, int batch, hipStream_t st) {
   return launch_tile<KIND, 128, 2, 2>(p, batch, st);
 }
 
+template <int MP, bool FULL, int MODE>
+bm_status launch_tiny(const Tiny& t, int batch, hipStream_t st) {
+  auto kern = tiny_kernel<MP, FULL, MODE>;
+  static std::atomic<uint64_t> done{0};
+  constexpr int MOST = MODE == SOLO ? (MP == 64 ? 8 : 2) : MP == 64 ? 4 : 2;
+  static_assert(tiny_lds(MP, MOST, FULL) <= 160 * 1024, "a chunk with A or B");
+  BM_RETURN_IF(allow_lds(kern, tiny_lds(MP, MOST, FULL), &done));
+  hipLaunchKernelGGL(kern, dim3((unsigned)((long)batch * t.chunks)), dim3(TINY_THREADS), tiny_lds(MP, t.blocks, FULL), st, t);
+  BM_CHECK_LAUNCH("orthogonalize few rows");
+  return BM_OK;
+}
+
+template <int MP, bool FULL>
+bm_status run_tiny(Tiny t, int batch, const Workspace& w, hipStream_t st) {
+  if (t.chunks == 1) return launch_tiny<MP, FULL, SOLO>(t, batch, st);
+  t.sums_next = w.partial[0];
+  BM_RETURN_IF((launch_tiny<MP, FULL, FIRST>(t, batch, st)));
+  for (t.step = 0; t.step < t.steps; ++t.step) {
+    t.sums = w.partial[t.step & 1];
+    t.sums_next = w.partial[(t.step + 1) & 1];
+    BM_RETURN_IF((launch_tiny<MP, FULL, NEXT>(t, batch, st)));
+  }
+  return BM_OK;
+}
+
 bool sizes_ok(int dtype, int batch, int M, int N) {
   if (!good_dtype(dtype) || batch <= 0 || M <= 0 || N <= 0) return false;
   if (M > (1 << 20) || N > (1 << 20)) return false;
@@ -650,7 +956,7 @@ bool sizes_ok(int dtype, int batch, int M, int N) {
 using namespace bm;
 
 extern "C" size_t bm_orthogonalize_scratch_bytes(int32_t dtype, int32_t batch, int32_t M, int32_t N) {
-  return sizes_ok(dtype, batch, M, N) ? Workspace(nullptr, dtype, batch, Shape(M, N)).bytes : 0;
+  return sizes_ok(dtype, batch, M, N) ? Workspace(nullptr, dtype, batch, Shape(M, N), TinyPlan(Shape(M, N))).bytes : 0;
 }
 
 extern "C" bm_status bm_orthogonalize(int32_t dtype, int32_t batch, int32_t M, int32_t N, const float* grad, int32_t ld_g,
@@ -675,7 +981,8 @@ extern "C" bm_status bm_orthogonalize(int32_t dtype, int32_t batch, int32_t M, i
     set_error("bm_orthogonalize: singular values do not stay below 8 under these coefficients");
     return BM_ERR_UNSUPPORTED;
   }
-  const Workspace w(scratch, dtype, batch, q);
+  const TinyPlan tiny(q);
+  const Workspace w(scratch, dtype, batch, q, tiny);
   if (!scratch || scratch_bytes < w.bytes) {
     set_error("bm_orthogonalize needs %zu scratch bytes, got %zu", w.bytes, scratch_bytes);
     return BM_ERR_WORKSPACE_TOO_SMALL;
@@ -693,9 +1000,30 @@ extern "C" bm_status bm_orthogonalize(int32_t dtype, int32_t batch, int32_t M, i
   const uint32_t pieces = (uint32_t)((size_t)M * N / (vec ? 4 : 1)), per_row = ld_g == N ? pieces : (uint32_t)(vec ? N / 4 : N);
   // enough parts for 8 workgroups a CU, none without 4 pieces a thread
   const int parts = std::max(1, std::min({NORM_PARTS, cdiv(2048, batch), cdiv(pieces, 1024)}));
-  hipLaunchKernelGGL((vec ? norm_kernel<4> : norm_kernel<1>), dim3((unsigned)batch * parts), dim3(256), 0, st, grad, (long)ld_g,
-                     (long)stride_g, per_row, pieces, parts, w.sums);
-  BM_CHECK_LAUNCH("orthogonalize norm");
+  auto norms = [&]() -> bm_status {
+    hipLaunchKernelGGL((vec ? norm_kernel<4> : norm_kernel<1>), dim3((unsigned)batch * parts), dim3(256), 0, st, grad, (long)ld_g,
+                       (long)stride_g, per_row, pieces, parts, w.sums);
+    BM_CHECK_LAUNCH("orthogonalize norm");
+    return BM_OK;
+  };
+  if (tiny.chunks) {
+    ProfScope prof(PROF_GEMM_NT, steps * (double)batch * terms * ((double)q.m * q.m * (3.0 * q.n + q.m)), st);
+    if (tiny.chunks > 1) BM_RETURN_IF(norms());
+    Tiny t{};
+    t.g = grad; t.ld_g = ld_g; t.stride_g = stride_g;
+    t.M = M; t.N = N; t.tall = q.tall;
+    t.norms = w.sums; t.parts = parts;
+    t.eps = eps; t.s = k.s; t.t = k.t; t.u = k.u;
+    t.a = a; t.b = b; t.c = c;
+    t.steps = steps;
+    t.full_from = full ? steps : std::max(0, steps - 2);
+    t.blocks = tiny.blocks; t.chunks = tiny.chunks;
+    t.image = w.image;
+    t.out = out; t.ld_o = ld_o; t.stride_o = stride_o;
+    if (tiny.mp == 64) return full ? run_tiny<64, true>(t, batch, w, st) : run_tiny<64, false>(t, batch, w, st);
+    return full ? run_tiny<128, true>(t, batch, w, st) : run_tiny<128, false>(t, batch, w, st);
+  }
+  BM_RETURN_IF(norms());
   const int tiles_n = q.np / PAD, across = std::max(1, std::min(4, (int)((long)tiles_n * (q.mp / PAD) * batch / 2048)));
   const int runs_n = cdiv(tiles_n, across), runs = q.mp / PAD * runs_n;
   const bool rows_vec = ld_g % 4 == 0 && (batch == 1 || stride_g % 4 == 0);

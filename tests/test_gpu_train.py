@@ -401,7 +401,9 @@ def spectrum(rng, M, N, kind):
 SHAPES = [(1, 1, 1, "noise"), (1, 1, 40, "noise"), (1, 40, 1, "noise"), (1, 5, 3, "one"), (1, 64, 64, "noise"), (1, 65, 63, "noise"),
           (3, 20, 200, "falls"), (2, 200, 20, "falls"), (1, 130, 130, "falls"), (1, 192, 64, "noise"), (2, 257, 129, "noise"),
           (1, 256, 256, "falls"), (1, 300, 700, "noise"), (2, 513, 320, "noise"), (1, 640, 520, "falls"), (17, 33, 70, "noise"),
-          (1, 16, 3000, "noise"), (1, 3000, 100, "falls"), (1, 96, 96, "one"), (2, 768, 1000, "noise"), (1, 1030, 1100, "noise")]
+          (1, 16, 3000, "noise"), (1, 3000, 100, "falls"), (1, 96, 96, "one"), (2, 768, 1000, "noise"), (1, 1030, 1100, "noise"),
+          (1, 64, 512, "falls"), (2, 513, 64, "noise"), (1, 10, 1025, "falls"), (3, 128, 128, "falls"), (1, 65, 129, "falls"), (2, 700, 128, "falls"),
+          (1, 129, 140, "noise"), (1, 1, 700, "one"), (5, 100, 300, "noise")]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
