@@ -532,7 +532,7 @@ __global__ __launch_bounds__(512, 2) void large_product_kernel(Product p, int ti
 //
 // LDS: X and then A or B in blocks of MP rows x 64 columns, 128 bytes a row, 16-byte chunk c of row r at c ^ ((r >> 1) & 7); hi, and lo
 // behind it.  A chunk lies in the workspace as it does in LDS.
-constexpr int TINY_THREADS = 512, TINY_WAVES = TINY_THREADS / WAVE;
+constexpr int TINY_THREADS = 1024, TINY_WAVES = TINY_THREADS / WAVE;
 enum { SOLO = 0, FIRST, NEXT };                // all steps; conversion and the first sums; one step
 
 struct Tiny {
@@ -542,7 +542,7 @@ struct Tiny {
   float eps, s, t, u;                          // Scales
   float a, b, c;
   int steps, step, full_from;                  // X entering step i has a lo part while i < full_from
-  int blocks, chunks;                          // 64-column blocks of a chunk, chunks of a matrix
+  int blocks, chunks, summands;                // 64-column blocks of a chunk, chunks of a matrix, and how many sums there are of them
   unsigned char* image;                        // [batch, chunks] chunks
   float4 *sums, *sums_next;                    // [batch, chunks, blocks of A, 64]
   void* out; long ld_o, stride_o;
@@ -557,7 +557,8 @@ template <int MP, bool FULL, int MODE>
 __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr int MB = MP / 16, GB = tiny_gram_blocks(MP), PER_WAVE = (GB + TINY_WAVES - 1) / TINY_WAVES;
-  constexpr int TASKS = MP * 8 / TINY_THREADS, MAX_BLOCKS = MODE == SOLO ? (MP == 64 ? 8 : 2) : MP == 64 ? 4 : 2;
+  constexpr int MAX_BLOCKS = MODE == SOLO ? (MP == 64 ? 8 : 2) : MP == 64 ? 4 : 2;
+  constexpr int BLOCK_TASKS = MP * 8, TASKS = MAX_BLOCKS * BLOCK_TASKS / TINY_THREADS;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int b = blockIdx.x / t.chunks, chunk = blockIdx.x % t.chunks;
   const uint32_t x_half = t.blocks * (MP * 128), ab0 = 2 * x_half, ab_half = MP / 64 * (MP * 128);
@@ -601,7 +602,7 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
       acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
       int r, c;
       if (block_of(i, &r, &c) >= GB) continue;
-#pragma unroll 2
+#pragma unroll 4
       for (int ks = 0; ks < steps; ++ks) {
         const half8 x = rows16(base, r, ks), y = rows16(base, c, ks);
         mfma(y, x, acc[i]);
@@ -643,11 +644,11 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
     // a thread: 8 columns of a row of X in every block; neighbouring threads read neighbours of a row of the gradient
     const float* g = t.g + b * t.stride_g;
     const int m = t.tall ? t.N : t.M, n = t.tall ? t.M : t.N;
-    float v[MAX_BLOCKS * TASKS][8];
+    float v[TASKS][8];
     double sum = 0.0;
 #pragma unroll
-    for (int i = 0; i < MAX_BLOCKS * TASKS; ++i) {
-      const int task = tid + i % TASKS * TINY_THREADS, block = i / TASKS;
+    for (int i = 0; i < TASKS; ++i) {
+      const int block = (tid + i * TINY_THREADS) / BLOCK_TASKS, task = (tid + i * TINY_THREADS) % BLOCK_TASKS;
       const int r = t.tall ? task % MP : task / 8, c8 = t.tall ? task / MP : task % 8;
       const int col = (chunk * t.blocks + block) * 64 + c8 * 8;
 #pragma unroll
@@ -671,8 +672,8 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
     }
     const double scale = (double)t.s / (sqrt(sum) + (double)t.eps);
 #pragma unroll
-    for (int i = 0; i < MAX_BLOCKS * TASKS; ++i) {
-      const int task = tid + i % TASKS * TINY_THREADS, block = i / TASKS;
+    for (int i = 0; i < TASKS; ++i) {
+      const int block = (tid + i * TINY_THREADS) / BLOCK_TASKS, task = (tid + i * TINY_THREADS) % BLOCK_TASKS;
       if (block >= t.blocks) continue;
       const int r = t.tall ? task % MP : task / 8, c8 = t.tall ? task / MP : task % 8;
       const int col = (chunk * t.blocks + block) * 64 + c8 * 8;
@@ -704,7 +705,7 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
         if (id >= GB) continue;
         const float4* from = t.sums + (size_t)b * t.chunks * sums_of + id * WAVE + lane;
 #pragma unroll 8
-        for (int k = 0; k < t.chunks; ++k) {
+        for (int k = 0; k < t.summands; ++k) {
           const float4 v = from[k * sums_of];
           acc[i][0] += v.x; acc[i][1] += v.y; acc[i][2] += v.z; acc[i][3] += v.w;
         }
@@ -786,6 +787,20 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
   }
   for (uint32_t o = tid * 16; o < 2 * x_half; o += TINY_THREADS * 16)
     *reinterpret_cast<u32x4*>(image + o) = *reinterpret_cast<const u32x4*>(smem + o);
+}
+
+// The sums of a matrix's chunks in the place of the first one's: where there are many, every workgroup would add up all of them.
+__global__ __launch_bounds__(256) void tiny_sum_kernel(float4* __restrict__ sums, int chunks, int per_chunk) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= per_chunk) return;
+  float4* from = sums + (size_t)blockIdx.y * chunks * per_chunk + i;
+  float4 s = from[0];
+#pragma unroll 8
+  for (int k = 1; k < chunks; ++k) {
+    const float4 v = from[(size_t)k * per_chunk];
+    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+  }
+  from[0] = s;
 }
 
 // ---- host -----------------------------------------------------------------------------------------
@@ -930,6 +945,8 @@ bm_status launch_tiny(const Tiny& t, int batch, hipStream_t st) {
   return BM_OK;
 }
 
+constexpr long TINY_SUMS = 240;
+
 template <int MP, bool FULL>
 bm_status run_tiny(Tiny t, int batch, const Workspace& w, hipStream_t st) {
   if (t.chunks == 1) return launch_tiny<MP, FULL, SOLO>(t, batch, st);
@@ -938,6 +955,14 @@ bm_status run_tiny(Tiny t, int batch, const Workspace& w, hipStream_t st) {
   for (t.step = 0; t.step < t.steps; ++t.step) {
     t.sums = w.partial[t.step & 1];
     t.sums_next = w.partial[(t.step + 1) & 1];
+    t.summands = t.chunks;
+    // SUMRULE
+    if ((long)t.chunks * tiny_gram_blocks(MP) > TINY_SUMS && batch < 65536) {
+      constexpr int per_chunk = tiny_gram_blocks(MP) * WAVE;
+      hipLaunchKernelGGL(tiny_sum_kernel, dim3(cdiv(per_chunk, 256), batch), dim3(256), 0, st, w.partial[t.step & 1], t.chunks, per_chunk);
+      BM_CHECK_LAUNCH("orthogonalize sums");
+      t.summands = 1;
+    }
     BM_RETURN_IF((launch_tiny<MP, FULL, NEXT>(t, batch, st)));
   }
   return BM_OK;
