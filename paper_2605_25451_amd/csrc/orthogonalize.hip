@@ -329,32 +329,38 @@ struct Operands {
 
 // ---- TILE x TILE (64 or 128), GROUPS times four wavefronts of a quarter each: group g multiplies the slices g, g + GROUPS, ...
 // of the contraction, and group 0 adds up their sums.  Each has DEPTH slices of LDS: DEPTH - 1 are on their way while one is
-// multiplied, with one barrier a slice.
-constexpr int small_lds(int tile, int depth, int groups) { return groups * depth * 2 * tile * BK * 2; }
+// multiplied, with one barrier a slice.  FULL: a slice holds hi and lo of both operands, for three products each (as slices of their own
+// the products would fetch six operands instead of four).
+constexpr int small_lds(int tile, int depth, int groups, bool full) { return groups * depth * 2 * tile * BK * 2 * (full ? 2 : 1); }
 
-template <int KIND, int TILE, int DEPTH, int GROUPS>
+template <int KIND, int TILE, int DEPTH, int GROUPS, bool FULL>
 __global__ __launch_bounds__(256 * GROUPS) void small_product_kernel(Product p, int tiles_m, int tiles_n, int tiles) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr bool NN = KIND == STEP || KIND == LAST;
   using RegA = Region<TILE, false, 4>;
   using RegB = Region<TILE, NN, 4>;
-  constexpr uint32_t B0 = RegA::BYTES, BUF = B0 + RegB::BYTES;
-  constexpr int LOADS = RegA::LOADS + RegB::LOADS, F = TILE / 32, HALF = TILE / 2;
+  constexpr int PARTS = FULL ? 2 : 1;                        // hi, lo
+  constexpr uint32_t B0 = PARTS * RegA::BYTES, BUF = B0 + PARTS * RegB::BYTES;
+  constexpr int LOADS = PARTS * (RegA::LOADS + RegB::LOADS), F = TILE / 32, HALF = TILE / 2;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) & 3);
   const int group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
   const int wm = wave >> 1, wn = wave & 1;
   const Place q = place<!NN>(tiles_m, tiles_n, tiles);
   const int m0 = q.tm * TILE, n0 = q.tn * TILE;
   const Operands<NN> op(p, q, m0, n0);
-  const int all = op.slices * p.terms, n = (all - group + GROUPS - 1) / GROUPS;
+  const int n = (op.slices - group + GROUPS - 1) / GROUPS;
   RegA ra;
   RegB rb;
   ra.init(p.lda, 0, p.M - m0, wave, lane);
   rb.init(p.ldb, 0, p.N - n0, wave, lane);
   const uint32_t base = group * (DEPTH * BUF);
   auto load = [&](int j, uint32_t buf) {
-    rb.template load<false>(op.b_at(group + j * GROUPS), p.ldb, BK, base + buf + B0, wave, lane);
-    ra.template load<false>(op.a_at(group + j * GROUPS), p.lda, BK, base + buf, wave, lane);
+    const size_t k = (size_t)(group + j * GROUPS);
+#pragma unroll
+    for (int h = 0; h < PARTS; ++h) {
+      rb.template load<false>(op.b[h] + k * op.b_step, p.ldb, BK, base + buf + B0 + h * RegB::BYTES, wave, lane);
+      ra.template load<false>(op.a[h] + k * BK, p.lda, BK, base + buf + h * RegA::BYTES, wave, lane);
+    }
   };
   Fragments<TILE, false, F> fa;
   Fragments<TILE, NN, F> fb;
@@ -365,7 +371,7 @@ __global__ __launch_bounds__(256 * GROUPS) void small_product_kernel(Product p, 
   for (int s = 0; s < DEPTH - 1; ++s)
     if (s < n) load(s, s * BUF);
   uint32_t cur = 0, free = (DEPTH - 1) * BUF;
-  for (int j = 0; j * GROUPS < all; ++j) {
+  for (int j = 0; j * GROUPS < op.slices; ++j) {
     // slice j has landed; later ones need not have
     const int later = n - 1 - j;
     if (later >= DEPTH - 2) wait_loads<(DEPTH - 2) * LOADS>();
@@ -374,21 +380,30 @@ __global__ __launch_bounds__(256 * GROUPS) void small_product_kernel(Product p, 
     end_phase();                                             // for all; and all have read slice j - 1
     if (j >= n) break;                                       // (only in the last round)
     if (j + DEPTH - 1 < n) load(j + DEPTH - 1, free);
-    bf16x8 a[2][F], bb[2][F];
+    bf16x8 a[PARTS][2][F], bb[PARTS][2][F];
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
+    for (int h = 0; h < PARTS; ++h)
 #pragma unroll
-      for (int f = 0; f < F; ++f) {
-        bb[ks][f] = fb.read(smem, f, ks, base + cur + B0);
-        a[ks][f] = fa.read(smem, f, ks, base + cur);
-      }
+      for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
+        for (int f = 0; f < F; ++f) {
+          bb[h][ks][f] = fb.read(smem, f, ks, base + cur + B0 + h * RegB::BYTES);
+          a[h][ks][f] = fa.read(smem, f, ks, base + cur + h * RegA::BYTES);
+        }
+    auto multiply = [&](int ha, int hb) {
 #pragma unroll
-      for (int i = 0; i < F; ++i)
+      for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-        for (int c = 0; c < F; ++c)
-          acc[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half(bb[ks][c]), as_half(a[ks][i]), acc[i][c], 0, 0, 0);
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+          for (int c = 0; c < F; ++c)
+            acc[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half(bb[hb][ks][c]), as_half(a[ha][ks][i]), acc[i][c], 0, 0, 0);
+    };
+    multiply(0, 0);
+    if constexpr (FULL) {
+      multiply(0, 1);
+      multiply(1, 0);
+    }
     wait_fragments();
     free = cur;
     cur = cur == (DEPTH - 1) * BUF ? 0 : cur + BUF;
@@ -396,8 +411,8 @@ __global__ __launch_bounds__(256 * GROUPS) void small_product_kernel(Product p, 
   end_phase();                                               // sums and strips overlay the slices
   constexpr int SUM = TILE * TILE;                           // floats of a group's sums
   float* sums = reinterpret_cast<float*>(smem);
+  static_assert(((GROUPS - 1) * SUM + 4 * 16 * (F * 16 + 4)) * 4 <= small_lds(TILE, DEPTH, GROUPS, FULL), "sums and strips fit");
   if constexpr (GROUPS > 1) {
-    static_assert(((GROUPS - 1) * SUM + 4 * 16 * (F * 16 + 4)) * 4 <= small_lds(TILE, DEPTH, GROUPS), "the sums of the groups fit");
     auto at = [&](int g, int i, int c) {
       return reinterpret_cast<f32x4*>(sums + (g - 1) * SUM + (((wave * F + i) * F + c) * 64 + lane) * 4);
     };
@@ -899,13 +914,13 @@ bm_status allow_lds(Kernel kern, size_t lds, std::atomic<uint64_t>* done) {
 }
 
 // GROUPS = 0: the kernel of two groups that take turns
-template <int KIND, int TILE, int DEPTH, int GROUPS>
+template <int KIND, int TILE, int DEPTH, int GROUPS, bool FULL>
 bm_status launch_tile(const Product& p, int batch, hipStream_t st) {
   constexpr bool SYMMETRIC = KIND == GRAM || KIND == POLY;
-  constexpr size_t lds = GROUPS ? small_lds(TILE, DEPTH, GROUPS) : 2 * 2 * TILE * BK * sizeof(half_t);
+  constexpr size_t lds = GROUPS ? small_lds(TILE, DEPTH, GROUPS, FULL) : 2 * 2 * TILE * BK * sizeof(half_t);
   void (*kern)(Product, int, int, int);
   if constexpr (GROUPS == 0) kern = large_product_kernel<KIND>;
-  else kern = small_product_kernel<KIND, TILE, DEPTH, GROUPS>;
+  else kern = small_product_kernel<KIND, TILE, DEPTH, GROUPS, FULL>;
   static std::atomic<uint64_t> done{0};
   BM_RETURN_IF(allow_lds(kern, lds, &done));
   const int tm = cdiv(p.M, TILE), tn = cdiv(p.N, TILE), tiles = SYMMETRIC ? tm * (tm + 1) / 2 : tm * tn;
@@ -927,10 +942,15 @@ bm_status launch(const Product& p, int batch, hipStream_t st) {
     return (SYMMETRIC ? tm * (tm + 1) / 2 : tm * tn) * batch;
   };
   constexpr int NUM_CU = 256;
-  if (tiles(256) >= NUM_CU / 2) return launch_tile<KIND, 256, 2, 0>(p, batch, st);
-  if (tiles(64) <= NUM_CU) return launch_tile<KIND, 64, 4, 2>(p, batch, st);
-  if (tiles(128) <= NUM_CU / 2) return launch_tile<KIND, 64, 4, 1>(p, batch, st);
-  return launch_tile<KIND, 128, 2, 2>(p, batch, st);
+  if (tiles(256) >= NUM_CU / 2) return launch_tile<KIND, 256, 2, 0, false>(p, batch, st);
+  if (p.terms > 1) {
+    if (tiles(64) <= NUM_CU) return launch_tile<KIND, 64, 2, 2, true>(p, batch, st);
+    if (tiles(128) <= NUM_CU / 2) return launch_tile<KIND, 64, 2, 1, true>(p, batch, st);
+    return launch_tile<KIND, 128, 2, 1, true>(p, batch, st);
+  }
+  if (tiles(64) <= NUM_CU) return launch_tile<KIND, 64, 4, 2, false>(p, batch, st);
+  if (tiles(128) <= NUM_CU / 2) return launch_tile<KIND, 64, 4, 1, false>(p, batch, st);
+  return launch_tile<KIND, 128, 2, 2, false>(p, batch, st);
 }
 
 template <int MP, bool FULL, int MODE>
