@@ -538,12 +538,15 @@ __global__ __launch_bounds__(512, 2) void large_product_kernel(Product p, int ti
                      });
 }
 
-// ---- few rows: 64 or 128 of X at most ----------------------------------------------------------------
+// ---- few rows: 32, 64 or 128 of X at most ----------------------------------------------------------------
 //
 // A and B fit the LDS of a workgroup, so that a whole step is one launch: a workgroup holds a chunk of X's columns, has A from the sums
 // of all chunks, computes B for itself, moves its chunk on and adds up the chunk's share of the next A.  Where X is one
-// chunk (64 x 512, 128 x 128), all steps are one launch.  The products of the tiled kernels would be three launches a step of one to a few workgroups:
+// chunk (32 x 1024, 64 x 512, 128 x 128), all steps are one launch.  The products of the tiled kernels would be three launches a step of one to a few workgroups:
 // 192 x 64 59 us, here TINY192; 29 x 2350 93 and TINY29; 100 x 4096 127 and TINY100.
+//
+// Up to 32 rows take the three products for bf16 results, too: single roundings do not average out there (16 x 64: up to 0.18 % off
+// with a single product), and what they cost is launches.
 //
 // LDS: X and then A or B in blocks of MP rows x 64 columns, 128 bytes a row, 16-byte chunk c of row r at c ^ ((r >> 1) & 7); hi, and lo
 // behind it.  A chunk lies in the workspace as it does in LDS.
@@ -561,22 +564,26 @@ struct Tiny {
   unsigned char* image;                        // [batch, chunks] chunks
   float4 *sums, *sums_next;                    // [batch, chunks, blocks of A, 64]
   void* out; long ld_o, stride_o;
+  int out_fp32;
 };
 
+// the most 64-column blocks of a chunk: of a matrix that is one, and of others (64 KiB of X, so that two chunks of up to 64 rows share a CU)
+constexpr int tiny_blocks(int mp, bool solo) { return mp == 128 ? 2 : solo ? 512 / mp : 256 / mp; }
 // blocks of 16 x 16 on and above the diagonal of A
 constexpr int tiny_gram_blocks(int mp) { return (mp / 16) * (mp / 16 + 1) / 2; }
 constexpr size_t tiny_x_bytes(int mp, int blocks) { return (size_t)blocks * mp * 64 * 2 * 2; }
-constexpr size_t tiny_lds(int mp, int blocks, bool full) { return tiny_x_bytes(mp, blocks) + (size_t)mp * mp * 2 * (full ? 2 : 1) + 64; }
+constexpr uint32_t tiny_ab_bytes(int mp) { return (mp + 63) / 64 * mp * 128; }
+constexpr size_t tiny_lds(int mp, int blocks, bool full) { return tiny_x_bytes(mp, blocks) + tiny_ab_bytes(mp) * (full ? 2 : 1) + 256 + (mp == 32 ? 16 * 1024 : 0); }
 
 template <int MP, bool FULL, int MODE>
 __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr int MB = MP / 16, GB = tiny_gram_blocks(MP), PER_WAVE = (GB + TINY_WAVES - 1) / TINY_WAVES;
-  constexpr int MAX_BLOCKS = MODE == SOLO ? (MP == 64 ? 8 : 2) : MP == 64 ? 4 : 2;
-  constexpr int BLOCK_TASKS = MP * 8, TASKS = MAX_BLOCKS * BLOCK_TASKS / TINY_THREADS;
+  constexpr int MAX_BLOCKS = tiny_blocks(MP, MODE == SOLO);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int b = blockIdx.x / t.chunks, chunk = blockIdx.x % t.chunks;
-  const uint32_t x_half = t.blocks * (MP * 128), ab0 = 2 * x_half, ab_half = MP / 64 * (MP * 128);
+  const uint32_t x_half = t.blocks * (MP * 128), ab0 = 2 * x_half;
+  constexpr uint32_t ab_half = tiny_ab_bytes(MP);
   double* sm = reinterpret_cast<double*>(smem + ab0 + ab_half * (FULL ? 2 : 1));
   const int m_in = lane & 15, q4 = (lane >> 4) * 4;
   auto at = [](int block, int row, int c) { return (uint32_t)((block * MP + row) * 128 + ((c ^ ((row >> 1) & 7)) << 4)); };
@@ -610,21 +617,48 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
     *c = (tm + left) * 16;
     return id;
   };
-  // the symmetric product of the rows at `base`, over `steps` k steps
+  // a block of the symmetric product of the rows at `base`, over k steps from .. to - 1
+  auto gram_block = [&](uint32_t base, uint32_t half, int r, int c, int from, int to) {
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    auto step = [&](int ks) {
+      const half8 x = rows16(base, r, ks), y = rows16(base, c, ks);
+      mfma(y, x, v);
+      if (FULL) {
+        mfma(rows16(base + half, c, ks), x, v);
+        mfma(y, rows16(base + half, r, ks), v);
+      }
+    };
+    // (two a trip; the compiler unrolls no loop of MFMAs whose length it does not know)
+    int ks = from;
+    for (; ks + 2 <= to; ks += 2) { step(ks); step(ks + 1); }
+    if (ks < to) step(ks);
+    return v;
+  };
   auto gram = [&](uint32_t base, uint32_t half, int steps, f32x4 (&acc)[PER_WAVE]) {
 #pragma unroll
     for (int i = 0; i < PER_WAVE; ++i) {
-      acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
       int r, c;
-      if (block_of(i, &r, &c) >= GB) continue;
-#pragma unroll 4
-      for (int ks = 0; ks < steps; ++ks) {
-        const half8 x = rows16(base, r, ks), y = rows16(base, c, ks);
-        mfma(y, x, acc[i]);
-        if (FULL) {
-          mfma(rows16(base + half, c, ks), x, acc[i]);
-          mfma(y, rows16(base + half, r, ks), acc[i]);
-        }
+      acc[i] = block_of(i, &r, &c) < GB ? gram_block(base, half, r, c, 0, steps) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  // that of X, whose columns are shared by as many wavefronts as there are for a block
+  constexpr int SHARE = TINY_WAVES / GB > 1 ? TINY_WAVES / GB : 1;
+  auto gram_x = [&](f32x4 (&acc)[PER_WAVE]) {
+    if constexpr (SHARE == 1) {
+      gram(0, x_half, t.blocks * 2, acc);
+    } else {
+      static_assert(PER_WAVE == 1, "a block a wavefront");
+      f32x4* shares = reinterpret_cast<f32x4*>(smem + ab0 + ab_half * (FULL ? 2 : 1) + 256);
+      const int part = wave / GB, block = wave % GB, per = (t.blocks * 2 + SHARE - 1) / SHARE;
+      int r = 0, left = block;
+      while (left >= MB - r) { left -= MB - r; ++r; }
+      acc[0] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (part < SHARE) acc[0] = gram_block(0, x_half, r * 16, (r + left) * 16, part * per, min(t.blocks * 2, part * per + per));
+      if (part > 0 && part < SHARE) shares[((part - 1) * GB + block) * WAVE + lane] = acc[0];
+      __syncthreads();
+      if (part == 0) {
+#pragma unroll
+        for (int p = 1; p < SHARE; ++p) acc[0] += shares[((p - 1) * GB + block) * WAVE + lane];
       }
     }
   };
@@ -651,67 +685,70 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
   };
 
   // ---- X: converted from the gradient, or as the last step has left it
+  // a thread's elements of a 64-column block in the gradient and the result, and their steps: neighbours have neighbours of a row
+  constexpr int EACH = MP * 64 / TINY_THREADS;
+  const int first_col = chunk * t.blocks * 64;
+  auto element = [&](int k, int r, int c) { return at(k, r, c >> 3) + (c & 7) * 2; };
+  auto each_element = [&](auto body) {
+    if (t.tall) body(Int<1>{}, tid % MP, tid / MP);
+    else body(Int<0>{}, tid / 64, tid % 64);
+  };
   unsigned char* image = t.image + (size_t)blockIdx.x * tiny_x_bytes(MP, t.blocks);
   if (MODE == NEXT) {
     for (uint32_t o = tid * 16; o < 2 * x_half; o += TINY_THREADS * 16)
       *reinterpret_cast<u32x4*>(smem + o) = *reinterpret_cast<const u32x4*>(image + o);
   } else {
-    // a thread: 8 columns of a row of X in every block; neighbouring threads read neighbours of a row of the gradient
-    const float* g = t.g + b * t.stride_g;
-    const int m = t.tall ? t.N : t.M, n = t.tall ? t.M : t.N;
-    float v[TASKS][8];
-    double sum = 0.0;
+    each_element([&](auto tall_t, int r0, int c0) {
+      constexpr bool TALL = decltype(tall_t)::value;
+      constexpr int DR = TALL ? 0 : TINY_THREADS / 64, DC = TALL ? TINY_THREADS / MP : 0;
+      const float* g = t.g + b * t.stride_g + (TALL ? (first_col + c0) * t.ld_g + r0 : r0 * t.ld_g + first_col + c0);
+      const int m = TALL ? t.N : t.M, n = TALL ? t.M : t.N;
+      float v[MAX_BLOCKS][EACH];
+      double sum = 0.0;
 #pragma unroll
-    for (int i = 0; i < TASKS; ++i) {
-      const int block = (tid + i * TINY_THREADS) / BLOCK_TASKS, task = (tid + i * TINY_THREADS) % BLOCK_TASKS;
-      const int r = t.tall ? task % MP : task / 8, c8 = t.tall ? task / MP : task % 8;
-      const int col = (chunk * t.blocks + block) * 64 + c8 * 8;
+      for (int k = 0; k < MAX_BLOCKS; ++k)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool in = block < t.blocks && r < m && col + e < n;
-        v[i][e] = in ? (t.tall ? g[(col + e) * t.ld_g + r] : g[r * t.ld_g + col + e]) : 0.f;
-        if (MODE == SOLO) sum += (double)v[i][e] * v[i][e];
+        for (int e = 0; e < EACH && k < t.blocks; ++e)
+          v[k][e] = r0 + e * DR < m && first_col + k * 64 + c0 + e * DC < n ? g[TALL ? (k * 64 + e * DC) * t.ld_g : e * DR * t.ld_g + k * 64] : 0.f;
+      if (MODE == SOLO) {
+#pragma unroll
+        for (int k = 0; k < MAX_BLOCKS; ++k)
+#pragma unroll
+          for (int e = 0; e < EACH && k < t.blocks; ++e) sum += (double)v[k][e] * v[k][e];
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, WAVE);
+        if (lane == 0) sm[wave] = sum;
+        __syncthreads();
+        sum = 0.0;
+        for (int w = 0; w < TINY_WAVES; ++w) sum += sm[w];
+      } else {
+        for (int p = lane; p < t.parts; p += WAVE) sum += t.norms[(size_t)b * t.parts + p];
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, WAVE);
       }
-    }
-    if (MODE == SOLO) {
+      const double scale = (double)t.s / (sqrt(sum) + (double)t.eps);
 #pragma unroll
-      for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, WAVE);
-      if (lane == 0) sm[wave] = sum;
-      __syncthreads();
-      sum = 0.0;
-      for (int w = 0; w < TINY_WAVES; ++w) sum += sm[w];
-    } else {
-      for (int p = lane; p < t.parts; p += WAVE) sum += t.norms[(size_t)b * t.parts + p];
+      for (int k = 0; k < MAX_BLOCKS; ++k)
 #pragma unroll
-      for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, WAVE);
-    }
-    const double scale = (double)t.s / (sqrt(sum) + (double)t.eps);
-#pragma unroll
-    for (int i = 0; i < TASKS; ++i) {
-      const int block = (tid + i * TINY_THREADS) / BLOCK_TASKS, task = (tid + i * TINY_THREADS) % BLOCK_TASKS;
-      if (block >= t.blocks) continue;
-      const int r = t.tall ? task % MP : task / 8, c8 = t.tall ? task / MP : task % 8;
-      const int col = (chunk * t.blocks + block) * 64 + c8 * 8;
-      float x[8];
-      // (what lies outside of the matrix stays 0 whatever the scale is)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = r < m && col + e < n ? (float)((double)v[i][e] * scale) : 0.f;
-      half8 hi, lo;
-      split8(x, &hi, &lo);
-      *reinterpret_cast<half8*>(smem + at(block, r, c8)) = hi;
-      *reinterpret_cast<half8*>(smem + x_half + at(block, r, c8)) = lo;
-    }
+        for (int e = 0; e < EACH && k < t.blocks; ++e) {
+          // (what lies outside of the matrix stays 0 whatever the scale is)
+          const float x = r0 + e * DR < m && first_col + k * 64 + c0 + e * DC < n ? (float)((double)v[k][e] * scale) : 0.f;
+          const half_t hi = (half_t)x;
+          const uint32_t o = element(k, r0 + e * DR, c0 + e * DC);
+          *reinterpret_cast<half_t*>(smem + o) = hi;
+          *reinterpret_cast<half_t*>(smem + x_half + o) = (half_t)(x - (float)hi);
+        }
+    });
   }
   __syncthreads();
 
-  const int k_steps = t.blocks * 2;
   const size_t sums_of = (size_t)GB * WAVE;    // float4 of a chunk
   f32x4 acc[PER_WAVE];
   const int first = MODE == NEXT ? t.step : 0, last = MODE == SOLO ? t.steps : MODE == NEXT ? t.step + 1 : 0;
   for (int step = first; step < last; ++step) {
     // A
     if (MODE == SOLO) {
-      gram(0, x_half, k_steps, acc);
+      gram_x(acc);
     } else {
 #pragma unroll
       for (int i = 0; i < PER_WAVE; ++i) {
@@ -728,7 +765,15 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
     }
     const float alpha = t.t / (t.s * t.s);
 #pragma unroll
-    for (int i = 0; i < PER_WAVE; ++i) acc[i] *= alpha;
+    for (int i = 0; i < PER_WAVE; ++i) {
+      acc[i] *= alpha;
+      // both terms of B with the same A: an error that X itself could have had is one that the iteration damps (64 x 192, unrounded
+      // here: 0.19-0.22 % off before the last rounding, so 0.11)
+      if (!FULL) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][e] = (float)(half_t)acc[i][e];
+      }
+    }
     put_symmetric(acc);
     __syncthreads();
     // B in its place
@@ -743,6 +788,18 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
     // X, 16 columns at a time; no other wavefront reads them
     const bool old_lo = step < t.full_from, new_lo = step + 1 < t.full_from, end = step + 1 == t.steps;
     const float as = end ? t.a / t.s : t.a, us = (end ? 1.f / t.s : 1.f) / t.u;
+    // (B's fragments stay in registers where there is room)
+    constexpr bool HELD = MP <= 64;
+    half8 w_hi[HELD ? MP / 32 : 1][HELD ? MB : 1], w_lo[HELD && FULL ? MP / 32 : 1][HELD && FULL ? MB : 1];
+    if constexpr (HELD) {
+#pragma unroll
+      for (int ks = 0; ks < MP / 32; ++ks)
+#pragma unroll
+        for (int i = 0; i < MB; ++i) {
+          w_hi[ks][i] = rows16(ab0, i * 16, ks);
+          if constexpr (FULL) w_lo[ks][i] = rows16(ab0 + ab_half, i * 16, ks);
+        }
+    }
     for (int strip = wave; strip < t.blocks * 4; strip += TINY_WAVES) {
       const int col0 = strip * 16;
       f32x4 y[MB] = {};
@@ -753,11 +810,13 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
         if (FULL) xl = cols16(x_half, col0, ks);
 #pragma unroll
         for (int i = 0; i < MB; ++i) {
-          const half8 w = rows16(ab0, i * 16, ks);
+          half8 w, wl;
+          if constexpr (HELD) w = w_hi[ks][i]; else w = rows16(ab0, i * 16, ks);
           mfma(x, w, y[i]);
-          if (FULL) {
+          if constexpr (FULL) {
+            if constexpr (HELD) wl = w_lo[ks][i]; else wl = rows16(ab0 + ab_half, i * 16, ks);
             mfma(xl, w, y[i]);
-            mfma(x, rows16(ab0 + ab_half, i * 16, ks), y[i]);
+            mfma(x, wl, y[i]);
           }
         }
       }
@@ -778,22 +837,45 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
           if (new_lo) *lo_at = lo;
           continue;
         }
-        const int gc = chunk * t.blocks * 64 + c;
+        // the result's bits in their place, to be stored by whole rows
+        typedef unsigned short u16x4 __attribute__((ext_vector_type(4)));
+        u16x4 up, low;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int row = t.tall ? gc + e : r, col = t.tall ? r : gc + e;
-          if (row >= t.M || col >= t.N) continue;
-          const long o = b * t.stride_o + row * t.ld_o + col;
-          if (FULL) ((float*)t.out)[o] = v[e];
-          else ((bf16_t*)t.out)[o] = (bf16_t)v[e];
+          const uint32_t bits = __builtin_bit_cast(uint32_t, v[e]);
+          up[e] = t.out_fp32 ? (unsigned short)(bits >> 16) : __builtin_bit_cast(unsigned short, (bf16_t)v[e]);
+          low[e] = (unsigned short)bits;
         }
+        *reinterpret_cast<u16x4*>(hi_at) = up;
+        if (t.out_fp32) *reinterpret_cast<u16x4*>(lo_at) = low;
       }
     }
     __syncthreads();
   }
-  if (MODE == SOLO || (MODE == NEXT && t.step + 1 == t.steps)) return;
+  if (MODE == SOLO || (MODE == NEXT && t.step + 1 == t.steps)) {
+    each_element([&](auto tall_t, int r0, int c0) {
+      constexpr bool TALL = decltype(tall_t)::value;
+      constexpr int DR = TALL ? 0 : TINY_THREADS / 64, DC = TALL ? TINY_THREADS / MP : 0;
+      const long to = b * t.stride_o + (TALL ? (first_col + c0) * t.ld_o + r0 : r0 * t.ld_o + first_col + c0);
+      const int m = TALL ? t.N : t.M, n = TALL ? t.M : t.N;
+#pragma unroll
+      for (int k = 0; k < MAX_BLOCKS; ++k)
+#pragma unroll
+        for (int e = 0; e < EACH && k < t.blocks; ++e) {
+          if (!(r0 + e * DR < m && first_col + k * 64 + c0 + e * DC < n)) continue;
+          const uint32_t o = element(k, r0 + e * DR, c0 + e * DC);
+          const long i = to + (TALL ? (k * 64 + e * DC) * t.ld_o : e * DR * t.ld_o + k * 64);
+          const uint32_t up = *reinterpret_cast<const unsigned short*>(smem + o);
+          if (t.out_fp32)
+            ((uint32_t*)t.out)[i] = up << 16 | *reinterpret_cast<const unsigned short*>(smem + x_half + o);
+          else
+            ((unsigned short*)t.out)[i] = (unsigned short)up;
+        }
+    });
+    return;
+  }
   // the chunk's share of the next A, and the chunk
-  gram(0, x_half, k_steps, acc);
+  gram_x(acc);
 #pragma unroll
   for (int i = 0; i < PER_WAVE; ++i) {
     const int id = wave + i * TINY_WAVES;
@@ -864,9 +946,9 @@ struct TinyPlan {
   int mp = 0, blocks = 0, chunks = 0;
   TinyPlan(const Shape& q) {
     if (q.m > 128) return;
-    mp = q.m <= 64 ? 64 : 128;
-    const int all = cdiv(q.n, 64), solo = mp == 64 ? 8 : 2;
-    blocks = all <= solo ? all : mp == 64 ? 4 : 2;
+    mp = q.m <= 32 ? 32 : q.m <= 64 ? 64 : 128;
+    const int all = cdiv(q.n, 64);
+    blocks = all <= tiny_blocks(mp, true) ? all : tiny_blocks(mp, false);
     chunks = cdiv(all, blocks);
   }
 };
@@ -957,7 +1039,7 @@ template <int MP, bool FULL, int MODE>
 bm_status launch_tiny(const Tiny& t, int batch, hipStream_t st) {
   auto kern = tiny_kernel<MP, FULL, MODE>;
   static std::atomic<uint64_t> done{0};
-  constexpr int MOST = MODE == SOLO ? (MP == 64 ? 8 : 2) : MP == 64 ? 4 : 2;
+  constexpr int MOST = tiny_blocks(MP, MODE == SOLO);
   static_assert(tiny_lds(MP, MOST, FULL) <= 160 * 1024, "a chunk with A or B");
   BM_RETURN_IF(allow_lds(kern, tiny_lds(MP, MOST, FULL), &done));
   hipLaunchKernelGGL(kern, dim3((unsigned)((long)batch * t.chunks)), dim3(TINY_THREADS), tiny_lds(MP, t.blocks, FULL), st, t);
@@ -1061,10 +1143,12 @@ extern "C" bm_status bm_orthogonalize(int32_t dtype, int32_t batch, int32_t M, i
     t.eps = eps; t.s = k.s; t.t = k.t; t.u = k.u;
     t.a = a; t.b = b; t.c = c;
     t.steps = steps;
-    t.full_from = full ? steps : std::max(0, steps - 2);
+    t.full_from = full || tiny.mp == 32 ? steps : std::max(0, steps - 2);
     t.blocks = tiny.blocks; t.chunks = tiny.chunks;
     t.image = w.image;
     t.out = out; t.ld_o = ld_o; t.stride_o = stride_o;
+    t.out_fp32 = full;
+    if (tiny.mp == 32) return run_tiny<32, true>(t, batch, w, st);
     if (tiny.mp == 64) return full ? run_tiny<64, true>(t, batch, w, st) : run_tiny<64, false>(t, batch, w, st);
     return full ? run_tiny<128, true>(t, batch, w, st) : run_tiny<128, false>(t, batch, w, st);
   }
