@@ -71,7 +71,8 @@ bm_status bm_cross_entropy(int32_t dtype, int32_t T, int32_t V, const void* logi
  *   out  dev  dtype, matrix b at out + b*stride_o, rows of ld_o >= N elements; overwritten
  *   coefficients host [3]: a, b, c.  steps 1..64.  eps >= 0; with eps = 0 a matrix of zeros gives NaN.
  * Strides are in elements and not negative; stride_g may be 0; matrices of `out` lie one behind the other or side by
- * side, and may take the place of grad (all of which is read before any of them is written).
+ * side.  out may be grad itself with the same strides (BM_DTYPE_FP32); otherwise the memory from the first to the last element of
+ * the one and that of the other do not overlap.
  * The products run on the matrix cores in 11-bit significands (fp16, scaled; X itself is kept in 22 bits until the
  * last two steps, in which only singular values near the fixed points are still moved) for dtype BM_DTYPE_BF16 and more than
  * 32 rows and columns, and in 22 bits otherwise; sums are fp32, the norm fp64.

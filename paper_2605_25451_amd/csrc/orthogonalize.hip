@@ -989,7 +989,7 @@ bm_status allow_lds(Kernel kern, size_t lds, std::atomic<uint64_t>* done) {
   int dev = 0;
   BM_CHECK_HIP(hipGetDevice(&dev));
   const uint64_t bit = 1ull << (dev & 63);
-  if (done->load(std::memory_order_relaxed) & bit) return BM_OK;
+  if (dev < 64 && (done->load(std::memory_order_relaxed) & bit)) return BM_OK;
   BM_CHECK_HIP(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
   if (dev < 64) done->fetch_or(bit, std::memory_order_relaxed);
   return BM_OK;
@@ -1114,8 +1114,16 @@ extern "C" bm_status bm_orthogonalize(int32_t dtype, int32_t batch, int32_t M, i
     set_error("bm_orthogonalize needs %zu scratch bytes, got %zu", w.bytes, scratch_bytes);
     return BM_ERR_WORKSPACE_TOO_SMALL;
   }
-  hipStream_t st = (hipStream_t)hip_stream;
   const bool full = dtype == BM_DTYPE_FP32;
+  // matrices of few rows are read and written by a workgroup each, without regard to the others
+  const bool same = full && (const void*)grad == out && ld_o == ld_g && (batch == 1 || stride_o == stride_g);
+  auto end_of = [&](const void* p, int64_t stride, int ld, int bytes) {
+    return reinterpret_cast<uintptr_t>(p) + (uintptr_t)((batch - 1) * stride + (int64_t)(M - 1) * ld + N) * bytes;
+  };
+  BM_ARG_CHECK(same || end_of(grad, stride_g, ld_g, 4) <= reinterpret_cast<uintptr_t>(out) ||
+                   end_of(out, stride_o, ld_o, full ? 4 : 2) <= reinterpret_cast<uintptr_t>(grad),
+               "bm_orthogonalize: the result overlaps the gradient without being it");
+  hipStream_t st = (hipStream_t)hip_stream;
   const int terms = full ? 3 : 1;
   const float a = coefficients[0], b = coefficients[1], c = coefficients[2];
   // X that enters step i is kept in 22 bits where that step's result still feeds two more

@@ -102,3 +102,12 @@ def test_orthogonalize_workspace():
     for args in ((2, 1, 8, 8), (0, 0, 8, 8), (0, 1, 0, 8), (0, 1, 8, (1 << 20) + 1), (0, 1, 1 << 20, 1 << 20)):
         assert bm.orthogonalize_scratch_bytes(*args) == 0
     bm.orthogonalize(0, 0, 8, 8, None, 8, 64, None, 8, 64, (1.0, 0.0, 0.0), 1, 0.0, None, 0, stream=0)
+
+
+@pytest.mark.parametrize("dtype,batch,ld_g,stride_g,out,ld_o,stride_o", [
+    (0, 2, 30, 600, 0, 30, 600), (0, 1, 30, 600, 0, 30, 600), (1, 2, 30, 0, 0, 30, 600), (1, 2, 32, 640, 0, 30, 600),
+    (1, 2, 30, 640, 0, 30, 600), (1, 2, 30, 600, 16, 30, 600), (0, 2, 30, 600, -16, 30, 600), (1, 2, 30, 600, 4784, 30, 600)])
+def test_orthogonalize_refuses_results_that_overlap_the_gradient(dtype, batch, ld_g, stride_g, out, ld_o, stride_o):
+    refused(bm.BM_ERR_INVALID_ARG, bm.orthogonalize, dtype, batch, 20, 30, 1 << 20, ld_g, stride_g, (1 << 20) + out, ld_o, stride_o,
+            (1.0, 0.0, 0.0), 1, 0.0, 1 << 30, 1 << 30)
+    assert "overlaps" in bm.last_error()
