@@ -81,7 +81,7 @@ __device__ inline void split8(const float (&v)[8], half8* hi, half8* lo) {
 
 // ---- norm and conversion ----------------------------------------------------------------------
 
-constexpr int NORM_PARTS = 256;                // at most
+constexpr int NORM_PARTS = 1024;               // at most
 
 // sums of squares of parts of every matrix, in fp64: squares of fp32 values neither overflow nor vanish there.  A row is `per_row`
 // pieces of VEC elements.
@@ -111,10 +111,10 @@ __global__ __launch_bounds__(256) void norm_kernel(const float* __restrict__ g, 
   if (threadIdx.x == 0) sums[blockIdx.x] = sm[0] + sm[1] + sm[2] + sm[3];
 }
 
-// The sum of a matrix's parts, in every thread: four wavefronts, one part per lane.
+// The sum of a matrix's parts, in every thread: four wavefronts.
 __device__ inline double sum_parts(const double* __restrict__ sums, int parts, double* sm) {
-  static_assert(NORM_PARTS <= 256, "a part for each of four wavefronts' lanes");
-  double s = (int)threadIdx.x < parts ? sums[threadIdx.x] : 0.0;
+  double s = 0.0;
+  for (int p = threadIdx.x; p < parts; p += 256) s += sums[p];
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off, WAVE);
   if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = s;
