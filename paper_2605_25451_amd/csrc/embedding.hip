@@ -453,7 +453,7 @@ __global__ __launch_bounds__(256) void fold_kernel(Grouped g, int n, int d, int 
 // ---- host -------------------------------------------------------------------------------------
 
 // Rows of a chunk: as many as leave 32 wavefronts for every CU.  Longer chunks leave fewer pieces to the words that occur often
-// (32768 tokens of 4096 columns, one word in eleven the same: folding chunks of 16 rows 25 us, of 60 rows FOLD60).
+// (32768 tokens of 4096 columns, one word in eleven the same: folding chunks of 16 rows 25 us, of 60 rows 13).
 constexpr int SUM_WAVES = 8192;
 int chunk_rows(int T, int d) {
   const long rows = (long)T * cdiv(d, SLICE) / SUM_WAVES;

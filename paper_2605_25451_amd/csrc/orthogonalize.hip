@@ -542,8 +542,8 @@ __global__ __launch_bounds__(512, 2) void large_product_kernel(Product p, int ti
 //
 // A and B fit the LDS of a workgroup, so that a whole step is one launch: a workgroup holds a chunk of X's columns, has A from the sums
 // of all chunks, computes B for itself, moves its chunk on and adds up the chunk's share of the next A.  Where X is one
-// chunk (32 x 1024, 64 x 512, 128 x 128), all steps are one launch.  The products of the tiled kernels would be three launches a step of one to a few workgroups:
-// 192 x 64 59 us, here TINY192; 29 x 2350 93 and TINY29; 100 x 4096 127 and TINY100.
+// chunk (32 x 1024, 64 x 512, 128 x 128), all steps are one launch.  The tiled kernels would be three
+// launches a step of one to a few workgroups: 192 x 64 59 us, here 20; 29 x 2350 93 and 47; 100 x 4096 127 and 88.
 //
 // Up to 32 rows take the three products for bf16 results, too: single roundings do not average out there (16 x 64: up to 0.18 % off
 // with a single product), and what they cost is launches.
@@ -1047,7 +1047,11 @@ bm_status launch_tiny(const Tiny& t, int batch, hipStream_t st) {
   return BM_OK;
 }
 
-constexpr long TINY_SUMS = 240;
+// Chunks whose sums every workgroup adds up for itself.  A whole update in us without and with a launch that does it once:
+//   128 x 512 (4 chunks) 72.0, 73.5    128 x 896 (7) 85.6, 77.7    100 x 4096 (32) 117.6, 88.3
+//   64 x 8192 (32) 60.1, 66.5    64 x 16384 (64) 79.9, 79.3    64 x 32768 (128) 113.5, 101.5
+//   32 x 131072 (256) 135.7, 144.2    32 x 262144 (512) 391, 258
+constexpr int tiny_summands(int mp) { return mp == 128 ? 4 : mp == 64 ? 64 : 256; }
 
 template <int MP, bool FULL>
 bm_status run_tiny(Tiny t, int batch, const Workspace& w, hipStream_t st) {
@@ -1058,8 +1062,7 @@ bm_status run_tiny(Tiny t, int batch, const Workspace& w, hipStream_t st) {
     t.sums = w.partial[t.step & 1];
     t.sums_next = w.partial[(t.step + 1) & 1];
     t.summands = t.chunks;
-    // SUMRULE
-    if ((long)t.chunks * tiny_gram_blocks(MP) > TINY_SUMS && batch < 65536) {
+    if (t.chunks > tiny_summands(MP) && batch < 65536) {
       constexpr int per_chunk = tiny_gram_blocks(MP) * WAVE;
       hipLaunchKernelGGL(tiny_sum_kernel, dim3(cdiv(per_chunk, 256), batch), dim3(256), 0, st, w.partial[t.step & 1], t.chunks, per_chunk);
       BM_CHECK_LAUNCH("orthogonalize sums");
