@@ -92,7 +92,7 @@ def embedding_backward(dtype, V, d, dy, ld_dy, ids, T, scale, dtable, ld):
 CASES = [(1, 1, 1, 0, "one"), (2, 3, 5, 0, "one"), (5, 300, 8, 8, "any"), (64, 256, 24, 0, "images"), (65, 257, 100, 3, "past"),
          (777, 1000, 1152, 16, "ranked"), (2048, 3000, 72, 0, "any"), (2049, 500, 520, 0, "few"), (4099, 9, 1028, 4, "one"),
          (8193, 70000, 36, 0, "ranked"), (9000, 300000, 8, 0, "ranked"), (33000, 400, 17, 1, "images"), (33000, 50, 64, 0, "one"),
-         (130, 40, 513, 0, "none"), (1500, 4, 2048, 0, "any")]
+         (130, 40, 513, 0, "none"), (1500, 4, 2048, 0, "any"), (70001, 5000, 12, 0, "ranked"), (66000, 257, 9, 0, "past"), (65537, 3, 8, 0, "one")]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
@@ -193,7 +193,7 @@ def check_loss(loss, grad, z64, labels, weight, dtype):
 @pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
 @pytest.mark.parametrize("T,V,pad", [(1, 1, 0), (1, 2, 0), (3, 7, 0), (2, 8, 8), (5, 9, 1), (64, 300, 20), (17, 1001, 0), (300, 520, 0),
                                      (9, 4096, 0), (7, 8191, 2), (4, 33000, 0), (3, 50257, 0), (2, 65537, 7), (2, 128000, 0),
-                                     (2, 131075, 0), (1, 200003, 0), (1100, 2050, 0)])
+                                     (2, 131075, 0), (1, 200003, 0), (1100, 2050, 0), (40, 131075, 0), (34, 98309, 3)])
 def test_cross_entropy(T, V, pad, dtype):
     rng = np.random.default_rng(T + V)
     z = rng.standard_normal((T, V)) * rng.choice([0.1, 2.0, 12.0], (T, 1)) + rng.choice([0.0, 30.0, -100.0], (T, 1))
@@ -429,6 +429,17 @@ def test_orthogonalize(B, M, N, kind, dtype):
         rows = out[b][:M * ld_o].reshape(M, ld_o)
         assert (rows[:, N:] == 9).all() and (out[b][M * ld_o:] == 9).all()
         assert np.linalg.norm(rows[:, :N] - want) <= worst_case(Xs, MUON, dtype)
+
+
+@pytest.mark.parametrize("M,N,kind", [(16, 64, "noise"), (9, 16, "noise"), (20, 900, "falls"), (200, 32, "falls"), (31, 2350, "noise")])
+def test_up_to_32_rows_in_22_bits(M, N, kind):
+    """bf16 results are fp32's, rounded once more."""
+    import torch
+    G = spectrum(np.random.default_rng(M), M, N, kind).astype(np.float32)
+    Xs = to.orthogonalize(G, MUON, 5, 1e-7)
+    got = orthogonalize(0, torch.from_numpy(G).cuda(), N, 0, 1, M, N, N, M * N).double().cpu().numpy().reshape(M, N)
+    want = Xs[-1] if M <= N else Xs[-1].T
+    assert np.linalg.norm(got - want) <= worst_case(Xs, MUON, 1) + U[0] * np.linalg.norm(want)
 
 
 def emulate(G, coefficients, steps, eps):
