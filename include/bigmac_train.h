@@ -32,7 +32,7 @@ extern "C" {
  *              as it was, its dy is not read.  An id of V or more is the caller's mistake: its y is
  *              NaN, its dy is not read.
  *   y, dy dev  [T, ld >= d]  storage dtype
- * T may be 0 (nothing is done, and pointers may be NULL). */
+ * T may be 0 (nothing is done, and pointers may be NULL).  T and d are 2^30 at most. */
 bm_status bm_embedding_forward(int32_t dtype, int32_t V, int32_t d, const void* table, int32_t ld_table,
                                const int32_t* ids, int32_t T, float scale, void* y, int32_t ld_y,
                                void* hip_stream);

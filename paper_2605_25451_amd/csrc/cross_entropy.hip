@@ -216,8 +216,6 @@ __device__ inline Stat2 block_join(Stat2 a, Stat2* sm) {
   return r;
 }
 
-typedef unsigned int Quad __attribute__((ext_vector_type(4)));
-
 // A workgroup holds a row in its registers, NV vectors per thread, so that the logits are read once.  Neither they nor the gradient are
 // used again before a cache has lost them: with non-temporal accesses 256 x 128000 take 26 us instead of 31.  One workgroup per
 // row: persistent ones that fetch the next row under the gradient of the last keep in step with one another, so that all read, compute
@@ -398,6 +396,17 @@ extern "C" bm_status bm_cross_entropy(int32_t dtype, int32_t T, int32_t V, const
   }
   hipStream_t st = (hipStream_t)hip_stream;
   ProfScope prof(PROF_ELEMENTWISE, (dlogits ? 2.0 : 1.0) * T * V * elt_size(dtype), st);
-  return dtype == BM_DTYPE_BF16 ? run<bf16_t>(dtype, T, V, logits, ld, labels, weight, loss, dlogits, ld_d, w, st)
-                                : run<float>(dtype, T, V, logits, ld, labels, weight, loss, dlogits, ld_d, w, st);
+  // (a grid has fewer than 2^32 threads; what is left of the rows has no more parts than all of them together)
+  constexpr int MOST = 1 << 21;
+  const size_t elt = elt_size(dtype);
+  for (int first = 0; first < T; first += std::min(MOST, T - first)) {
+    const int n = std::min(MOST, T - first);
+    const void* x = (const char*)logits + (size_t)first * ld * elt;
+    void* g = dlogits ? (char*)dlogits + (size_t)first * ld_d * elt : nullptr;
+    const float* f = weight ? weight + first : nullptr;
+    float* l = loss ? loss + first : nullptr;
+    BM_RETURN_IF(dtype == BM_DTYPE_BF16 ? run<bf16_t>(dtype, n, V, x, ld, labels + first, f, l, g, ld_d, w, st)
+                                        : run<float>(dtype, n, V, x, ld, labels + first, f, l, g, ld_d, w, st));
+  }
+  return BM_OK;
 }

@@ -465,7 +465,7 @@ size_t max_chunks(int T, int d) {
   return std::max((size_t)cdiv(T, CHUNK_MAX), std::min((size_t)cdiv(T, CHUNK_MIN), before));
 }
 
-constexpr int MAX_TOKENS = 1 << 30;
+constexpr int MAX_TOKENS = 1 << 30, MAX_COLUMNS = 1 << 30;
 
 struct Workspace {
   Grouped g;
@@ -485,20 +485,21 @@ struct Workspace {
 };
 
 template <typename T>
-void launch_embed(const void* table, int ld_table, const int32_t* ids, int n, int V, int d, float scale, void* y, int ld_y,
+void launch_embed(const void* table, int ld_table, const int32_t* ids, int rows, int V, int d, float scale, void* y, int ld_y,
                   hipStream_t st) {
   constexpr int W = Elt<T>::VEC;
   const bool vec = d % W == 0 && ld_table % W == 0 && ld_y % W == 0;
   const int chunks = vec ? d / W : d;
   int log_lanes = 0;
   while (log_lanes < 6 && (1 << log_lanes) < chunks) ++log_lanes;
-  const unsigned blocks = (unsigned)((((long)n << log_lanes) + 255) / 256);
-  if (vec)
-    hipLaunchKernelGGL((embed_kernel<T, true>), dim3(blocks), dim3(256), 0, st, (const T*)table, (long)ld_table, ids, n, V, d, scale,
-                       (T*)y, (long)ld_y, log_lanes);
-  else
-    hipLaunchKernelGGL((embed_kernel<T, false>), dim3(blocks), dim3(256), 0, st, (const T*)table, (long)ld_table, ids, n, V, d, scale,
-                       (T*)y, (long)ld_y, log_lanes);
+  // (a grid has fewer than 2^32 threads)
+  const long most = 1l << (31 - log_lanes);
+  for (long first = 0; first < rows; first += most) {
+    const int n = (int)std::min(most, rows - first);
+    const unsigned blocks = (unsigned)((((long)n << log_lanes) + 255) / 256);
+    hipLaunchKernelGGL((vec ? embed_kernel<T, true> : embed_kernel<T, false>), dim3(blocks), dim3(256), 0, st, (const T*)table,
+                       (long)ld_table, ids + first, n, V, d, scale, (T*)y + first * ld_y, (long)ld_y, log_lanes);
+  }
 }
 
 template <typename T, bool VEC>
@@ -521,6 +522,7 @@ bm_status launch_sums(const void* dy, int ld_dy, const Workspace& w, int n, int 
 bm_status check(const char* name, int32_t dtype, int32_t V, int32_t d, int32_t T, int32_t ld0, int32_t ld1) {
   BM_ARG_CHECK(good_dtype(dtype), "%s: dtype %d", name, dtype);
   BM_ARG_CHECK(V > 0 && d > 0, "%s: V and d must be positive", name);
+  BM_ARG_CHECK(d <= MAX_COLUMNS, "%s: %d columns", name, d);
   BM_ARG_CHECK(T >= 0 && T <= MAX_TOKENS, "%s: %d tokens", name, T);
   BM_ARG_CHECK(ld0 >= d && ld1 >= d, "%s: leading dimension too small", name);
   // workgroups of a grid
@@ -547,7 +549,7 @@ extern "C" bm_status bm_embedding_forward(int32_t dtype, int32_t V, int32_t d, c
 }
 
 extern "C" size_t bm_embedding_backward_scratch_bytes(int32_t T, int32_t d) {
-  if (T <= 0 || T > MAX_TOKENS || d <= 0) return 0;
+  if (T <= 0 || T > MAX_TOKENS || d <= 0 || d > MAX_COLUMNS) return 0;
   return Workspace(nullptr, T, d).bytes;
 }
 

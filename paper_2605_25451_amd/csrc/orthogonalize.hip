@@ -958,9 +958,12 @@ struct Workspace {
   Split X[2], A, B;
   unsigned char* image = nullptr;
   float4* partial[2] = {nullptr, nullptr};
+  int most;                                    // matrices of a launch: a grid has fewer than 2^32 threads
   size_t bytes;
-  Workspace(void* scratch, int dtype, int batch, const Shape& q, const TinyPlan& tiny) {
+  Workspace(void* scratch, int dtype, int batch, const Shape& q, const TinyPlan& tiny)
+      : most((int)std::max((size_t)1, ((size_t)1 << 21) / (q.x / (PAD * PAD)))) {
     Arena w(scratch);
+    batch = std::min(batch, most);
     const bool full = dtype == BM_DTYPE_FP32;
     if (tiny.chunks != 1) sums = w.take<double>((size_t)batch * NORM_PARTS * sizeof(double));
     if (tiny.chunks) {
@@ -1080,6 +1083,89 @@ bool sizes_ok(int dtype, int batch, int M, int N) {
   return q.x < MAX_ELEMENTS && (double)batch * (q.mp / 64) * (q.np / 64) < 2147483648.0;
 }
 
+bm_status run(bool full, int batch, int M, int N, const Shape& q, const TinyPlan& tiny, const Scales& k, const Workspace& w,
+              const float* grad, int32_t ld_g, int64_t stride_g, void* out, int32_t ld_o, int64_t stride_o,
+              const float* coefficients, int32_t steps, float eps, hipStream_t st) {
+  const int terms = full ? 3 : 1;
+  const float a = coefficients[0], b = coefficients[1], c = coefficients[2];
+  // X that enters step i is kept in 22 bits where that step's result still feeds two more
+  auto in_full = [&](int i) { return full || i + 2 < steps; };
+  auto view = [](Split x, bool lo) { if (!lo) x.lo = nullptr; return x; };
+
+  // rows of G that start on 16 bytes are read four elements at a time (matrices of an odd stride start where they like); rows without a
+  // gap are one long row
+  const bool vec = aligned16(grad) && ld_g % 4 == 0 && N % 4 == 0 && (batch == 1 || stride_g % 4 == 0);
+  const uint32_t pieces = (uint32_t)((size_t)M * N / (vec ? 4 : 1)), per_row = ld_g == N ? pieces : (uint32_t)(vec ? N / 4 : N);
+  // enough parts for 8 workgroups a CU, none without 4 pieces a thread
+  const int parts = std::max(1, std::min({NORM_PARTS, cdiv(2048, batch), cdiv(pieces, 1024)}));
+  auto norms = [&]() -> bm_status {
+    hipLaunchKernelGGL((vec ? norm_kernel<4> : norm_kernel<1>), dim3((unsigned)batch * parts), dim3(256), 0, st, grad, (long)ld_g,
+                       (long)stride_g, per_row, pieces, parts, w.sums);
+    BM_CHECK_LAUNCH("orthogonalize norm");
+    return BM_OK;
+  };
+  if (tiny.chunks) {
+    ProfScope prof(PROF_GEMM_NT, steps * (double)batch * terms * ((double)q.m * q.m * (3.0 * q.n + q.m)), st);
+    if (tiny.chunks > 1) BM_RETURN_IF(norms());
+    Tiny t{};
+    t.g = grad; t.ld_g = ld_g; t.stride_g = stride_g;
+    t.M = M; t.N = N; t.tall = q.tall;
+    t.norms = w.sums; t.parts = parts;
+    t.eps = eps; t.s = k.s; t.t = k.t; t.u = k.u;
+    t.a = a; t.b = b; t.c = c;
+    t.steps = steps;
+    t.full_from = full || tiny.mp == 32 ? steps : std::max(0, steps - 2);
+    t.blocks = tiny.blocks; t.chunks = tiny.chunks;
+    t.image = w.image;
+    t.out = out; t.ld_o = ld_o; t.stride_o = stride_o;
+    t.out_fp32 = full;
+    if (tiny.mp == 32) return run_tiny<32, true>(t, batch, w, st);
+    if (tiny.mp == 64) return full ? run_tiny<64, true>(t, batch, w, st) : run_tiny<64, false>(t, batch, w, st);
+    return full ? run_tiny<128, true>(t, batch, w, st) : run_tiny<128, false>(t, batch, w, st);
+  }
+  BM_RETURN_IF(norms());
+  const int tiles_n = q.np / PAD, across = std::max(1, std::min(4, (int)((long)tiles_n * (q.mp / PAD) * batch / 2048)));
+  const int runs_n = cdiv(tiles_n, across), runs = q.mp / PAD * runs_n;
+  const bool rows_vec = aligned16(grad) && ld_g % 4 == 0 && (batch == 1 || stride_g % 4 == 0);
+  const auto convert = q.tall ? (rows_vec ? convert_kernel<true, true> : convert_kernel<true, false>)
+                              : (rows_vec ? convert_kernel<false, true> : convert_kernel<false, false>);
+  hipLaunchKernelGGL(convert, dim3((unsigned)((long)batch * runs)), dim3(256), 0, st, grad, (long)ld_g, (long)stride_g, M, N, w.sums, parts,
+                     eps, k.s, view(w.X[0], in_full(0)), q.np, q.x, tiles_n, runs_n, across, runs);
+  BM_CHECK_LAUNCH("orthogonalize convert");
+  for (int i = 0; i < steps; ++i) {
+    const Split x = view(w.X[i & 1], in_full(i)), next = view(w.X[(i + 1) & 1], in_full(i + 1));
+    Product p{};
+    p.terms = terms;
+    p.A = x; p.B = x; p.C = w.A;
+    p.M = p.N = q.mp; p.K = q.np;
+    p.lda = p.ldb = q.np; p.ldc = q.mp;
+    p.stride_a = p.stride_b = q.x; p.stride_c = q.a;
+    p.alpha = k.t / (k.s * k.s);
+    BM_RETURN_IF(launch<GRAM>(p, batch, st));
+    p.A = w.A; p.B = w.A; p.C = w.B; p.old = w.A;
+    p.K = q.mp; p.lda = p.ldb = q.mp;
+    p.stride_a = p.stride_b = q.a;
+    p.alpha = c * (k.u / k.t) / k.t;
+    p.beta = b * (k.u / k.t);
+    BM_RETURN_IF(launch<POLY>(p, batch, st));
+    p.A = w.B; p.B = x; p.C = next; p.old = x;
+    p.N = q.np; p.ldb = p.ldc = q.np;
+    p.stride_b = p.stride_c = q.x;
+    p.alpha = 1.f / k.u;
+    p.beta = a;
+    if (i + 1 < steps) {
+      BM_RETURN_IF(launch<STEP>(p, batch, st));
+    } else {
+      p.alpha /= k.s;
+      p.beta /= k.s;
+      p.out = out; p.ld_o = ld_o; p.stride_o = stride_o;
+      p.rows = q.m; p.cols = q.n; p.transposed = q.tall; p.out_fp32 = full;
+      BM_RETURN_IF(launch<LAST>(p, batch, st));
+    }
+  }
+  return BM_OK;
+}
+
 }  // namespace
 }  // namespace bm
 
@@ -1126,82 +1212,8 @@ extern "C" bm_status bm_orthogonalize(int32_t dtype, int32_t batch, int32_t M, i
   BM_ARG_CHECK(same || end_of(grad, stride_g, ld_g, 4) <= reinterpret_cast<uintptr_t>(out) ||
                    end_of(out, stride_o, ld_o, full ? 4 : 2) <= reinterpret_cast<uintptr_t>(grad),
                "bm_orthogonalize: the result overlaps the gradient without being it");
-  hipStream_t st = (hipStream_t)hip_stream;
-  const int terms = full ? 3 : 1;
-  const float a = coefficients[0], b = coefficients[1], c = coefficients[2];
-  // X that enters step i is kept in 22 bits where that step's result still feeds two more
-  auto in_full = [&](int i) { return full || i + 2 < steps; };
-  auto view = [](Split x, bool lo) { if (!lo) x.lo = nullptr; return x; };
-
-  // rows of G that start on 16 bytes are read four elements at a time; rows without a gap are one long row
-  const bool vec = ld_g % 4 == 0 && N % 4 == 0 && (batch == 1 || stride_g % 4 == 0);
-  const uint32_t pieces = (uint32_t)((size_t)M * N / (vec ? 4 : 1)), per_row = ld_g == N ? pieces : (uint32_t)(vec ? N / 4 : N);
-  // enough parts for 8 workgroups a CU, none without 4 pieces a thread
-  const int parts = std::max(1, std::min({NORM_PARTS, cdiv(2048, batch), cdiv(pieces, 1024)}));
-  auto norms = [&]() -> bm_status {
-    hipLaunchKernelGGL((vec ? norm_kernel<4> : norm_kernel<1>), dim3((unsigned)batch * parts), dim3(256), 0, st, grad, (long)ld_g,
-                       (long)stride_g, per_row, pieces, parts, w.sums);
-    BM_CHECK_LAUNCH("orthogonalize norm");
-    return BM_OK;
-  };
-  if (tiny.chunks) {
-    ProfScope prof(PROF_GEMM_NT, steps * (double)batch * terms * ((double)q.m * q.m * (3.0 * q.n + q.m)), st);
-    if (tiny.chunks > 1) BM_RETURN_IF(norms());
-    Tiny t{};
-    t.g = grad; t.ld_g = ld_g; t.stride_g = stride_g;
-    t.M = M; t.N = N; t.tall = q.tall;
-    t.norms = w.sums; t.parts = parts;
-    t.eps = eps; t.s = k.s; t.t = k.t; t.u = k.u;
-    t.a = a; t.b = b; t.c = c;
-    t.steps = steps;
-    t.full_from = full || tiny.mp == 32 ? steps : std::max(0, steps - 2);
-    t.blocks = tiny.blocks; t.chunks = tiny.chunks;
-    t.image = w.image;
-    t.out = out; t.ld_o = ld_o; t.stride_o = stride_o;
-    t.out_fp32 = full;
-    if (tiny.mp == 32) return run_tiny<32, true>(t, batch, w, st);
-    if (tiny.mp == 64) return full ? run_tiny<64, true>(t, batch, w, st) : run_tiny<64, false>(t, batch, w, st);
-    return full ? run_tiny<128, true>(t, batch, w, st) : run_tiny<128, false>(t, batch, w, st);
-  }
-  BM_RETURN_IF(norms());
-  const int tiles_n = q.np / PAD, across = std::max(1, std::min(4, (int)((long)tiles_n * (q.mp / PAD) * batch / 2048)));
-  const int runs_n = cdiv(tiles_n, across), runs = q.mp / PAD * runs_n;
-  const bool rows_vec = ld_g % 4 == 0 && (batch == 1 || stride_g % 4 == 0);
-  const auto convert = q.tall ? (rows_vec ? convert_kernel<true, true> : convert_kernel<true, false>)
-                              : (rows_vec ? convert_kernel<false, true> : convert_kernel<false, false>);
-  hipLaunchKernelGGL(convert, dim3((unsigned)((long)batch * runs)), dim3(256), 0, st, grad, (long)ld_g, (long)stride_g, M, N, w.sums, parts,
-                     eps, k.s, view(w.X[0], in_full(0)), q.np, q.x, tiles_n, runs_n, across, runs);
-  BM_CHECK_LAUNCH("orthogonalize convert");
-  for (int i = 0; i < steps; ++i) {
-    const Split x = view(w.X[i & 1], in_full(i)), next = view(w.X[(i + 1) & 1], in_full(i + 1));
-    Product p{};
-    p.terms = terms;
-    p.A = x; p.B = x; p.C = w.A;
-    p.M = p.N = q.mp; p.K = q.np;
-    p.lda = p.ldb = q.np; p.ldc = q.mp;
-    p.stride_a = p.stride_b = q.x; p.stride_c = q.a;
-    p.alpha = k.t / (k.s * k.s);
-    BM_RETURN_IF(launch<GRAM>(p, batch, st));
-    p.A = w.A; p.B = w.A; p.C = w.B; p.old = w.A;
-    p.K = q.mp; p.lda = p.ldb = q.mp;
-    p.stride_a = p.stride_b = q.a;
-    p.alpha = c * (k.u / k.t) / k.t;
-    p.beta = b * (k.u / k.t);
-    BM_RETURN_IF(launch<POLY>(p, batch, st));
-    p.A = w.B; p.B = x; p.C = next; p.old = x;
-    p.N = q.np; p.ldb = p.ldc = q.np;
-    p.stride_b = p.stride_c = q.x;
-    p.alpha = 1.f / k.u;
-    p.beta = a;
-    if (i + 1 < steps) {
-      BM_RETURN_IF(launch<STEP>(p, batch, st));
-    } else {
-      p.alpha /= k.s;
-      p.beta /= k.s;
-      p.out = out; p.ld_o = ld_o; p.stride_o = stride_o;
-      p.rows = q.m; p.cols = q.n; p.transposed = q.tall; p.out_fp32 = full;
-      BM_RETURN_IF(launch<LAST>(p, batch, st));
-    }
-  }
+  for (int first = 0; first < batch; first += std::min(w.most, batch - first))
+    BM_RETURN_IF(run(full, std::min(w.most, batch - first), M, N, q, tiny, k, w, grad + first * stride_g, ld_g, stride_g,
+                     (char*)out + first * stride_o * (full ? 4 : 2), ld_o, stride_o, coefficients, steps, eps, (hipStream_t)hip_stream));
   return BM_OK;
 }

@@ -532,3 +532,64 @@ def test_orthogonalize_replayed():
         step()
         torch.cuda.synchronize()
         assert torch.equal(got, out)
+
+
+# ---- more than one launch has threads for ------------------------------------------------------------------
+
+def test_lookup_of_more_rows_than_a_launch():
+    import torch
+    T, V, d = (1 << 26) + 3, 5, 33
+    table = torch.randn((V, d), device="cuda").to(torch.bfloat16)
+    ids = torch.arange(T, dtype=torch.int32, device="cuda") % V
+    y = torch.zeros((T, d), dtype=torch.bfloat16, device="cuda")
+    bm.embedding_forward(0, V, d, table, d, ids, T, 2.0, y, d)
+    for first in range(0, T, 1 << 24):
+        part = slice(first, min(T, first + (1 << 24)))
+        assert torch.equal(y[part], 2 * table[ids[part].long()])
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
+def test_loss_of_more_rows_than_a_launch(dtype):
+    import torch
+    T, V, ld, few = (1 << 21) + 700, 5, 7, 300
+    z = torch.randn((few, ld), device="cuda").to(torch_type(dtype))
+    labels = torch.randint(-1, V, (few,), dtype=torch.int32, device="cuda")
+    weight = torch.rand(few, device="cuda")
+    at = torch.arange(T, device="cuda") % few
+    d = torch.full((T, ld), 3.0, dtype=z.dtype, device="cuda")
+    got = cross_entropy(dtype, T, V, z[at].contiguous(), ld, labels[at].contiguous(), weight[at].contiguous(), d, ld)
+    assert (d[:, V:] == 3).all()
+    # copies of a row start at different places between two boundaries, and are added up in different orders: the least and the
+    # largest of every element
+    fill = slice(T % few, few)
+    got = torch.cat([got, got[fill]]).view(-1, few).double().cpu().numpy()
+    d = torch.cat([d[:, :V], d[fill, :V]]).view(-1, few, V)
+    z64, labels, weight = z[:, :V].double().cpu().numpy(), labels.cpu().numpy(), weight.cpu().numpy()
+    for end in ("amin", "amax"):
+        check_loss(getattr(np, end)(got, axis=0), getattr(d, end)(dim=0).double().cpu().numpy(), z64, labels, weight, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
+def test_more_matrices_than_a_launch(dtype):
+    import torch
+    B, M, N, stride, few = (1 << 21) + 1, 3, 2, 7, 5
+    some = torch.randn((few, stride), device="cuda")
+    want = orthogonalize(dtype, some, N, stride, few, M, N, N, M * N).view(few, M * N)
+    at = torch.arange(B, device="cuda") % few
+    assert torch.equal(orthogonalize(dtype, some[at].contiguous(), N, stride, B, M, N, N, M * N).view(B, M * N), want[at])
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
+def test_the_last_matrix_in_a_launch_of_its_own(dtype):
+    """It starts at an odd element."""
+    import torch
+    B, M, N, few = 4097, 3, 32768, 2
+    stride = M * N + 1
+    some = torch.randn((few, stride), device="cuda")
+    at = torch.arange(B, device="cuda") % few
+    got = orthogonalize(dtype, some[at].contiguous(), N, stride, B, M, N, N, M * N).view(B, M, N)
+    for f in range(few):
+        Xs = to.orthogonalize(some[f, :M * N].view(M, N).cpu().numpy(), MUON, 5, 1e-7)
+        for b in (f, 2000 + f, 4094 + f, 4096 - f):
+            if b % few == f:
+                assert np.linalg.norm(got[b].double().cpu().numpy() - Xs[-1]) <= worst_case(Xs, MUON, dtype)

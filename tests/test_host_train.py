@@ -17,7 +17,7 @@ LOOKUP = dict(dtype=0, V=100, d=16, table=P, ld_table=16, ids=Q, T=4, scale=1.0,
 
 @pytest.mark.parametrize("bad", [dict(dtype=2), dict(V=0), dict(d=0), dict(T=-1), dict(ld_table=15), dict(ld_y=8),
                                  dict(table=None), dict(ids=None), dict(y=None), dict(table=P + 2), dict(y=R + 8),
-                                 dict(ids=Q + 4), dict(T=1 << 30, d=8192, ld_table=8192, ld_y=8192)])
+                                 dict(ids=Q + 4), dict(d=(1 << 30) + 1, ld_table=(1 << 30) + 1, ld_y=(1 << 30) + 1), dict(T=1 << 30, d=8192, ld_table=8192, ld_y=8192)])
 def test_lookup_refusals(bad):
     refused(bm.BM_ERR_INVALID_ARG, bm.embedding_forward, *{**LOOKUP, **bad}.values())
 
@@ -44,7 +44,7 @@ def test_embedding_workspace_grows_with_tokens_and_columns():
     assert all(b > 0 for b in sizes)
     assert all(b >= a for a, b in zip(sizes, sizes[1:]))
     assert bm.embedding_backward_scratch_bytes(777, 65) >= bm.embedding_backward_scratch_bytes(777, 64)
-    for T, d in ((0, 8), (8, 0), (-1, 8), ((1 << 30) + 1, 8)):
+    for T, d in ((0, 8), (8, 0), (-1, 8), ((1 << 30) + 1, 8), (8, (1 << 30) + 1)):
         assert bm.embedding_backward_scratch_bytes(T, d) == 0
 
 
