@@ -538,6 +538,66 @@ __global__ __launch_bounds__(512, 2) void large_product_kernel(Product p, int ti
                      });
 }
 
+// ---- 192 x 192, of the symmetric products: twelve wavefronts of 48 x 64, three slices of LDS with one barrier a slice.
+constexpr int MIDDLE = 192, MIDDLE_DEPTH = 3;
+constexpr size_t middle_lds() { return (size_t)MIDDLE_DEPTH * 2 * MIDDLE * BK * sizeof(half_t); }
+
+template <int KIND>
+__global__ __launch_bounds__(768) void middle_product_kernel(Product p, int tiles_m, int tiles_n, int tiles) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  static_assert(KIND == GRAM || KIND == POLY, "operands whose k is contiguous");
+  using Reg = Region<MIDDLE, false, 12>;
+  constexpr uint32_t BUF = 2 * Reg::BYTES;
+  constexpr int LOADS = 2 * Reg::LOADS, FM = 3, FN = 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 3, wn = wave >> 2;
+  const Place q = place<true>(tiles_m, tiles_n, tiles);
+  const int m0 = q.tm * MIDDLE, n0 = q.tn * MIDDLE;
+  const Operands<false> op(p, q, m0, n0);
+  const int n = op.slices * p.terms;
+  Reg ra, rb;
+  ra.init(p.lda, 0, p.M - m0, wave, lane);
+  rb.init(p.ldb, 0, p.N - n0, wave, lane);
+  auto load = [&](int j, uint32_t buf) {
+    rb.template load<false>(op.b_at(j), p.ldb, BK, buf + Reg::BYTES, wave, lane);
+    ra.template load<false>(op.a_at(j), p.lda, BK, buf, wave, lane);
+  };
+  Fragments<MIDDLE, false, FM> fa;
+  Fragments<MIDDLE, false, FN> fb;
+  fa.init(wm * FM * 16, lane);
+  fb.init(wn * FN * 16, lane);
+  f32x4 acc[FM][FN] = {};
+  load(0, 0);
+  if (n > 1) load(1, BUF);
+  uint32_t cur = 0, free = 2 * BUF;
+  for (int j = 0; j < n; ++j) {
+    if (j + 1 < n) wait_loads<LOADS>();
+    else wait_loads<0>();
+    end_phase();                                             // slice j is there for all, and all have read slice j - 1
+    if (j + 2 < n) load(j + 2, free);
+    bf16x8 a[2][FM], b[2][FN];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+      for (int f = 0; f < FN; ++f) b[ks][f] = fb.read(smem, f, ks, cur + Reg::BYTES);
+#pragma unroll
+      for (int f = 0; f < FM; ++f) a[ks][f] = fa.read(smem, f, ks, cur);
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int c = 0; c < FN; ++c)
+          acc[i][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_half(b[ks][c]), as_half(a[ks][i]), acc[i][c], 0, 0, 0);
+    wait_fragments();
+    free = cur;
+    cur = cur == 2 * BUF ? 0 : cur + BUF;
+  }
+  end_phase();                                               // strips overlay the slices
+  finish<KIND, FM, FN>(p, q.b, acc, reinterpret_cast<float*>(smem) + wave * 16 * 68, lane, n0 + wn * 64, q.tm != q.tn,
+                       [&](int i) { return m0 + (wm * FM + i) * 16; }, [] {});
+}
+
 // ---- few rows: 32, 64 or 128 of X at most ----------------------------------------------------------------
 //
 // A and B fit the LDS of a workgroup, so that a whole step is one launch: a workgroup holds a chunk of X's columns, has A from the sums
@@ -1015,10 +1075,25 @@ bm_status launch_tile(const Product& p, int batch, hipStream_t st) {
   return BM_OK;
 }
 
+template <int KIND>
+bm_status launch_middle(const Product& p, int batch, hipStream_t st) {
+  static std::atomic<uint64_t> done{0};
+  auto kern = middle_product_kernel<KIND>;
+  BM_RETURN_IF(allow_lds(kern, middle_lds(), &done));
+  const int t = cdiv(p.M, MIDDLE), tiles = t * (t + 1) / 2;
+  ProfScope prof(PROF_GEMM_NT, (double)batch * p.terms * p.M * p.N * p.K, st);
+  hipLaunchKernelGGL(kern, dim3((unsigned)((long)tiles * batch)), dim3(768), middle_lds(), st, p, t, t, tiles);
+  BM_CHECK_LAUNCH("orthogonalize product");
+  return BM_OK;
+}
+
 // Operands come from L2 at 50-60 bytes per ns and CU whatever the kernel (deeper prefetch, fragments read ahead, wavefronts with whole
 // tiles of their own and a compact order of the tiles in an XCD changed nothing), so tiles are as large as leaves one for every CU.
 // A whole update in us, 256x256 / 128x128 / 64x64 two workgroups a CU / 64x64 two groups:
 //   1024 x 1024 420, 243, 160, 149     1536 x 1536 555, 325, 282, 335     2048 x 2048 704, 424, 499, 575     16 of 1024 x 1024 598, 757, 805, 1060
+// A CU fetches the operands of one tile after the other, so a symmetric product takes the rounds of the chip times the tile's size:
+// 4096 rows are 136 tiles of 256 for 256 CUs, but 253 of 192.  A whole update without and with 192 x 192:
+//   4096 x 4096 1448, 1374 (fp32 3822, 3682)     4096 x 14336 3900, 3769     3584 x 3584 1153, 1033     50 of 300 x 300 246, 217
 template <int KIND>
 bm_status launch(const Product& p, int batch, hipStream_t st) {
   constexpr bool SYMMETRIC = KIND == GRAM || KIND == POLY;
@@ -1027,6 +1102,10 @@ bm_status launch(const Product& p, int batch, hipStream_t st) {
     return (SYMMETRIC ? tm * (tm + 1) / 2 : tm * tn) * batch;
   };
   constexpr int NUM_CU = 256;
+  if constexpr (SYMMETRIC) {
+    auto rounds = [&](int size) { return (tiles(size) + NUM_CU - 1) / NUM_CU * size; };
+    if (tiles(MIDDLE) > NUM_CU / 2 && rounds(MIDDLE) < std::min(rounds(128), rounds(256))) return launch_middle<KIND>(p, batch, st);
+  }
   if (tiles(256) >= NUM_CU / 2) return launch_tile<KIND, 256, 2, 0, false>(p, batch, st);
   if (p.terms > 1) {
     if (tiles(64) <= NUM_CU) return launch_tile<KIND, 64, 2, 2, true>(p, batch, st);

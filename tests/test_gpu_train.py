@@ -472,6 +472,22 @@ def test_orthogonalize_is_as_exact_as_its_roundings(M, N, kind):
     assert np.linalg.norm((got.T if M > N else got) - want) / size <= 1e-5
 
 
+@pytest.mark.parametrize("B,M,N", [(200, 190, 400), (50, 310, 260), (160, 129, 200), (30, 448, 500)])
+def test_batches_in_tiles_of_192(B, M, N):
+    """Whole, cut off and side by side; the first, a middle and the last matrix to the same bars."""
+    import torch
+    G = np.random.default_rng(B).standard_normal((B, M, N)).astype(np.float32)
+    grad = torch.from_numpy(G).cuda()
+    turn = lambda x: x.T if M > N else x
+    got = [orthogonalize(t, grad, N, M * N, B, M, N, N, M * N).double().cpu().numpy().reshape(B, M, N) for t in TYPES]
+    for b in (0, B // 2, B - 1):
+        want = to.orthogonalize(G[b], MUON, 5, 1e-7)[-1]
+        size = np.linalg.norm(want)
+        inner = np.linalg.norm(emulate(G[b], MUON, 5, 1e-7) - want) / size
+        assert np.linalg.norm(turn(got[0][b]) - want) / size <= 1.5 * np.hypot(inner, 2.0 ** -8 / 3 ** 0.5)
+        assert np.linalg.norm(turn(got[1][b]) - want) / size <= 1e-5
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
 @pytest.mark.parametrize("coefficients,steps", [(MUON, 1), (MUON, 2), (MUON, 9), ((1.5, -0.5, 0.0), 12), ((1.875, -1.25, 0.375), 6),
                                                 ((1.0, 0.0, 0.0), 3), ((0.5, 0.25, 0.125), 4)])
