@@ -538,49 +538,55 @@ __global__ __launch_bounds__(512, 2) void large_product_kernel(Product p, int ti
                      });
 }
 
-// ---- 192 x 192, of the symmetric products: twelve wavefronts of 48 x 64, three slices of LDS with one barrier a slice.
-constexpr int MIDDLE = 192, MIDDLE_DEPTH = 3;
-constexpr size_t middle_lds() { return (size_t)MIDDLE_DEPTH * 2 * MIDDLE * BK * sizeof(half_t); }
+// ---- 192 x 192 and 96 x 96, of the symmetric products: twelve wavefronts of 48 x 64, or twice six of 48 x 32 that share the slices
+// as above; three slices of LDS each, with one barrier a slice.
+constexpr int MIDDLE_DEPTH = 3;
+constexpr size_t middle_lds(int tile) { return (size_t)(tile == 96 ? 2 : 1) * MIDDLE_DEPTH * 2 * tile * BK * sizeof(half_t); }
 
-template <int KIND>
+template <int KIND, int TILE>
 __global__ __launch_bounds__(768) void middle_product_kernel(Product p, int tiles_m, int tiles_n, int tiles) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   static_assert(KIND == GRAM || KIND == POLY, "operands whose k is contiguous");
-  using Reg = Region<MIDDLE, false, 12>;
+  static_assert(TILE == 96 || TILE == 192, "48 rows a wavefront");
+  constexpr int GROUPS = TILE == 96 ? 2 : 1, WAVES = 12 / GROUPS, WM = TILE / 48, FM = 3, FN = TILE / 48;
+  using Reg = Region<TILE, false, WAVES>;
   constexpr uint32_t BUF = 2 * Reg::BYTES;
-  constexpr int LOADS = 2 * Reg::LOADS, FM = 3, FN = 4;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 3, wn = wave >> 2;
+  constexpr int LOADS = 2 * Reg::LOADS;
+  const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = GROUPS > 1 ? id / WAVES : 0, wave = id - group * WAVES, wm = wave % WM, wn = wave / WM;
   const Place q = place<true>(tiles_m, tiles_n, tiles);
-  const int m0 = q.tm * MIDDLE, n0 = q.tn * MIDDLE;
+  const int m0 = q.tm * TILE, n0 = q.tn * TILE;
   const Operands<false> op(p, q, m0, n0);
-  const int n = op.slices * p.terms;
+  const int all = op.slices * p.terms, n = (all - group + GROUPS - 1) / GROUPS;
   Reg ra, rb;
   ra.init(p.lda, 0, p.M - m0, wave, lane);
   rb.init(p.ldb, 0, p.N - n0, wave, lane);
+  const uint32_t base = group * (MIDDLE_DEPTH * BUF);
   auto load = [&](int j, uint32_t buf) {
-    rb.template load<false>(op.b_at(j), p.ldb, BK, buf + Reg::BYTES, wave, lane);
-    ra.template load<false>(op.a_at(j), p.lda, BK, buf, wave, lane);
+    rb.template load<false>(op.b_at(group + j * GROUPS), p.ldb, BK, base + buf + Reg::BYTES, wave, lane);
+    ra.template load<false>(op.a_at(group + j * GROUPS), p.lda, BK, base + buf, wave, lane);
   };
-  Fragments<MIDDLE, false, FM> fa;
-  Fragments<MIDDLE, false, FN> fb;
+  Fragments<TILE, false, FM> fa;
+  Fragments<TILE, false, FN> fb;
   fa.init(wm * FM * 16, lane);
   fb.init(wn * FN * 16, lane);
   f32x4 acc[FM][FN] = {};
-  load(0, 0);
+  if (n > 0) load(0, 0);
   if (n > 1) load(1, BUF);
   uint32_t cur = 0, free = 2 * BUF;
-  for (int j = 0; j < n; ++j) {
+  for (int j = 0; j * GROUPS < all; ++j) {
     if (j + 1 < n) wait_loads<LOADS>();
     else wait_loads<0>();
     end_phase();                                             // slice j is there for all, and all have read slice j - 1
+    if (j >= n) break;                                       // (only in the last round)
     if (j + 2 < n) load(j + 2, free);
     bf16x8 a[2][FM], b[2][FN];
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
 #pragma unroll
-      for (int f = 0; f < FN; ++f) b[ks][f] = fb.read(smem, f, ks, cur + Reg::BYTES);
+      for (int f = 0; f < FN; ++f) b[ks][f] = fb.read(smem, f, ks, base + cur + Reg::BYTES);
 #pragma unroll
-      for (int f = 0; f < FM; ++f) a[ks][f] = fa.read(smem, f, ks, cur);
+      for (int f = 0; f < FM; ++f) a[ks][f] = fa.read(smem, f, ks, base + cur);
     }
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
@@ -593,8 +599,26 @@ __global__ __launch_bounds__(768) void middle_product_kernel(Product p, int tile
     free = cur;
     cur = cur == 2 * BUF ? 0 : cur + BUF;
   }
-  end_phase();                                               // strips overlay the slices
-  finish<KIND, FM, FN>(p, q.b, acc, reinterpret_cast<float*>(smem) + wave * 16 * 68, lane, n0 + wn * 64, q.tm != q.tn,
+  end_phase();                                               // sums and strips overlay the slices
+  constexpr int SUM = (GROUPS - 1) * TILE * TILE, STRIP = 16 * (FN * 16 + 4);
+  float* sums = reinterpret_cast<float*>(smem);
+  static_assert((SUM + WAVES * STRIP) * 4 <= middle_lds(TILE), "sums and strips fit");
+  if constexpr (GROUPS > 1) {
+    auto at = [&](int i, int c) { return reinterpret_cast<f32x4*>(sums + (((wave * FM + i) * FN + c) * 64 + lane) * 4); };
+    if (group > 0) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int c = 0; c < FN; ++c) *at(i, c) = acc[i][c];
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int c = 0; c < FN; ++c) acc[i][c] += *at(i, c);
+  }
+  finish<KIND, FM, FN>(p, q.b, acc, sums + SUM + wave * STRIP, lane, n0 + wn * FN * 16, q.tm != q.tn,
                        [&](int i) { return m0 + (wm * FM + i) * 16; }, [] {});
 }
 
@@ -1075,14 +1099,14 @@ bm_status launch_tile(const Product& p, int batch, hipStream_t st) {
   return BM_OK;
 }
 
-template <int KIND>
+template <int KIND, int TILE>
 bm_status launch_middle(const Product& p, int batch, hipStream_t st) {
   static std::atomic<uint64_t> done{0};
-  auto kern = middle_product_kernel<KIND>;
-  BM_RETURN_IF(allow_lds(kern, middle_lds(), &done));
-  const int t = cdiv(p.M, MIDDLE), tiles = t * (t + 1) / 2;
+  auto kern = middle_product_kernel<KIND, TILE>;
+  BM_RETURN_IF(allow_lds(kern, middle_lds(TILE), &done));
+  const int t = cdiv(p.M, TILE), tiles = t * (t + 1) / 2;
   ProfScope prof(PROF_GEMM_NT, (double)batch * p.terms * p.M * p.N * p.K, st);
-  hipLaunchKernelGGL(kern, dim3((unsigned)((long)tiles * batch)), dim3(768), middle_lds(), st, p, t, t, tiles);
+  hipLaunchKernelGGL(kern, dim3((unsigned)((long)tiles * batch)), dim3(768), middle_lds(TILE), st, p, t, t, tiles);
   BM_CHECK_LAUNCH("orthogonalize product");
   return BM_OK;
 }
@@ -1094,6 +1118,8 @@ bm_status launch_middle(const Product& p, int batch, hipStream_t st) {
 // A CU fetches the operands of one tile after the other, so a symmetric product takes the rounds of the chip times the tile's size:
 // 4096 rows are 136 tiles of 256 for 256 CUs, but 253 of 192.  A whole update without and with 192 x 192:
 //   4096 x 4096 1448, 1374 (fp32 3822, 3682)     4096 x 14336 3900, 3769     3584 x 3584 1153, 1033     50 of 300 x 300 246, 217
+// and with 96 x 96:
+//   2048 x 2048 359, 317     2048 x 8192 840, 732     1792 x 7168 611, 573     1536 x 1536 224, 227
 template <int KIND>
 bm_status launch(const Product& p, int batch, hipStream_t st) {
   constexpr bool SYMMETRIC = KIND == GRAM || KIND == POLY;
@@ -1104,7 +1130,9 @@ bm_status launch(const Product& p, int batch, hipStream_t st) {
   constexpr int NUM_CU = 256;
   if constexpr (SYMMETRIC) {
     auto rounds = [&](int size) { return (tiles(size) + NUM_CU - 1) / NUM_CU * size; };
-    if (tiles(MIDDLE) > NUM_CU / 2 && rounds(MIDDLE) < std::min(rounds(128), rounds(256))) return launch_middle<KIND>(p, batch, st);
+    if (tiles(192) > NUM_CU / 2 && rounds(192) < std::min(rounds(128), rounds(256))) return launch_middle<KIND, 192>(p, batch, st);
+    if (p.terms == 1 && tiles(96) > NUM_CU / 2 && tiles(64) > NUM_CU && rounds(96) < std::min(rounds(128), rounds(256)))
+      return launch_middle<KIND, 96>(p, batch, st);
   }
   if (tiles(256) >= NUM_CU / 2) return launch_tile<KIND, 256, 2, 0, false>(p, batch, st);
   if (p.terms > 1) {

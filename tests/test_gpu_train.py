@@ -472,8 +472,9 @@ def test_orthogonalize_is_as_exact_as_its_roundings(M, N, kind):
     assert np.linalg.norm((got.T if M > N else got) - want) / size <= 1e-5
 
 
-@pytest.mark.parametrize("B,M,N", [(200, 190, 400), (50, 310, 260), (160, 129, 200), (30, 448, 500)])
-def test_batches_in_tiles_of_192(B, M, N):
+@pytest.mark.parametrize("B,M,N", [(200, 190, 400), (50, 310, 260), (160, 129, 200), (30, 448, 500), (60, 150, 200), (55, 190, 133),
+                                   (45, 192, 192)])
+def test_batches_in_tiles_of_192_and_96(B, M, N):
     """Whole, cut off and side by side; the first, a middle and the last matrix to the same bars."""
     import torch
     G = np.random.default_rng(B).standard_normal((B, M, N)).astype(np.float32)
