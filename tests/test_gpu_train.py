@@ -92,7 +92,9 @@ def embedding_backward(dtype, V, d, dy, ld_dy, ids, T, scale, dtable, ld):
 CASES = [(1, 1, 1, 0, "one"), (2, 3, 5, 0, "one"), (5, 300, 8, 8, "any"), (64, 256, 24, 0, "images"), (65, 257, 100, 3, "past"),
          (777, 1000, 1152, 16, "ranked"), (2048, 3000, 72, 0, "any"), (2049, 500, 520, 0, "few"), (4099, 9, 1028, 4, "one"),
          (8193, 70000, 36, 0, "ranked"), (9000, 300000, 8, 0, "ranked"), (33000, 400, 17, 1, "images"), (33000, 50, 64, 0, "one"),
-         (130, 40, 513, 0, "none"), (1500, 4, 2048, 0, "any"), (70001, 5000, 12, 0, "ranked"), (66000, 257, 9, 0, "past"), (65537, 3, 8, 0, "one")]
+         (130, 40, 513, 0, "none"), (1500, 4, 2048, 0, "any"), (70001, 5000, 12, 0, "ranked"), (66000, 257, 9, 0, "past"), (65537, 3, 8, 0, "one"),
+         (127, 5000, 65, 0, "past"), (128, 40, 4096, 0, "any"), (128, 3, 63, 2, "one"), (129, 60, 192, 0, "ranked"), (100, 128, 130, 6, "images"),
+         (128, 100000, 1000, 0, "any"), (33, 9, 7, 0, "none")]
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
