@@ -553,6 +553,46 @@ def test_orthogonalize_replayed():
         assert torch.equal(got, out)
 
 
+def test_calls_at_the_same_time():
+    """On two streams, each with a workspace of its own."""
+    import torch
+    rng = np.random.default_rng(8)
+    T, V, d, M, N = 900, 700, 264, 500, 640
+    jobs = []
+    for _ in range(2):
+        ids, labels = ints(rng.integers(-1, V, T)), ints(rng.integers(-1, V, T))
+        dy = torch.randn((T, d), device="cuda").to(torch.bfloat16)
+        z = torch.randn((T, V), device="cuda").to(torch.bfloat16)
+        grad = torch.randn((M, N), device="cuda")
+        out = [torch.zeros((V, d), device="cuda"), torch.zeros(T, device="cuda"), torch.zeros_like(z),
+               torch.zeros((M, N), dtype=torch.bfloat16, device="cuda")]
+        sizes = [bm.embedding_backward_scratch_bytes(T, d), bm.cross_entropy_scratch_bytes(0, T, V), bm.orthogonalize_scratch_bytes(0, 1, M, N)]
+        scratch = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes]
+
+        def run(ids=ids, labels=labels, dy=dy, z=z, grad=grad, out=out, sizes=sizes, scratch=scratch):
+            out[0].zero_()
+            bm.embedding_backward(0, V, d, dy, d, ids, T, 1.0, out[0], d, scratch[0], sizes[0])
+            bm.cross_entropy(0, T, V, z, V, labels, None, out[1], out[2], V, scratch[1], sizes[1])
+            bm.orthogonalize(0, 1, M, N, grad, N, M * N, out[3], N, M * N, MUON, 5, 1e-7, scratch[2], sizes[2])
+
+        jobs.append((run, out, torch.cuda.Stream()))
+    want = []
+    for run, out, _ in jobs:
+        run()
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in out])
+        for t in out:
+            t.zero_()
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for run, _, stream in jobs:
+            with torch.cuda.stream(stream):
+                run()
+    torch.cuda.synchronize()
+    for (_, out, _), w in zip(jobs, want):
+        assert all(torch.equal(a, b) for a, b in zip(out, w))
+
+
 # ---- more than one launch has threads for ------------------------------------------------------------------
 
 def test_lookup_of_more_rows_than_a_launch():
