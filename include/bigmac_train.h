@@ -73,9 +73,9 @@ bm_status bm_cross_entropy(int32_t dtype, int32_t T, int32_t V, const void* logi
  * Strides are in elements and not negative; stride_g may be 0; matrices of `out` lie one behind the other or side by
  * side.  out may be grad itself with the same strides (BM_DTYPE_FP32); otherwise the memory from the first to the last element of
  * the one and that of the other do not overlap.
- * The products run on the matrix cores in 11-bit significands (fp16, scaled; X itself is kept in 22 bits until the
- * last two steps, in which only singular values near the fixed points are still moved) for dtype BM_DTYPE_BF16 and more than
- * 32 rows and columns, and in 22 bits otherwise; sums are fp32, the norm fp64.
+ * The products run on the matrix cores.  For BM_DTYPE_BF16 their operands are 11-bit significands (fp16, scaled); X itself is kept
+ * in 22 bits until the last two steps, in which only singular values near the fixed points are still moved, and up to 128
+ * rows or columns so are A and B, up to 32 all of them.  For BM_DTYPE_FP32 everything has 22 bits.  Sums are fp32, the norm fp64.
  * BM_ERR_UNSUPPORTED for coefficients under which a singular value of [0, 1] exceeds 8 within `steps` steps.
  * A matrix that holds an infinity or a NaN gives NaN; other matrices of the batch are not affected.
  * scratch: bm_orthogonalize_scratch_bytes(dtype, batch, M, N) bytes.  batch may be 0. */

@@ -9,9 +9,9 @@
 // Numbers.  Operands are fp16, whose products the matrix cores add up in fp32.  bf16 would round eight times as coarsely:
 // 1-6 % off after five steps, against 0.2 % of the one rounding that a bf16 result needs anyway.  What decides is X: a
 // small singular value has few of X's bits, and five steps enlarge it 500 times.  So X is kept as hi + lo (22 bits)
-// until the last two steps, where it enters the sum a X in full and the products as hi alone: 0.08-0.14 % off on noise and on spectra that
-// fall over three decades (hi alone all the time: 0.14 and 0.4-0.7 %).  For fp32 results all of X, A and B are hi + lo and every
-// product is three, hi hi + hi lo + lo hi: 3e-7 to 1.3e-6 off.
+// until the last two steps, where it enters the sum a X in full and the products as hi alone: 0.08-0.16 % off on noise and on spectra that
+// fall over three decades (hi alone all the time: 0.14 and 0.4-0.7 %).  Few rows need more, see there.  For fp32 results all
+// of X, A and B are hi + lo and every product is three, hi hi + hi lo + lo hi: 3e-7 to 1.3e-6 off.
 // fp16's range: with powers of two s, t and u the buffers hold s X, t A and u B (see Scales).
 #include "gemm_phases.h"
 #include "train.h"
@@ -627,10 +627,11 @@ __global__ __launch_bounds__(768) void middle_product_kernel(Product p, int tile
 // A and B fit the LDS of a workgroup, so that a whole step is one launch: a workgroup holds a chunk of X's columns, has A from the sums
 // of all chunks, computes B for itself, moves its chunk on and adds up the chunk's share of the next A.  Where X is one
 // chunk (32 x 1024, 64 x 512, 128 x 128), all steps are one launch.  The tiled kernels would be three
-// launches a step of one to a few workgroups: 192 x 64 59 us, here 20; 29 x 2350 93 and 47; 100 x 4096 127 and 88.
+// launches a step of one to a few workgroups: 192 x 64 59 us, here 23; 29 x 2350 93 and 47; 100 x 4096 127 and 96.
 //
-// Up to 32 rows take the three products for bf16 results, too: single roundings do not average out there (16 x 64: up to 0.18 % off
-// with a single product), and what they cost is launches.
+// Roundings average out less the fewer rows there are: with A and B of 11 bits a bf16 result would be 0.3 % off at 35 x 704 and
+// 0.18 % at 64 x 192, beside 0.17 % of its own rounding.  So A and B are hi + lo here for all results: 0.08 and 0.1 % (22.7 us at 192 x 64
+// instead of 20.4, 96 at 100 x 4096 instead of 88), and X, too, up to 32 rows (16 x 64: up to 0.18 % with a single product).
 //
 // LDS: X and then A or B in blocks of MP rows x 64 columns, 128 bytes a row, 16-byte chunk c of row r at c ^ ((r >> 1) & 7); hi, and lo
 // behind it.  A chunk lies in the workspace as it does in LDS.
@@ -657,7 +658,7 @@ constexpr int tiny_blocks(int mp, bool solo) { return mp == 128 ? 2 : solo ? 512
 constexpr int tiny_gram_blocks(int mp) { return (mp / 16) * (mp / 16 + 1) / 2; }
 constexpr size_t tiny_x_bytes(int mp, int blocks) { return (size_t)blocks * mp * 64 * 2 * 2; }
 constexpr uint32_t tiny_ab_bytes(int mp) { return (mp + 63) / 64 * mp * 128; }
-constexpr size_t tiny_lds(int mp, int blocks, bool full) { return tiny_x_bytes(mp, blocks) + tiny_ab_bytes(mp) * (full ? 2 : 1) + 256 + (mp == 32 ? 16 * 1024 : 0); }
+constexpr size_t tiny_lds(int mp, int blocks) { return tiny_x_bytes(mp, blocks) + tiny_ab_bytes(mp) * 2 + 256 + (mp == 32 ? 16 * 1024 : 0); }
 
 template <int MP, bool FULL, int MODE>
 __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
@@ -668,7 +669,7 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
   const int b = blockIdx.x / t.chunks, chunk = blockIdx.x % t.chunks;
   const uint32_t x_half = t.blocks * (MP * 128), ab0 = 2 * x_half;
   constexpr uint32_t ab_half = tiny_ab_bytes(MP);
-  double* sm = reinterpret_cast<double*>(smem + ab0 + ab_half * (FULL ? 2 : 1));
+  double* sm = reinterpret_cast<double*>(smem + ab0 + ab_half * 2);
   const int m_in = lane & 15, q4 = (lane >> 4) * 4;
   auto at = [](int block, int row, int c) { return (uint32_t)((block * MP + row) * 128 + ((c ^ ((row >> 1) & 7)) << 4)); };
   // 16 rows x 32 k of an operand whose k is contiguous; k step ks of 32
@@ -701,13 +702,13 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
     *c = (tm + left) * 16;
     return id;
   };
-  // a block of the symmetric product of the rows at `base`, over k steps from .. to - 1
-  auto gram_block = [&](uint32_t base, uint32_t half, int r, int c, int from, int to) {
+  // a block of the symmetric product of the rows at `base`, over k steps from .. to - 1; of both parts of their values or of hi alone
+  auto gram_block = [&](auto parts_t, uint32_t base, uint32_t half, int r, int c, int from, int to) {
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     auto step = [&](int ks) {
       const half8 x = rows16(base, r, ks), y = rows16(base, c, ks);
       mfma(y, x, v);
-      if (FULL) {
+      if constexpr (decltype(parts_t)::value > 1) {
         mfma(rows16(base + half, c, ks), x, v);
         mfma(y, rows16(base + half, r, ks), v);
       }
@@ -718,26 +719,26 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
     if (ks < to) step(ks);
     return v;
   };
-  auto gram = [&](uint32_t base, uint32_t half, int steps, f32x4 (&acc)[PER_WAVE]) {
+  auto gram = [&](auto parts_t, uint32_t base, uint32_t half, int steps, f32x4 (&acc)[PER_WAVE]) {
 #pragma unroll
     for (int i = 0; i < PER_WAVE; ++i) {
       int r, c;
-      acc[i] = block_of(i, &r, &c) < GB ? gram_block(base, half, r, c, 0, steps) : f32x4{0.f, 0.f, 0.f, 0.f};
+      acc[i] = block_of(i, &r, &c) < GB ? gram_block(parts_t, base, half, r, c, 0, steps) : f32x4{0.f, 0.f, 0.f, 0.f};
     }
   };
   // that of X, whose columns are shared by as many wavefronts as there are for a block
-  constexpr int SHARE = TINY_WAVES / GB > 1 ? TINY_WAVES / GB : 1;
+  constexpr int X_PARTS = FULL ? 2 : 1, SHARE = TINY_WAVES / GB > 1 ? TINY_WAVES / GB : 1;
   auto gram_x = [&](f32x4 (&acc)[PER_WAVE]) {
     if constexpr (SHARE == 1) {
-      gram(0, x_half, t.blocks * 2, acc);
+      gram(Int<X_PARTS>{}, 0, x_half, t.blocks * 2, acc);
     } else {
       static_assert(PER_WAVE == 1, "a block a wavefront");
-      f32x4* shares = reinterpret_cast<f32x4*>(smem + ab0 + ab_half * (FULL ? 2 : 1) + 256);
+      f32x4* shares = reinterpret_cast<f32x4*>(smem + ab0 + ab_half * 2 + 256);
       const int part = wave / GB, block = wave % GB, per = (t.blocks * 2 + SHARE - 1) / SHARE;
       int r = 0, left = block;
       while (left >= MB - r) { left -= MB - r; ++r; }
       acc[0] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (part < SHARE) acc[0] = gram_block(0, x_half, r * 16, (r + left) * 16, part * per, min(t.blocks * 2, part * per + per));
+      if (part < SHARE) acc[0] = gram_block(Int<X_PARTS>{}, 0, x_half, r * 16, (r + left) * 16, part * per, min(t.blocks * 2, part * per + per));
       if (part > 0 && part < SHARE) shares[((part - 1) * GB + block) * WAVE + lane] = acc[0];
       __syncthreads();
       if (part == 0) {
@@ -756,14 +757,14 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) { hi[e] = (half_t)v[i][e]; lo[e] = (half_t)(v[i][e] - (float)hi[e]); }
       *reinterpret_cast<half4*>(four(ab0, r + m_in, c + q4)) = hi;
-      if (FULL) *reinterpret_cast<half4*>(four(ab0 + ab_half, r + m_in, c + q4)) = lo;
+      *reinterpret_cast<half4*>(four(ab0 + ab_half, r + m_in, c + q4)) = lo;
       if (r == c) continue;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int row = c + q4 + e, col = r + m_in;
         const uint32_t o = ab0 + at(col >> 6, row, (col & 63) >> 3) + (col & 7) * 2;
         *reinterpret_cast<half_t*>(smem + o) = hi[e];
-        if (FULL) *reinterpret_cast<half_t*>(smem + o + ab_half) = lo[e];
+        *reinterpret_cast<half_t*>(smem + o + ab_half) = lo[e];
       }
     }
   };
@@ -849,20 +850,12 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
     }
     const float alpha = t.t / (t.s * t.s);
 #pragma unroll
-    for (int i = 0; i < PER_WAVE; ++i) {
-      acc[i] *= alpha;
-      // both terms of B with the same A: an error that X itself could have had is one that the iteration damps (64 x 192, unrounded
-      // here: 0.19-0.22 % off before the last rounding, so 0.11)
-      if (!FULL) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][e] = (float)(half_t)acc[i][e];
-      }
-    }
+    for (int i = 0; i < PER_WAVE; ++i) acc[i] *= alpha;
     put_symmetric(acc);
     __syncthreads();
     // B in its place
     f32x4 square[PER_WAVE];
-    gram(ab0, ab_half, MP / 32, square);
+    gram(Int<2>{}, ab0, ab_half, MP / 32, square);
     const float cs = t.c * (t.u / t.t) / t.t, bs = t.b * (t.u / t.t);
 #pragma unroll
     for (int i = 0; i < PER_WAVE; ++i) square[i] = cs * square[i] + bs * acc[i];
@@ -874,14 +867,14 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
     const float as = end ? t.a / t.s : t.a, us = (end ? 1.f / t.s : 1.f) / t.u;
     // (B's fragments stay in registers where there is room)
     constexpr bool HELD = MP <= 64;
-    half8 w_hi[HELD ? MP / 32 : 1][HELD ? MB : 1], w_lo[HELD && FULL ? MP / 32 : 1][HELD && FULL ? MB : 1];
+    half8 w_hi[HELD ? MP / 32 : 1][HELD ? MB : 1], w_lo[HELD ? MP / 32 : 1][HELD ? MB : 1];
     if constexpr (HELD) {
 #pragma unroll
       for (int ks = 0; ks < MP / 32; ++ks)
 #pragma unroll
         for (int i = 0; i < MB; ++i) {
           w_hi[ks][i] = rows16(ab0, i * 16, ks);
-          if constexpr (FULL) w_lo[ks][i] = rows16(ab0 + ab_half, i * 16, ks);
+          w_lo[ks][i] = rows16(ab0 + ab_half, i * 16, ks);
         }
     }
     for (int strip = wave; strip < t.blocks * 4; strip += TINY_WAVES) {
@@ -896,12 +889,10 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
         for (int i = 0; i < MB; ++i) {
           half8 w, wl;
           if constexpr (HELD) w = w_hi[ks][i]; else w = rows16(ab0, i * 16, ks);
+          if constexpr (HELD) wl = w_lo[ks][i]; else wl = rows16(ab0 + ab_half, i * 16, ks);
           mfma(x, w, y[i]);
-          if constexpr (FULL) {
-            if constexpr (HELD) wl = w_lo[ks][i]; else wl = rows16(ab0 + ab_half, i * 16, ks);
-            mfma(xl, w, y[i]);
-            mfma(x, wl, y[i]);
-          }
+          mfma(x, wl, y[i]);
+          if constexpr (FULL) mfma(xl, w, y[i]);
         }
       }
 #pragma unroll
@@ -1150,17 +1141,17 @@ bm_status launch_tiny(const Tiny& t, int batch, hipStream_t st) {
   auto kern = tiny_kernel<MP, FULL, MODE>;
   static std::atomic<uint64_t> done{0};
   constexpr int MOST = tiny_blocks(MP, MODE == SOLO);
-  static_assert(tiny_lds(MP, MOST, FULL) <= 160 * 1024, "a chunk with A or B");
-  BM_RETURN_IF(allow_lds(kern, tiny_lds(MP, MOST, FULL), &done));
-  hipLaunchKernelGGL(kern, dim3((unsigned)((long)batch * t.chunks)), dim3(TINY_THREADS), tiny_lds(MP, t.blocks, FULL), st, t);
+  static_assert(tiny_lds(MP, MOST) <= 160 * 1024, "a chunk with A or B");
+  BM_RETURN_IF(allow_lds(kern, tiny_lds(MP, MOST), &done));
+  hipLaunchKernelGGL(kern, dim3((unsigned)((long)batch * t.chunks)), dim3(TINY_THREADS), tiny_lds(MP, t.blocks), st, t);
   BM_CHECK_LAUNCH("orthogonalize few rows");
   return BM_OK;
 }
 
 // Chunks whose sums every workgroup adds up for itself.  A whole update in us without and with a launch that does it once:
-//   128 x 512 (4 chunks) 72.0, 73.5    128 x 896 (7) 85.6, 77.7    100 x 4096 (32) 117.6, 88.3
-//   64 x 8192 (32) 60.1, 66.5    64 x 16384 (64) 79.9, 79.3    64 x 32768 (128) 113.5, 101.5
-//   32 x 131072 (256) 135.7, 144.2    32 x 262144 (512) 391, 258
+//   128 x 512 (4 chunks) 80.2, 81.3    128 x 896 (7) 93.8, 86.1    100 x 4096 (32) 125.4, 96.7
+//   64 x 8192 (32) 62.0, 68.9    64 x 16384 (64) 82.2, 82.3    64 x 32768 (128) 115.9, 103.7
+//   32 x 131072 (256) 135.3, 143.2    32 x 262144 (512) 391, 257
 constexpr int tiny_summands(int mp) { return mp == 128 ? 4 : mp == 64 ? 64 : 256; }
 
 template <int MP, bool FULL>
