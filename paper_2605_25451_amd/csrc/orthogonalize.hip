@@ -11,7 +11,7 @@
 // small singular value has few of X's bits, and five steps enlarge it 500 times.  So X is kept as hi + lo (22 bits)
 // until the last two steps, where it enters the sum a X in full and the products as hi alone: 0.08-0.16 % off on noise and on spectra that
 // fall over three decades (hi alone all the time: 0.14 and 0.4-0.7 %).  Few rows need more, see there.  For fp32 results all
-// of X, A and B are hi + lo and every product is three, hi hi + hi lo + lo hi: 3e-7 to 1.3e-6 off.
+// of X, A and B are hi + lo and every product is three, hi hi + hi lo + lo hi: 3e-7 to 3e-6 off, as in fp32 arithmetic.
 // fp16's range: with powers of two s, t and u the buffers hold s X, t A and u B (see Scales).
 #include "gemm_phases.h"
 #include "train.h"
@@ -658,7 +658,11 @@ constexpr int tiny_blocks(int mp, bool solo) { return mp == 128 ? 2 : solo ? 512
 constexpr int tiny_gram_blocks(int mp) { return (mp / 16) * (mp / 16 + 1) / 2; }
 constexpr size_t tiny_x_bytes(int mp, int blocks) { return (size_t)blocks * mp * 64 * 2 * 2; }
 constexpr uint32_t tiny_ab_bytes(int mp) { return (mp + 63) / 64 * mp * 128; }
-constexpr size_t tiny_lds(int mp, int blocks) { return tiny_x_bytes(mp, blocks) + tiny_ab_bytes(mp) * 2 + 256 + (mp == 32 ? 16 * 1024 : 0); }
+constexpr uint32_t tiny_norm_bytes(bool solo) { return solo ? 256 : 0; }
+constexpr size_t tiny_lds(int mp, int blocks, bool solo) {
+  return tiny_x_bytes(mp, blocks) + tiny_ab_bytes(mp) * 2 + tiny_norm_bytes(solo) + (mp == 32 ? 16 * 1024 : 0);
+}
+static_assert(tiny_lds(64, tiny_blocks(64, false), false) * 2 <= 160 * 1024, "two share a CU");
 
 template <int MP, bool FULL, int MODE>
 __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
@@ -733,7 +737,7 @@ __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
       gram(Int<X_PARTS>{}, 0, x_half, t.blocks * 2, acc);
     } else {
       static_assert(PER_WAVE == 1, "a block a wavefront");
-      f32x4* shares = reinterpret_cast<f32x4*>(smem + ab0 + ab_half * 2 + 256);
+      f32x4* shares = reinterpret_cast<f32x4*>(smem + ab0 + ab_half * 2 + tiny_norm_bytes(MODE == SOLO));
       const int part = wave / GB, block = wave % GB, per = (t.blocks * 2 + SHARE - 1) / SHARE;
       int r = 0, left = block;
       while (left >= MB - r) { left -= MB - r; ++r; }
@@ -1141,9 +1145,9 @@ bm_status launch_tiny(const Tiny& t, int batch, hipStream_t st) {
   auto kern = tiny_kernel<MP, FULL, MODE>;
   static std::atomic<uint64_t> done{0};
   constexpr int MOST = tiny_blocks(MP, MODE == SOLO);
-  static_assert(tiny_lds(MP, MOST) <= 160 * 1024, "a chunk with A or B");
-  BM_RETURN_IF(allow_lds(kern, tiny_lds(MP, MOST), &done));
-  hipLaunchKernelGGL(kern, dim3((unsigned)((long)batch * t.chunks)), dim3(TINY_THREADS), tiny_lds(MP, t.blocks), st, t);
+  static_assert(tiny_lds(MP, MOST, MODE == SOLO) <= 160 * 1024, "a chunk with A or B");
+  BM_RETURN_IF(allow_lds(kern, tiny_lds(MP, MOST, MODE == SOLO), &done));
+  hipLaunchKernelGGL(kern, dim3((unsigned)((long)batch * t.chunks)), dim3(TINY_THREADS), tiny_lds(MP, t.blocks, MODE == SOLO), st, t);
   BM_CHECK_LAUNCH("orthogonalize few rows");
   return BM_OK;
 }
