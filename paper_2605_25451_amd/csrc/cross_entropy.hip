@@ -173,19 +173,25 @@ __global__ __launch_bounds__(PART_THREADS) void part_finish_kernel(const T* logi
 
 typedef unsigned int Quad __attribute__((ext_vector_type(4)));
 
-// The same statistics with an instruction less per element: exp(x - m) as 2^(x L - c), c = m L rounded once, which is a
-// common factor of all terms.  c is kept inside fp32's range, which makes rows whose largest logit is past 1e38 in
-// magnitude wrong (a row of nothing but the lowest finite value, say); those are done again with the difference first.
+// The same statistics with an instruction less per element: exp(x - m) as 2^(x L - c), c = m L rounded once, which makes 2^(m L - c)
+// a common factor of all terms.  m L - c is half a step of c at most: 1/2 up to |m| = MOST, but from 1e9 on the factor can leave fp32's
+// range.  So the maximum starts at -MOST (a thread whose words are all masked with -1e30 or -inf adds nothing), and a row whose
+// largest logit is not between -MOST and MOST is done again with the difference first.
 struct Stat2 {
+  static constexpr float MOST = 0x1p23f;
   float m, c, s;
-  static __device__ inline float bound(float m) { return __builtin_amdgcn_fmed3f(m * LOG2E, -3e38f, 3e38f); }
-  static __device__ inline Stat2 none() { return Stat2{-FLT_MAX, -3e38f, 0.f}; }
+  // (the same rounded product wherever it is taken, never part of a fused multiply-add)
+  static __device__ inline float scaled(float m) {
+#pragma clang fp contract(off)
+    return m * LOG2E;
+  }
+  static __device__ inline Stat2 none() { return Stat2{-MOST, -MOST * LOG2E, 0.f}; }
   static __device__ inline float term(float x, float c) { return __builtin_amdgcn_exp2f(fmaf(x, LOG2E, -c)); }
   template <int N> __device__ inline void add(const float (&x)[N]) {
     float top = m;
 #pragma unroll
     for (int e = 0; e < N; ++e) top = fmaxf(top, x[e]);
-    const float c1 = bound(top);
+    const float c1 = scaled(top);
     s *= __builtin_amdgcn_exp2f(c - c1);
 #pragma unroll
     for (int e = 0; e < N; ++e) s += term(x[e], c1);
@@ -195,7 +201,7 @@ struct Stat2 {
 };
 template <int THREADS>
 __device__ inline Stat2 block_join(Stat2 a, Stat2* sm) {
-  const float m = wave_max(a.m), c = Stat2::bound(m);
+  const float m = wave_max(a.m), c = Stat2::scaled(m);
   const float s = wave_sum(a.s * __builtin_amdgcn_exp2f(a.c - c));
   if (THREADS == WAVE) return Stat2{m, c, s};
   __syncthreads();
@@ -207,7 +213,7 @@ __device__ inline Stat2 block_join(Stat2 a, Stat2* sm) {
   float top = r.m;
 #pragma unroll
   for (int off = 1; off < WAVES; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, WAVE));
-  const float c1 = Stat2::bound(top);
+  const float c1 = Stat2::scaled(top);
   r.s *= __builtin_amdgcn_exp2f(r.c - c1);
 #pragma unroll
   for (int off = 1; off < WAVES; off <<= 1) r.s += __shfl_xor(r.s, off, WAVE);
@@ -267,7 +273,7 @@ __global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long ld, 
     a.add(f);
   }
   a = block_join<THREADS>(a, sm);
-  if (!(fabsf(a.m) <= 1e38f)) {
+  if (!(fabsf(a.m) < Stat2::MOST)) {
     Stat b = Stat::none();
 #pragma unroll 1
     for (int i = tid; i < V; i += THREADS) {
