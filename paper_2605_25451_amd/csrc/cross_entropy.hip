@@ -290,7 +290,8 @@ __global__ __launch_bounds__(THREADS) void row_kernel(const T* logits, long ld, 
     return;
   }
   const float scale = w / a.s;
-  if (tid == 0 && loss) loss[row] = w * ((a.c + __builtin_amdgcn_logf(a.s)) * LN2 - xl);
+  // log of the terms' sum without their common factor, to what the label is behind: c itself would round the loss at the logits' size
+  if (tid == 0 && loss) loss[row] = w * ((a.m - xl) + (__builtin_amdgcn_logf(a.s) - fmaf(a.m, LOG2E, -a.c)) * LN2);
   if (!dlogits) return;
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
