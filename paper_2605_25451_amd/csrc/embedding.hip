@@ -659,13 +659,19 @@ extern "C" bm_status bm_embedding_backward(int32_t dtype, int32_t V, int32_t d, 
   const int W = dtype == BM_DTYPE_BF16 ? 8 : 4;
   const bool vec = d % W == 0 && ld_dy % W == 0 && ld_dtable % 4 == 0;
   if (T <= FEW) {
-    auto few = [&](auto kern, auto* rows) {
-      hipLaunchKernelGGL(kern, dim3(cdiv(d, WAVE)), dim3(FEW_THREADS), 0, st, rows, (long)ld_dy, ids, T, V, d, scale, dtable, (long)ld_dtable);
+    // (a grid has fewer than 2^32 threads)
+    constexpr int MOST = 1 << 27;                           // columns of a launch
+    auto few = [&](auto kern, auto* rows) -> bm_status {
+      for (int c = 0; c < d; c += std::min(MOST, d - c)) {
+        const int n = std::min(MOST, d - c);
+        hipLaunchKernelGGL(kern, dim3(cdiv(n, WAVE)), dim3(FEW_THREADS), 0, st, rows + c, (long)ld_dy, ids, T, V, n, scale, dtable + c,
+                           (long)ld_dtable);
+        BM_CHECK_LAUNCH("embedding gradient of few tokens");
+      }
+      return BM_OK;
     };
-    if (dtype == BM_DTYPE_BF16) few(vec ? few_kernel<bf16_t, true> : few_kernel<bf16_t, false>, (const bf16_t*)dy);
-    else few(vec ? few_kernel<float, true> : few_kernel<float, false>, (const float*)dy);
-    BM_CHECK_LAUNCH("embedding gradient of few tokens");
-    return BM_OK;
+    return dtype == BM_DTYPE_BF16 ? few(vec ? few_kernel<bf16_t, true> : few_kernel<bf16_t, false>, (const bf16_t*)dy)
+                                  : few(vec ? few_kernel<float, true> : few_kernel<float, false>, (const float*)dy);
   }
   int bits = 0;                                             // of the ids, above those of the bucket
   while (bits < 31 - BUCKET_BITS && ((V - 1) >> (BUCKET_BITS + bits))) ++bits;

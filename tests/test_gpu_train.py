@@ -612,6 +612,27 @@ def test_lookup_of_more_rows_than_a_launch():
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
+@pytest.mark.parametrize("ids,V,d", [([0], 1, (1 << 28) + 3), ([1, 0, 1], 2, (1 << 28) + 72), ([2, -1, 2, 0, 7], 3, (1 << 27) + 1)])
+def test_gradient_of_few_tokens_of_more_columns_than_a_launch(ids, V, d, dtype):
+    import torch
+    T = len(ids)
+    dy = torch.randn((T, d), device="cuda").to(torch_type(dtype))
+    start = torch.randn((V, d), device="cuda")
+    dtable = start.clone()
+    embedding_backward(dtype, V, d, dy, d, ints(ids), T, 0.75, dtable, d)
+    for first in range(0, d, 1 << 26):
+        part = slice(first, min(d, first + (1 << 26)))
+        for v in range(V):
+            mine = dy[[t for t in range(T) if ids[t] == v], part].double()
+            old, got = start[v, part].double(), dtable[v, part].double()
+            if len(mine) == 0:
+                assert torch.equal(got, old)
+                continue
+            size = old.abs() + 0.75 * mine.abs().sum(0)
+            assert ((got - (old + 0.75 * mine.sum(0))).abs() <= (len(mine) + 2) * F * size).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=NAMES)
 def test_loss_of_more_rows_than_a_launch(dtype):
     import torch
     T, V, ld, few = (1 << 21) + 700, 5, 7, 300
