@@ -652,7 +652,11 @@ struct Tiny {
   int out_fp32;
 };
 
-// the most 64-column blocks of a chunk: of a matrix that is one, and of others (64 KiB of X, so that two chunks of up to 64 rows share a CU)
+// the most 64-column blocks of a chunk: of a matrix that is one, and of others.  A CU runs one workgroup of a step: 64 rows leave 4
+// wavefronts a SIMD their registers (B's fragments take 64 of 112), 32 rows take 88 KiB of LDS.  Short chunks are faster while a matrix
+// is fewer of them than there are CUs, long ones beyond; what is taken lies between.  bf16, us, with 128 / 256 / 512 over the rows:
+//   64 x 1024 39, 46, 60    64 x 8192 69, 61, 70    64 x 131072 426, 267, 190    128 of 64 x 2048 385, 276, 229
+//   32 x 2350 37, 46, 62    29 x 16384 51, 52, 65    32 x 81920 147, 97, 92    256 of 32 x 2048 205, 252, 216
 constexpr int tiny_blocks(int mp, bool solo) { return mp == 128 ? 2 : solo ? 512 / mp : 256 / mp; }
 // blocks of 16 x 16 on and above the diagonal of A
 constexpr int tiny_gram_blocks(int mp) { return (mp / 16) * (mp / 16 + 1) / 2; }
@@ -662,7 +666,6 @@ constexpr uint32_t tiny_norm_bytes(bool solo) { return solo ? 256 : 0; }
 constexpr size_t tiny_lds(int mp, int blocks, bool solo) {
   return tiny_x_bytes(mp, blocks) + tiny_ab_bytes(mp) * 2 + tiny_norm_bytes(solo) + (mp == 32 ? 16 * 1024 : 0);
 }
-static_assert(tiny_lds(64, tiny_blocks(64, false), false) * 2 <= 160 * 1024, "two share a CU");
 
 template <int MP, bool FULL, int MODE>
 __global__ __launch_bounds__(TINY_THREADS) void tiny_kernel(Tiny t) {
