@@ -11,7 +11,8 @@
 // small singular value has few of X's bits, and five steps enlarge it 500 times.  So X is kept as hi + lo (22 bits)
 // until the last two steps, where it enters the sum a X in full and the products as hi alone: 0.08-0.16 % off on noise and on spectra that
 // fall over three decades (hi alone all the time: 0.14 and 0.4-0.7 %).  Few rows need more, see there.  For fp32 results all
-// of X, A and B are hi + lo and every product is three, hi hi + hi lo + lo hi: 3e-7 to 3e-6 off, as in fp32 arithmetic.
+// of X, A and B are hi + lo and every product is three, hi hi + hi lo + lo hi: 3e-7 to 3e-6 off, as in fp32 arithmetic.  Where one
+// direction is 1000 times all others, both are off by more: 0.22 to 0.28 % and 5e-5 to 1e-4 (fp32 arithmetic 8e-5 to 3e-4).
 // fp16's range: with powers of two s, t and u the buffers hold s X, t A and u B (see Scales).
 #include "gemm_phases.h"
 #include "train.h"
