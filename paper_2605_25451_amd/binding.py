@@ -106,6 +106,15 @@ class PipeReplayResult(C.Structure):
 
 
 
+ROTARY_MAX_AXES, WINDOW_MAX_SINKS = 4, 128
+
+
+class QkRotaryDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("n_axes", C.c_int32), ("pairs", C.c_int32 * ROTARY_MAX_AXES), ("own_frequencies", C.c_int32),
+                ("base", C.c_float), ("norm", C.c_int32), ("eps", C.c_float)]
+
+
 _lib = None
 
 
@@ -238,6 +247,20 @@ def lib() -> C.CDLL:
         l.bm_orthogonalize_scratch_bytes.argtypes = [i32] * 4
         l.bm_orthogonalize_scratch_bytes.restype = sz
         l.bm_orthogonalize.argtypes = [i32] * 4 + [vp, i32, i64, vp, i32, i64, C.POINTER(f32), i32, f32, vp, sz, vp]
+        rd = C.POINTER(QkRotaryDesc)
+        l.bm_qk_rotary_forward.argtypes = [rd, i32, vp, vp, i32, vp, vp, vp, vp, vp, i32, vp]
+        l.bm_qk_rotary_backward_scratch_bytes.argtypes = [rd, i32]
+        l.bm_qk_rotary_backward.argtypes = [rd, i32, vp, vp, i32, vp, vp, vp, vp, vp, i32, vp, vp, i32, vp, vp, vp, sz, vp]
+        l.bm_window_attention_scratch_bytes.argtypes = l.bm_window_attention_backward_scratch_bytes.argtypes = [i32] * 9
+        for name in ("bm_qk_rotary_backward_scratch_bytes", "bm_window_attention_scratch_bytes",
+                     "bm_window_attention_backward_scratch_bytes"):
+            getattr(l, name).restype = sz
+        l.bm_window_attention_forward.argtypes = [i32] * 6 + [vp, i32, vp, vp, i32] + [vp] * 6 + [i32, vp, vp, vp, sz, vp]
+        l.bm_window_attention_backward.argtypes = ([i32] * 6 + [vp, i32, vp, vp, i32, vp, vp, vp] + [vp] * 6 +
+                                                   [i32, vp, i32, vp, vp, i32, vp, sz, vp])
+        for name in ("bm_qk_rotary_forward", "bm_qk_rotary_backward", "bm_window_attention_forward",
+                     "bm_window_attention_backward"):
+            getattr(l, name).restype = i32
         for name in ("bm_embedding_forward", "bm_embedding_backward", "bm_cross_entropy", "bm_orthogonalize"):
             getattr(l, name).restype = C.c_int
         _lib = l
@@ -521,6 +544,63 @@ def orthogonalize(dtype, batch, M, N, grad, ld_g, stride_g, out, ld_o, stride_o,
     c = None if coefficients is None else (C.c_float * 3)(*coefficients)
     _check(lib().bm_orthogonalize(dtype, batch, M, N, _ptr(grad), ld_g, stride_g, _ptr(out), ld_o, stride_o, c, steps,
                                   eps, _ptr(scratch), scratch_bytes, _stream() if stream is None else stream))
+
+
+def make_qk_rotary_desc(dtype, n_q_heads, n_kv_heads, head_dim, pairs, base, own_frequencies=False, norm=False,
+                        eps=1e-6) -> QkRotaryDesc:
+    """pairs: rotation pairs of every axis; more axes than the struct holds are left for the library to refuse."""
+    shown = list(pairs)[:ROTARY_MAX_AXES]
+    return QkRotaryDesc(dtype, n_q_heads, n_kv_heads, head_dim, len(pairs), (C.c_int32 * ROTARY_MAX_AXES)(*shown),
+                        int(own_frequencies), base, int(norm), eps)
+
+
+def qk_rotary_forward(desc, T, q, k, ld, positions, q_gain, k_gain, q_out, k_out, ld_out, stream=None):
+    _check(lib().bm_qk_rotary_forward(C.byref(desc), T, _ptr(q), _ptr(k), ld, _ptr(positions), _ptr(q_gain), _ptr(k_gain),
+                                      _ptr(q_out), _ptr(k_out), ld_out, _stream() if stream is None else stream))
+
+
+def qk_rotary_backward_scratch_bytes(desc, T) -> int:
+    return lib().bm_qk_rotary_backward_scratch_bytes(C.byref(desc), T)
+
+
+def qk_rotary_backward(desc, T, q, k, ld, positions, q_gain, k_gain, dq_out, dk_out, ld_dout, dq, dk, ld_dqk, dq_gain, dk_gain,
+                       scratch=None, scratch_bytes=0, stream=None):
+    _check(lib().bm_qk_rotary_backward(C.byref(desc), T, _ptr(q), _ptr(k), ld, _ptr(positions), _ptr(q_gain), _ptr(k_gain),
+                                       _ptr(dq_out), _ptr(dk_out), ld_dout, _ptr(dq), _ptr(dk), ld_dqk, _ptr(dq_gain),
+                                       _ptr(dk_gain), _ptr(scratch), scratch_bytes, _stream() if stream is None else stream))
+
+
+def window_attention_scratch_bytes(dtype, window, sinks, Hq, Hkv, dh, S, Tq, Tk) -> int:
+    return lib().bm_window_attention_scratch_bytes(dtype, window, sinks, Hq, Hkv, dh, S, Tq, Tk)
+
+
+def window_attention_backward_scratch_bytes(dtype, window, sinks, Hq, Hkv, dh, S, Tq, Tk) -> int:
+    return lib().bm_window_attention_backward_scratch_bytes(dtype, window, sinks, Hq, Hkv, dh, S, Tq, Tk)
+
+
+def _host_offsets(*arrays):
+    kept = [None if a is None else _host_cu(a) for a in arrays]
+    return kept, [None if a is None else a.ctypes.data for a in kept]
+
+
+def window_attention_forward(dtype, window, sinks, Hq, Hkv, dh, q, ld_q, k, v, ld_kv, cu_q_dev, cu_q_host, k_begin_dev,
+                             k_end_dev, k_begin_host, k_end_host, S, o, lse, scratch=None, scratch_bytes=0, stream=None):
+    """The four key arrays are None where keys have the queries' packing."""
+    kept, (cq, kb, ke) = _host_offsets(cu_q_host, k_begin_host, k_end_host)
+    _check(lib().bm_window_attention_forward(dtype, window, sinks, Hq, Hkv, dh, _ptr(q), ld_q, _ptr(k), _ptr(v), ld_kv,
+                                             _ptr(cu_q_dev), cq, _ptr(k_begin_dev), _ptr(k_end_dev), kb, ke, S, _ptr(o),
+                                             _ptr(lse), _ptr(scratch), scratch_bytes,
+                                             _stream() if stream is None else stream))
+
+
+def window_attention_backward(dtype, window, sinks, Hq, Hkv, dh, q, ld_q, k, v, ld_kv, o, d_o, lse, cu_q_dev, cu_q_host,
+                              k_begin_dev, k_end_dev, k_begin_host, k_end_host, S, dq, ld_dq, dk, dv, ld_dkv, scratch,
+                              scratch_bytes, stream=None):
+    kept, (cq, kb, ke) = _host_offsets(cu_q_host, k_begin_host, k_end_host)
+    _check(lib().bm_window_attention_backward(dtype, window, sinks, Hq, Hkv, dh, _ptr(q), ld_q, _ptr(k), _ptr(v), ld_kv,
+                                              _ptr(o), _ptr(d_o), _ptr(lse), _ptr(cu_q_dev), cq, _ptr(k_begin_dev),
+                                              _ptr(k_end_dev), kb, ke, S, _ptr(dq), ld_dq, _ptr(dk), _ptr(dv), ld_dkv,
+                                              _ptr(scratch), scratch_bytes, _stream() if stream is None else stream))
 
 
 def probe_mfma(blocks, iters, out, stream=None):

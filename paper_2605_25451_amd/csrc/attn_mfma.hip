@@ -226,13 +226,15 @@ struct SeqOrder {
 // a tile loops over (its running time).  sorted = false keeps the pack order: under a causal mask
 // a pack has tiles of every length whatever the order, and the long sequences' tiles all running at
 // once measured slower (their operands no longer fit the L2 of an XCD together).
-SeqOrder make_seq_order(const int32_t* cu_tiles, const int32_t* cu_cost, int S, int rows, bool sorted) {
+// (end: where the sequences end, when rows may lie between them.)
+SeqOrder make_seq_order(const int32_t* cu_tiles, const int32_t* cu_cost, int S, int rows, bool sorted, const int32_t* end = nullptr) {
+  if (!end) end = cu_tiles + 1;
   SeqOrder o;
   o.n = 0;
   for (int i = 0; i < 64; ++i) o.w[i] = 0;          // unused positions: sequence 0, no tile
   if (S < 1 || S > 64) return o;
   for (int s = 0; s < S; ++s)
-    if ((cu_tiles[s + 1] - cu_tiles[s] + rows - 1) / rows >= (1 << 24)) return o;
+    if ((end[s] - cu_tiles[s] + rows - 1) / rows >= (1 << 24)) return o;
   unsigned char idx[64];
   for (int i = 0; i < S; ++i) idx[i] = (unsigned char)i;
   // stable insertion sort by descending length
@@ -245,7 +247,7 @@ SeqOrder make_seq_order(const int32_t* cu_tiles, const int32_t* cu_cost, int S, 
   }
   o.n = (S + 15) / 16 * 16;
   for (int i = 0; i < S; ++i) {
-    const int nt = (cu_tiles[idx[i] + 1] - cu_tiles[idx[i]] + rows - 1) / rows;
+    const int nt = (end[idx[i]] - cu_tiles[idx[i]] + rows - 1) / rows;
     o.w[i] = ((uint32_t)nt << 8) | idx[i];
   }
   return o;
@@ -286,6 +288,54 @@ __device__ inline bool find_tile(const int32_t* __restrict__ cu, const SeqOrder&
   return false;
 }
 
+// the same where rows may lie between the sequences
+__device__ inline bool find_tile(const int32_t* __restrict__ begin, const int32_t* __restrict__ end, const SeqOrder& ord, int S,
+                                 int rows, int id, int* seq, int* tile, int* ntiles) {
+  if (ord.n) return find_tile(begin, ord, S, rows, id, seq, tile, ntiles);
+  for (int s = 0; s < S; ++s) {
+    const int nt = (end[s] - begin[s] + rows - 1) / rows;
+    if (id < nt) { *seq = s; *tile = nt - 1 - id; *ntiles = nt; return true; }
+    id -= nt;
+  }
+  return false;
+}
+
+// Sliding window (LocalMask): the key tiles of FKT rows that a tile of query rows walks -- those of the first tokens, then
+// those from its first query's window to its last query.  Queries stand at `off` + their row.
+template <int FKT>
+struct KeyWalk {
+  int sinks, near, n;                // tiles of first tokens in front of the window, the window's first tile, tiles in all
+  __device__ inline KeyWalk(const LocalMask& w, int off, int q0, int rows, int Lk) {
+    const int kend = min(Lk, off + q0 + rows);
+    near = max(0, off + q0 - w.window + 1) / FKT;
+    sinks = min((min(w.sinks, kend) + FKT - 1) / FKT, near);
+    n = (kend + FKT - 1) / FKT + sinks - near;
+  }
+  __device__ inline int tile(int t) const { return t >= sinks ? t - sinks + near : t; }
+};
+// every tile from the first one on
+template <int FKT>
+struct AllKeys {
+  int n;
+  __device__ inline AllKeys(bool causal, int q0, int rows, int Lk) {
+    const int kend = causal ? min(Lk, q0 + rows) : Lk;
+    n = (kend + FKT - 1) / FKT;
+  }
+  __device__ inline int tile(int t) const { return t; }
+};
+// all of the keys key0 .. key0 + n - 1 visible to all of the queries at a .. a + m - 1; none to any of them
+__device__ inline bool all_visible(const LocalMask& w, int key0, int n, int a, int m) {
+  return key0 + n - 1 <= a && (a + m - 1 - key0 < w.window || key0 + n <= w.sinks);
+}
+__device__ inline bool none_visible(const LocalMask& w, int key0, int n, int a, int m) {
+  return key0 > a + m - 1 || (a - (key0 + n - 1) >= w.window && key0 >= w.sinks);
+}
+__device__ inline bool hidden(const LocalMask& w, int key, int at) {
+  return key > at || (at - key >= w.window && key >= w.sinks);
+}
+// the running maximum before the first visible key: finite, so that masked scores (-inf) of a first tile give 0
+constexpr float NO_MAX = -3e38f;
+
 // Linear workgroup id -> (tile id, head).  Heads vary fastest, and since workgroup
 // ids go round-robin over the 8 XCDs, head index i lands on XCD i%8: give XCD x
 // the consecutive heads x*(H/8).., so every tile of one head -- and the q heads of
@@ -303,12 +353,12 @@ constexpr int NUM_CU = 256;
 constexpr int FQ = 128;   // query rows per workgroup (32 per wavefront)
 constexpr int FK = 64;    // keys per step
 
-template <int DH, bool CAUSAL>
+template <int DH, bool CAUSAL, bool WINDOW>
 __global__ __launch_bounds__(256, 2) void fa_fwd_kernel(
     const bf16_t* __restrict__ q, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v, int ld,
     int ldk, const int32_t* __restrict__ cu, const int32_t* __restrict__ cuk, int S,
     bf16_t* __restrict__ o, int ldo, float* __restrict__ lse, int Ttot, int Hq, int group,
-    float scale_log2, SeqOrder ord) {
+    float scale_log2, SeqOrder ord, LocalMask w) {
   // K and V tiles are double-buffered: tile kt+1 streams into LDS while tile kt is consumed
   constexpr int TILE = FK * HeadDim<DH>::DHL;
   __shared__ __attribute__((aligned(1024))) bf16_t Kbuf[2 * TILE];
@@ -319,7 +369,7 @@ __global__ __launch_bounds__(256, 2) void fa_fwd_kernel(
   const int hk = hq / group;
   const int lo = cu[seq], L = cu[seq + 1] - lo;
   // keys and values may be packed on their own (a chunk of a context-parallel partition)
-  const int lok = cuk[seq], Lk = cuk[seq + 1] - lok;
+  const int lok = cuk[seq], Lk = (WINDOW ? w.key_end[seq] : cuk[seq + 1]) - lok;
   const int q0 = qt * FQ;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int half = lane >> 5;
@@ -349,10 +399,14 @@ __global__ __launch_bounds__(256, 2) void fa_fwd_kernel(
   for (int j = 0; j < HeadDim<DH>::NB; ++j)
 #pragma unroll
     for (int r = 0; r < 16; ++r) oacc[j][r] = 0.f;
-  float m = -INFINITY, lsum = 0.f;
+  float m = WINDOW ? NO_MAX : -INFINITY, lsum = 0.f;
 
-  const int kend = CAUSAL ? min(Lk, q0 + FQ) : Lk;
-  const int nkt = (kend + FK - 1) / FK;
+  const int off = WINDOW ? Lk - L : 0;
+  const auto walk = [&] {
+    if constexpr (WINDOW) return KeyWalk<FK>(w, off, q0, FQ, Lk);
+    else return AllKeys<FK>(CAUSAL, q0, FQ, Lk);
+  }();
+  const int nkt = walk.n;
   const bf16_t* kbase = k + (size_t)lok * ldk + hk * DH;
   const bf16_t* vbase = v + (size_t)lok * ldk + hk * DH;
   using Tile = TileAsync<FK, DH, 256>;
@@ -364,8 +418,9 @@ __global__ __launch_bounds__(256, 2) void fa_fwd_kernel(
     Tile::zero_padding(Kbuf + b * TILE, tid);
     Tile::zero_padding(Vbuf + b * TILE, tid);
   }
-  tile.issue(kbase, ldk, Lk, Kbuf, wave_u);
-  tile.issue(vbase, ldk, Lk, Vbuf, wave_u);
+  const size_t first = WINDOW ? (size_t)walk.tile(0) * FK * ldk : 0;
+  tile.issue(kbase + first, ldk, Lk - walk.tile(0) * FK, Kbuf, wave_u);
+  tile.issue(vbase + first, ldk, Lk - walk.tile(0) * FK, Vbuf, wave_u);
   settle_compiler_loads();                 // the Q fragments (and, with them, tile 0)
 
   // The step comes in two copies, without and with the per-element mask test, each in a loop of
@@ -383,11 +438,13 @@ __global__ __launch_bounds__(256, 2) void fa_fwd_kernel(
     wait_async_tiles();
     __syncthreads();
     if (kt + 1 < nkt) {
-      const size_t next = (size_t)(kt + 1) * FK * ldk;
-      tile.issue(kbase + next, ldk, Lk - (kt + 1) * FK, Kbuf + (1 - PAR) * TILE, wave_u);
-      tile.issue(vbase + next, ldk, Lk - (kt + 1) * FK, Vbuf + (1 - PAR) * TILE, wave_u);
+      const int nt = walk.tile(kt + 1);
+      const size_t next = (size_t)nt * FK * ldk;
+      tile.issue(kbase + next, ldk, Lk - nt * FK, Kbuf + (1 - PAR) * TILE, wave_u);
+      tile.issue(vbase + next, ldk, Lk - nt * FK, Vbuf + (1 - PAR) * TILE, wave_u);
     }
-    const int key0 = kt * FK;
+    const int key0 = walk.tile(kt) * FK;
+    if (WINDOW && MASKED && none_visible(w, key0, FK, off + q0 + wave_u * 32, 32)) return;
     // S^T = K Q^T for both 32-key blocks first: the MFMAs of block 1 run while the
     // softmax arithmetic of block 0 occupies the vector unit, and the P V MFMAs of
     // block 0 run under the softmax of block 1.
@@ -416,7 +473,7 @@ __global__ __launch_bounds__(256, 2) void fa_fwd_kernel(
       for (int r = 0; r < 16; ++r) {
         if (MASKED) {
           const int key = key0 + b * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
-          if (key >= Lk || (CAUSAL && key > qpos)) sacc[b][r] = -INFINITY;
+          if (WINDOW ? hidden(w, key, off + qpos) : key >= Lk || (CAUSAL && key > qpos)) sacc[b][r] = -INFINITY;
         }
         mx = fmaxf(mx, sacc[b][r]);
       }
@@ -469,7 +526,7 @@ __global__ __launch_bounds__(256, 2) void fa_fwd_kernel(
   using P0 = std::integral_constant<int, 0>;
   using P1 = std::integral_constant<int, 1>;
   for (int kt = 0; kt < nkt; ++kt) {
-    const bool plain = kt < n_plain;
+    const bool plain = WINDOW ? all_visible(w, walk.tile(kt) * FK, FK, off + q0 + wave_u * 32, 32) : kt < n_plain;
     if (kt & 1) { if (plain) step(kt, std::false_type{}, P1{}); else step(kt, std::true_type{}, P1{}); }
     else { if (plain) step(kt, std::false_type{}, P0{}); else step(kt, std::true_type{}, P0{}); }
   }
@@ -793,9 +850,9 @@ bm_status fwd_launch(const AttnArgs& a, void* o, float* lse, hipStream_t st) {
   // a query tile runs as long as its sequence has keys
   const SeqOrder ord = make_seq_order(a.cu_host, a.kv_cu_host(), a.S, FQ, !a.causal);
 #define BM_L(C)                                                                                  \
-  hipLaunchKernelGGL((fa_fwd_kernel<DH, C>), grid, block, 0, st, (const bf16_t*)a.q,             \
+  hipLaunchKernelGGL((fa_fwd_kernel<DH, C, false>), grid, block, 0, st, (const bf16_t*)a.q,             \
                      (const bf16_t*)a.k, (const bf16_t*)a.v, a.ld_qkv, a.kv_ld(), a.cu_dev,      \
-                     a.kv_cu_dev(), a.S, (bf16_t*)o, a.Hq * a.dh, lse, a.T, a.Hq, a.Hq / a.Hkv, sl2, ord)
+                     a.kv_cu_dev(), a.S, (bf16_t*)o, a.Hq * a.dh, lse, a.T, a.Hq, a.Hq / a.Hkv, sl2, ord, a.local)
   if (a.causal) BM_L(true); else BM_L(false);
 #undef BM_L
   BM_CHECK_LAUNCH("fa_fwd");
@@ -833,16 +890,68 @@ constexpr int WIDE_KEYS = 256;  // keys per workgroup of the wide dK/dV kernel
 constexpr int BK_KEYS = 128;   // keys per workgroup in the dK/dV kernel (32 per wavefront)
 constexpr int BK_Q = 64;       // query rows per step
 
+// Sliding window: the first 128 keys of a sequence hold its first tokens, which all of its queries see.  Where that is more
+// than `rows` query rows, their tile is split into parts of so many, which leave fp32 partials,
+// [part][kv head x split][dK, dV][128][DH].
+struct FirstKeys {
+  LocalMask mask = {0, 0, nullptr};
+  int rows = 0, wgs = 0;              // query rows of a part; workgroups of the parts, in front of the key tiles'
+  float* out = nullptr;
+  SeqOrder ord = {};                  // the parts of the sequences, in pack order
+  __host__ __device__ inline int parts(int Lq) const { return mask.sinks > 0 && Lq > rows ? (Lq + rows - 1) / rows : 0; }
+};
+// which sequence's part `id` is, and which of its parts; parts number from 0 in pack order
+__device__ inline bool find_part(const FirstKeys& f, const int32_t* __restrict__ cuq, int S, int id, int* seq, int* part) {
+  int n;
+  if (f.ord.n) {
+    if (!find_tile(cuq, f.ord, S, f.rows, id, seq, part, &n)) return false;
+    *part = n - 1 - *part;                                 // (find_tile counts tiles from the last one)
+    return true;
+  }
+  for (int s = 0; s < S; ++s) {
+    n = f.parts(cuq[s + 1] - cuq[s]);
+    if (id < n) { *seq = s; *part = id; return true; }
+    id -= n;
+  }
+  return false;
+}
+// Where a workgroup of dK/dV works with it: a tile of KEYS keys, or a part of the first one, and the query rows that it walks
+struct KeyTile { int seq, kt, part, hk_gs, qlo, qhi; };
+template <int KEYS>
+__device__ inline bool find_key_tile(const FirstKeys& f, const SeqOrder& ord, const int32_t* __restrict__ cu,
+                                     const int32_t* __restrict__ cuq, int S, int heads, int block, KeyTile* t) {
+  int tile_id, n;
+  if (block < f.wgs) {
+    tile_and_head(heads, &tile_id, &t->hk_gs, block);
+    if (!find_part(f, cuq, S, tile_id, &t->seq, &n)) return false;
+    t->kt = 0;
+    t->part = tile_id;
+    t->qlo = n * f.rows;
+    t->qhi = min(cuq[t->seq + 1] - cuq[t->seq], t->qlo + f.rows);
+    return true;
+  }
+  tile_and_head(heads, &tile_id, &t->hk_gs, block - f.wgs);
+  if (!find_tile(cu, f.mask.key_end, ord, S, KEYS, tile_id, &t->seq, &t->kt, &n)) return false;
+  t->kt = n - 1 - t->kt;
+  t->part = -1;
+  const int L = f.mask.key_end[t->seq] - cu[t->seq], Lq = cuq[t->seq + 1] - cuq[t->seq], off = L - Lq;
+  const bool seen_by_all = t->kt == 0 && f.mask.sinks > 0;
+  if (seen_by_all && f.parts(Lq) > 0) return false;
+  t->qlo = max(0, t->kt * KEYS - off);
+  t->qhi = seen_by_all ? Lq : min(Lq, min((t->kt + 1) * KEYS, L) - 1 - off + f.mask.window);
+  return true;
+}
+
 // dK, dV of one 128-key tile of one kv head: walks the q heads of the group and the
 // query tiles; scores are kept as S[q, key] so that P and dS are B operands as they are.
 template <int DH> constexpr int dkdv_lds_bytes() { return 4 * BK_Q * HeadDim<DH>::DHL * 2 + 4 * BK_Q * 4; }
-template <int DH, bool CAUSAL>
+template <int DH, bool CAUSAL, bool WINDOW = false>
 __device__ inline void dkdv_tile(unsigned char* lds, int block, const bf16_t* __restrict__ q, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v, int ld,
     int ldk, const bf16_t* __restrict__ d_o, int ldo, const float* __restrict__ lse,
     const float* __restrict__ delta, const int32_t* __restrict__ cuq, const int32_t* __restrict__ cu,
     int S, bf16_t* __restrict__ dk, bf16_t* __restrict__ dv, int ldd, int Tq, int Ttot, int Hkv, int group,
     float scale, float scale_log2, int gsplit,
-    float* __restrict__ part /* [gsplit][2][Ttot][Hkv*DH] fp32 when gsplit > 1 */, SeqOrder ord) {
+    float* __restrict__ part /* [gsplit][2][Ttot][Hkv*DH] fp32 when gsplit > 1 */, SeqOrder ord, const FirstKeys& first = {}) {
   // cu, Ttot, ldk: the packing of the keys/values (and of dk, dv); cuq, Tq, ld: of the queries
   // Q and dO tiles are double-buffered and streamed into LDS (see TileAsync)
   constexpr int TILE = BK_Q * HeadDim<DH>::DHL;
@@ -854,14 +963,23 @@ __device__ inline void dkdv_tile(unsigned char* lds, int block, const bf16_t* __
   // with gsplit > 1 a workgroup takes group/gsplit of the q heads that share this kv head
   // and leaves an fp32 partial; the (kv head, q-head part) pair plays the head's role
   int hk_gs;
-  tile_and_head(Hkv * gsplit, &tile_id, &hk_gs, block);
+  KeyTile where;                                       // sliding window
+  if constexpr (WINDOW) {
+    if (!find_key_tile<BK_KEYS>(first, ord, cu, cuq, S, Hkv * gsplit, block, &where)) return;
+    hk_gs = where.hk_gs; seq = where.seq; kt = where.kt;
+  } else {
+    tile_and_head(Hkv * gsplit, &tile_id, &hk_gs, block);
+  }
   hk = hk_gs / gsplit;
   const int gs = hk_gs % gsplit;
   const int gpart = group / gsplit;
-  if (!find_tile(cu, ord, S, BK_KEYS, tile_id, &seq, &kt, &nkt)) return;
-  kt = nkt - 1 - kt;                                   // early key tiles see the most queries
-  const int lo = cu[seq], L = cu[seq + 1] - lo;
+  if constexpr (!WINDOW) {
+    if (!find_tile(cu, ord, S, BK_KEYS, tile_id, &seq, &kt, &nkt)) return;
+    kt = nkt - 1 - kt;                                   // early key tiles see the most queries
+  }
+  const int lo = cu[seq], L = (WINDOW ? first.mask.key_end[seq] : cu[seq + 1]) - lo;
   const int loq = cuq[seq], Lq = cuq[seq + 1] - loq;
+  const int off = WINDOW ? L - Lq : 0;
   const int kb0 = kt * BK_KEYS;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
   const int kpos = kb0 + wave * 32 + (lane & 31);       // this lane's key (column of S)
@@ -886,8 +1004,8 @@ __device__ inline void dkdv_tile(unsigned char* lds, int block, const bf16_t* __
 #pragma unroll
     for (int r = 0; r < 16; ++r) { dkacc[j][r] = 0.f; dvacc[j][r] = 0.f; }
 
-  const int qstart = CAUSAL ? (kb0 / BK_Q) * BK_Q : 0;
-  const int nqt = Lq > qstart ? (Lq - qstart + BK_Q - 1) / BK_Q : 0;   // no query: dk = dv = 0
+  const int qstart = CAUSAL ? ((WINDOW ? where.qlo : kb0) / BK_Q) * BK_Q : 0, qend = WINDOW ? where.qhi : Lq;
+  const int nqt = qend > qstart ? (qend - qstart + BK_Q - 1) / BK_Q : 0;   // no query: dk = dv = 0
   const int iters = nqt * gpart;
   using Tile = TileAsync<BK_Q, DH, 256>;
   Tile tq, td;
@@ -979,7 +1097,7 @@ __device__ inline void dkdv_tile(unsigned char* lds, int block, const bf16_t* __
           float p = __builtin_amdgcn_exp2f(fmaf(sacc[qb][r], scale_log2, -l4[e]));
           if (MASKED) {
             const int qi = q0 + qoff + e;
-            if (qi >= Lq || kpos >= L || (CAUSAL && kpos > qi)) p = 0.f;
+            if (qi >= qend || kpos >= L || (WINDOW ? hidden(first.mask, kpos, off + qi) : CAUSAL && kpos > qi)) p = 0.f;
           }
           sacc[qb][r] = p;
           dpacc[qb][r] = FOLD_DELTA ? p * dpacc[qb][r] : p * (dpacc[qb][r] - d4[e]);
@@ -1023,15 +1141,22 @@ __device__ inline void dkdv_tile(unsigned char* lds, int block, const bf16_t* __
     const int n_front = CAUSAL ? min(nqt, (wave * 32 + 32 + BK_Q - 1) / BK_Q) : 0;
     const int n_whole = max(n_front, (Lq - qstart) % BK_Q ? nqt - 1 : nqt);
     for (int it = 0, t = 0; it < iters; ++it, t = (t + 1 == nqt ? 0 : t + 1)) {
-      const bool masked = all_masked || t < n_front || t >= n_whole;
+      const int q0 = qstart + t * BK_Q;
+      const bool masked = WINDOW ? all_masked || q0 + BK_Q > qend || !all_visible(first.mask, kb0 + wave_u * 32, 32, off + q0, BK_Q)
+                                 : all_masked || t < n_front || t >= n_whole;
       if (it & 1) { if (masked) step(it, std::true_type{}, P1{}); else step(it, std::false_type{}, P1{}); }
       else { if (masked) step(it, std::true_type{}, P0{}); else step(it, std::false_type{}, P0{}); }
     }
   }
-  if (kpos < L && gsplit > 1) {
+  const bool leaves_part = WINDOW && where.part >= 0;
+  if (kpos < L && (gsplit > 1 || leaves_part)) {
     const size_t plane = (size_t)Ttot * Hkv * DH;
     float* pk = part + ((size_t)gs * 2 + 0) * plane + (size_t)(lo + kpos) * (Hkv * DH) + hk * DH;
     float* pv = part + ((size_t)gs * 2 + 1) * plane + (size_t)(lo + kpos) * (Hkv * DH) + hk * DH;
+    if (leaves_part) {
+      pk = first.out + (((size_t)where.part * (Hkv * gsplit) + hk_gs) * 2 * BK_KEYS + kpos) * DH;
+      pv = pk + BK_KEYS * DH;
+    }
 #pragma unroll
     for (int j = 0; j < HeadDim<DH>::NB; ++j)
 #pragma unroll
@@ -1074,14 +1199,14 @@ __device__ inline void dkdv_tile(unsigned char* lds, int block, const bf16_t* __
 // bf16 in the operand layout: role 0 feeds exactly these values to its own MFMAs, and role 1
 // owns the same (key, query) elements in the same lanes, so the exchange is lane-private.
 template <int DH> constexpr int dkdv_pair_lds_bytes() { return 4 * BK_Q * HeadDim<DH>::DHL * 2 + 4 * (BK_Q / 32) * 2 * 64 * 16 + 4 * BK_Q * 4; }
-template <int DH, bool CAUSAL>
+template <int DH, bool CAUSAL, bool WINDOW = false>
 __device__ inline void dkdv_pair_tile(
     unsigned char* lds, int block, const bf16_t* __restrict__ q, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v, int ld,
     int ldk, const bf16_t* __restrict__ d_o, int ldo, const float* __restrict__ lse,
     const float* __restrict__ delta, const int32_t* __restrict__ cuq, const int32_t* __restrict__ cu,
     int S, bf16_t* __restrict__ dk, bf16_t* __restrict__ dv, int ldd, int Tq, int Ttot, int Hkv, int group,
     float scale, float scale_log2, int gsplit,
-    float* __restrict__ part /* [gsplit][2][Ttot][Hkv*DH] fp32 when gsplit > 1 */, SeqOrder ord) {
+    float* __restrict__ part /* [gsplit][2][Ttot][Hkv*DH] fp32 when gsplit > 1 */, SeqOrder ord, const FirstKeys& first = {}) {
   constexpr int DHL = HeadDim<DH>::DHL, KS = HeadDim<DH>::KS, NB = HeadDim<DH>::NB, NQB = BK_Q / 32;
   // Q and dO tiles are double-buffered and streamed into LDS (see TileAsync): with one workgroup
   // per CU nothing else runs while a tile is parked between two barriers
@@ -1094,14 +1219,23 @@ __device__ inline void dkdv_pair_tile(
   float* const Dlbuf = Lbuf + 2 * BK_Q;
   bf16_t* const Dbuf = reinterpret_cast<bf16_t*>(Dlbuf + 2 * BK_Q);
   int seq, kt, nkt, tile_id, hk, hk_gs;
-  tile_and_head(Hkv * gsplit, &tile_id, &hk_gs, block);
+  KeyTile where;                                       // sliding window
+  if constexpr (WINDOW) {
+    if (!find_key_tile<BK_KEYS>(first, ord, cu, cuq, S, Hkv * gsplit, block, &where)) return;
+    hk_gs = where.hk_gs; seq = where.seq; kt = where.kt;
+  } else {
+    tile_and_head(Hkv * gsplit, &tile_id, &hk_gs, block);
+  }
   hk = hk_gs / gsplit;
   const int gs = hk_gs % gsplit;
   const int gpart = group / gsplit;
-  if (!find_tile(cu, ord, S, BK_KEYS, tile_id, &seq, &kt, &nkt)) return;
-  kt = nkt - 1 - kt;                                   // early key tiles see the most queries
-  const int lo = cu[seq], L = cu[seq + 1] - lo;
+  if constexpr (!WINDOW) {
+    if (!find_tile(cu, ord, S, BK_KEYS, tile_id, &seq, &kt, &nkt)) return;
+    kt = nkt - 1 - kt;                                   // early key tiles see the most queries
+  }
+  const int lo = cu[seq], L = (WINDOW ? first.mask.key_end[seq] : cu[seq + 1]) - lo;
   const int loq = cuq[seq], Lq = cuq[seq + 1] - loq;
+  const int off = WINDOW ? L - Lq : 0;
   const int kb0 = kt * BK_KEYS;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
   const int kb = wave & 3, role = wave >> 2;            // wavefronts w and w+4 share a SIMD
@@ -1122,8 +1256,8 @@ __device__ inline void dkdv_pair_tile(
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
 
-  const int qstart = CAUSAL ? (kb0 / BK_Q) * BK_Q : 0;
-  const int nqt = Lq > qstart ? (Lq - qstart + BK_Q - 1) / BK_Q : 0;   // no query: dk = dv = 0
+  const int qstart = CAUSAL ? ((WINDOW ? where.qlo : kb0) / BK_Q) * BK_Q : 0, qend = WINDOW ? where.qhi : Lq;
+  const int nqt = qend > qstart ? (qend - qstart + BK_Q - 1) / BK_Q : 0;   // no query: dk = dv = 0
   const int iters = nqt * gpart;
   // role 0's wavefronts bring in the Q tile, role 1's the dO tile; lse and delta of the tile's
   // queries pass through registers of the first wavefront
@@ -1196,7 +1330,7 @@ __device__ inline void dkdv_pair_tile(
             float p = __builtin_amdgcn_exp2f(fmaf(xacc[qb][r], scale_log2, -l4[e]));
             if (MASKED) {
               const int qi = q0 + qoff + e;
-              if (qi >= Lq || kpos >= L || (CAUSAL && kpos > qi)) p = 0.f;
+              if (qi >= qend || kpos >= L || (WINDOW ? hidden(first.mask, kpos, off + qi) : CAUSAL && kpos > qi)) p = 0.f;
             }
             xacc[qb][r] = p;
           }
@@ -1259,12 +1393,17 @@ __device__ inline void dkdv_pair_tile(
     const int n_front = CAUSAL ? min(nqt, (kb * 32 + 32 + BK_Q - 1) / BK_Q) : 0;
     const int n_whole = max(n_front, (Lq - qstart) % BK_Q ? nqt - 1 : nqt);
     for (int it = 0, t = 0; it < iters; ++it, t = (t + 1 == nqt ? 0 : t + 1))
-      step_of(it, all_masked || t < n_front || t >= n_whole);
+      step_of(it, WINDOW ? all_masked || qstart + (t + 1) * BK_Q > qend ||
+                               !all_visible(first.mask, kb0 + wave_r * 32, 32, off + qstart + t * BK_Q, BK_Q)
+                         : all_masked || t < n_front || t >= n_whole);
   }
   const float out_scale = role == 0 ? 1.0f : scale;     // dV as it is, dK times the softmax scale
-  if (kpos < L && gsplit > 1) {
+  const bool leaves_part = WINDOW && where.part >= 0;
+  if (kpos < L && (gsplit > 1 || leaves_part)) {
     const size_t plane = (size_t)Ttot * Hkv * DH;
     float* pp = part + ((size_t)gs * 2 + (role == 0 ? 1 : 0)) * plane + (size_t)(lo + kpos) * (Hkv * DH) + hk * DH;
+    if (leaves_part)
+      pp = first.out + ((((size_t)where.part * (Hkv * gsplit) + hk_gs) * 2 + (role == 0 ? 1 : 0)) * BK_KEYS + kpos) * DH;
 #pragma unroll
     for (int j = 0; j < NB; ++j)
 #pragma unroll
@@ -1575,12 +1714,12 @@ __device__ inline void dkdv_wide_tile(
 // dQ of one 128-row query tile of one q head: walks the key tiles, scores kept as
 // S^T[key, q] as in the forward kernel.
 template <int DH> constexpr int dq_lds_bytes() { return 4 * (DH > 72 ? 32 : FK) * HeadDim<DH>::DHL * 2; }
-template <int DH, bool CAUSAL>
+template <int DH, bool CAUSAL, bool WINDOW = false>
 __device__ inline void dq_tile(unsigned char* lds, int tid, int tile_id, int hq, bool live, const bf16_t* __restrict__ q, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v, int ld,
     int ldk, const bf16_t* __restrict__ d_o, int ldo, const float* __restrict__ lse,
     const float* __restrict__ delta, const int32_t* __restrict__ cu, const int32_t* __restrict__ cuk,
     int S, bf16_t* __restrict__ dq, int ldd, int Ttot, int group, float scale, float scale_log2,
-    SeqOrder ord) {
+    SeqOrder ord, LocalMask w = {0, 0, nullptr}) {
   // K and V tiles are double-buffered and streamed into LDS as in the forward kernel; Q and dO of
   // this wavefront's 32 queries stay in registers.  At head size 128 a step is one 32-key block:
   // with two blocks' fragments and masks in flight next to Q, dO and the dQ accumulator the
@@ -1594,7 +1733,7 @@ __device__ inline void dq_tile(unsigned char* lds, int tid, int tile_id, int hq,
   if (!find_tile(cu, ord, S, FQ, tile_id, &seq, &qt, &nqt)) return;
   const int hk = hq / group;
   const int lo = cu[seq], L = cu[seq + 1] - lo;
-  const int lok = cuk[seq], Lk = cuk[seq + 1] - lok;
+  const int lok = cuk[seq], Lk = (WINDOW ? w.key_end[seq] : cuk[seq + 1]) - lok;
   const int q0 = qt * FQ;
   const int lane = tid & 63, wave = tid >> 6, half = lane >> 5;
   const int qpos = q0 + wave * 32 + (lane & 31);
@@ -1629,8 +1768,12 @@ __device__ inline void dq_tile(unsigned char* lds, int tid, int tile_id, int hq,
 #pragma unroll
     for (int r = 0; r < 16; ++r) dqacc[j][r] = 0.f;
 
-  const int kend = CAUSAL ? min(Lk, q0 + FQ) : Lk;
-  const int nkt = (kend + FKD - 1) / FKD;
+  const int off = WINDOW ? Lk - L : 0;
+  const auto walk = [&] {
+    if constexpr (WINDOW) return KeyWalk<FKD>(w, off, q0, FQ, Lk);
+    else return AllKeys<FKD>(CAUSAL, q0, FQ, Lk);
+  }();
+  const int nkt = walk.n;
   const bf16_t* kbase = k + (size_t)lok * ldk + hk * DH;
   const bf16_t* vbase = v + (size_t)lok * ldk + hk * DH;
   using Tile = TileAsync<FKD, DH, 256>;
@@ -1642,8 +1785,9 @@ __device__ inline void dq_tile(unsigned char* lds, int tid, int tile_id, int hq,
     Tile::zero_padding(Kbuf + b * TILE, tid);
     Tile::zero_padding(Vbuf + b * TILE, tid);
   }
-  tile.issue(kbase, ldk, Lk, Kbuf, wave_u);
-  tile.issue(vbase, ldk, Lk, Vbuf, wave_u);
+  const size_t first = WINDOW ? (size_t)walk.tile(0) * FKD * ldk : 0;
+  tile.issue(kbase + first, ldk, Lk - walk.tile(0) * FKD, Kbuf, wave_u);
+  tile.issue(vbase + first, ldk, Lk - walk.tile(0) * FKD, Vbuf, wave_u);
   settle_compiler_loads();                 // the Q and dO fragments, lse, delta (and, with them, tile 0)
   // two copies of the step, without and with the mask test, as in the forward kernel
   constexpr bool FOLD_DELTA = DH <= 64;      // dP accumulators start at -delta: the MFMAs leave dP - delta
@@ -1659,11 +1803,13 @@ __device__ inline void dq_tile(unsigned char* lds, int tid, int tile_id, int hq,
     wait_async_tiles();
     __syncthreads();      // tile kt is there for everyone, and everyone is done with tile kt-1
     if (kt + 1 < nkt) {
-      const size_t next = (size_t)(kt + 1) * FKD * ldk;
-      tile.issue(kbase + next, ldk, Lk - (kt + 1) * FKD, Kbuf + (1 - PAR) * TILE, wave_u);
-      tile.issue(vbase + next, ldk, Lk - (kt + 1) * FKD, Vbuf + (1 - PAR) * TILE, wave_u);
+      const int nt = walk.tile(kt + 1);
+      const size_t next = (size_t)nt * FKD * ldk;
+      tile.issue(kbase + next, ldk, Lk - nt * FKD, Kbuf + (1 - PAR) * TILE, wave_u);
+      tile.issue(vbase + next, ldk, Lk - nt * FKD, Vbuf + (1 - PAR) * TILE, wave_u);
     }
-    const int key0 = kt * FKD;
+    const int key0 = walk.tile(kt) * FKD;
+    if (WINDOW && MASKED && none_visible(w, key0, FKD, off + q0 + wave_u * 32, 32)) return;
     // S^T = K Q^T and dP^T = V dO^T of BP 32-key blocks are issued before any softmax arithmetic,
     // so that one block's MFMAs run under the other's vector work; at head size 128 that is one
     // block at a time (two sets of accumulators do not fit next to two resident wavefronts).
@@ -1701,7 +1847,7 @@ __device__ inline void dq_tile(unsigned char* lds, int tid, int tile_id, int hq,
           float p = __builtin_amdgcn_exp2f(fmaf(sacc[bi][r], scale_log2, -my_lse));
           if (MASKED) {
             const int key = key0 + b * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
-            if (key >= Lk || (CAUSAL && key > qpos)) p = 0.f;
+            if (WINDOW ? hidden(w, key, off + qpos) : key >= Lk || (CAUSAL && key > qpos)) p = 0.f;
           }
           dpacc[bi][r] = FOLD_DELTA ? p * dpacc[bi][r] : p * (dpacc[bi][r] - my_delta);
         }
@@ -1732,7 +1878,7 @@ __device__ inline void dq_tile(unsigned char* lds, int tid, int tile_id, int hq,
   using P0 = std::integral_constant<int, 0>;
   using P1 = std::integral_constant<int, 1>;
   for (int kt = 0; kt < nkt; ++kt) {
-    const bool plain = kt < n_plain;
+    const bool plain = WINDOW ? all_visible(w, walk.tile(kt) * FKD, FKD, off + q0 + wave_u * 32, 32) : kt < n_plain;
     if (kt & 1) { if (plain) step(kt, std::false_type{}, P1{}); else step(kt, std::true_type{}, P1{}); }
     else { if (plain) step(kt, std::false_type{}, P0{}); else step(kt, std::true_type{}, P0{}); }
   }
@@ -2140,7 +2286,190 @@ bm_status bwd_launch(const AttnArgs& a, const void* o, const void* d_o, const fl
   return BM_OK;
 }
 
+// =============================================================================
+// sliding window: the kernels above with WINDOW, and what joins the parts of first keys
+// =============================================================================
+template <int DH>
+__global__ __launch_bounds__(DH <= 64 ? 256 : 512, 2) void fa_window_dkdv_kernel(
+    const bf16_t* __restrict__ q, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v, int ld, int ldk,
+    const bf16_t* __restrict__ d_o, int ldo, const float* __restrict__ lse, const float* __restrict__ delta,
+    const int32_t* __restrict__ cuq, const int32_t* __restrict__ cuk, int S, bf16_t* __restrict__ dk, bf16_t* __restrict__ dv,
+    int ldd, int Tq, int Tk, int Hkv, int group, float scale, float scale_log2, int gsplit, float* __restrict__ part, SeqOrder ord,
+    FirstKeys first) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[DH <= 64 ? dkdv_lds_bytes<DH>() : dkdv_pair_lds_bytes<DH>()];
+  if constexpr (DH <= 64)
+    dkdv_tile<DH, true, true>(lds, blockIdx.x, q, k, v, ld, ldk, d_o, ldo, lse, delta, cuq, cuk, S, dk, dv, ldd, Tq, Tk, Hkv, group,
+                              scale, scale_log2, gsplit, part, ord, first);
+  else
+    dkdv_pair_tile<DH, true, true>(lds, blockIdx.x, q, k, v, ld, ldk, d_o, ldo, lse, delta, cuq, cuk, S, dk, dv, ldd, Tq, Tk, Hkv,
+                                   group, scale, scale_log2, gsplit, part, ord, first);
+}
+
+template <int DH>
+__global__ __launch_bounds__(256, 2) void fa_window_dq_kernel(
+    const bf16_t* __restrict__ q, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v, int ld, int ldk,
+    const bf16_t* __restrict__ d_o, int ldo, const float* __restrict__ lse, const float* __restrict__ delta,
+    const int32_t* __restrict__ cu, const int32_t* __restrict__ cuk, int S, bf16_t* __restrict__ dq, int ldd, int Ttot, int Hq,
+    int group, float scale, float scale_log2, SeqOrder ord, LocalMask w) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[dq_lds_bytes<DH>()];
+  int tile, head;
+  tile_and_head(Hq, &tile, &head, blockIdx.x);
+  dq_tile<DH, true, true>(lds, threadIdx.x, tile, head, true, q, k, v, ld, ldk, d_o, ldo, lse, delta, cu, cuk, S, dq, ldd, Ttot,
+                          group, scale, scale_log2, ord, w);
+}
+
+// dk, dv of the key tiles that were left in fp32 -- parts of the first keys, q-head parts of any -- summed in order and
+// rounded once.  grid: x the key tiles (all of them, or with one q-head part the first ones), y kv heads, z 16 rows.
+__global__ __launch_bounds__(256) void fa_window_reduce_kernel(
+    const float* __restrict__ part, int gsplit, const int32_t* __restrict__ cuq, const int32_t* __restrict__ cuk, int S, int Ttot,
+    int Hkv, int dh, bf16_t* __restrict__ dk, bf16_t* __restrict__ dv, int ldd, int all_tiles, SeqOrder ord, FirstKeys first) {
+  __shared__ int before;
+  int seq = blockIdx.x, kt = 0, nkt;
+  if (all_tiles) {
+    if (!find_tile(cuk, first.mask.key_end, ord, S, BK_KEYS, blockIdx.x, &seq, &kt, &nkt)) return;
+    kt = nkt - 1 - kt;
+  }
+  const int parts = kt == 0 ? first.parts(cuq[seq + 1] - cuq[seq]) : 0;
+  if (!all_tiles && parts == 0) return;
+  const int lo = cuk[seq], L = first.mask.key_end[seq] - lo, hk = blockIdx.y;
+  const float* src;
+  size_t step_gs, step_part, row_stride, which_stride;
+  int n = 1;
+  if (parts > 0) {
+    if (threadIdx.x == 0) before = 0;
+    __syncthreads();
+    int mine = 0;
+    for (int s = threadIdx.x; s < seq; s += 256) mine += first.parts(cuq[s + 1] - cuq[s]);
+    if (mine) atomicAdd(&before, mine);                    // (whole numbers: any order)
+    __syncthreads();
+    n = parts;
+    which_stride = (size_t)BK_KEYS * dh;
+    step_gs = 2 * which_stride;
+    step_part = step_gs * Hkv * gsplit;
+    row_stride = dh;
+    src = first.out + before * step_part + (size_t)hk * gsplit * step_gs;
+  } else {
+    which_stride = (size_t)Ttot * Hkv * dh;
+    step_gs = 2 * which_stride;
+    step_part = 0;
+    row_stride = (size_t)Hkv * dh;
+    src = part + (size_t)(lo + kt * BK_KEYS) * row_stride + hk * dh;
+  }
+  const int row0 = blockIdx.z * 16, rows = min(16, L - kt * BK_KEYS - row0), quads = dh / 4;
+  for (int i = threadIdx.x; i < 2 * rows * quads; i += 256) {
+    const int c = i % quads * 4, r = i / quads % rows, which = i / quads / rows;
+    const float* p = src + which * which_stride + (size_t)(row0 + r) * row_stride + c;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < n; ++j)
+      for (int g = 0; g < gsplit; ++g) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(p + j * step_part + g * step_gs);
+        s[0] += v[0]; s[1] += v[1]; s[2] += v[2]; s[3] += v[3];
+      }
+    const bf16x4 w = {(bf16_t)s[0], (bf16_t)s[1], (bf16_t)s[2], (bf16_t)s[3]};
+    *reinterpret_cast<bf16x4*>((which == 0 ? dk : dv) + (size_t)(lo + kt * BK_KEYS + row0 + r) * ldd + hk * dh + c) = w;
+  }
+}
+
+int count_tiles(const int32_t* begin, const int32_t* end, int S, int rows) {
+  long n = 0;
+  for (int s = 0; s < S; ++s) n += (end[s] - begin[s] + rows - 1) / rows;
+  return (int)n;
+}
+
+template <int DH>
+bm_status window_fwd_launch(const AttnArgs& a, void* o, float* lse, hipStream_t st) {
+  const dim3 grid(count_tiles(a.cu_host, a.S, FQ) * a.Hq);
+  if (grid.x == 0) return BM_OK;
+  const SeqOrder ord = make_seq_order(a.cu_host, a.kv_cu_host(), a.S, FQ, false);
+  hipLaunchKernelGGL((fa_fwd_kernel<DH, true, true>), grid, dim3(256), 0, st, (const bf16_t*)a.q, (const bf16_t*)a.k,
+                     (const bf16_t*)a.v, a.ld_qkv, a.kv_ld(), a.cu_dev, a.kv_cu_dev(), a.S, (bf16_t*)o, a.Hq * a.dh, lse, a.T,
+                     a.Hq, a.Hq / a.Hkv, LOG2E / sqrtf((float)a.dh), ord, a.local);
+  BM_CHECK_LAUNCH("fa_window_fwd");
+  return BM_OK;
+}
+
+// What the backward pass of a window takes as workspace, by sizes that do not depend on single lengths
+struct WindowBwd {
+  int gsplit, part_rows;
+  long parts;                          // at most
+  size_t delta, split, first;          // floats of the three pieces
+};
+WindowBwd window_bwd(int window, int sinks, int Hq, int Hkv, int dh, int S, int Tq, int Tk) {
+  WindowBwd w;
+  const int tiles = cdiv(Tk, BK_KEYS) > S ? cdiv(Tk, BK_KEYS) : S;
+  w.gsplit = dkdv_group_split(tiles, Hkv, Hq / Hkv);
+  // parts of the first keys about as long as the tiles of other keys
+  const int rows = (int)align_up(window < 4096 ? window : 4096, BK_Q);
+  w.part_rows = rows < 512 ? 512 : rows;
+  w.parts = sinks > 0 ? 2L * Tq / w.part_rows : 0;         // a sequence that is split has more rows than one part
+  w.delta = align_up((size_t)Hq * Tq, 64);
+  w.split = w.gsplit > 1 ? (size_t)w.gsplit * 2 * Tk * Hkv * dh : 0;
+  w.first = (size_t)w.parts * Hkv * w.gsplit * 2 * BK_KEYS * dh;
+  return w;
+}
+
+template <int DH>
+bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, const float* lse, void* dq, void* dk, void* dv,
+                            int ldd, float* delta, hipStream_t st) {
+  const int ldo = a.Hq * a.dh, Tk = a.kv_T(), group = a.Hq / a.Hkv;
+  const float scale = 1.0f / sqrtf((float)a.dh), sl2 = scale * LOG2E;
+  const WindowBwd wb = window_bwd(a.local.window, a.local.sinks, a.Hq, a.Hkv, a.dh, a.S, a.T, Tk);
+  float* part = delta + wb.delta;
+  FirstKeys first;
+  first.mask = a.local;
+  first.rows = wb.part_rows;
+  first.out = part + wb.split;
+  long parts = 0;
+  for (int s = 0; s < a.S; ++s) parts += first.parts(a.cu_host[s + 1] - a.cu_host[s]);
+  first.wgs = (int)parts * a.Hkv * wb.gsplit;
+  first.ord = make_seq_order(a.cu_host, a.cu_host, a.S, wb.part_rows, false);
+  for (int i = 0; i < first.ord.n && i < a.S; ++i)
+    first.ord.w[i] = (uint32_t)first.parts(a.cu_host[i + 1] - a.cu_host[i]) << 8 | (uint32_t)i;
+  if (a.T > 0)
+    hipLaunchKernelGGL((fa_delta_kernel<DH>), dim3(cdiv((long)a.T * a.Hq * DeltaLanes<DH>::N, 256)), dim3(256), 0, st,
+                       (const bf16_t*)o, (const bf16_t*)d_o, ldo, delta, a.T, a.Hq);
+  const int ktiles = count_tiles(a.kv_cu_host(), a.key_end_host, a.S, BK_KEYS);
+  const SeqOrder ord_kv = make_seq_order(a.kv_cu_host(), a.cu_host, a.S, BK_KEYS, false, a.key_end_host);
+  const int kv_wgs = first.wgs + ktiles * a.Hkv * wb.gsplit;
+  if (kv_wgs > 0)
+    hipLaunchKernelGGL((fa_window_dkdv_kernel<DH>), dim3(kv_wgs), dim3(DH <= 64 ? 256 : 512), 0, st, (const bf16_t*)a.q,
+                       (const bf16_t*)a.k, (const bf16_t*)a.v, a.ld_qkv, a.kv_ld(), (const bf16_t*)d_o, ldo, lse,
+                       (const float*)delta, a.cu_dev, a.kv_cu_dev(), a.S, (bf16_t*)dk, (bf16_t*)dv, a.ld_dkv, a.T, Tk, a.Hkv, group,
+                       scale, sl2, wb.gsplit, part, ord_kv, first);
+  const int q_wgs = count_tiles(a.cu_host, a.S, FQ) * a.Hq;
+  const SeqOrder ord_q = make_seq_order(a.cu_host, a.cu_host, a.S, FQ, false);
+  if (q_wgs > 0)
+    hipLaunchKernelGGL((fa_window_dq_kernel<DH>), dim3(q_wgs), dim3(256), 0, st, (const bf16_t*)a.q, (const bf16_t*)a.k,
+                       (const bf16_t*)a.v, a.ld_qkv, a.kv_ld(), (const bf16_t*)d_o, ldo, lse, (const float*)delta, a.cu_dev,
+                       a.kv_cu_dev(), a.S, (bf16_t*)dq, ldd, a.T, a.Hq, group, scale, sl2, ord_q, a.local);
+  const int all_tiles = wb.gsplit > 1;
+  if (kv_wgs > 0 && (all_tiles || parts > 0))
+    hipLaunchKernelGGL(fa_window_reduce_kernel, dim3(all_tiles ? ktiles : a.S, a.Hkv, BK_KEYS / 16), dim3(256), 0, st, part,
+                       wb.gsplit, a.cu_dev, a.kv_cu_dev(), a.S, Tk, a.Hkv, a.dh, (bf16_t*)dk, (bf16_t*)dv, a.ld_dkv, all_tiles,
+                       ord_kv, first);
+  BM_CHECK_LAUNCH("fa_window_bwd");
+  return BM_OK;
+}
+
 }  // namespace
+
+size_t window_backward_mfma_scratch_bytes(int window, int sinks, int Hq, int Hkv, int dh, int S, int Tq, int Tk) {
+  const WindowBwd w = window_bwd(window, sinks, Hq, Hkv, dh, S, Tq, Tk);
+  return align_up((w.delta + w.split + w.first) * sizeof(float), 256);
+}
+
+bm_status window_forward_mfma(const AttnArgs& a, void* o, float* lse, hipStream_t st) {
+  if (a.dh == 128) return window_fwd_launch<128>(a, o, lse, st);
+  if (a.dh == 72) return window_fwd_launch<72>(a, o, lse, st);
+  return window_fwd_launch<64>(a, o, lse, st);
+}
+
+bm_status window_backward_mfma(const AttnArgs& a, const void* o, const void* d_o, const float* lse, void* dq, void* dk,
+                               void* dv, int ld_dq, void* scratch, hipStream_t st) {
+  if (a.dh == 128) return window_bwd_launch<128>(a, o, d_o, lse, dq, dk, dv, ld_dq, (float*)scratch, st);
+  if (a.dh == 72) return window_bwd_launch<72>(a, o, d_o, lse, dq, dk, dv, ld_dq, (float*)scratch, st);
+  return window_bwd_launch<64>(a, o, d_o, lse, dq, dk, dv, ld_dq, (float*)scratch, st);
+}
 
 bool attention_mfma_supported(const AttnArgs& a) {
   return a.dtype == BM_DTYPE_BF16 && (a.dh == 64 || a.dh == 72 || a.dh == 128) && a.ld_qkv % 8 == 0 &&

@@ -321,6 +321,12 @@ bm_status gemm_mfma(int layout, int M, int N, int K, const void* A, int lda, con
                     hipStream_t st);
 
 // ---------------------------------------------------------------- attention
+// Sliding window (window > 0, with causal): query i of a sequence, at position p = (keys - queries) + i, sees key j <= p
+// with p - j < window or j < sinks.  Key rows of sequence s: cu_k[s] .. key_end[s]-1.
+struct LocalMask {
+  int window, sinks;
+  const int32_t* key_end;      // dev
+};
 struct AttnArgs {
   int dtype, causal, Hq, Hkv, dh;
   const void *q, *k, *v;   // row stride ld_qkv elements
@@ -338,6 +344,8 @@ struct AttnArgs {
   // backward: a gradient lies in memory that an input takes up (set by attention_backward).  dK/dV and dQ tiles then do not
   // run side by side: either would read what the other has already overwritten.
   bool in_place = false;
+  LocalMask local = {0, 0, nullptr};
+  const int32_t* key_end_host = nullptr;    // with local
   const int32_t* kv_cu_dev() const { return cu_k_dev ? cu_k_dev : cu_dev; }
   const int32_t* kv_cu_host() const { return cu_k_dev ? cu_k_host : cu_host; }
   int kv_T() const { return cu_k_dev ? Tk : T; }
