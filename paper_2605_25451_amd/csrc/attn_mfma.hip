@@ -20,6 +20,7 @@
 // each recomputing P from the saved log-sum-exp: every output element has one
 // owner, so there are no floating-point atomics and results are reproducible.
 #include "common.h"
+#include "attn_window.h"
 
 #include <type_traits>
 
@@ -300,19 +301,6 @@ __device__ inline bool find_tile(const int32_t* __restrict__ begin, const int32_
   return false;
 }
 
-// Sliding window (LocalMask): the key tiles of FKT rows that a tile of query rows walks -- those of the first tokens, then
-// those from its first query's window to its last query.  Queries stand at `off` + their row.
-template <int FKT>
-struct KeyWalk {
-  int sinks, near, n;                // tiles of first tokens in front of the window, the window's first tile, tiles in all
-  __device__ inline KeyWalk(const LocalMask& w, int off, int q0, int rows, int Lk) {
-    const int kend = min(Lk, off + q0 + rows);
-    near = max(0, off + q0 - w.window + 1) / FKT;
-    sinks = min((min(w.sinks, kend) + FKT - 1) / FKT, near);
-    n = (kend + FKT - 1) / FKT + sinks - near;
-  }
-  __device__ inline int tile(int t) const { return t >= sinks ? t - sinks + near : t; }
-};
 // every tile from the first one on
 template <int FKT>
 struct AllKeys {
@@ -330,12 +318,6 @@ __device__ inline bool all_visible(const LocalMask& w, int key0, int n, int a, i
 __device__ inline bool none_visible(const LocalMask& w, int key0, int n, int a, int m) {
   return key0 > a + m - 1 || (a - (key0 + n - 1) >= w.window && key0 >= w.sinks);
 }
-__device__ inline bool hidden(const LocalMask& w, int key, int at) {
-  return key > at || (at - key >= w.window && key >= w.sinks);
-}
-// the running maximum before the first visible key: finite, so that masked scores (-inf) of a first tile give 0
-constexpr float NO_MAX = -3e38f;
-
 // Linear workgroup id -> (tile id, head).  Heads vary fastest, and since workgroup
 // ids go round-robin over the 8 XCDs, head index i lands on XCD i%8: give XCD x
 // the consecutive heads x*(H/8).., so every tile of one head -- and the q heads of
@@ -2388,6 +2370,161 @@ bm_status window_fwd_launch(const AttnArgs& a, void* o, float* lse, hipStream_t 
   return BM_OK;
 }
 
+// Few queries of a sequence (rows x heads of a group <= 32) behind long key lists: a workgroup takes a part of the keys of one
+// sequence and kv head, its four wavefronts a quarter of it each.  The rows -- token by token, head by head of the group -- are the
+// 32 columns of S^T, so K and V are read once for the whole group.  Each wavefront streams its own tiles of 32 keys through its own
+// ring in LDS, without a barrier; the four meet in LDS at the end, the parts of a sequence in window_join_kernel.
+// Bound by reading K and V.
+template <int DH> constexpr int token_ring() { return DH == 64 ? 4 : DH == 72 ? 3 : 2; }
+template <int DH>
+__global__ __launch_bounds__(256, 1) void fa_window_token_kernel(
+    const bf16_t* __restrict__ q, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v, int ld, int ldk,
+    const int32_t* __restrict__ cu, const int32_t* __restrict__ cuk, int S, bf16_t* __restrict__ o, int ldo,
+    float* __restrict__ lse, int Ttot, int Hkv, int group, float scale_log2, LocalMask w, TokenSplit split) {
+  constexpr int DHL = HeadDim<DH>::DHL, KS = HeadDim<DH>::KS, NB = HeadDim<DH>::NB, TILE = TOKEN_KEYS * DHL;
+  constexpr int RING = token_ring<DH>(), OS = DH + 4;        // OS: row stride of what a wavefront leaves
+  using Tile = TileAsync<TOKEN_KEYS, DH, 64>;
+  static_assert(RING * 2 * TILE * 2 >= 32 * OS * 4, "a wavefront's sums take its ring's place");
+  __shared__ __attribute__((aligned(1024))) bf16_t ring[4 * RING * 2 * TILE];
+  __shared__ float stats[4][32][2];
+  const int hk = blockIdx.x % Hkv, slot = blockIdx.x / Hkv;
+  int seq, part, nparts;
+  if (!find_token_part(split, w, cu, cuk, S, slot, &seq, &part, &nparts)) return;
+  const int lo = cu[seq], L = cu[seq + 1] - lo, lok = cuk[seq], Lk = w.key_end[seq] - lok, off = Lk - L;
+  const KeyWalk<TOKEN_KEYS> walk(w, off, 0, L, Lk);
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int first = part * split.per, last = min(walk.n, first + split.per), share = (last - first + 3) / 4;
+  const int t0 = first + wave * share, t1 = min(last, t0 + share), n = t1 - t0;   // this wavefront's tiles (n <= 0: none)
+  const int rows = L * group, row = min(lane & 31, rows - 1), at = off + row / group;
+  bf16_t* const mine = ring + wave * (RING * 2 * TILE);
+  bf16x8 qf[KS];
+  {
+    const bf16_t* qp = q + (size_t)(lo + row / group) * ld + (hk * group + row % group) * DH;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = load_chunk<DH>(qp, ks * 2 + half);
+  }
+  Tile tile;
+  tile.init(ldk, lane);
+#pragma unroll
+  for (int b = 0; b < 2 * RING; ++b) Tile::zero_padding(mine + b * TILE, lane);
+  const bf16_t* kbase = k + (size_t)lok * ldk + hk * DH;
+  const bf16_t* vbase = v + (size_t)lok * ldk + hk * DH;
+  settle_compiler_loads();                                 // Q, offsets
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the padding
+  auto fetch = [&](int i, int place) {                     // this wavefront's tile i: 2 * Tile::CH loads
+    const int key0 = walk.tile(t0 + i) * TOKEN_KEYS;
+    bf16_t* dst = mine + place * 2 * TILE;
+    tile.issue(kbase + (size_t)key0 * ldk, ldk, Lk - key0, dst, 0);
+    tile.issue(vbase + (size_t)key0 * ldk, ldk, Lk - key0, dst + TILE, 0);
+  };
+  f32x16 oacc[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) oacc[j] = f32x16{};
+  float m = NO_MAX, lsum = 0.f;
+#pragma unroll
+  for (int i = 0; i < RING - 1; ++i)
+    if (i < n) fetch(i, i);
+  int place = 0;                                           // i % RING
+  for (int i = 0; i < n; ++i) {
+    // the place of tile i - 1 is free: its reads are done
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (i + RING - 1 < n) {
+      fetch(i + RING - 1, place == 0 ? RING - 1 : place - 1);
+      // all but the RING - 1 younger tiles have landed
+      asm volatile("s_waitcnt vmcnt(%0)" :: "n"((RING - 1) * 2 * Tile::CH) : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    const bf16_t* Ks = mine + place * 2 * TILE;
+    const bf16_t* Vs = Ks + TILE;
+    f32x16 sacc = {};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const bf16x8 f = frag_rows<DHL>(Ks, 0, ks, lane);
+      sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[ks], sacc, 0, 0, 0);
+    }
+    const int key0 = walk.tile(t0 + i) * TOKEN_KEYS;
+    if (!all_visible(w, key0, TOKEN_KEYS, off, L))
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (hidden(w, key0 + (r >> 2) * 8 + half * 4 + (r & 3), at)) sacc[r] = -INFINITY;
+    float mx = sacc[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sacc[r]);
+    mx = max_with_other_half(mx) * scale_log2;
+    if (__builtin_amdgcn_ballot_w64(mx > m + 8.0f) != 0) {  // lazy rescaling, as in fa_fwd_kernel
+      const float m_new = fmaxf(m, mx), corr = __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      lsum *= corr;
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[j][r] *= corr;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      sacc[r] = __builtin_amdgcn_exp2f(fmaf(sacc[r], scale_log2, -m));
+      lsum += sacc[r];
+    }
+    const bf16x8 p0 = acc_to_operand(sacc, 0), p1 = acc_to_operand(sacc, 1);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      oacc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DHL>(Vs, j * 32, 0, lane), p0, oacc[j], 0, 0, 0);
+      oacc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DHL>(Vs, j * 32, 16, lane), p1, oacc[j], 0, 0, 0);
+    }
+    place = place + 1 == RING ? 0 : place + 1;
+  }
+  lsum = sum_with_other_half(lsum);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  float* const sums = reinterpret_cast<float*>(mine);
+  if ((lane & 31) < rows) {
+    if (half == 0) { stats[wave][lane & 31][0] = m; stats[wave][lane & 31][1] = lsum; }
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        if (DH % 32 == 0 || j * 32 + g * 8 + half * 4 < DH)
+          *reinterpret_cast<f32x4*>(sums + (lane & 31) * OS + j * 32 + g * 8 + half * 4) =
+              f32x4{oacc[j][g * 4], oacc[j][g * 4 + 1], oacc[j][g * 4 + 2], oacc[j][g * 4 + 3]};
+  }
+  __syncthreads();
+  const float* all = reinterpret_cast<const float*>(ring);
+  constexpr int WSTRIDE = RING * TILE;                     // floats between the wavefronts' sums
+  for (int e = tid; e < rows * DH; e += 256) {
+    const int r = e / DH, c = e % DH;
+    float top = NO_MAX;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) top = fmaxf(top, stats[x][r][0]);
+    float sum = 0.f, val = 0.f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float f = __builtin_amdgcn_exp2f(stats[x][r][0] - top);
+      sum = fmaf(f, stats[x][r][1], sum);
+      val = fmaf(f, all[x * WSTRIDE + r * OS + c], val);
+    }
+    const int t = lo + r / group, h = hk * group + r % group;
+    if (nparts == 1) {
+      o[(size_t)t * ldo + h * DH + c] = (bf16_t)(val / sum);
+      if (c == 0) lse[(size_t)h * Ttot + t] = (top + log2f(sum)) * LN2;
+    } else {
+      split.sums[((size_t)blockIdx.x * split.rows + r) * DH + c] = val;
+      if (c == 0) {
+        split.stats[((size_t)blockIdx.x * split.rows + r) * 2] = top;
+        split.stats[((size_t)blockIdx.x * split.rows + r) * 2 + 1] = sum;
+      }
+    }
+  }
+}
+
+template <int DH>
+bm_status window_token_launch(const AttnArgs& a, const TokenSplit& split, void* o, float* lse, hipStream_t st) {
+  hipLaunchKernelGGL((fa_window_token_kernel<DH>), dim3(split.wgs), dim3(256), 0, st, (const bf16_t*)a.q, (const bf16_t*)a.k,
+                     (const bf16_t*)a.v, a.ld_qkv, a.kv_ld(), a.cu_dev, a.kv_cu_dev(), a.S, (bf16_t*)o, a.Hq * a.dh, lse, a.T, a.Hkv,
+                     a.Hq / a.Hkv, LOG2E / sqrtf((float)a.dh), a.local, split);
+  BM_CHECK_LAUNCH("fa_window_token");
+  return BM_OK;
+}
+
 // What the backward pass of a window takes as workspace, by sizes that do not depend on single lengths
 struct WindowBwd {
   int gsplit, part_rows;
@@ -2462,6 +2599,12 @@ bm_status window_forward_mfma(const AttnArgs& a, void* o, float* lse, hipStream_
   if (a.dh == 128) return window_fwd_launch<128>(a, o, lse, st);
   if (a.dh == 72) return window_fwd_launch<72>(a, o, lse, st);
   return window_fwd_launch<64>(a, o, lse, st);
+}
+
+bm_status window_tokens_mfma(const AttnArgs& a, const TokenSplit& split, void* o, float* lse, hipStream_t st) {
+  if (a.dh == 128) return window_token_launch<128>(a, split, o, lse, st);
+  if (a.dh == 72) return window_token_launch<72>(a, split, o, lse, st);
+  return window_token_launch<64>(a, split, o, lse, st);
 }
 
 bm_status window_backward_mfma(const AttnArgs& a, const void* o, const void* d_o, const float* lse, void* dq, void* dk,

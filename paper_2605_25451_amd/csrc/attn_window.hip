@@ -1,6 +1,6 @@
-// Entry points of attention with a sliding window and first tokens that stay visible: argument checks, and the choice
-// between the matrix-core kernels and those in plain fp32 arithmetic.
-#include "common.h"
+// Attention with a sliding window and first tokens that stay visible: entry points, argument checks, the choice between the
+// matrix-core kernels and those in plain fp32 arithmetic, and few queries in the latter.
+#include "attn_window.h"
 #include "../../include/bigmac_window_attention.h"
 
 #include <algorithm>
@@ -10,10 +10,280 @@ namespace bm {
 bool attention_mfma_supported(const AttnArgs& a);
 size_t window_backward_mfma_scratch_bytes(int window, int sinks, int Hq, int Hkv, int dh, int S, int Tq, int Tk);
 bm_status window_forward_mfma(const AttnArgs& a, void* o, float* lse, hipStream_t st);
+bm_status window_tokens_mfma(const AttnArgs& a, const TokenSplit& split, void* o, float* lse, hipStream_t st);
 bm_status window_backward_mfma(const AttnArgs& a, const void* o, const void* d_o, const float* lse, void* dq, void* dk,
                                void* dv, int ld_dq, void* scratch, hipStream_t st);
 
 namespace {
+
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+
+template <int P> __device__ inline float lanes_sum(float v) {      // over the lanes P, 2 P, ... apart
+#pragma unroll
+  for (int off = P; off < 64; off <<= 1) v += __shfl_xor(v, off, 64);
+  return v;
+}
+
+// Few queries in plain arithmetic (fp32, small heads): a workgroup takes a part of the keys of one sequence and kv head and RB of
+// its rows (token by token, head by head of the group), a wavefront 64 keys at a time.
+//   scores: eight lanes share a key, so that they read 128 bytes of its row at once; their sums meet in the vector unit
+//   values: the lanes of a row hold 16 bytes of it each, the weights come back from LDS
+// Bound by reading K and V up to four rows.
+constexpr int RB = 4;
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void window_token_kernel(
+    const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, int ld, int ldk, const int32_t* __restrict__ cu,
+    const int32_t* __restrict__ cuk, int S, T* __restrict__ o, int ldo, float* __restrict__ lse, int Ttot, int Hkv, int group,
+    float scale_log2, LocalMask w, TokenSplit split) {
+  constexpr int VEC = Elt<T>::VEC, CH = DH / VEC, CL = (CH + 7) / 8;      // chunks of a row, of a lane
+  constexpr int LV = CH <= 1 ? 1 : CH <= 2 ? 2 : CH <= 4 ? 4 : CH <= 8 ? 8 : CH <= 16 ? 16 : 32;   // lanes of a row of values
+  constexpr int KV = 64 / LV;                                             // its rows at a time
+  __shared__ float weight[4][64][RB];
+  __shared__ float sums[4][RB][DH], stats[4][RB][2];
+  const int hk = blockIdx.x % Hkv, slot = blockIdx.x / Hkv;
+  int seq, part, nparts;
+  if (!find_token_part(split, w, cu, cuk, S, slot, &seq, &part, &nparts)) return;
+  const int lo = cu[seq], L = cu[seq + 1] - lo, lok = cuk[seq], Lk = w.key_end[seq] - lok, off = Lk - L;
+  const int rows = L * group, r0 = blockIdx.y * RB;
+  if (r0 >= rows) return;
+  const KeyWalk<TOKEN_KEYS> walk(w, off, 0, L, Lk);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int first = part * split.per, last = min(walk.n, first + split.per);
+  const int kg = lane >> 3, j = lane & 7, vg = lane / LV, vc = lane % LV;
+  float qr[RB][CL][VEC];
+  int at[RB];
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+    const int row = min(r0 + r, rows - 1);
+    at[r] = off + row / group;
+    const T* p = q + (size_t)(lo + row / group) * ld + (hk * group + row % group) * DH;
+#pragma unroll
+    for (int i = 0; i < CL; ++i) {
+      load16(p + min(j + 8 * i, CH - 1) * VEC, qr[r][i]);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) qr[r][i][e] = j + 8 * i < CH ? qr[r][i][e] * scale_log2 : 0.f;
+    }
+  }
+  float m[RB], l[RB], acc[RB][VEC];
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+    m[r] = NO_MAX; l[r] = 0.f;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) acc[r][e] = 0.f;
+  }
+  const T* kb = k + (size_t)lok * ldk + hk * DH;
+  const T* vb = v + (size_t)lok * ldk + hk * DH;
+  // 64 keys: two tiles that may lie apart (first tokens and window); past the part's last one nothing is visible
+  for (int t = first + wave * 2; t < last; t += 8) {
+    const int ka = walk.tile(t) * TOKEN_KEYS, kn = t + 1 < last ? walk.tile(t + 1) * TOKEN_KEYS : Lk;
+    auto key_of = [&](int i) { return i < TOKEN_KEYS ? ka + i : kn + i - TOKEN_KEYS; };
+    float sc[RB];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {                          // keys i * 8 + kg; lane j keeps those of i == j
+      const T* row = kb + (size_t)min(key_of(i * 8 + kg), Lk - 1) * ldk;
+      float d[RB];
+#pragma unroll
+      for (int r = 0; r < RB; ++r) d[r] = 0.f;
+#pragma unroll
+      for (int n = 0; n < CL; ++n) {
+        float x[VEC];
+        load16(row + min(j + 8 * n, CH - 1) * VEC, x);
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) d[r] = fmaf(qr[r][n][e], x[e], d[r]);
+      }
+#pragma unroll
+      for (int r = 0; r < RB; ++r) {
+        // the eight lanes: neighbours, pairs, then the two halves of eight
+        d[r] += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(d[r]), 0xB1, 0xf, 0xf, true));
+        d[r] += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(d[r]), 0x4E, 0xf, 0xf, true));
+        d[r] += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(d[r]), 0x141, 0xf, 0xf, true));
+        sc[r] = i == j ? d[r] : sc[r];
+      }
+    }
+    const int key = key_of(j * 8 + kg);
+    float p[RB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      const float x = key >= Lk || hidden(w, key, at[r]) ? -INFINITY : sc[r];
+      float mx = x;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
+      const float mn = fmaxf(m[r], mx), corr = exp2f(m[r] - mn);
+      m[r] = mn;
+      p[r] = exp2f(x - mn);
+      l[r] = l[r] * corr + p[r];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) acc[r][e] *= corr;
+    }
+    *reinterpret_cast<float4*>(weight[wave][j * 8 + kg]) = float4{p[0], p[1], p[2], p[3]};
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (a wavefront's own rows: no barrier)
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 8
+    for (int i = 0; i < 64 / KV; ++i) {
+      const int n = i * KV + vg;
+      float x[VEC];
+      load16(vb + (size_t)min(key_of(n), Lk - 1) * ldk + min(vc, CH - 1) * VEC, x);
+      const float4 f = *reinterpret_cast<const float4*>(weight[wave][n]);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        acc[0][e] = fmaf(f.x, x[e], acc[0][e]);
+        acc[1][e] = fmaf(f.y, x[e], acc[1][e]);
+        acc[2][e] = fmaf(f.z, x[e], acc[2][e]);
+        acc[3][e] = fmaf(f.w, x[e], acc[3][e]);
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+  }
+#pragma unroll
+  for (int r = 0; r < RB; ++r) {
+    l[r] = lanes_sum<1>(l[r]);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) acc[r][e] = lanes_sum<LV>(acc[r][e]);
+    if (vg == 0 && vc < CH)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sums[wave][r][vc * VEC + e] = acc[r][e];
+    if (lane == 0) { stats[wave][r][0] = m[r]; stats[wave][r][1] = l[r]; }
+  }
+  __syncthreads();
+  for (int e = tid; e < min(RB, rows - r0) * DH; e += 256) {
+    const int r = e / DH, c = e % DH, row = r0 + r;
+    float top = NO_MAX;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) top = fmaxf(top, stats[x][r][0]);
+    float sum = 0.f, val = 0.f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float f = exp2f(stats[x][r][0] - top);
+      sum = fmaf(f, stats[x][r][1], sum);
+      val = fmaf(f, sums[x][r][c], val);
+    }
+    const int t = lo + row / group, h = hk * group + row % group;
+    if (nparts == 1) {
+      o[(size_t)t * ldo + h * DH + c] = Elt<T>::from_f(val / sum);
+      if (c == 0) lse[(size_t)h * Ttot + t] = (top + log2f(sum)) * LN2;
+    } else {
+      split.sums[((size_t)blockIdx.x * split.rows + row) * DH + c] = val;
+      if (c == 0) {
+        split.stats[((size_t)blockIdx.x * split.rows + row) * 2] = top;
+        split.stats[((size_t)blockIdx.x * split.rows + row) * 2 + 1] = sum;
+      }
+    }
+  }
+}
+
+// o and lse from the parts of a sequence, in part order.  grid: x sequences, y kv heads, z rows; a thread per column.
+template <typename T>
+__global__ __launch_bounds__(128) void window_join_kernel(const int32_t* __restrict__ cu, const int32_t* __restrict__ cuk, T* __restrict__ o,
+                                                          int ldo, float* __restrict__ lse, int Ttot, int Hkv, int group, int dh,
+                                                          LocalMask w, TokenSplit split) {
+  __shared__ int before;
+  const int seq = blockIdx.x, hk = blockIdx.y, row = blockIdx.z;
+  const int lo = cu[seq], rows = (cu[seq + 1] - lo) * group, n = token_parts(split, w, cu, cuk, seq);
+  if (row >= rows || n < 2) return;
+  if (threadIdx.x == 0) before = 0;
+  __syncthreads();
+  int mine = 0;
+  for (int s = threadIdx.x; s < seq; s += 128) mine += token_parts(split, w, cu, cuk, s);
+  if (mine) atomicAdd(&before, mine);                      // (whole numbers: any order)
+  __syncthreads();
+  const int c = threadIdx.x;
+  if (c >= dh) return;
+  const size_t step = (size_t)Hkv * split.rows, at = ((size_t)before * Hkv + hk) * split.rows + row;
+  float top = NO_MAX;
+#pragma unroll 8
+  for (int i = 0; i < n; ++i) top = fmaxf(top, split.stats[(at + i * step) * 2]);
+  float sum = 0.f, val = 0.f;
+#pragma unroll 8
+  for (int i = 0; i < n; ++i) {
+    const float f = exp2f(split.stats[(at + i * step) * 2] - top);
+    sum = fmaf(f, split.stats[(at + i * step) * 2 + 1], sum);
+    val = fmaf(f, split.sums[(at + i * step) * dh + c], val);
+  }
+  const int t = lo + row / group, h = hk * group + row % group;
+  o[(size_t)t * ldo + h * dh + c] = Elt<T>::from_f(val / sum);
+  if (c == 0) lse[(size_t)h * Ttot + t] = (top + log2f(sum)) * LN2;
+}
+
+template <typename T, int DH>
+void token_launch(const AttnArgs& a, const TokenSplit& split, void* o, float* lse, hipStream_t st) {
+  hipLaunchKernelGGL((window_token_kernel<T, DH>), dim3(split.wgs, cdiv(split.rows, RB)), dim3(256), 0, st, (const T*)a.q,
+                     (const T*)a.k, (const T*)a.v, a.ld_qkv, a.kv_ld(), a.cu_dev, a.kv_cu_dev(), a.S, (T*)o, a.Hq * a.dh, lse, a.T,
+                     a.Hkv, a.Hq / a.Hkv, LOG2E / sqrtf((float)a.dh), a.local, split);
+}
+
+bool mfma_head(int dtype, int dh) { return dtype == BM_DTYPE_BF16 && (dh == 64 || dh == 72 || dh == 128); }
+
+// Workgroups that the parts of few queries come to, at most next to one per sequence and kv head
+#ifndef BM_TOKEN_WGS
+#define BM_TOKEN_WGS 1024
+#endif
+constexpr int TOKEN_WGS = BM_TOKEN_WGS, TOKEN_TILES = 8;           // ... and the tiles that a part has at least
+size_t token_slots(int Hkv, int S) { return TOKEN_WGS + (size_t)S * Hkv; }
+// rows x heads of a group that the parts have room for: 0 where some sequence must have too many
+int token_rows(int Hq, int Hkv, int S, int Tq) {
+  const long group = Hq / Hkv, most = (long)Tq * group;
+  if (group > TOKEN_ROWS || Tq > S * (TOKEN_ROWS / group)) return 0;
+  return (int)std::min<long>(most, TOKEN_ROWS);
+}
+
+bm_status window_tokens(const AttnArgs& a, void* scratch, void* o, float* lse, hipStream_t st) {
+  TokenSplit t{};
+  const int32_t *cq = a.cu_host, *kb = a.cu_k_host, *ke = a.key_end_host;
+  long tiles = 0;
+  t.per = 1;
+  for (int s = 0; s < a.S; ++s) tiles += t.count(a.local, cq[s + 1] - cq[s], ke[s] - kb[s]);
+  t.per = std::max(TOKEN_TILES, cdiv(tiles * a.Hkv, TOKEN_WGS));
+  t.rows = a.max_seqlen * (a.Hq / a.Hkv);
+  long parts = 0;
+  bool joins = false;
+  t.n = a.S <= 64 ? a.S : 0;
+  for (int s = 0; s < a.S; ++s) {
+    const int n = t.count(a.local, cq[s + 1] - cq[s], ke[s] - kb[s]);
+    if (s < 64) t.parts[s] = (uint16_t)n;                    // below 2^16: TOKEN_WGS at most
+    parts += n;
+    joins = joins || n > 1;
+  }
+  t.wgs = (int)(parts * a.Hkv);
+  t.sums = (float*)scratch;
+  t.stats = t.sums + align_up((size_t)t.wgs * t.rows * a.dh, 64);
+  if (mfma_head(a.dtype, a.dh)) {
+    BM_RETURN_IF(window_tokens_mfma(a, t, o, lse, st));
+  } else {
+#define BM_HEAD(TT)                                              \
+  switch (a.dh) {                                                \
+    case 8: token_launch<TT, 8>(a, t, o, lse, st); break;        \
+    case 16: token_launch<TT, 16>(a, t, o, lse, st); break;      \
+    default: token_launch<TT, 32>(a, t, o, lse, st);             \
+  }
+    if (a.dtype == BM_DTYPE_BF16) {
+      BM_HEAD(bf16_t)
+    } else if (a.dh == 64) {
+      token_launch<float, 64>(a, t, o, lse, st);
+    } else if (a.dh == 72) {
+      token_launch<float, 72>(a, t, o, lse, st);
+    } else if (a.dh == 128) {
+      token_launch<float, 128>(a, t, o, lse, st);
+    } else {
+      BM_HEAD(float)
+    }
+#undef BM_HEAD
+    BM_CHECK_LAUNCH("window_token");
+  }
+  if (joins) {
+    const dim3 grid(a.S, a.Hkv, t.rows), block(128);
+#define BM_L(TT)                                                                                                              \
+  hipLaunchKernelGGL(window_join_kernel<TT>, grid, block, 0, st, a.cu_dev, a.kv_cu_dev(), (TT*)o, a.Hq * a.dh, lse, a.T, a.Hkv, \
+                     a.Hq / a.Hkv, a.dh, a.local, t)
+    if (a.dtype == BM_DTYPE_BF16) BM_L(bf16_t); else BM_L(float);
+#undef BM_L
+    BM_CHECK_LAUNCH("window_join");
+  }
+  return BM_OK;
+}
 
 constexpr int MAX_ROWS = 1 << 28;        // offsets of rows stay far from 2^31
 
@@ -79,8 +349,6 @@ bm_status check_args(int dtype, int window, int sinks, int Hq, int Hkv, int dh, 
   return BM_OK;
 }
 
-bool mfma_head(int dtype, int dh) { return dtype == BM_DTYPE_BF16 && (dh == 64 || dh == 72 || dh == 128); }
-
 bm_status check_scratch(const void* scratch, size_t bytes, size_t need) {
   BM_ARG_CHECK(al16(scratch), "window attention: misaligned scratch");
   if (need > 0 && (!scratch || bytes < need)) {
@@ -99,7 +367,8 @@ using namespace bm;
 extern "C" size_t bm_window_attention_scratch_bytes(int32_t dtype, int32_t window, int32_t sinks, int32_t Hq, int32_t Hkv,
                                                     int32_t dh, int32_t S, int32_t Tq, int32_t Tk) {
   if (check_sizes(dtype, window, sinks, Hq, Hkv, dh, S) != BM_OK || Tq < 0 || Tk < 0 || Tq > MAX_ROWS || Tk > MAX_ROWS) return 0;
-  return 0;
+  const size_t rows = (size_t)token_rows(Hq, Hkv, S, Tq), slots = token_slots(Hkv, S);
+  return rows ? align_up((align_up(slots * rows * dh, 64) + slots * rows * 2) * sizeof(float), 256) : 0;
 }
 
 extern "C" bm_status bm_window_attention_forward(int32_t dtype, int32_t window, int32_t sinks, int32_t Hq, int32_t Hkv,
@@ -120,6 +389,7 @@ extern "C" bm_status bm_window_attention_forward(int32_t dtype, int32_t window, 
   a.q = q; a.k = k; a.v = v;
   hipStream_t st = (hipStream_t)hip_stream;
   ProfScope prof(PROF_ATTN_FWD, 4.0 * dh * Hq * pairs, st);
+  if (a.max_seqlen * (long)(Hq / Hkv) <= TOKEN_ROWS) return window_tokens(a, scratch, o, lse, st);
   if (mfma_head(dtype, dh)) return window_forward_mfma(a, o, lse, st);
   return attention_forward_generic(a, o, lse, st);
 }

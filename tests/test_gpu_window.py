@@ -369,6 +369,20 @@ def test_window_of_the_last_queries(case, dtype, dh):
     x.check_backward(*x.backward())
 
 
+TOKENS = [
+    (32, 1, [(1, 5000)], 4500, 100), (16, 2, [(4, 700), (1, 1), (3, 3), (2, 1500)], 1000, 33), (12, 12, [(1, 2300), (1, 40)], 2000, 1),
+    (6, 2, [(1, 100 + 31 * i) for i in range(70)], 1200, 5), (2, 1, [(1 + i % 16, 20 + i * i % 900) for i in range(66)], 64, 65)]
+
+
+@pytest.mark.parametrize("dtype,dh", HEADS + [("bf16", 8), ("fp32", 128), ("fp32", 8), ("fp32", 32)])
+@pytest.mark.parametrize("case", TOKENS, ids=lambda c: "%d-%d-%d-%d-%d" % (c[0], c[1], len(c[2]), *c[3:]))
+def test_window_of_few_queries(case, dtype, dh):
+    """Keys split over workgroups, with and without the table of the sequences' parts in the kernel's arguments."""
+    Hq, Hkv, seqs, window, sinks = case
+    x = Window(dtype, Hq, Hkv, dh, seqs, window, sinks, seed=9, gap=2)
+    x.check_forward(*x.forward())
+
+
 @pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("bf16", 72), ("bf16", 128), ("fp32", 32)])
 def test_window_in_wider_rows(dtype, dh):
     x = Window(dtype, 4, 2, dh, pack(100, 333), 50, 2, seed=2, pad=8)
