@@ -83,14 +83,16 @@ bm_status bm_qk_rotary_backward(const bm_qk_rotary_desc* desc, int32_t T, const 
  *                    between them (slots of a cache), which are neither read nor written
  *   cu_q, k_begin, k_end are given twice, in device and in host memory, with the same values
  *   o, d_o    dev    [Tq, Hq*dh], lse dev [Hq, Tq] fp32, Tq = cu_q[S]
- * S < 65536, Hq < 65536, Tq x Hq and Tk x Hkv below 2^28.  Lq <= Lk for every sequence; Lq = 0 is allowed (its dk, dv are 0), and so is Lk = 0 with it.
- * Rows of a sequence that lie 256 and more away from every key that one of its queries sees are not read by the forward
- * pass; nearer ones hold finite values (a hidden one takes part with weight 0).
+ * S < 65536, Hq < 65536, Tq x Hq and Tk x Hkv below 2^27, S x Hq below 2^23.  Lq <= Lk for every sequence; Lq = 0 is allowed (its
+ * dk, dv are 0), and so is Lk = 0 with it.
+ * The forward pass does not read keys and values that no query of the call sees: they may be anything.  A key or value that some
+ * queries see and others do not has weight 0 for the latter and is finite, in the backward pass all of them are.
  * dh is 8, 16, 32, 64, 72 or 128; q head a uses kv head a / (Hq/Hkv).  bf16 with head sizes 64, 72 and 128 runs on the
  * matrix cores, in which probabilities are rounded to bf16; everything else is fp32 arithmetic.
  * Few queries behind long key lists are split over the keys; the parts are joined in a fixed order. */
 #define BM_WINDOW_MAX_SINKS 128
-/* Tq and Tk: rows of the query and of the key buffers (Tk: the largest k_end).  0 for sizes that are refused. */
+/* Tq = cu_q[S], Tk = the largest k_end.  0 for sizes that are refused.  A size that is enough for S sequences and Tq queries
+ * is enough for fewer of either, whatever their lengths. */
 size_t    bm_window_attention_scratch_bytes(int32_t dtype, int32_t window, int32_t sinks, int32_t Hq, int32_t Hkv,
                                             int32_t dh, int32_t S, int32_t Tq, int32_t Tk);
 bm_status bm_window_attention_forward(int32_t dtype, int32_t window, int32_t sinks, int32_t Hq, int32_t Hkv, int32_t dh,
@@ -100,7 +102,7 @@ bm_status bm_window_attention_forward(int32_t dtype, int32_t window, int32_t sin
                                       const int32_t* k_begin_host, const int32_t* k_end_host, int32_t S,
                                       void* o, float* lse, void* scratch, size_t scratch_bytes, void* hip_stream);
 
-/* Gradients from d_o and the forward's q, k, v, o and lse: dq in rows of ld_dq elements, dk and dv (rows k_begin ..
+/* The scratch is that of exactly these sizes.  Gradients from d_o and the forward's q, k, v, o and lse: dq in rows of ld_dq elements, dk and dv (rows k_begin ..
  * k_end-1 of every sequence) in rows of ld_dkv; overwritten, and apart from the inputs. */
 size_t    bm_window_attention_backward_scratch_bytes(int32_t dtype, int32_t window, int32_t sinks, int32_t Hq,
                                                      int32_t Hkv, int32_t dh, int32_t S, int32_t Tq, int32_t Tk);

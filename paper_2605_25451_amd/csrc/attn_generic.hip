@@ -44,9 +44,10 @@ template <int P> __device__ inline float lanes_max(float v) {
 // 25 -> 15 / 21; 16 heads of 64 70 / 156 -> 43 / 93; 5 x 200 rows, 8 heads of 128 335 / 803 -> 156 / 373; 4 x 1024 rows, 4 heads of 32,
 // 183 / 542 -> 84 / 279.  More than four pairs at once cost registers: all 18 of head size 72 left the forward one wavefront
 // per SIMD, and it was slower than with the branches (16 x 1024 rows 923 -> 1045); by sixes 768, 5 x 200 rows of 8 heads 74 -> 40 / 326 -> 190.
+// Rows hide .. seen - 1 are not read, but row `seen` in their place.
 template <int DH, int LD, typename T>
 __device__ inline void load_tiles(const T* __restrict__ a, int lda, const T* __restrict__ b, int ldb, int r0, int rows, float scale,
-                                  float (*A)[LD], float (*B)[LD]) {
+                                  float (*A)[LD], float (*B)[LD], int hide = 0, int seen = 0) {
   constexpr int N = BT * DH / NT, U = N == 8 ? 8 : N % 4 == 0 ? 4 : N % 6 == 0 ? 6 : N;
   static_assert(BT * DH % NT == 0, "whole trips");
 #pragma unroll 1
@@ -54,7 +55,9 @@ __device__ inline void load_tiles(const T* __restrict__ a, int lda, const T* __r
     float x[U], y[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int idx = (it + u) * NT + threadIdx.x, r = min(r0 + idx / DH, rows - 1);
+      const int idx = (it + u) * NT + threadIdx.x;
+      int r = min(r0 + idx / DH, rows - 1);
+      if (seen > 0 && r >= hide) r = max(r, seen);
       x[u] = Elt<T>::to_f(a[(size_t)r * lda + idx % DH]);
       y[u] = Elt<T>::to_f(b[(size_t)r * ldb + idx % DH]);
     }
@@ -68,7 +71,7 @@ __device__ inline void load_tiles(const T* __restrict__ a, int lda, const T* __r
 }
 
 template <typename T, int DH, bool CAUSAL, int P, bool WINDOW>
-__global__ __launch_bounds__(NT) void attn_fwd_generic_kernel(
+__global__ __launch_bounds__(NT, WINDOW ? 2 : 1) void attn_fwd_generic_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, int ld, int ldk,
     const int32_t* __restrict__ cu, const int32_t* __restrict__ cuk, T* __restrict__ o, int ldo,
     float* __restrict__ lse, int Ttot, int group, float scale, LocalMask w) {
@@ -94,7 +97,8 @@ __global__ __launch_bounds__(NT) void attn_fwd_generic_kernel(
   const int kend = CAUSAL ? min(Lk, off + q0 + BQ) : Lk;
   const int near = WINDOW ? max(0, off + q0 - w.window + 1) / BT * BT : 0;   // the first tile of the window
   for (int k0 = WINDOW && w.sinks == 0 ? near : 0; k0 < kend; k0 = WINDOW && k0 + BT >= w.sinks ? max(k0 + BT, near) : k0 + BT) {
-    load_tiles<DH>(k + (size_t)lok * ldk + hk * DH, ldk, v + (size_t)lok * ldk + hk * DH, ldk, k0, Lk, 1.f, Ks, Vs);
+    load_tiles<DH>(k + (size_t)lok * ldk + hk * DH, ldk, v + (size_t)lok * ldk + hk * DH, ldk, k0, Lk, 1.f, Ks, Vs, WINDOW ? w.sinks : 0,
+                   WINDOW ? max(0, off + q0 - w.window + 1) : 0);
     __syncthreads();
     if (active) {
       float sc[BT / P];

@@ -116,6 +116,12 @@ __device__ inline bf16x8 acc_to_operand(const f32x16& a, int t) {
   return r;
 }
 
+__device__ inline const bf16_t* scalar_ptr(const void* p) {
+  const uint64_t b = reinterpret_cast<uint64_t>(p);
+  return reinterpret_cast<const bf16_t*>(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32)) << 32) |
+                                         (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b));
+}
+
 // ---- global -> LDS: a [ROWS][DH] tile brought in by NT threads -------------------
 // 16-byte loads that write LDS directly (no registers, no LDS store
 // instructions): lane l of a wavefront fills bytes [16 l, 16 l + 16) of a 1 KiB run of slots, so the
@@ -191,6 +197,25 @@ struct TileAsync {
         int row, c;
         if (place(i, &row, &c, t_op))
           load16(base, (uint32_t)min(row, rows_left - 1) * (uint32_t)ld * 2u + (uint32_t)c * 16u, dst + i * NT * 16);
+      }
+    }
+  }
+  // the same for the tile of keys from key0 on under a window: rows that no query from the one with this `begin` on sees are not
+  // read, but the last of the first tokens or the first row of the window in their place
+  __device__ inline void issue(const LocalMask& w, int begin, const bf16_t* __restrict__ keys, int ld, int key0, int Lk, bf16_t* t,
+                               int wave) const {
+    const int hidden_from = max(key0, w.sinks), instead = key0 < w.sinks ? w.sinks - 1 : begin;
+    if (begin <= hidden_from || hidden_from >= key0 + ROWS) return issue(keys + (size_t)key0 * ld, ld, Lk - key0, t, wave);
+    const bf16_t* const base = scalar_ptr(keys + (size_t)key0 * ld);
+    const uint32_t dst = (uint32_t)(size_t)(__attribute__((address_space(3))) char*)(t + wave * 512);
+    int t_op = tid_;
+    asm volatile("" : "+v"(t_op));
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      int row, c;
+      if (place(i, &row, &c, t_op)) {
+        const int j = key0 + row, from = j >= hidden_from && j < begin ? instead : min(j, Lk - 1);
+        load16(base, (uint32_t)(from - key0) * (uint32_t)ld * 2u + (uint32_t)c * 16u, dst + i * NT * 16);
       }
     }
   }
@@ -289,16 +314,11 @@ __device__ inline bool find_tile(const int32_t* __restrict__ cu, const SeqOrder&
   return false;
 }
 
-// the same where rows may lie between the sequences
+// the same where rows may lie between the sequences, and faster for packs without a table
 __device__ inline bool find_tile(const int32_t* __restrict__ begin, const int32_t* __restrict__ end, const SeqOrder& ord, int S,
                                  int rows, int id, int* seq, int* tile, int* ntiles) {
   if (ord.n) return find_tile(begin, ord, S, rows, id, seq, tile, ntiles);
-  for (int s = 0; s < S; ++s) {
-    const int nt = (end[s] - begin[s] + rows - 1) / rows;
-    if (id < nt) { *seq = s; *tile = nt - 1 - id; *ntiles = nt; return true; }
-    id -= nt;
-  }
-  return false;
+  return find_tile_by_lanes(begin, end, S, rows, id, seq, tile, ntiles);
 }
 
 // every tile from the first one on
@@ -347,7 +367,7 @@ __global__ __launch_bounds__(256, 2) void fa_fwd_kernel(
   __shared__ __attribute__((aligned(1024))) bf16_t Vbuf[2 * TILE];
   int seq, qt, nqt, tile_id, hq;
   tile_and_head(Hq, &tile_id, &hq, blockIdx.x);
-  if (!find_tile(cu, ord, S, FQ, tile_id, &seq, &qt, &nqt)) return;
+  if (WINDOW ? !find_tile(cu, cu + 1, ord, S, FQ, tile_id, &seq, &qt, &nqt) : !find_tile(cu, ord, S, FQ, tile_id, &seq, &qt, &nqt)) return;
   const int hk = hq / group;
   const int lo = cu[seq], L = cu[seq + 1] - lo;
   // keys and values may be packed on their own (a chunk of a context-parallel partition)
@@ -400,9 +420,13 @@ __global__ __launch_bounds__(256, 2) void fa_fwd_kernel(
     Tile::zero_padding(Kbuf + b * TILE, tid);
     Tile::zero_padding(Vbuf + b * TILE, tid);
   }
-  const size_t first = WINDOW ? (size_t)walk.tile(0) * FK * ldk : 0;
-  tile.issue(kbase + first, ldk, Lk - walk.tile(0) * FK, Kbuf, wave_u);
-  tile.issue(vbase + first, ldk, Lk - walk.tile(0) * FK, Vbuf, wave_u);
+  const int begin = WINDOW ? window_begin(w, off + q0) : 0;
+  auto fetch = [&](const bf16_t* base, int t, bf16_t* dst) {
+    if constexpr (WINDOW) tile.issue(w, begin, base, ldk, t * FK, Lk, dst, wave_u);
+    else tile.issue(base + (size_t)t * FK * ldk, ldk, Lk - t * FK, dst, wave_u);
+  };
+  fetch(kbase, walk.tile(0), Kbuf);
+  fetch(vbase, walk.tile(0), Vbuf);
   settle_compiler_loads();                 // the Q fragments (and, with them, tile 0)
 
   // The step comes in two copies, without and with the per-element mask test, each in a loop of
@@ -420,10 +444,8 @@ __global__ __launch_bounds__(256, 2) void fa_fwd_kernel(
     wait_async_tiles();
     __syncthreads();
     if (kt + 1 < nkt) {
-      const int nt = walk.tile(kt + 1);
-      const size_t next = (size_t)nt * FK * ldk;
-      tile.issue(kbase + next, ldk, Lk - nt * FK, Kbuf + (1 - PAR) * TILE, wave_u);
-      tile.issue(vbase + next, ldk, Lk - nt * FK, Vbuf + (1 - PAR) * TILE, wave_u);
+      fetch(kbase, walk.tile(kt + 1), Kbuf + (1 - PAR) * TILE);
+      fetch(vbase, walk.tile(kt + 1), Vbuf + (1 - PAR) * TILE);
     }
     const int key0 = walk.tile(kt) * FK;
     if (WINDOW && MASKED && none_visible(w, key0, FK, off + q0 + wave_u * 32, 32)) return;
@@ -568,12 +590,6 @@ struct RunTile {
     return u.v;
   }
 };
-
-__device__ inline const bf16_t* scalar_ptr(const void* p) {
-  const uint64_t b = reinterpret_cast<uint64_t>(p);
-  return reinterpret_cast<const bf16_t*>(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32)) << 32) |
-                                         (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b));
-}
 
 // end of a phase: this wavefront's LDS accesses are done, then the workgroup meets
 __device__ inline void phase_barrier() {
@@ -890,10 +906,17 @@ __device__ inline bool find_part(const FirstKeys& f, const int32_t* __restrict__
     *part = n - 1 - *part;                                 // (find_tile counts tiles from the last one)
     return true;
   }
-  for (int s = 0; s < S; ++s) {
-    n = f.parts(cuq[s + 1] - cuq[s]);
-    if (id < n) { *seq = s; *part = id; return true; }
-    id -= n;
+  const int lane = threadIdx.x & 63;
+  for (int s0 = 0; s0 < S; s0 += 64) {
+    const int s = min(s0 + lane, S - 1), mine = s0 + lane < S ? f.parts(cuq[s + 1] - cuq[s]) : 0, upto = scan_lanes(mine);
+    const uint64_t past = __builtin_amdgcn_ballot_w64(id < upto);
+    if (past != 0) {
+      const int l = __builtin_ctzll(past);
+      *seq = s0 + l;
+      *part = id - __builtin_amdgcn_readlane(upto - mine, l);
+      return true;
+    }
+    id -= __builtin_amdgcn_readlane(upto, 63);
   }
   return false;
 }
@@ -1712,7 +1735,7 @@ __device__ inline void dq_tile(unsigned char* lds, int tid, int tile_id, int hq,
   bf16_t* const Kbuf = reinterpret_cast<bf16_t*>(lds);
   bf16_t* const Vbuf = Kbuf + 2 * TILE;
   int seq, qt, nqt;
-  if (!find_tile(cu, ord, S, FQ, tile_id, &seq, &qt, &nqt)) return;
+  if (WINDOW ? !find_tile(cu, cu + 1, ord, S, FQ, tile_id, &seq, &qt, &nqt) : !find_tile(cu, ord, S, FQ, tile_id, &seq, &qt, &nqt)) return;
   const int hk = hq / group;
   const int lo = cu[seq], L = cu[seq + 1] - lo;
   const int lok = cuk[seq], Lk = (WINDOW ? w.key_end[seq] : cuk[seq + 1]) - lok;
@@ -2372,77 +2395,78 @@ bm_status window_fwd_launch(const AttnArgs& a, void* o, float* lse, hipStream_t 
 
 // Few queries of a sequence (rows x heads of a group <= 32) behind long key lists: a workgroup takes a part of the keys of one
 // sequence and kv head, its four wavefronts a quarter of it each.  The rows -- token by token, head by head of the group -- are the
-// 32 columns of S^T, so K and V are read once for the whole group.  Each wavefront streams its own tiles of 32 keys through its own
-// ring in LDS, without a barrier; the four meet in LDS at the end, the parts of a sequence in window_join_kernel.
+// 32 columns of S^T, so K and V are read once for the whole group.  Each wavefront streams its own tiles of 32 keys through places of
+// its own in LDS, without a barrier: the next tile's K follows as soon as this one's is in registers, its V behind the products with
+// V.  The four meet in LDS at the end, the parts of a sequence in window_join_kernel.
 // Bound by reading K and V.
-template <int DH> constexpr int token_ring() { return DH == 64 ? 4 : DH == 72 ? 3 : 2; }
+template <int DH> constexpr int token_ring() { return DH == 64 ? 2 : 1; }
 template <int DH>
-__global__ __launch_bounds__(256, 1) void fa_window_token_kernel(
+__global__ __launch_bounds__(256, 2) void fa_window_token_kernel(
     const bf16_t* __restrict__ q, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v, int ld, int ldk,
     const int32_t* __restrict__ cu, const int32_t* __restrict__ cuk, int S, bf16_t* __restrict__ o, int ldo,
     float* __restrict__ lse, int Ttot, int Hkv, int group, float scale_log2, LocalMask w, TokenSplit split) {
   constexpr int DHL = HeadDim<DH>::DHL, KS = HeadDim<DH>::KS, NB = HeadDim<DH>::NB, TILE = TOKEN_KEYS * DHL;
-  constexpr int RING = token_ring<DH>(), OS = DH + 4;        // OS: row stride of what a wavefront leaves
+  constexpr int RING = token_ring<DH>(), OS = DH == 128 ? DH : DH + 4;       // OS: row stride of what a wavefront leaves
   using Tile = TileAsync<TOKEN_KEYS, DH, 64>;
-  static_assert(RING * 2 * TILE * 2 >= 32 * OS * 4, "a wavefront's sums take its ring's place");
+  constexpr int CH = Tile::CH;                             // loads of a tile of K or V
+  static_assert(RING * 2 * TILE * 2 >= 32 * OS * 4, "a wavefront's sums take its tiles' place");
   __shared__ __attribute__((aligned(1024))) bf16_t ring[4 * RING * 2 * TILE];
   __shared__ float stats[4][32][2];
   const int hk = blockIdx.x % Hkv, slot = blockIdx.x / Hkv;
-  int seq, part, nparts;
-  if (!find_token_part(split, w, cu, cuk, S, slot, &seq, &part, &nparts)) return;
+  TokenPart where;
+  if (!find_token_part(split, S, slot, &where)) return;
+  const int seq = where.seq, nparts = where.parts;
   const int lo = cu[seq], L = cu[seq + 1] - lo, lok = cuk[seq], Lk = w.key_end[seq] - lok, off = Lk - L;
   const KeyWalk<TOKEN_KEYS> walk(w, off, 0, L, Lk);
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int first = part * split.per, last = min(walk.n, first + split.per), share = (last - first + 3) / 4;
+  const int per = (walk.n + nparts - 1) / nparts, first = where.part * per, last = min(walk.n, first + per), share = (last - first + 3) / 4;
   const int t0 = first + wave * share, t1 = min(last, t0 + share), n = t1 - t0;   // this wavefront's tiles (n <= 0: none)
-  const int rows = L * group, row = min(lane & 31, rows - 1), at = off + row / group;
+  const int rows = L * group, row = min(lane & 31, rows - 1), at = off + row / group, begin = window_begin(w, off);
   bf16_t* const mine = ring + wave * (RING * 2 * TILE);
-  bf16x8 qf[KS];
-  {
-    const bf16_t* qp = q + (size_t)(lo + row / group) * ld + (hk * group + row % group) * DH;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = load_chunk<DH>(qp, ks * 2 + half);
-  }
   Tile tile;
   tile.init(ldk, lane);
 #pragma unroll
   for (int b = 0; b < 2 * RING; ++b) Tile::zero_padding(mine + b * TILE, lane);
   const bf16_t* kbase = k + (size_t)lok * ldk + hk * DH;
   const bf16_t* vbase = v + (size_t)lok * ldk + hk * DH;
-  settle_compiler_loads();                                 // Q, offsets
+  bf16x8 qf[KS];
+  {
+    const bf16_t* qp = q + (size_t)(lo + row / group) * ld + (hk * group + row % group) * DH;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = load_chunk<DH>(qp, ks * 2 + half);
+  }
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the padding
-  auto fetch = [&](int i, int place) {                     // this wavefront's tile i: 2 * Tile::CH loads
-    const int key0 = walk.tile(t0 + i) * TOKEN_KEYS;
-    bf16_t* dst = mine + place * 2 * TILE;
-    tile.issue(kbase + (size_t)key0 * ldk, ldk, Lk - key0, dst, 0);
-    tile.issue(vbase + (size_t)key0 * ldk, ldk, Lk - key0, dst + TILE, 0);
+  // this wavefront's tile i into its place; K and V lie behind one another
+  auto fetch = [&](const bf16_t* base, int i, bf16_t* dst) {
+    tile.issue(w, begin, base, ldk, walk.tile(t0 + i) * TOKEN_KEYS, Lk, dst, 0);
   };
   f32x16 oacc[NB];
 #pragma unroll
   for (int j = 0; j < NB; ++j) oacc[j] = f32x16{};
   float m = NO_MAX, lsum = 0.f;
+  settle_compiler_loads();                                 // Q, offsets
 #pragma unroll
-  for (int i = 0; i < RING - 1; ++i)
-    if (i < n) fetch(i, i);
+  for (int i = 0; i < RING; ++i)
+    if (i < n) {
+      fetch(kbase, i, mine + i * 2 * TILE);
+      fetch(vbase, i, mine + i * 2 * TILE + TILE);
+    }
   int place = 0;                                           // i % RING
   for (int i = 0; i < n; ++i) {
-    // the place of tile i - 1 is free: its reads are done
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (i + RING - 1 < n) {
-      fetch(i + RING - 1, place == 0 ? RING - 1 : place - 1);
-      // all but the RING - 1 younger tiles have landed
-      asm volatile("s_waitcnt vmcnt(%0)" :: "n"((RING - 1) * 2 * Tile::CH) : "memory");
-    } else {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    }
-    const bf16_t* Ks = mine + place * 2 * TILE;
-    const bf16_t* Vs = Ks + TILE;
+    bf16_t* const Ks = mine + place * 2 * TILE;
+    bf16_t* const Vs = Ks + TILE;
+    // K of tile i is there: behind it only its V and the whole tiles up to i + RING - 1
+    if (RING == 2 && i + 1 < n) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(3 * CH) : "memory");
+    else asm volatile("s_waitcnt vmcnt(%0)" :: "n"(CH) : "memory");
     f32x16 sacc = {};
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const bf16x8 f = frag_rows<DHL>(Ks, 0, ks, lane);
       sacc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, qf[ks], sacc, 0, 0, 0);
     }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // K has been read: its place is free
+    const bool more = i + RING < n;
+    if (more) fetch(kbase, i + RING, Ks);
     const int key0 = walk.tile(t0 + i) * TOKEN_KEYS;
     if (!all_visible(w, key0, TOKEN_KEYS, off, L))
 #pragma unroll
@@ -2467,15 +2491,19 @@ __global__ __launch_bounds__(256, 1) void fa_window_token_kernel(
       lsum += sacc[r];
     }
     const bf16x8 p0 = acc_to_operand(sacc, 0), p1 = acc_to_operand(sacc, 1);
+    // V of tile i is there: behind it only the loads of later tiles
+    if (more) asm volatile("s_waitcnt vmcnt(%0)" :: "n"((2 * RING - 1) * CH) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
       oacc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DHL>(Vs, j * 32, 0, lane), p0, oacc[j], 0, 0, 0);
       oacc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DHL>(Vs, j * 32, 16, lane), p1, oacc[j], 0, 0, 0);
     }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // so has V
+    if (more) fetch(vbase, i + RING, Vs);
     place = place + 1 == RING ? 0 : place + 1;
   }
   lsum = sum_with_other_half(lsum);
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   float* const sums = reinterpret_cast<float*>(mine);
   if ((lane & 31) < rows) {
     if (half == 0) { stats[wave][lane & 31][0] = m; stats[wave][lane & 31][1] = lsum; }
@@ -2507,10 +2535,11 @@ __global__ __launch_bounds__(256, 1) void fa_window_token_kernel(
       o[(size_t)t * ldo + h * DH + c] = (bf16_t)(val / sum);
       if (c == 0) lse[(size_t)h * Ttot + t] = (top + log2f(sum)) * LN2;
     } else {
-      split.sums[((size_t)blockIdx.x * split.rows + r) * DH + c] = val;
+      const size_t at_row = ((size_t)where.place * Hkv + hk) * split.rows + r;
+      split.sums[at_row * DH + c] = val;
       if (c == 0) {
-        split.stats[((size_t)blockIdx.x * split.rows + r) * 2] = top;
-        split.stats[((size_t)blockIdx.x * split.rows + r) * 2 + 1] = sum;
+        split.stats[at_row * 2] = top;
+        split.stats[at_row * 2 + 1] = sum;
       }
     }
   }

@@ -42,14 +42,16 @@ __global__ __launch_bounds__(256) void window_token_kernel(
   __shared__ float weight[4][64][RB];
   __shared__ float sums[4][RB][DH], stats[4][RB][2];
   const int hk = blockIdx.x % Hkv, slot = blockIdx.x / Hkv;
-  int seq, part, nparts;
-  if (!find_token_part(split, w, cu, cuk, S, slot, &seq, &part, &nparts)) return;
+  TokenPart where;
+  if (!find_token_part(split, S, slot, &where)) return;
+  const int seq = where.seq, part = where.part, nparts = where.parts;
   const int lo = cu[seq], L = cu[seq + 1] - lo, lok = cuk[seq], Lk = w.key_end[seq] - lok, off = Lk - L;
   const int rows = L * group, r0 = blockIdx.y * RB;
   if (r0 >= rows) return;
   const KeyWalk<TOKEN_KEYS> walk(w, off, 0, L, Lk);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int first = part * split.per, last = min(walk.n, first + split.per);
+  const int per = (walk.n + nparts - 1) / nparts, first = part * per, last = min(walk.n, first + per);
+  const int begin = window_begin(w, off);
   const int kg = lane >> 3, j = lane & 7, vg = lane / LV, vc = lane % LV;
   float qr[RB][CL][VEC];
   int at[RB];
@@ -81,7 +83,7 @@ __global__ __launch_bounds__(256) void window_token_kernel(
     float sc[RB];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {                          // keys i * 8 + kg; lane j keeps those of i == j
-      const T* row = kb + (size_t)min(key_of(i * 8 + kg), Lk - 1) * ldk;
+      const T* row = kb + (size_t)min(seen_row(w, begin, key_of(i * 8 + kg)), Lk - 1) * ldk;
       float d[RB];
 #pragma unroll
       for (int r = 0; r < RB; ++r) d[r] = 0.f;
@@ -125,7 +127,7 @@ __global__ __launch_bounds__(256) void window_token_kernel(
     for (int i = 0; i < 64 / KV; ++i) {
       const int n = i * KV + vg;
       float x[VEC];
-      load16(vb + (size_t)min(key_of(n), Lk - 1) * ldk + min(vc, CH - 1) * VEC, x);
+      load16(vb + (size_t)min(seen_row(w, begin, key_of(n)), Lk - 1) * ldk + min(vc, CH - 1) * VEC, x);
       const float4 f = *reinterpret_cast<const float4*>(weight[wave][n]);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
@@ -166,42 +168,93 @@ __global__ __launch_bounds__(256) void window_token_kernel(
       o[(size_t)t * ldo + h * DH + c] = Elt<T>::from_f(val / sum);
       if (c == 0) lse[(size_t)h * Ttot + t] = (top + log2f(sum)) * LN2;
     } else {
-      split.sums[((size_t)blockIdx.x * split.rows + row) * DH + c] = val;
+      const size_t at = ((size_t)where.place * Hkv + hk) * split.rows + row;
+      split.sums[at * DH + c] = val;
       if (c == 0) {
-        split.stats[((size_t)blockIdx.x * split.rows + row) * 2] = top;
-        split.stats[((size_t)blockIdx.x * split.rows + row) * 2 + 1] = sum;
+        split.stats[at * 2] = top;
+        split.stats[at * 2 + 1] = sum;
       }
     }
   }
 }
 
-// o and lse from the parts of a sequence, in part order.  grid: x sequences, y kv heads, z rows; a thread per column.
+// Where the parts of more sequences than a table in the arguments holds begin; a workgroup for 256 sequences, which sums the
+// parts of all those in front of them for itself.
+__global__ __launch_bounds__(256) void window_map_kernel(const int32_t* __restrict__ cu, const int32_t* __restrict__ cuk, int S,
+                                                         LocalMask w, TokenSplit t) {
+  __shared__ int sums[3][4], front[3][4];
+  const int tid = threadIdx.x, wave = tid >> 6, s0 = blockIdx.x * 256, s = s0 + tid;
+  auto parts = [&](int i) { return i < S ? t.count(w, cu[i + 1] - cu[i], w.key_end[i] - cuk[i]) : 0; };
+  // parts, places and split sequences: in front of this workgroup's, then up to this thread's
+  int before[3] = {0, 0, 0};
+#pragma unroll 4
+  for (int i = tid; i < s0; i += 256) {
+    const int n = parts(i);
+    before[0] += n;
+    before[1] += n > 1 ? n : 0;
+    before[2] += n > 1;
+  }
+  const int mine = parts(s), own[3] = {mine, mine > 1 ? mine : 0, mine > 1};
+  int at[3];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    const int upto = scan_lanes(own[k]);
+    at[k] = upto - own[k];
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) before[k] += __shfl_xor(before[k], d, 64);
+    if ((tid & 63) == 63) { sums[k][wave] = upto; front[k][wave] = before[k]; }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+    for (int x = 0; x < 4; ++x) at[k] += front[k][x] + (x < wave ? sums[k][x] : 0);
+  if (s >= S) return;
+  t.map[s] = at[0];
+  if (s == S - 1) t.map[S] = at[0] + mine;
+  t.map[S + 1 + s] = at[1];
+  if (mine > 1) t.map[2 * S + 1 + at[2]] = s;
+  for (int i = 0; i < mine; ++i) t.map[3 * S + 1 + at[0] + i] = s;
+}
+
+// o and lse from the parts of a sequence, in part order: four threads share a column, each a quarter of the parts.
+// grid: x sequences of more than one part, y kv heads, z rows.
+constexpr int JOIN_COLS = 128;
 template <typename T>
-__global__ __launch_bounds__(128) void window_join_kernel(const int32_t* __restrict__ cu, const int32_t* __restrict__ cuk, T* __restrict__ o,
-                                                          int ldo, float* __restrict__ lse, int Ttot, int Hkv, int group, int dh,
-                                                          LocalMask w, TokenSplit split) {
-  __shared__ int before;
-  const int seq = blockIdx.x, hk = blockIdx.y, row = blockIdx.z;
-  const int lo = cu[seq], rows = (cu[seq + 1] - lo) * group, n = token_parts(split, w, cu, cuk, seq);
-  if (row >= rows || n < 2) return;
-  if (threadIdx.x == 0) before = 0;
-  __syncthreads();
-  int mine = 0;
-  for (int s = threadIdx.x; s < seq; s += 128) mine += token_parts(split, w, cu, cuk, s);
-  if (mine) atomicAdd(&before, mine);                      // (whole numbers: any order)
-  __syncthreads();
-  const int c = threadIdx.x;
-  if (c >= dh) return;
-  const size_t step = (size_t)Hkv * split.rows, at = ((size_t)before * Hkv + hk) * split.rows + row;
+__global__ __launch_bounds__(4 * JOIN_COLS) void window_join_kernel(const int32_t* __restrict__ cu, int S, T* __restrict__ o, int ldo,
+                                                                    float* __restrict__ lse, int Ttot, int Hkv, int group, int dh,
+                                                                    TokenSplit split) {
+  __shared__ float tops[4], sums[4], vals[3][JOIN_COLS];
+  const int hk = blockIdx.y, row = blockIdx.z;
+  const TokenPart p = split_sequence(split, S, blockIdx.x);
+  const int lo = cu[p.seq], rows = (cu[p.seq + 1] - lo) * group, n = p.parts;
+  if (row >= rows) return;
+  const int c = threadIdx.x % JOIN_COLS, quarter = threadIdx.x / JOIN_COLS, share = (n + 3) / 4;
+  const int i0 = quarter * share, i1 = min(n, i0 + share);
+  const size_t step = (size_t)Hkv * split.rows, at = ((size_t)p.place * Hkv + hk) * split.rows + row;
   float top = NO_MAX;
 #pragma unroll 8
-  for (int i = 0; i < n; ++i) top = fmaxf(top, split.stats[(at + i * step) * 2]);
+  for (int i = i0; i < i1; ++i) top = fmaxf(top, split.stats[(at + i * step) * 2]);
+  if (c == 0) tops[quarter] = top;
   float sum = 0.f, val = 0.f;
 #pragma unroll 8
-  for (int i = 0; i < n; ++i) {
+  for (int i = i0; i < i1; ++i) {
     const float f = exp2f(split.stats[(at + i * step) * 2] - top);
     sum = fmaf(f, split.stats[(at + i * step) * 2 + 1], sum);
-    val = fmaf(f, split.sums[(at + i * step) * dh + c], val);
+    val = fmaf(f, split.sums[(at + i * step) * dh + min(c, dh - 1)], val);
+  }
+  if (c == 0) sums[quarter] = sum;
+  if (quarter > 0) vals[quarter - 1][c] = val;
+  __syncthreads();
+  if (quarter > 0 || c >= dh) return;
+  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+  float f = exp2f(tops[0] - top);
+  sum = f * sums[0];
+  val *= f;
+#pragma unroll
+  for (int x = 1; x < 4; ++x) {
+    f = exp2f(tops[x] - top);
+    sum = fmaf(f, sums[x], sum);
+    val = fmaf(f, vals[x - 1][c], val);
   }
   const int t = lo + row / group, h = hk * group + row % group;
   o[(size_t)t * ldo + h * dh + c] = Elt<T>::from_f(val / sum);
@@ -217,39 +270,50 @@ void token_launch(const AttnArgs& a, const TokenSplit& split, void* o, float* ls
 
 bool mfma_head(int dtype, int dh) { return dtype == BM_DTYPE_BF16 && (dh == 64 || dh == 72 || dh == 128); }
 
-// Workgroups that the parts of few queries come to, at most next to one per sequence and kv head
-#ifndef BM_TOKEN_WGS
-#define BM_TOKEN_WGS 1024
-#endif
-constexpr int TOKEN_WGS = BM_TOKEN_WGS, TOKEN_TILES = 8;           // ... and the tiles that a part has at least
-size_t token_slots(int Hkv, int S) { return TOKEN_WGS + (size_t)S * Hkv; }
-// rows x heads of a group that the parts have room for: 0 where some sequence must have too many
-int token_rows(int Hq, int Hkv, int S, int Tq) {
-  const long group = Hq / Hkv, most = (long)Tq * group;
-  if (group > TOKEN_ROWS || Tq > S * (TOKEN_ROWS / group)) return 0;
-  return (int)std::min<long>(most, TOKEN_ROWS);
+// Workgroups that the parts of few queries come to, at most next to one per sequence and kv head, and tiles that a part may always have:
+// twice as many where the sequences alone fill the chip, so that fewer are split.  us (32 / 8 heads of 128, two workgroups to a CU), 1024 -> 2048
+// workgroups: 64 sequences of up to 4096 visible keys 175 -> 172, 256 of 1024 174 -> 193, 16 of 8192 102 both.  4 -> 8 -> 16 tiles: one sequence of
+// 8192 18.6 -> 15.7 -> 15.7, 4 of 4096 26.4 -> 24.0 -> 25.2, 55 of 300 20.8 -> 18.1 -> 12.7, 59 of 300, 16 heads of 64, 20.4 -> 19.4 -> 14.9.
+constexpr int TOKEN_WGS = 1024, TOKEN_TILES = 8, NUM_CU = 256;
+// A sequence of more than one part has at most twice as many as its tiles come to, TOKEN_WGS in all.
+constexpr size_t TOKEN_PLACES = 2 * TOKEN_WGS;
+// rows x heads of a group that the parts have room for, for any lengths of Tq queries
+int token_rows(int Hq, int Hkv, int Tq) {
+  const long group = Hq / Hkv;
+  return group > TOKEN_ROWS ? 0 : (int)std::min<long>(Tq * group, TOKEN_ROWS);
 }
+size_t token_map_ints(int S) { return S > TOKEN_TABLE ? 4 * (size_t)S + 1 + TOKEN_WGS : 0; }
 
 bm_status window_tokens(const AttnArgs& a, void* scratch, void* o, float* lse, hipStream_t st) {
   TokenSplit t{};
   const int32_t *cq = a.cu_host, *kb = a.cu_k_host, *ke = a.key_end_host;
-  long tiles = 0;
+  long tiles = 0, whole = 0;
   t.per = 1;
-  for (int s = 0; s < a.S; ++s) tiles += t.count(a.local, cq[s + 1] - cq[s], ke[s] - kb[s]);
-  t.per = std::max(TOKEN_TILES, cdiv(tiles * a.Hkv, TOKEN_WGS));
-  t.rows = a.max_seqlen * (a.Hq / a.Hkv);
-  long parts = 0;
-  bool joins = false;
-  t.n = a.S <= 64 ? a.S : 0;
   for (int s = 0; s < a.S; ++s) {
     const int n = t.count(a.local, cq[s + 1] - cq[s], ke[s] - kb[s]);
-    if (s < 64) t.parts[s] = (uint16_t)n;                    // below 2^16: TOKEN_WGS at most
+    tiles += n;
+    whole += n > 0;
+  }
+  t.per = std::max(whole * a.Hkv >= NUM_CU ? 2 * TOKEN_TILES : TOKEN_TILES, cdiv(tiles * a.Hkv, TOKEN_WGS));
+  t.rows = a.max_seqlen * (a.Hq / a.Hkv);
+  long parts = 0, places = 0;
+  int joins = 0;                     // sequences of more than one part
+  t.n = a.S <= TOKEN_TABLE ? a.S : 0;
+  for (int s = 0; s < a.S; ++s) {
+    const int n = t.count(a.local, cq[s + 1] - cq[s], ke[s] - kb[s]);
+    if (s < TOKEN_TABLE) t.parts[s] = (uint16_t)n;           // below 2^16: about TOKEN_WGS at most
     parts += n;
-    joins = joins || n > 1;
+    places += n > 1 ? n : 0;
+    joins += n > 1;
   }
   t.wgs = (int)(parts * a.Hkv);
   t.sums = (float*)scratch;
-  t.stats = t.sums + align_up((size_t)t.wgs * t.rows * a.dh, 64);
+  t.stats = t.sums + (size_t)places * a.Hkv * t.rows * a.dh;
+  t.map = (int32_t*)(t.stats + (size_t)places * a.Hkv * t.rows * 2);
+  if (!t.n) {
+    hipLaunchKernelGGL(window_map_kernel, dim3(cdiv(a.S, 256)), dim3(256), 0, st, a.cu_dev, a.kv_cu_dev(), a.S, a.local, t);
+    BM_CHECK_LAUNCH("window_map");
+  }
   if (mfma_head(a.dtype, a.dh)) {
     BM_RETURN_IF(window_tokens_mfma(a, t, o, lse, st));
   } else {
@@ -273,11 +337,11 @@ bm_status window_tokens(const AttnArgs& a, void* scratch, void* o, float* lse, h
 #undef BM_HEAD
     BM_CHECK_LAUNCH("window_token");
   }
-  if (joins) {
-    const dim3 grid(a.S, a.Hkv, t.rows), block(128);
-#define BM_L(TT)                                                                                                              \
-  hipLaunchKernelGGL(window_join_kernel<TT>, grid, block, 0, st, a.cu_dev, a.kv_cu_dev(), (TT*)o, a.Hq * a.dh, lse, a.T, a.Hkv, \
-                     a.Hq / a.Hkv, a.dh, a.local, t)
+  if (joins > 0) {
+    const dim3 grid(joins, a.Hkv, t.rows), block(4 * JOIN_COLS);
+#define BM_L(TT)                                                                                                           \
+  hipLaunchKernelGGL(window_join_kernel<TT>, grid, block, 0, st, a.cu_dev, a.S, (TT*)o, a.Hq * a.dh, lse, a.T, a.Hkv, a.Hq / a.Hkv, \
+                     a.dh, t)
     if (a.dtype == BM_DTYPE_BF16) BM_L(bf16_t); else BM_L(float);
 #undef BM_L
     BM_CHECK_LAUNCH("window_join");
@@ -285,7 +349,7 @@ bm_status window_tokens(const AttnArgs& a, void* scratch, void* o, float* lse, h
   return BM_OK;
 }
 
-constexpr int MAX_ROWS = 1 << 28;        // offsets of rows stay far from 2^31
+constexpr int MAX_ROWS = 1 << 27;        // offsets of rows stay far from 2^31
 
 bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -339,8 +403,9 @@ bm_status check_args(int dtype, int window, int sinks, int Hq, int Hkv, int dh, 
     *pairs += pairs_of(lq, lk, window, sinks);
   }
   // grids stay below 2^32 threads
-  BM_ARG_CHECK((long)c.cu_q_host[S] * Hq < (1L << 28) && (long)rows * Hkv < (1L << 28),
-               "window attention: %d queries of %d heads and %d keys of %d (rows x heads below 2^28)", c.cu_q_host[S], Hq, rows, Hkv);
+  BM_ARG_CHECK((long)c.cu_q_host[S] * Hq < (1L << 27) && (long)rows * Hkv < (1L << 27) && (long)S * Hq < (1L << 23),
+               "window attention: %d sequences, %d queries of %d heads and %d keys of %d (rows x heads below 2^27, sequences x heads below 2^23)",
+               S, c.cu_q_host[S], Hq, rows, Hkv);
   a->dtype = dtype; a->causal = 1; a->Hq = Hq; a->Hkv = Hkv; a->dh = dh;
   a->ld_qkv = ld_q; a->cu_dev = c.cu_q_dev; a->cu_host = c.cu_q_host; a->S = S; a->T = c.cu_q_host[S]; a->max_seqlen = max_q;
   a->cu_k_dev = own ? c.k_begin_dev : c.cu_q_dev; a->cu_k_host = kb; a->Tk = rows; a->ld_kv = ld_kv; a->max_klen = max_k;
@@ -367,8 +432,8 @@ using namespace bm;
 extern "C" size_t bm_window_attention_scratch_bytes(int32_t dtype, int32_t window, int32_t sinks, int32_t Hq, int32_t Hkv,
                                                     int32_t dh, int32_t S, int32_t Tq, int32_t Tk) {
   if (check_sizes(dtype, window, sinks, Hq, Hkv, dh, S) != BM_OK || Tq < 0 || Tk < 0 || Tq > MAX_ROWS || Tk > MAX_ROWS) return 0;
-  const size_t rows = (size_t)token_rows(Hq, Hkv, S, Tq), slots = token_slots(Hkv, S);
-  return rows ? align_up((align_up(slots * rows * dh, 64) + slots * rows * 2) * sizeof(float), 256) : 0;
+  const size_t rows = (size_t)token_rows(Hq, Hkv, Tq);
+  return rows ? align_up((TOKEN_PLACES * rows * (dh + 2) + token_map_ints(S)) * sizeof(float), 256) : 0;
 }
 
 extern "C" bm_status bm_window_attention_forward(int32_t dtype, int32_t window, int32_t sinks, int32_t Hq, int32_t Hkv,

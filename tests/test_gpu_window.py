@@ -371,7 +371,8 @@ def test_window_of_the_last_queries(case, dtype, dh):
 
 TOKENS = [
     (32, 1, [(1, 5000)], 4500, 100), (16, 2, [(4, 700), (1, 1), (3, 3), (2, 1500)], 1000, 33), (12, 12, [(1, 2300), (1, 40)], 2000, 1),
-    (6, 2, [(1, 100 + 31 * i) for i in range(70)], 1200, 5), (2, 1, [(1 + i % 16, 20 + i * i % 900) for i in range(66)], 64, 65)]
+    (6, 2, [(1, 100 + 31 * i) for i in range(70)], 1200, 5), (2, 1, [(1 + i % 16, 20 + i * i % 900) for i in range(66)], 64, 65),
+    (2, 2, [(i % 2, 1 + i * 37 % 700) for i in range(600)], 600, 2)]
 
 
 @pytest.mark.parametrize("dtype,dh", HEADS + [("bf16", 8), ("fp32", 128), ("fp32", 8), ("fp32", 32)])
@@ -415,15 +416,17 @@ def test_a_wide_window_is_causal_attention(dtype, dh):
     assert (host(o2) - host(o[:x.Tq])).max() <= 4 * U[dtype] * np.abs(host(o2)).max()
 
 
-@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("bf16", 128), ("fp32", 32)])
-def test_far_hidden_keys_are_not_read(dtype, dh):
-    """Infinities and NaN in rows 256 and more away from every key that a query sees, as an emptied part of a cache holds them."""
+@pytest.mark.parametrize("seqs", [[(2, 1400), (1, 900), (1, 70)], [(40, 1400), (300, 900)], [(1, 60 + 11 * i) for i in range(70)]], ids=["few", "many", "long list"])
+@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("bf16", 72), ("bf16", 128), ("fp32", 32), ("fp32", 128)])
+@pytest.mark.parametrize("window,sinks", [(40, 3), (37, 0), (65, 70)])
+def test_keys_that_no_query_sees_are_not_read(window, sinks, dtype, dh, seqs):
+    """Infinities and NaN in them, as an emptied part of a cache holds them."""
     import torch
-    x = Window(dtype, 4, 2, dh, [(2, 1400), (1, 900)], 40, 3, seed=5, gap=9)
+    x = Window(dtype, 4, 2, dh, seqs, window, sinks, seed=5, gap=9)
     o, lse = (t.clone() for t in x.forward())
-    for n, b, e in zip((2, 1), x.begin, x.end):
-        x.keep[1][b + 3 + 256:e - n - 39 - 256] = float("nan")
-        x.keep[2][b + 3 + 256:e - n - 39 - 256] = float("inf")
+    for (n, _), b, e in zip(seqs, x.begin, x.end):
+        x.keep[1][b + sinks:max(b + sinks, e - n - window + 1)] = float("nan")
+        x.keep[2][b + sinks:max(b + sinks, e - n - window + 1)] = float("inf")
     x.fwd()
     assert torch.equal(o[:x.Tq], x.o[:x.Tq]) and torch.equal(lse[:4 * x.Tq], x.lse[:4 * x.Tq])
 

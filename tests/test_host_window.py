@@ -122,6 +122,21 @@ def test_window_workspace_stays_small_for_many_short_sequences():
     assert many < 4 * 32 * 32768 + 2 * 32 * 8 * 2 * 128 * 128 * 4 + (1 << 20)
 
 
+@pytest.mark.parametrize("dtype,dh,Hq,Hkv", [(0, 128, 32, 8), (1, 64, 4, 4), (0, 16, 32, 1)])
+def test_workspace_of_more_rows_is_enough_for_fewer(dtype, dh, Hq, Hkv):
+    size = lambda S, Tq: bm.window_attention_scratch_bytes(dtype, 1024, 4, Hq, Hkv, dh, S, Tq, 100000)
+    for S in (1, 64, 65, 1000):
+        got = [size(S, Tq) for Tq in (0, 1, 2, 31, 64, 1000, 8192)]
+        assert got == sorted(got) and size(S, 8192) <= size(S + 1, 8192) and got[1] > 0
+
+
+def test_window_refuses_grids_past_32_bits():
+    S = 40000
+    one = np.arange(S + 1, dtype=np.int32)
+    call = {**CALL, "cu_q_host": one, "k_begin_host": one[:-1], "k_end_host": one[1:], "S": S, "ld_q": 1 << 15, "ld_kv": 1 << 15}
+    refused(bm.BM_ERR_INVALID_ARG, bm.window_attention_forward, *{**SIZES, "Hq": 256, "Hkv": 256, **call}.values())
+
+
 def test_window_of_no_rows():
     none = np.zeros(3, np.int32)
     call = {**CALL, "cu_q_host": none, "k_begin_host": none, "k_end_host": none}
