@@ -1203,6 +1203,16 @@ __device__ inline void dkdv_tile(unsigned char* lds, int block, const bf16_t* __
 // two are resident per SIMD and one's vector work runs under the other's MFMAs.  P travels as
 // bf16 in the operand layout: role 0 feeds exactly these values to its own MFMAs, and role 1
 // owns the same (key, query) elements in the same lanes, so the exchange is lane-private.
+// (sliding windows: dS from P in fp16 times 2^15, 2^-12 off down to probabilities of 2^-29, instead of from what bf16 leaves; dK carries
+// the factor to the end.)
+using f16x8 = __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16;
+constexpr float HANDED_SCALE = 32768.f;
+__device__ inline f16x8 handed_p(const f32x16& p, int t) {
+  f16x8 r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = (_Float16)(p[t * 8 + e] * HANDED_SCALE);
+  return r;
+}
 template <int DH> constexpr int dkdv_pair_lds_bytes() { return 4 * BK_Q * HeadDim<DH>::DHL * 2 + 4 * (BK_Q / 32) * 2 * 64 * 16 + 4 * BK_Q * 4; }
 template <int DH, bool CAUSAL, bool WINDOW = false>
 __device__ inline void dkdv_pair_tile(
@@ -1342,16 +1352,20 @@ __device__ inline void dkdv_pair_tile(
         }
         op[qb][0] = acc_to_operand(xacc[qb], 0);
         op[qb][1] = acc_to_operand(xacc[qb], 1);
-        *reinterpret_cast<bf16x8*>(my_p + (qb * 2 + 0) * 64 * 8) = op[qb][0];
-        *reinterpret_cast<bf16x8*>(my_p + (qb * 2 + 1) * 64 * 8) = op[qb][1];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if constexpr (WINDOW) *reinterpret_cast<f16x8*>(my_p + (qb * 2 + t) * 64 * 8) = handed_p(xacc[qb], t);
+          else *reinterpret_cast<bf16x8*>(my_p + (qb * 2 + t) * 64 * 8) = op[qb][t];
+        }
       }
     }
     __syncthreads();                                    // P of this step is in LDS
     if (role == 1) {
 #pragma unroll
       for (int qb = 0; qb < NQB; ++qb) {
-        const bf16x8 pa = *reinterpret_cast<const bf16x8*>(my_p + (qb * 2 + 0) * 64 * 8);
-        const bf16x8 pb = *reinterpret_cast<const bf16x8*>(my_p + (qb * 2 + 1) * 64 * 8);
+        using Handed = std::conditional_t<WINDOW, f16x8, bf16x8>;
+        const Handed pa = *reinterpret_cast<const Handed*>(my_p + (qb * 2 + 0) * 64 * 8);
+        const Handed pb = *reinterpret_cast<const Handed*>(my_p + (qb * 2 + 1) * 64 * 8);
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const f32x4 d4 = *reinterpret_cast<const f32x4*>(Dl + qb * 32 + g * 8 + half * 4);
@@ -1402,7 +1416,8 @@ __device__ inline void dkdv_pair_tile(
                                !all_visible(first.mask, kb0 + wave_r * 32, 32, off + qstart + t * BK_Q, BK_Q)
                          : all_masked || t < n_front || t >= n_whole);
   }
-  const float out_scale = role == 0 ? 1.0f : scale;     // dV as it is, dK times the softmax scale
+  // dV as it is, dK times the softmax scale
+  const float out_scale = role == 0 ? 1.0f : WINDOW ? scale * (1.0f / HANDED_SCALE) : scale;
   const bool leaves_part = WINDOW && where.part >= 0;
   if (kpos < L && (gsplit > 1 || leaves_part)) {
     const size_t plane = (size_t)Ttot * Hkv * DH;
@@ -1948,13 +1963,13 @@ __global__ __launch_bounds__(256, 2) void fa_bwd_joint_kernel(
 // us, two workgroups of four wavefronts -> this: 8192 x 8192 keys, 32 / 8 heads, 1522 -> 1332, causal 782 -> 687; 32768 tokens
 // of causal documents 4217 -> 3630; 8192 tokens of documents, 32 heads, 262 -> 253; 16 samples of about 1130, 24 heads, 445 both.
 constexpr int DQ_ALT_LDS_BYTES = (4 + 3) * RunTile<128>::bytes(FK);
-template <bool CAUSAL>
+template <bool CAUSAL, bool WINDOW = false>
 __device__ inline void dq_alt_tile(
     unsigned char* lds, int block, const bf16_t* __restrict__ q, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v, int ld,
     int ldk, const bf16_t* __restrict__ d_o, int ldo, const float* __restrict__ lse,
     const float* __restrict__ delta, const int32_t* __restrict__ cu, const int32_t* __restrict__ cuk,
     int S, bf16_t* __restrict__ dq, int ldd, int Ttot, int Hq, int group, float scale, float scale_log2,
-    SeqOrder ord) {
+    SeqOrder ord, LocalMask w = {0, 0, nullptr}) {
   constexpr int DH = 128;
   using RT = RunTile<DH>;
   constexpr int KS = DH / 16, NB = DH / 32, KBL = FK / 32, TILE = RT::bytes(FK), RUNS = FK / RT::RPR / 8;
@@ -1964,10 +1979,10 @@ __device__ inline void dq_alt_tile(
   unsigned char* const Vbuf = lds + KRING * TILE;
   int seq, qt, nqt, tile_id, hq;
   tile_and_head(Hq, &tile_id, &hq, block);
-  if (!find_tile(cu, ord, S, AQ, tile_id, &seq, &qt, &nqt)) return;
+  if (WINDOW ? !find_tile(cu, cu + 1, ord, S, AQ, tile_id, &seq, &qt, &nqt) : !find_tile(cu, ord, S, AQ, tile_id, &seq, &qt, &nqt)) return;
   const int hk = hq / group;
   const int lo = cu[seq], L = cu[seq + 1] - lo;
-  const int lok = cuk[seq], Lk = cuk[seq + 1] - lok;
+  const int lok = cuk[seq], Lk = (WINDOW ? w.key_end[seq] : cuk[seq + 1]) - lok, off = WINDOW ? Lk - L : 0;
   const int q0 = qt * AQ;
   const int lane = threadIdx.x & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1990,24 +2005,34 @@ __device__ inline void dq_alt_tile(
 #pragma unroll
   for (int j = 0; j < NB; ++j) dqacc[j] = f32x16{};
   // key tiles of the workgroup, and those of this wavefront (none if its queries lie past the sequence)
-  const int nkt = ((CAUSAL ? min(Lk, q0 + AQ) : Lk) + FK - 1) / FK;
+  const auto walk = [&] {
+    if constexpr (WINDOW) return KeyWalk<FK>(w, off, q0, AQ, Lk);
+    else return AllKeys<FK>(CAUSAL, q0, AQ, Lk);
+  }();
+  const int nkt = walk.n;
   const int mine = qfirst >= L ? 0 : CAUSAL ? min(nkt, (qfirst + 31) / FK + 1) : nkt;
   const int plain = CAUSAL ? min(Lk / FK, (qfirst + 1) / FK) : Lk / FK;   // leading tiles that need no mask test
   const bf16_t* kbase = scalar_ptr(k + (size_t)lok * ldk + hk * DH);
   const bf16_t* vbase = scalar_ptr(v + (size_t)lok * ldk + hk * DH);
   const uint32_t klds = (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char*)Kbuf;
   const uint32_t vlds = (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char*)Vbuf;
+  // does this wavefront take part in tile t
+  auto takes = [&](int t) {
+    if constexpr (WINDOW) return t < nkt && qfirst < L && !none_visible(w, walk.tile(t) * FK, FK, off + qfirst, 32);
+    else return t < mine;
+  };
   // tile t of K or V into a ring slot; rows past the keys are clamped (their dS is 0)
   auto fetch = [&](const bf16_t* base, uint32_t dst, int t) {
     if (t >= nkt) return;
     const int l = fresh_lane();
-    const bf16_t* src = base + (size_t)t * FK * ldk;
-    const int last = Lk - t * FK - 1;
+    const int key0 = walk.tile(t) * FK;
+    const bf16_t* src = base + (size_t)key0 * ldk;
+    const int last = Lk - key0 - 1;
 #pragma unroll
     for (int i = 0; i < RUNS; ++i) {
       const int r = wave * RUNS + i;
-      const uint32_t off = (uint32_t)min(r * RT::RPR + RT::load_row(l), last) * (uint32_t)ldk * 2u + (uint32_t)RT::load_chunk(l) * 16u;
-      TileAsync<FK, DH, 512>::load16(src, off, dst + r * RT::RUN);
+      const uint32_t at = (uint32_t)min(r * RT::RPR + RT::load_row(l), last) * (uint32_t)ldk * 2u + (uint32_t)RT::load_chunk(l) * 16u;
+      TileAsync<FK, DH, 512>::load16(src, at, dst + r * RT::RUN);
     }
   };
   f32x16 sacc[KBL], dpacc[KBL];
@@ -2049,15 +2074,17 @@ __device__ inline void dq_alt_tile(
     }
   };
   auto softmax = [&](int t) {
-    if (t >= plain) {
+    const int key0 = walk.tile(t) * FK;
+    if (WINDOW ? !all_visible(w, key0, FK, off + qfirst, 32) : t >= plain) {
       asm volatile("");                                    // keeps the tests out of the tiles that need none
-      const int h4 = (fresh_lane() >> 5) * 4, left = Lk - t * FK - h4, ahead = qfirst + (fresh_lane() & 31) - t * FK - h4;
+      const int h4 = (fresh_lane() >> 5) * 4, left = Lk - key0 - h4, ahead = off + qfirst + (fresh_lane() & 31) - key0 - h4;
+      const int behind = ahead - (WINDOW ? w.window : 0), sinks = WINDOW ? w.sinks - key0 - h4 : 0;
 #pragma unroll
       for (int b = 0; b < KBL; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int e = b * 32 + (r >> 2) * 8 + (r & 3);
-          if (e >= left || (CAUSAL && e > ahead)) sacc[b][r] = -INFINITY;   // P = 0
+          if (WINDOW ? e > ahead || (e <= behind && e >= sinks) : e >= left || (CAUSAL && e > ahead)) sacc[b][r] = -INFINITY;   // P = 0
         }
     }
 #pragma unroll
@@ -2079,16 +2106,16 @@ __device__ inline void dq_alt_tile(
   wait_async_tiles();
   phase_barrier();
   if (wave >= 4) phase_barrier();                         // the second group stays one phase behind
-  if (mine > 0) scores(0, 0);
+  if (takes(0)) scores(0, 0);
   phase_barrier();
   for (int t = 0, v1 = 1, v2 = 2; t < nkt; ++t) {         // V slots of tiles t + 1, t + 2
     // both groups are past the tiles these overwrite (K t - 2, V t - 1); they are read two phases from now
     fetch(kbase, klds + ((t + 2) & (KRING - 1)) * TILE, t + 2);
     fetch(vbase, vlds + v2 * TILE, t + 2);
-    if (t < mine) softmax(t);
+    if (takes(t)) softmax(t);
     phase_barrier();
-    if (t < mine) accumulate(t & (KRING - 1));
-    if (t + 1 < mine) scores((t + 1) & (KRING - 1), v1);
+    if (takes(t)) accumulate(t & (KRING - 1));
+    if (takes(t + 1)) scores((t + 1) & (KRING - 1), v1);
     wait_async_tiles();
     phase_barrier();
     v1 = v2;
@@ -2294,48 +2321,94 @@ bm_status bwd_launch(const AttnArgs& a, const void* o, const void* d_o, const fl
 // =============================================================================
 // sliding window: the kernels above with WINDOW, and what joins the parts of first keys
 // =============================================================================
+// The backward pass in one grid: the parts of first keys, the other key tiles, then dQ, which fills what they leave (as in
+// fa_bwd_joint_kernel and fa_bwd_joint512_kernel); at head size 72 dQ of 128 rows on its own where that is ahead, two workgroups to a CU.
+// At head size 128 dQ takes 256 rows and turns for any length: the 128-row tile, with the window's bounds, holds more than 256 registers
+// (dQ of 8192 queries, window 2048, 809 -> about 380 us; the whole pass of 777 queries, window 131, 73 -> 64).
+struct WindowBwdArgs {
+  const bf16_t *q, *k, *v, *d_o;
+  const float *lse, *delta;
+  const int32_t *cuq, *cuk;
+  bf16_t *dq, *dk, *dv;
+  float* part;
+  int ld, ldk, ldo, ldd, ldd_kv, S, Tq, Tk, Hkv, group, gsplit, kv_wgs;      // kv_wgs: the parts' among them
+  float scale, scale_log2;
+};
 template <int DH>
-__global__ __launch_bounds__(DH <= 64 ? 256 : 512, 2) void fa_window_dkdv_kernel(
-    const bf16_t* __restrict__ q, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v, int ld, int ldk,
-    const bf16_t* __restrict__ d_o, int ldo, const float* __restrict__ lse, const float* __restrict__ delta,
-    const int32_t* __restrict__ cuq, const int32_t* __restrict__ cuk, int S, bf16_t* __restrict__ dk, bf16_t* __restrict__ dv,
-    int ldd, int Tq, int Tk, int Hkv, int group, float scale, float scale_log2, int gsplit, float* __restrict__ part, SeqOrder ord,
-    FirstKeys first) {
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[DH <= 64 ? dkdv_lds_bytes<DH>() : dkdv_pair_lds_bytes<DH>()];
-  if constexpr (DH <= 64)
-    dkdv_tile<DH, true, true>(lds, blockIdx.x, q, k, v, ld, ldk, d_o, ldo, lse, delta, cuq, cuk, S, dk, dv, ldd, Tq, Tk, Hkv, group,
-                              scale, scale_log2, gsplit, part, ord, first);
-  else
-    dkdv_pair_tile<DH, true, true>(lds, blockIdx.x, q, k, v, ld, ldk, d_o, ldo, lse, delta, cuq, cuk, S, dk, dv, ldd, Tq, Tk, Hkv,
-                                   group, scale, scale_log2, gsplit, part, ord, first);
+__global__ __launch_bounds__(256, 2) void fa_window_bwd_kernel(WindowBwdArgs a, SeqOrder ord_kv, SeqOrder ord_q, FirstKeys first) {
+  constexpr int LDS = dkdv_lds_bytes<DH>() > dq_lds_bytes<DH>() ? dkdv_lds_bytes<DH>() : dq_lds_bytes<DH>();
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS];
+  if ((int)blockIdx.x < a.kv_wgs) {
+    dkdv_tile<DH, true, true>(lds, blockIdx.x, a.q, a.k, a.v, a.ld, a.ldk, a.d_o, a.ldo, a.lse, a.delta, a.cuq, a.cuk, a.S, a.dk, a.dv,
+                              a.ldd_kv, a.Tq, a.Tk, a.Hkv, a.group, a.scale, a.scale_log2, a.gsplit, a.part, ord_kv, first);
+  } else {
+    int tile, head;
+    tile_and_head(a.Hkv * a.group, &tile, &head, blockIdx.x - a.kv_wgs);
+    dq_tile<DH, true, true>(lds, threadIdx.x, tile, head, true, a.q, a.k, a.v, a.ld, a.ldk, a.d_o, a.ldo, a.lse, a.delta, a.cuq, a.cuk,
+                            a.S, a.dq, a.ldd, a.Tq, a.group, a.scale, a.scale_log2, ord_q, first.mask);
+  }
 }
 
 template <int DH>
-__global__ __launch_bounds__(256, 2) void fa_window_dq_kernel(
-    const bf16_t* __restrict__ q, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v, int ld, int ldk,
-    const bf16_t* __restrict__ d_o, int ldo, const float* __restrict__ lse, const float* __restrict__ delta,
-    const int32_t* __restrict__ cu, const int32_t* __restrict__ cuk, int S, bf16_t* __restrict__ dq, int ldd, int Ttot, int Hq,
-    int group, float scale, float scale_log2, SeqOrder ord, LocalMask w) {
+__global__ __launch_bounds__(512, 2) void fa_window_bwd512_kernel(WindowBwdArgs a, SeqOrder ord_kv, SeqOrder ord_q, FirstKeys first) {
+  constexpr int KV = dkdv_pair_lds_bytes<DH>(), Q = DH == 128 ? DQ_ALT_LDS_BYTES : 2 * dq_lds_bytes<DH>();
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[KV > Q ? KV : Q];
+  const int Hq = a.Hkv * a.group;
+  if ((int)blockIdx.x < a.kv_wgs) {
+    dkdv_pair_tile<DH, true, true>(lds, blockIdx.x, a.q, a.k, a.v, a.ld, a.ldk, a.d_o, a.ldo, a.lse, a.delta, a.cuq, a.cuk, a.S, a.dk, a.dv,
+                                   a.ldd_kv, a.Tq, a.Tk, a.Hkv, a.group, a.scale, a.scale_log2, a.gsplit, a.part, ord_kv, first);
+  } else if constexpr (DH == 128) {
+    dq_alt_tile<true, true>(lds, blockIdx.x - a.kv_wgs, a.q, a.k, a.v, a.ld, a.ldk, a.d_o, a.ldo, a.lse, a.delta, a.cuq, a.cuk, a.S, a.dq,
+                            a.ldd, a.Tq, Hq, a.group, a.scale, a.scale_log2, ord_q, first.mask);
+  } else {
+    int tile, heads;
+    tile_and_head((Hq + 1) / 2, &tile, &heads, blockIdx.x - a.kv_wgs);
+    const int side = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), head = heads * 2 + side;
+    dq_tile<DH, true, true>(lds + side * dq_lds_bytes<DH>(), threadIdx.x & 255, tile, min(head, Hq - 1), head < Hq, a.q, a.k, a.v, a.ld,
+                            a.ldk, a.d_o, a.ldo, a.lse, a.delta, a.cuq, a.cuk, a.S, a.dq, a.ldd, a.Tq, a.group, a.scale, a.scale_log2,
+                            ord_q, first.mask);
+  }
+}
+
+template <int DH>
+__global__ __launch_bounds__(256, 2) void fa_window_dq_kernel(WindowBwdArgs a, SeqOrder ord, LocalMask w) {
   __shared__ __attribute__((aligned(1024))) unsigned char lds[dq_lds_bytes<DH>()];
   int tile, head;
-  tile_and_head(Hq, &tile, &head, blockIdx.x);
-  dq_tile<DH, true, true>(lds, threadIdx.x, tile, head, true, q, k, v, ld, ldk, d_o, ldo, lse, delta, cu, cuk, S, dq, ldd, Ttot,
-                          group, scale, scale_log2, ord, w);
+  tile_and_head(a.Hkv * a.group, &tile, &head, blockIdx.x);
+  dq_tile<DH, true, true>(lds, threadIdx.x, tile, head, true, a.q, a.k, a.v, a.ld, a.ldk, a.d_o, a.ldo, a.lse, a.delta, a.cuq, a.cuk, a.S,
+                          a.dq, a.ldd, a.Tq, a.group, a.scale, a.scale_log2, ord, w);
 }
 
+// the sequence that is the id-th of those whose first keys are in parts
+__device__ inline bool find_split(const FirstKeys& f, const int32_t* __restrict__ cuq, int S, int id, int* seq) {
+  const int lane = threadIdx.x & 63;
+  for (int s0 = 0; s0 < S; s0 += 64) {
+    const int s = min(s0 + lane, S - 1);
+    uint64_t split = __builtin_amdgcn_ballot_w64(s0 + lane < S && f.parts(cuq[s + 1] - cuq[s]) > 0);
+    const int n = __builtin_popcountll(split);
+    if (id < n) {
+      for (; id > 0; --id) split &= split - 1;
+      *seq = s0 + __builtin_ctzll(split);
+      return true;
+    }
+    id -= n;
+  }
+  return false;
+}
 // dk, dv of the key tiles that were left in fp32 -- parts of the first keys, q-head parts of any -- summed in order and
-// rounded once.  grid: x the key tiles (all of them, or with one q-head part the first ones), y kv heads, z 16 rows.
+// rounded once.  grid: x the key tiles (all of them, or with one q-head part the first ones that are in parts), y kv heads, z 16 rows.
 __global__ __launch_bounds__(256) void fa_window_reduce_kernel(
     const float* __restrict__ part, int gsplit, const int32_t* __restrict__ cuq, const int32_t* __restrict__ cuk, int S, int Ttot,
     int Hkv, int dh, bf16_t* __restrict__ dk, bf16_t* __restrict__ dv, int ldd, int all_tiles, SeqOrder ord, FirstKeys first) {
   __shared__ int before;
-  int seq = blockIdx.x, kt = 0, nkt;
+  int seq, kt = 0, nkt;
   if (all_tiles) {
     if (!find_tile(cuk, first.mask.key_end, ord, S, BK_KEYS, blockIdx.x, &seq, &kt, &nkt)) return;
     kt = nkt - 1 - kt;
+  } else if (!find_split(first, cuq, S, blockIdx.x, &seq)) {
+    return;
   }
   const int parts = kt == 0 ? first.parts(cuq[seq + 1] - cuq[seq]) : 0;
-  if (!all_tiles && parts == 0) return;
   const int lo = cuk[seq], L = first.mask.key_end[seq] - lo, hk = blockIdx.y;
   const float* src;
   size_t step_gs, step_part, row_stride, which_stride;
@@ -2381,14 +2454,14 @@ int count_tiles(const int32_t* begin, const int32_t* end, int S, int rows) {
   return (int)n;
 }
 
+// (256-row tiles and turns, as the backward pass has them, are slower: us, 32 / 8 heads of 128, 8192 tokens, window 1024 172 -> 216, 256 92 ->
+// 145; 4 documents of 8192, window 4096, 1776 -> 1787.)
 template <int DH>
 bm_status window_fwd_launch(const AttnArgs& a, void* o, float* lse, hipStream_t st) {
-  const dim3 grid(count_tiles(a.cu_host, a.S, FQ) * a.Hq);
-  if (grid.x == 0) return BM_OK;
   const SeqOrder ord = make_seq_order(a.cu_host, a.kv_cu_host(), a.S, FQ, false);
-  hipLaunchKernelGGL((fa_fwd_kernel<DH, true, true>), grid, dim3(256), 0, st, (const bf16_t*)a.q, (const bf16_t*)a.k,
-                     (const bf16_t*)a.v, a.ld_qkv, a.kv_ld(), a.cu_dev, a.kv_cu_dev(), a.S, (bf16_t*)o, a.Hq * a.dh, lse, a.T,
-                     a.Hq, a.Hq / a.Hkv, LOG2E / sqrtf((float)a.dh), ord, a.local);
+  hipLaunchKernelGGL((fa_fwd_kernel<DH, true, true>), dim3(count_tiles(a.cu_host, a.S, FQ) * a.Hq), dim3(256), 0, st, (const bf16_t*)a.q,
+                     (const bf16_t*)a.k, (const bf16_t*)a.v, a.ld_qkv, a.kv_ld(), a.cu_dev, a.kv_cu_dev(), a.S, (bf16_t*)o, a.Hq * a.dh, lse,
+                     a.T, a.Hq, a.Hq / a.Hkv, LOG2E / sqrtf((float)a.dh), ord, a.local);
   BM_CHECK_LAUNCH("fa_window_fwd");
   return BM_OK;
 }
@@ -2563,7 +2636,10 @@ struct WindowBwd {
 WindowBwd window_bwd(int window, int sinks, int Hq, int Hkv, int dh, int S, int Tq, int Tk) {
   WindowBwd w;
   const int tiles = cdiv(Tk, BK_KEYS) > S ? cdiv(Tk, BK_KEYS) : S;
-  w.gsplit = dkdv_group_split(tiles, Hkv, Hq / Hkv);
+  // as without a window, but for 512 workgroups: dQ follows in the same grid, and the tiles of a window are short for the fp32 partials.
+  // us, for 1024 -> 512 -> 256: 32 / 8 heads of 128, 8192 tokens, window 2048 1104 -> 1041 -> 1041, 256 650 -> 489 -> 489, 4096 448 -> 379 -> 347;
+  // 32 / 8 of 64, 4096 207 -> 190 -> 239, 2048 94 -> 94 -> 129; 8 / 1 of 128, 32768, window 4096, 1705 -> 1733 -> 2463.
+  w.gsplit = dkdv_group_split(2 * tiles, Hkv, Hq / Hkv);
   // parts of the first keys about as long as the tiles of other keys
   const int rows = (int)align_up(window < 4096 ? window : 4096, BK_Q);
   w.part_rows = rows < 512 ? 512 : rows;
@@ -2586,7 +2662,12 @@ bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, c
   first.rows = wb.part_rows;
   first.out = part + wb.split;
   long parts = 0;
-  for (int s = 0; s < a.S; ++s) parts += first.parts(a.cu_host[s + 1] - a.cu_host[s]);
+  int in_parts = 0;
+  for (int s = 0; s < a.S; ++s) {
+    const int n = first.parts(a.cu_host[s + 1] - a.cu_host[s]);
+    parts += n;
+    in_parts += n > 0;
+  }
   first.wgs = (int)parts * a.Hkv * wb.gsplit;
   first.ord = make_seq_order(a.cu_host, a.cu_host, a.S, wb.part_rows, false);
   for (int i = 0; i < first.ord.n && i < a.S; ++i)
@@ -2594,23 +2675,27 @@ bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, c
   if (a.T > 0)
     hipLaunchKernelGGL((fa_delta_kernel<DH>), dim3(cdiv((long)a.T * a.Hq * DeltaLanes<DH>::N, 256)), dim3(256), 0, st,
                        (const bf16_t*)o, (const bf16_t*)d_o, ldo, delta, a.T, a.Hq);
-  const int ktiles = count_tiles(a.kv_cu_host(), a.key_end_host, a.S, BK_KEYS);
+  const int query_rows = DH == 128 ? AQ : FQ, heads_per_wg = DH == 72 ? 2 : 1;
+  const int ktiles = count_tiles(a.kv_cu_host(), a.key_end_host, a.S, BK_KEYS), qtiles = count_tiles(a.cu_host, a.S, query_rows);
+  const int kv_wgs = first.wgs + ktiles * a.Hkv * wb.gsplit, q_wgs = qtiles * cdiv(a.Hq, heads_per_wg);
+  // (head size 72: as in bwd_plan)
+  const bool together = DH != 72 || kv_wgs + q_wgs <= NUM_CU * 3 / 2 || (kv_wgs > NUM_CU && kv_wgs + q_wgs <= 2 * NUM_CU);
   const SeqOrder ord_kv = make_seq_order(a.kv_cu_host(), a.cu_host, a.S, BK_KEYS, false, a.key_end_host);
-  const int kv_wgs = first.wgs + ktiles * a.Hkv * wb.gsplit;
-  if (kv_wgs > 0)
-    hipLaunchKernelGGL((fa_window_dkdv_kernel<DH>), dim3(kv_wgs), dim3(DH <= 64 ? 256 : 512), 0, st, (const bf16_t*)a.q,
-                       (const bf16_t*)a.k, (const bf16_t*)a.v, a.ld_qkv, a.kv_ld(), (const bf16_t*)d_o, ldo, lse,
-                       (const float*)delta, a.cu_dev, a.kv_cu_dev(), a.S, (bf16_t*)dk, (bf16_t*)dv, a.ld_dkv, a.T, Tk, a.Hkv, group,
-                       scale, sl2, wb.gsplit, part, ord_kv, first);
-  const int q_wgs = count_tiles(a.cu_host, a.S, FQ) * a.Hq;
-  const SeqOrder ord_q = make_seq_order(a.cu_host, a.cu_host, a.S, FQ, false);
-  if (q_wgs > 0)
-    hipLaunchKernelGGL((fa_window_dq_kernel<DH>), dim3(q_wgs), dim3(256), 0, st, (const bf16_t*)a.q, (const bf16_t*)a.k,
-                       (const bf16_t*)a.v, a.ld_qkv, a.kv_ld(), (const bf16_t*)d_o, ldo, lse, (const float*)delta, a.cu_dev,
-                       a.kv_cu_dev(), a.S, (bf16_t*)dq, ldd, a.T, a.Hq, group, scale, sl2, ord_q, a.local);
+  const SeqOrder ord_q = make_seq_order(a.cu_host, a.cu_host, a.S, query_rows, false);
+  const WindowBwdArgs w{(const bf16_t*)a.q, (const bf16_t*)a.k, (const bf16_t*)a.v, (const bf16_t*)d_o, lse, delta, a.cu_dev, a.kv_cu_dev(),
+                        (bf16_t*)dq, (bf16_t*)dk, (bf16_t*)dv, part, a.ld_qkv, a.kv_ld(), ldo, ldd, a.ld_dkv, a.S, a.T, Tk, a.Hkv, group,
+                        wb.gsplit, kv_wgs, scale, sl2};
+  const int wgs = kv_wgs + (together ? q_wgs : 0);
+  if (wgs > 0) {
+    if constexpr (DH <= 64) hipLaunchKernelGGL(fa_window_bwd_kernel<DH>, dim3(wgs), dim3(256), 0, st, w, ord_kv, ord_q, first);
+    else hipLaunchKernelGGL(fa_window_bwd512_kernel<DH>, dim3(wgs), dim3(512), 0, st, w, ord_kv, ord_q, first);
+  }
+  if constexpr (DH == 72)
+    if (!together && qtiles > 0)
+      hipLaunchKernelGGL((fa_window_dq_kernel<DH>), dim3(qtiles * a.Hq), dim3(256), 0, st, w, ord_q, a.local);
   const int all_tiles = wb.gsplit > 1;
   if (kv_wgs > 0 && (all_tiles || parts > 0))
-    hipLaunchKernelGGL(fa_window_reduce_kernel, dim3(all_tiles ? ktiles : a.S, a.Hkv, BK_KEYS / 16), dim3(256), 0, st, part,
+    hipLaunchKernelGGL(fa_window_reduce_kernel, dim3(all_tiles ? ktiles : in_parts, a.Hkv, BK_KEYS / 16), dim3(256), 0, st, part,
                        wb.gsplit, a.cu_dev, a.kv_cu_dev(), a.S, Tk, a.Hkv, a.dh, (bf16_t*)dk, (bf16_t*)dv, a.ld_dkv, all_tiles,
                        ord_kv, first);
   BM_CHECK_LAUNCH("fa_window_bwd");
