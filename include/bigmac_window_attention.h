@@ -63,7 +63,7 @@ bm_status bm_qk_rotary_forward(const bm_qk_rotary_desc* desc, int32_t T, const v
  *   dq, dk           dev  gradients of q and k, rows of ld_dqk elements, overwritten; may take the place of dq_out
  *                         and dk_out, or of q and k, in rows of the same stride
  *   dq_gain, dk_gain dev  [head_dim] fp32, added to (norm = 1); may be one buffer where both share a gain
- * scratch: bm_qk_rotary_backward_scratch_bytes(desc, T) bytes (0 without norm). */
+ * scratch: bm_qk_rotary_backward_scratch_bytes(desc, T) bytes (0 without norm), the same for every T. */
 size_t    bm_qk_rotary_backward_scratch_bytes(const bm_qk_rotary_desc* desc, int32_t T);
 bm_status bm_qk_rotary_backward(const bm_qk_rotary_desc* desc, int32_t T, const void* q, const void* k, int32_t ld,
                                 const int32_t* positions, const void* q_gain, const void* k_gain,

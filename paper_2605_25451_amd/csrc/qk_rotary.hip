@@ -6,7 +6,7 @@
 //
 // A group of lanes owns one token and walks heads; a lane keeps VEC pairs, so that cosines and sines are
 // formed once per token and walk, in fp64 up to the fraction of a turn.  Bound by memory: every row is read and
-// written once.
+// written once, at 4.6 TB/s forward and in the gradient (8192 tokens of 32 + 8 heads of 128, 37 and 55 us; a copy 4.9).
 #include "common.h"
 #include "../../include/bigmac_window_attention.h"
 
@@ -38,18 +38,23 @@ struct RotaryArgs {
 
 template <typename T, int VEC> struct alignas(sizeof(T) * VEC) Pack { T v[VEC]; };
 
-template <int VEC, typename T>
+template <int N> using Bytes = unsigned int __attribute__((ext_vector_type(N / 4)));
+template <int VEC, bool NT = false, typename T>
 __device__ inline void load_vec(const T* p, float (&out)[VEC]) {
-  const Pack<T, VEC> t = *reinterpret_cast<const Pack<T, VEC>*>(p);
+  using B = Bytes<sizeof(T) * VEC>;
+  const B raw = NT ? __builtin_nontemporal_load(reinterpret_cast<const B*>(p)) : *reinterpret_cast<const B*>(p);
+  const Pack<T, VEC> t = __builtin_bit_cast(Pack<T, VEC>, raw);
 #pragma unroll
   for (int e = 0; e < VEC; ++e) out[e] = Elt<T>::to_f(t.v[e]);
 }
-template <int VEC, typename T>
+template <int VEC, bool NT = false, typename T>
 __device__ inline void store_vec(T* p, const float (&in)[VEC]) {
   Pack<T, VEC> t;
 #pragma unroll
   for (int e = 0; e < VEC; ++e) t.v[e] = Elt<T>::from_f(in[e]);
-  *reinterpret_cast<Pack<T, VEC>*>(p) = t;
+  using B = Bytes<sizeof(T) * VEC>;
+  if (NT) __builtin_nontemporal_store(__builtin_bit_cast(B, t), reinterpret_cast<B*>(p));
+  else *reinterpret_cast<Pack<T, VEC>*>(p) = t;
 }
 
 // cosine and sine of a lane's pairs; the fraction of a turn in fp64
@@ -79,7 +84,7 @@ template <int LP> __device__ inline float lanes_sum(float v) {
 
 // LP lanes own a token (a power of two with the norm, whose sums go over them; otherwise just as many as there are
 // chunks, LP = 0).  grid: x walks tokens, y the heads of a walk, queries first.
-template <typename T, int VEC, int LP>
+template <typename T, int VEC, int LP, bool NT>
 __global__ __launch_bounds__(256) void qk_rotary_fwd_kernel(RotaryArgs a, Rotation rot, float sign) {
   constexpr bool NORM = LP > 0;
   constexpr int U = 4;                                     // heads in flight
@@ -104,8 +109,8 @@ __global__ __launch_bounds__(256) void qk_rotary_fwd_kernel(RotaryArgs a, Rotati
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const T* p = in + (size_t)min(h0 + u, last - 1) * a.dh;
-      load_vec<VEC>(p, x[u]);
-      load_vec<VEC>(p + half, y[u]);
+      load_vec<VEC, NT>(p, x[u]);
+      load_vec<VEC, NT>(p + half, y[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -126,15 +131,15 @@ __global__ __launch_bounds__(256) void qk_rotary_fwd_kernel(RotaryArgs a, Rotati
       }
       if (live && h0 + u < last) {
         T* o = out + (size_t)(h0 + u) * a.dh;
-        store_vec<VEC>(o, p);
-        store_vec<VEC>(o + half, q);
+        store_vec<VEC, NT>(o, p);
+        store_vec<VEC, NT>(o + half, q);
       }
     }
   }
 }
 
 // gradient with the norm: a workgroup walks tokens and leaves one row of gain gradients
-template <typename T, int VEC, int LP>
+template <typename T, int VEC, int LP, bool NT>
 __global__ __launch_bounds__(256) void qk_rotary_norm_bwd_kernel(RotaryArgs a, Rotation rot) {
   constexpr int GROUPS = 256 / LP, U = 2;
   __shared__ float sums[GROUPS][2 * LP * VEC + 1];
@@ -165,10 +170,10 @@ __global__ __launch_bounds__(256) void qk_rotary_norm_bwd_kernel(RotaryArgs a, R
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const size_t at = (size_t)min(h0 + u, last - 1) * a.dh;
-        load_vec<VEC>(in + at, d0[u]);
-        load_vec<VEC>(in + at + half, d1[u]);
-        load_vec<VEC>(raw + at, x0[u]);
-        load_vec<VEC>(raw + at + half, x1[u]);
+        load_vec<VEC, NT>(in + at, d0[u]);
+        load_vec<VEC, NT>(in + at + half, d1[u]);
+        load_vec<VEC, NT>(raw + at, x0[u]);
+        load_vec<VEC, NT>(raw + at + half, x1[u]);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -194,8 +199,8 @@ __global__ __launch_bounds__(256) void qk_rotary_norm_bwd_kernel(RotaryArgs a, R
             q[e] = r * (q[e] * gb[e] - n1 * k);
           }
           T* o = out + (size_t)(h0 + u) * a.dh;
-          store_vec<VEC>(o, p);
-          store_vec<VEC>(o + half, q);
+          store_vec<VEC, NT>(o, p);
+          store_vec<VEC, NT>(o + half, q);
         }
       }
     }
@@ -228,9 +233,10 @@ Lanes lanes_of(const bm_qk_rotary_desc& d) {
 
 // Walks over the heads of either side: few tokens have their heads dealt to more lanes, each of which forms the angles again.
 constexpr long WANTED_LANES = 1L << 18;
+constexpr int MAX_WALKS = 1 << 14;       // of a grid's 2^16
 void deal_heads(const bm_qk_rotary_desc& d, long lanes, RotaryArgs* a, int* groups) {
   const int H = d.n_q_heads + d.n_kv_heads;
-  const int walks = (int)std::min<long>(H, std::max<long>(1, WANTED_LANES / std::max<long>(lanes, 1)));
+  const int walks = (int)std::min<long>(std::min(H, MAX_WALKS), std::max<long>(1, WANTED_LANES / std::max<long>(lanes, 1)));
   const int per = cdiv(H, walks);
   a->heads[0] = d.n_q_heads;
   a->heads[1] = d.n_kv_heads;
@@ -251,7 +257,9 @@ BwdGrid bwd_grid(const bm_qk_rotary_desc& d, int T, RotaryArgs* a) {
   BwdGrid g;
   deal_heads(d, (long)T * l.pow2, a, &g.y);
   const int per = 256 / l.pow2;
-  g.x = std::max(1, std::min(cdiv(T, per), BWD_WORKGROUPS / g.y));
+  // every workgroup makes as many trips (8192 tokens of 32 + 8 heads: 2 or 1 in 204 x 5 workgroups -> 2 in 128 x 5, 67.5 -> 59.4 us)
+  const int chunks = cdiv(T, per);
+  g.x = cdiv(chunks, cdiv(chunks, std::max(1, BWD_WORKGROUPS / g.y)));
   g.slots[0] = g.x * a->groups_q;
   g.slots[1] = g.x * (g.y - a->groups_q);
   return g;
@@ -297,8 +305,14 @@ Rotation rotation(const bm_qk_rotary_desc& d) {
   int first = 0;
   for (int a = 0; a < BM_ROTARY_MAX_AXES; ++a) {
     const int n = a < d.n_axes ? d.pairs[a] : 0;
-    for (int j = 0; j < n; ++j)
-      r.turns[first + j] = std::exp(-log_base * (d.own_frequencies ? (double)j / n : (double)(first + j) / half)) / turn;
+    const double step = d.own_frequencies ? -log_base / std::max(n, 1) : -log_base / half;
+    const int j0 = d.own_frequencies ? 0 : first;
+    double fine[8];                                        // base^-(j) by eights and ones: two roundings more
+    for (int j = 0; j < std::min(n, 8); ++j) fine[j] = std::exp(step * j);
+    for (int j = 0; j < n; j += 8) {
+      const double coarse = std::exp(step * (j0 + j)) / turn;
+      for (int e = j; e < std::min(n, j + 8); ++e) r.turns[first + e] = coarse * fine[e - j];
+    }
     first += n;
     r.end[a] = first;
   }
@@ -306,11 +320,19 @@ Rotation rotation(const bm_qk_rotary_desc& d) {
   return r;
 }
 
-template <typename T, int VEC>
+// Do rows go past the caches?  Whole 16-byte accesses of more than the L2s hold together (32 MB): 32 + 8 heads of 128, us, through them
+// -> past: 8192 tokens with the norm 41.7 -> 37.3, gradient 59.4 -> 54.8; 32768 tokens 146 -> 137, gradient 230 -> 222.  Fewer tokens are
+// read again while they are still there (2048: 12.6 -> 13.4); accesses of 8 bytes are slower (16 + 16 heads of 72, 2601 tokens, 11.6 -> 14.2).
+bool past_caches(const bm_qk_rotary_desc& d, const Lanes& l, int T) {
+  const double bytes = (double)T * (d.n_q_heads + d.n_kv_heads) * d.head_dim * elt_size(d.dtype);
+  return l.vec * elt_size(d.dtype) == 16 && bytes > 32e6;
+}
+
+template <typename T, int VEC, bool NT>
 void launch_fwd(const RotaryArgs& a, const Rotation& r, const Lanes& l, bool norm, float sign, int groups, hipStream_t st) {
   const int lanes = norm ? l.pow2 : l.chunks;
   const dim3 grid(cdiv((long)a.T * lanes, 256), groups), block(256);
-#define BM_L(LP) hipLaunchKernelGGL((qk_rotary_fwd_kernel<T, VEC, LP>), grid, block, 0, st, a, r, sign)
+#define BM_L(LP) hipLaunchKernelGGL((qk_rotary_fwd_kernel<T, VEC, LP, NT>), grid, block, 0, st, a, r, sign)
   if (!norm) BM_L(0);
   else switch (l.pow2) {
     case 1: BM_L(1); break; case 2: BM_L(2); break; case 4: BM_L(4); break;
@@ -319,10 +341,10 @@ void launch_fwd(const RotaryArgs& a, const Rotation& r, const Lanes& l, bool nor
 #undef BM_L
 }
 
-template <typename T, int VEC>
+template <typename T, int VEC, bool NT>
 void launch_bwd(const RotaryArgs& a, const Rotation& r, const Lanes& l, const BwdGrid& g, hipStream_t st) {
   const dim3 grid(g.x, g.y), block(256);
-#define BM_L(LP) hipLaunchKernelGGL((qk_rotary_norm_bwd_kernel<T, VEC, LP>), grid, block, 0, st, a, r)
+#define BM_L(LP) hipLaunchKernelGGL((qk_rotary_norm_bwd_kernel<T, VEC, LP, NT>), grid, block, 0, st, a, r)
   switch (l.pow2) {
     case 1: BM_L(1); break; case 2: BM_L(2); break; case 4: BM_L(4); break;
     case 8: BM_L(8); break; case 16: BM_L(16); break; default: BM_L(32);
@@ -330,15 +352,23 @@ void launch_bwd(const RotaryArgs& a, const Rotation& r, const Lanes& l, const Bw
 #undef BM_L
 }
 
+#define BM_DISPATCH(D, L, PAST, FN, ...)                                                            \
+  if ((D).dtype == BM_DTYPE_FP32) {                                                                 \
+    if (PAST) FN<float, 4, true>(__VA_ARGS__); else FN<float, 4, false>(__VA_ARGS__);               \
+  } else if ((L).vec == 8) {                                                                        \
+    if (PAST) FN<bf16_t, 8, true>(__VA_ARGS__); else FN<bf16_t, 8, false>(__VA_ARGS__);             \
+  } else {                                                                                          \
+    FN<bf16_t, 4, false>(__VA_ARGS__);                                                              \
+  }
+
 // forward, and the gradient without the norm (sign -1)
 bm_status turn(const bm_qk_rotary_desc& d, RotaryArgs a, bool norm, float sign, hipStream_t st) {
   const Lanes l = lanes_of(d);
   int groups;
   deal_heads(d, (long)a.T * (norm ? l.pow2 : l.chunks), &a, &groups);
   const Rotation r = rotation(d);
-  if (d.dtype == BM_DTYPE_FP32) launch_fwd<float, 4>(a, r, l, norm, sign, groups, st);
-  else if (l.vec == 8) launch_fwd<bf16_t, 8>(a, r, l, norm, sign, groups, st);
-  else launch_fwd<bf16_t, 4>(a, r, l, norm, sign, groups, st);
+  const bool past = past_caches(d, l, a.T);
+  BM_DISPATCH(d, l, past, launch_fwd, a, r, l, norm, sign, groups, st)
   BM_CHECK_LAUNCH("qk_rotary");
   return BM_OK;
 }
@@ -381,9 +411,9 @@ extern "C" bm_status bm_qk_rotary_forward(const bm_qk_rotary_desc* d, int32_t T,
 
 extern "C" size_t bm_qk_rotary_backward_scratch_bytes(const bm_qk_rotary_desc* d, int32_t T) {
   if (check(d) != BM_OK || T < 1 || T > MAX_TOKENS || !d->norm) return 0;
-  RotaryArgs a{};
-  const BwdGrid g = bwd_grid(*d, T, &a);
-  return align_up((size_t)(g.slots[0] + g.slots[1]) * d->head_dim * sizeof(float), 256);
+  // the same for every T: no grid has more workgroups
+  const int slots = std::max(BWD_WORKGROUPS, std::min(d->n_q_heads + d->n_kv_heads, MAX_WALKS) + 1);
+  return align_up((size_t)slots * d->head_dim * sizeof(float), 256);
 }
 
 extern "C" bm_status bm_qk_rotary_backward(const bm_qk_rotary_desc* d, int32_t T, const void* q, const void* k, int32_t ld,
@@ -431,9 +461,8 @@ extern "C" bm_status bm_qk_rotary_backward(const bm_qk_rotary_desc* d, int32_t T
   const Lanes l = lanes_of(*d);
   const Rotation r = rotation(*d);
   ProfScope prof(PROF_ELEMENTWISE, bytes, st);
-  if (d->dtype == BM_DTYPE_FP32) launch_bwd<float, 4>(a, r, l, g, st);
-  else if (l.vec == 8) launch_bwd<bf16_t, 8>(a, r, l, g, st);
-  else launch_bwd<bf16_t, 4>(a, r, l, g, st);
+  const bool past = past_caches(*d, l, T);
+  BM_DISPATCH(*d, l, past, launch_bwd, a, r, l, g, st)
   BM_CHECK_LAUNCH("qk_rotary_bwd");
   ColumnSums sums;
   if (d->n_q_heads) BM_RETURN_IF(sums.add(a.part[0], g.slots[0], a.dh, a.dh, dq_gain));

@@ -159,6 +159,15 @@ def test_rotary_in_place_and_in_wider_rows(norm, dtype):
     r.check_backward(d, g)
 
 
+@pytest.mark.parametrize("dtype,T,Hq,Hkv", [("bf16", 9001, 12, 3), ("fp32", 4100, 10, 6), ("bf16", 3, 60000, 20000), ("fp32", 1, 1, 40000)])
+@pytest.mark.parametrize("norm", [False, True])
+def test_rotary_of_many_rows(dtype, T, Hq, Hkv, norm):
+    """Rows that go past the caches, several trips of a workgroup; more heads than a grid has rows."""
+    r = Rotary(dtype, norm, T, Hq, Hkv, 128 if T > 3 else 8, [20, 30, 14] if T > 3 else [4], False, seed=6)
+    r.check_forward(r.forward())
+    r.check_backward(*r.backward())
+
+
 def test_rotary_at_the_farthest_positions():
     r = Rotary("fp32", False, 40, 2, 1, 32, [8, 8], False, seed=2)
     r.pos[0, :4] = [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 2, -2 ** 31 + 1]

@@ -61,6 +61,12 @@ def test_rotary_workspace():
     assert bm.qk_rotary_backward_scratch_bytes(bm.make_qk_rotary_desc(**{**DESC, "pairs": [1]}), 5) == 0
 
 
+def test_rotary_workspace_is_enough_for_any_tokens():
+    for heads in ((32, 8), (4, 0), (1 << 16, 1 << 16)):
+        desc = bm.make_qk_rotary_desc(**{**DESC, "n_q_heads": heads[0], "n_kv_heads": heads[1]})
+        assert len({bm.qk_rotary_backward_scratch_bytes(desc, T) for T in (1, 7, 100, 2000, 8192, 1 << 26)}) == 1
+
+
 def test_rotary_of_no_tokens():
     desc = bm.make_qk_rotary_desc(**DESC)
     bm.qk_rotary_forward(desc, 0, None, None, 0, None, None, None, None, None, 0, stream=0)
