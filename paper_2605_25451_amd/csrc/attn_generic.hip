@@ -8,8 +8,6 @@
 //   forward : o = softmax(q k^T / sqrt(dh) + mask) v,  lse = log sum exp (scaled scores)
 //   backward: p = exp(s - lse), dv = p^T do, dp = do v^T, ds = p * (dp - delta),
 //             dq = ds k / sqrt(dh), dk = ds^T q / sqrt(dh), delta = rowsum(do * o)
-// WINDOW: the queries are the last of their sequence's rows, and see the last w.window keys and the first w.sinks;
-// tiles that no row of theirs sees are left out.
 #include "common.h"
 
 #include <type_traits>
@@ -44,10 +42,9 @@ template <int P> __device__ inline float lanes_max(float v) {
 // 25 -> 15 / 21; 16 heads of 64 70 / 156 -> 43 / 93; 5 x 200 rows, 8 heads of 128 335 / 803 -> 156 / 373; 4 x 1024 rows, 4 heads of 32,
 // 183 / 542 -> 84 / 279.  More than four pairs at once cost registers: all 18 of head size 72 left the forward one wavefront
 // per SIMD, and it was slower than with the branches (16 x 1024 rows 923 -> 1045); by sixes 768, 5 x 200 rows of 8 heads 74 -> 40 / 326 -> 190.
-// Rows hide .. seen - 1 are not read, but row `seen` in their place.
 template <int DH, int LD, typename T>
 __device__ inline void load_tiles(const T* __restrict__ a, int lda, const T* __restrict__ b, int ldb, int r0, int rows, float scale,
-                                  float (*A)[LD], float (*B)[LD], int hide = 0, int seen = 0) {
+                                  float (*A)[LD], float (*B)[LD]) {
   constexpr int N = BT * DH / NT, U = N == 8 ? 8 : N % 4 == 0 ? 4 : N % 6 == 0 ? 6 : N;
   static_assert(BT * DH % NT == 0, "whole trips");
 #pragma unroll 1
@@ -55,9 +52,7 @@ __device__ inline void load_tiles(const T* __restrict__ a, int lda, const T* __r
     float x[U], y[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int idx = (it + u) * NT + threadIdx.x;
-      int r = min(r0 + idx / DH, rows - 1);
-      if (seen > 0 && r >= hide) r = max(r, seen);
+      const int idx = (it + u) * NT + threadIdx.x, r = min(r0 + idx / DH, rows - 1);
       x[u] = Elt<T>::to_f(a[(size_t)r * lda + idx % DH]);
       y[u] = Elt<T>::to_f(b[(size_t)r * ldb + idx % DH]);
     }
@@ -70,17 +65,17 @@ __device__ inline void load_tiles(const T* __restrict__ a, int lda, const T* __r
   }
 }
 
-template <typename T, int DH, bool CAUSAL, int P, bool WINDOW>
-__global__ __launch_bounds__(NT, WINDOW ? 2 : 1) void attn_fwd_generic_kernel(
+template <typename T, int DH, bool CAUSAL, int P>
+__global__ __launch_bounds__(NT) void attn_fwd_generic_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, int ld, int ldk,
     const int32_t* __restrict__ cu, const int32_t* __restrict__ cuk, T* __restrict__ o, int ldo,
-    float* __restrict__ lse, int Ttot, int group, float scale, LocalMask w) {
+    float* __restrict__ lse, int Ttot, int group, float scale) {
   constexpr int BQ = NT / P;
   __shared__ float Ks[BT][tile_ld<DH, P>()];
   __shared__ float Vs[BT][tile_ld<DH, P>()];
   const int s = blockIdx.y, hq = blockIdx.z, hk = hq / group;
   const int lo = cu[s], L = cu[s + 1] - lo;
-  const int lok = cuk[s], Lk = (WINDOW ? w.key_end[s] : cuk[s + 1]) - lok;     // keys/values may be packed on their own
+  const int lok = cuk[s], Lk = cuk[s + 1] - lok;     // keys/values may be packed on their own
   const int q0 = blockIdx.x * BQ;
   if (q0 >= L) return;
   const int part = threadIdx.x % P;
@@ -93,12 +88,9 @@ __global__ __launch_bounds__(NT, WINDOW ? 2 : 1) void attn_fwd_generic_kernel(
     acc[c] = 0.f;
   }
   float m = -INFINITY, l = 0.f;
-  const int off = WINDOW ? Lk - L : 0;
-  const int kend = CAUSAL ? min(Lk, off + q0 + BQ) : Lk;
-  const int near = WINDOW ? max(0, off + q0 - w.window + 1) / BT * BT : 0;   // the first tile of the window
-  for (int k0 = WINDOW && w.sinks == 0 ? near : 0; k0 < kend; k0 = WINDOW && k0 + BT >= w.sinks ? max(k0 + BT, near) : k0 + BT) {
-    load_tiles<DH>(k + (size_t)lok * ldk + hk * DH, ldk, v + (size_t)lok * ldk + hk * DH, ldk, k0, Lk, 1.f, Ks, Vs, WINDOW ? w.sinks : 0,
-                   WINDOW ? max(0, off + q0 - w.window + 1) : 0);
+  const int kend = CAUSAL ? min(Lk, q0 + BQ) : Lk;
+  for (int k0 = 0; k0 < kend; k0 += BT) {
+    load_tiles<DH>(k + (size_t)lok * ldk + hk * DH, ldk, v + (size_t)lok * ldk + hk * DH, ldk, k0, Lk, 1.f, Ks, Vs);
     __syncthreads();
     if (active) {
       float sc[BT / P];
@@ -109,7 +101,7 @@ __global__ __launch_bounds__(NT, WINDOW ? 2 : 1) void attn_fwd_generic_kernel(
         float d = 0.f;
 #pragma unroll
         for (int c = 0; c < DH; ++c) d = fmaf(qr[c], Ks[j][c], d);
-        bool ok = kj < Lk && (!CAUSAL || kj <= off + qi) && (!WINDOW || off + qi - kj < w.window || kj < w.sinks);
+        bool ok = kj < Lk && (!CAUSAL || kj <= qi);
         sc[jj] = ok ? d : -INFINITY;
         tmax = sc[jj] > tmax || sc[jj] != sc[jj] ? sc[jj] : tmax;   // keeps NaN, which has to reach the row's sums
       }
@@ -152,18 +144,18 @@ __global__ __launch_bounds__(NT, WINDOW ? 2 : 1) void attn_fwd_generic_kernel(
 
 // dq, and on the way delta = rowsum(dO * O) of its rows, which a dk/dv kernel of its own reads: a small step is bound by
 // its launches, and delta's was one of 27 (4.2 us on its own).  bx: the row tile, s: the sequence, hq: the head.
-template <typename T, int DH, bool CAUSAL, int P, bool WINDOW>
+template <typename T, int DH, bool CAUSAL, int P>
 __device__ __forceinline__ void dq_rows(
     int bx, int s, int hq, const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, int ld, int ldk,
     const T* __restrict__ o, const T* __restrict__ d_o, int ldo, const float* __restrict__ lse,
     float* __restrict__ delta, const int32_t* __restrict__ cu, const int32_t* __restrict__ cuk,
-    T* __restrict__ dq, int ldd, int Ttot, int group, float scale, const LocalMask& w) {
+    T* __restrict__ dq, int ldd, int Ttot, int group, float scale) {
   constexpr int BQ = NT / P;
   __shared__ float Ks[BT][tile_ld<DH, P>()];
   __shared__ float Vs[BT][tile_ld<DH, P>()];
   const int hk = hq / group;
   const int lo = cu[s], L = cu[s + 1] - lo;
-  const int lok = cuk[s], Lk = (WINDOW ? w.key_end[s] : cuk[s + 1]) - lok;
+  const int lok = cuk[s], Lk = cuk[s + 1] - lok;
   const int q0 = bx * BQ;
   if (q0 >= L) return;
   const int part = threadIdx.x % P;
@@ -182,17 +174,14 @@ __device__ __forceinline__ void dq_rows(
 #pragma unroll
   for (int c = 0; c < DH; ++c) my_delta = fmaf(Elt<T>::to_f(o[(size_t)(lo + qrow) * ldo + hq * DH + c]), dor[c], my_delta);
   if (active && part == 0) delta[(size_t)hq * Ttot + lo + qi] = my_delta;
-  const int off = WINDOW ? Lk - L : 0;
-  const int kend = CAUSAL ? min(Lk, off + q0 + BQ) : Lk;
-  const int near = WINDOW ? max(0, off + q0 - w.window + 1) / BT * BT : 0;   // the first tile of the window
-  for (int k0 = WINDOW && w.sinks == 0 ? near : 0; k0 < kend; k0 = WINDOW && k0 + BT >= w.sinks ? max(k0 + BT, near) : k0 + BT) {
+  const int kend = CAUSAL ? min(Lk, q0 + BQ) : Lk;
+  for (int k0 = 0; k0 < kend; k0 += BT) {
     load_tiles<DH>(k + (size_t)lok * ldk + hk * DH, ldk, v + (size_t)lok * ldk + hk * DH, ldk, k0, Lk, 1.f, Ks, Vs);
     __syncthreads();
     if (active) {
       for (int j = part; j < BT; j += P) {
         int kj = k0 + j;
-        if (kj >= Lk || (CAUSAL && kj > off + qi)) break;
-        if (WINDOW && off + qi - kj >= w.window && kj >= w.sinks) continue;
+        if (kj >= Lk || (CAUSAL && kj > qi)) break;
         float sc = 0.f, dp = 0.f;
 #pragma unroll
         for (int c = 0; c < DH; ++c) {
@@ -217,32 +206,32 @@ __device__ __forceinline__ void dq_rows(
   }
 }
 
-template <typename T, int DH, bool CAUSAL, int P, bool WINDOW>
+template <typename T, int DH, bool CAUSAL, int P>
 __global__ __launch_bounds__(NT) void attn_dq_generic_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, int ld, int ldk,
     const T* __restrict__ o, const T* __restrict__ d_o, int ldo, const float* __restrict__ lse,
     float* __restrict__ delta, const int32_t* __restrict__ cu, const int32_t* __restrict__ cuk,
-    T* __restrict__ dq, int ldd, int Ttot, int group, float scale, LocalMask w) {
-  dq_rows<T, DH, CAUSAL, P, WINDOW>(blockIdx.x, blockIdx.y, blockIdx.z, q, k, v, ld, ldk, o, d_o, ldo, lse, delta, cu, cuk, dq,
-                                    ldd, Ttot, group, scale, w);
+    T* __restrict__ dq, int ldd, int Ttot, int group, float scale) {
+  dq_rows<T, DH, CAUSAL, P>(blockIdx.x, blockIdx.y, blockIdx.z, q, k, v, ld, ldk, o, d_o, ldo, lse, delta, cu, cuk, dq, ldd,
+                            Ttot, group, scale);
 }
 
 // P lanes per key row of one kv head; the q heads of the group and the query
 // tiles are walked in a fixed order, so dk/dv sums are reproducible.
 // OWN_DELTA: delta of the streamed rows from o and dO, by the same sum as in dq_rows, instead of from memory.
-template <typename T, int DH, bool CAUSAL, int P, bool OWN_DELTA, bool WINDOW>
+template <typename T, int DH, bool CAUSAL, int P, bool OWN_DELTA>
 __device__ __forceinline__ void dkdv_rows(
     int bx, int s, int hk, const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, int ld, int ldk,
     const T* __restrict__ o, const T* __restrict__ d_o, int ldo, const float* __restrict__ lse,
     const float* __restrict__ delta, const int32_t* __restrict__ cuq, const int32_t* __restrict__ cuk,
-    T* __restrict__ dk, T* __restrict__ dv, int ldd, int Ttot, int group, float scale, const LocalMask& w) {
+    T* __restrict__ dk, T* __restrict__ dv, int ldd, int Ttot, int group, float scale) {
   // this thread's key row lives in the key/value packing (cuk, ldk); queries, dO, lse and
   // delta (Ttot rows per head) in the queries' packing (cuq, ld)
   constexpr int BQ = NT / P;
   __shared__ float Qs[BT][tile_ld<DH, P>()];
   __shared__ float Ds[BT][tile_ld<DH, P>()];
   __shared__ float Ls[BT], Dl[BT];
-  const int lok = cuk[s], Lk = (WINDOW ? w.key_end[s] : cuk[s + 1]) - lok;
+  const int lok = cuk[s], Lk = cuk[s + 1] - lok;
   const int lo = cuq[s], L = cuq[s + 1] - lo;
   const int kb = bx * BQ;
   if (kb >= Lk) return;
@@ -257,12 +246,10 @@ __device__ __forceinline__ void dkdv_rows(
     vr[c] = Elt<T>::to_f(v[(size_t)(lok + krow) * ldk + hk * DH + c]);
     dkr[c] = 0.f; dvr[c] = 0.f;
   }
-  const int off = WINDOW ? Lk - L : 0;
-  const int qstart = CAUSAL ? ((WINDOW ? max(0, kb - off) : kb) / BT) * BT : 0;
-  const int qend = WINDOW && kb >= w.sinks ? min(L, max(0, kb + BQ - 1 - off + w.window)) : L;
+  const int qstart = CAUSAL ? (kb / BT) * BT : 0;
   for (int g = 0; g < group; ++g) {
     const int hq = hk * group + g;
-    for (int q0 = qstart; q0 < qend; q0 += BT) {
+    for (int q0 = qstart; q0 < L; q0 += BT) {
       load_tiles<DH>(q + (size_t)lo * ld + hq * DH, ld, d_o + (size_t)lo * ldo + hq * DH, ldo, q0, L, scale, Qs, Ds);
       if (threadIdx.x < BT) {
         int qi = q0 + threadIdx.x;
@@ -283,8 +270,7 @@ __device__ __forceinline__ void dkdv_rows(
         for (int i = part; i < BT; i += P) {
           int qi = q0 + i;
           if (qi >= L) break;
-          if (CAUSAL && kj > off + qi) continue;
-          if (WINDOW && off + qi - kj >= w.window && kj >= w.sinks) continue;
+          if (CAUSAL && kj > qi) continue;
           float sc = 0.f, dp = 0.f;
 #pragma unroll
           for (int c = 0; c < DH; ++c) {
@@ -316,33 +302,33 @@ __device__ __forceinline__ void dkdv_rows(
   }
 }
 
-template <typename T, int DH, bool CAUSAL, int P, bool WINDOW>
+template <typename T, int DH, bool CAUSAL, int P>
 __global__ __launch_bounds__(NT) void attn_dkdv_generic_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, int ld, int ldk,
     const T* __restrict__ d_o, int ldo, const float* __restrict__ lse,
     const float* __restrict__ delta, const int32_t* __restrict__ cuq, const int32_t* __restrict__ cuk,
-    T* __restrict__ dk, T* __restrict__ dv, int ldd, int Ttot, int group, float scale, LocalMask w) {
-  dkdv_rows<T, DH, CAUSAL, P, false, WINDOW>(blockIdx.x, blockIdx.y, blockIdx.z, q, k, v, ld, ldk, (const T*)nullptr, d_o, ldo,
-                                             lse, delta, cuq, cuk, dk, dv, ldd, Ttot, group, scale, w);
+    T* __restrict__ dk, T* __restrict__ dv, int ldd, int Ttot, int group, float scale) {
+  dkdv_rows<T, DH, CAUSAL, P, false>(blockIdx.x, blockIdx.y, blockIdx.z, q, k, v, ld, ldk, (const T*)nullptr, d_o, ldo, lse,
+                                     delta, cuq, cuk, dk, dv, ldd, Ttot, group, scale);
 }
 
 // Both, where eight lanes share a row on either side (few rows): one launch, dk/dv of the Hkv heads in front (they walk the
 // heads of their group) and dq of the Hq heads behind.  fp32 block of 40 tokens 91 -> 83 us, of 1000 107 -> 96.  On more rows the sums of delta
 // that every dk/dv tile forms for itself cost more than the launch: two launches -> one, 4 heads of 64, 797 rows ahead, 1597 580 -> 621,
 // 3997 2864 -> 3090; 4 heads of 16, 3997 rows 367 -> 410 (causal 415 -> 283); 8 / 1 heads of 64, 708 rows 1235 -> 1419.
-template <typename T, int DH, bool CAUSAL, bool WINDOW>
+template <typename T, int DH, bool CAUSAL>
 __global__ __launch_bounds__(NT) void attn_bwd_joint_generic_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, int ld, int ldk,
     const T* __restrict__ o, const T* __restrict__ d_o, int ldo, const float* __restrict__ lse, float* __restrict__ delta,
     const int32_t* __restrict__ cuq, const int32_t* __restrict__ cuk, T* __restrict__ dq, int ldd, T* __restrict__ dk,
-    T* __restrict__ dv, int ldd_kv, int Ttot, int Hkv, int group, float scale, LocalMask w) {
+    T* __restrict__ dv, int ldd_kv, int Ttot, int Hkv, int group, float scale) {
   const int z = blockIdx.z;
   if (z < Hkv)
-    dkdv_rows<T, DH, CAUSAL, 8, true, WINDOW>(blockIdx.x, blockIdx.y, z, q, k, v, ld, ldk, o, d_o, ldo, lse, nullptr, cuq, cuk,
-                                              dk, dv, ldd_kv, Ttot, group, scale, w);
+    dkdv_rows<T, DH, CAUSAL, 8, true>(blockIdx.x, blockIdx.y, z, q, k, v, ld, ldk, o, d_o, ldo, lse, nullptr, cuq, cuk, dk, dv,
+                                      ldd_kv, Ttot, group, scale);
   else
-    dq_rows<T, DH, CAUSAL, 8, WINDOW>(blockIdx.x, blockIdx.y, z - Hkv, q, k, v, ld, ldk, o, d_o, ldo, lse, delta, cuq, cuk, dq,
-                                      ldd, Ttot, group, scale, w);
+    dq_rows<T, DH, CAUSAL, 8>(blockIdx.x, blockIdx.y, z - Hkv, q, k, v, ld, ldk, o, d_o, ldo, lse, delta, cuq, cuk, dq, ldd,
+                              Ttot, group, scale);
 }
 
 // Lanes per row.  One lane walks every row of the other side by itself, so few rows leave the chip
@@ -358,19 +344,19 @@ void with_lanes(long rows, int heads, int dh, F&& launch) {
   else launch(std::integral_constant<int, 1>{});
 }
 
-template <typename T, int DH, bool CAUSAL, bool WINDOW>
+template <typename T, int DH, bool CAUSAL>
 bm_status fwd_launch(const AttnArgs& a, void* o, float* lse, hipStream_t st) {
   with_lanes(a.T, a.Hq, DH, [&](auto p) {
     constexpr int P = decltype(p)::value;
-    hipLaunchKernelGGL((attn_fwd_generic_kernel<T, DH, CAUSAL, P, WINDOW>), dim3(cdiv(a.max_seqlen, NT / P), a.S, a.Hq), dim3(NT),
+    hipLaunchKernelGGL((attn_fwd_generic_kernel<T, DH, CAUSAL, P>), dim3(cdiv(a.max_seqlen, NT / P), a.S, a.Hq), dim3(NT),
                        0, st, (const T*)a.q, (const T*)a.k, (const T*)a.v, a.ld_qkv, a.kv_ld(), a.cu_dev, a.kv_cu_dev(),
-                       (T*)o, a.Hq * a.dh, lse, a.T, a.Hq / a.Hkv, 1.0f / sqrtf((float)a.dh), a.local);
+                       (T*)o, a.Hq * a.dh, lse, a.T, a.Hq / a.Hkv, 1.0f / sqrtf((float)a.dh));
   });
   BM_CHECK_LAUNCH("attn_fwd_generic");
   return BM_OK;
 }
 
-template <typename T, int DH, bool CAUSAL, bool WINDOW>
+template <typename T, int DH, bool CAUSAL>
 bm_status bwd_launch(const AttnArgs& a, const void* o, const void* d_o, const float* lse, void* dq,
                      void* dk, void* dv, int ldd, float* delta, hipStream_t st) {
   const int ldo = a.Hq * a.dh;
@@ -378,29 +364,29 @@ bm_status bwd_launch(const AttnArgs& a, const void* o, const void* d_o, const fl
   if constexpr (DH <= 64)
     if (!a.in_place && a.T > 0 && a.kv_T() > 0 && eight_lanes(a.T, a.Hq, DH) && eight_lanes(a.kv_T(), a.Hkv, DH)) {
       const int longest = a.max_seqlen > a.kv_max_len() ? a.max_seqlen : a.kv_max_len();
-      hipLaunchKernelGGL((attn_bwd_joint_generic_kernel<T, DH, CAUSAL, WINDOW>), dim3(cdiv(longest, NT / 8), a.S, a.Hkv + a.Hq), dim3(NT),
+      hipLaunchKernelGGL((attn_bwd_joint_generic_kernel<T, DH, CAUSAL>), dim3(cdiv(longest, NT / 8), a.S, a.Hkv + a.Hq), dim3(NT),
                          0, st, (const T*)a.q, (const T*)a.k, (const T*)a.v, a.ld_qkv, a.kv_ld(), (const T*)o, (const T*)d_o,
                          ldo, lse, delta, a.cu_dev, a.kv_cu_dev(), (T*)dq, ldd, (T*)dk, (T*)dv,
-                         a.ld_dkv ? a.ld_dkv : ldd, a.T, a.Hkv, a.Hq / a.Hkv, scale, a.local);
+                         a.ld_dkv ? a.ld_dkv : ldd, a.T, a.Hkv, a.Hq / a.Hkv, scale);
       BM_CHECK_LAUNCH("attn_bwd_generic");
       return BM_OK;
     }
   if (a.T > 0) {
     with_lanes(a.T, a.Hq, DH, [&](auto p) {
       constexpr int P = decltype(p)::value;
-      hipLaunchKernelGGL((attn_dq_generic_kernel<T, DH, CAUSAL, P, WINDOW>), dim3(cdiv(a.max_seqlen, NT / P), a.S, a.Hq),
+      hipLaunchKernelGGL((attn_dq_generic_kernel<T, DH, CAUSAL, P>), dim3(cdiv(a.max_seqlen, NT / P), a.S, a.Hq),
                          dim3(NT), 0, st, (const T*)a.q, (const T*)a.k, (const T*)a.v, a.ld_qkv, a.kv_ld(),
                          (const T*)o, (const T*)d_o, ldo, lse, delta, a.cu_dev, a.kv_cu_dev(), (T*)dq, ldd, a.T,
-                         a.Hq / a.Hkv, scale, a.local);
+                         a.Hq / a.Hkv, scale);
     });
   }
   if (a.kv_T() > 0)
     with_lanes(a.kv_T(), a.Hkv, DH, [&](auto p) {
       constexpr int P = decltype(p)::value;
-      hipLaunchKernelGGL((attn_dkdv_generic_kernel<T, DH, CAUSAL, P, WINDOW>), dim3(cdiv(a.kv_max_len(), NT / P), a.S, a.Hkv),
+      hipLaunchKernelGGL((attn_dkdv_generic_kernel<T, DH, CAUSAL, P>), dim3(cdiv(a.kv_max_len(), NT / P), a.S, a.Hkv),
                          dim3(NT), 0, st, (const T*)a.q, (const T*)a.k, (const T*)a.v, a.ld_qkv, a.kv_ld(),
                          (const T*)d_o, ldo, lse, delta, a.cu_dev, a.kv_cu_dev(), (T*)dk, (T*)dv,
-                         a.ld_dkv ? a.ld_dkv : ldd, a.T, a.Hq / a.Hkv, scale, a.local);
+                         a.ld_dkv ? a.ld_dkv : ldd, a.T, a.Hq / a.Hkv, scale);
     });
   BM_CHECK_LAUNCH("attn_bwd_generic");
   return BM_OK;
@@ -419,23 +405,17 @@ bm_status bwd_launch(const AttnArgs& a, const void* o, const void* d_o, const fl
       return BM_ERR_UNSUPPORTED;                \
   }
 
-// bf16 windows of the matrix-core kernels' head sizes never come here
-template <typename T> constexpr bool window_comes_here(int dh) { return Elt<T>::VEC == 4 || !(dh == 64 || dh == 72 || dh == 128); }
-
 }  // namespace
 
 bm_status attention_forward_generic(const AttnArgs& a, void* o, float* lse, hipStream_t st) {
   if (a.T == 0) return BM_OK;
-#define BM_MASKS(T, D)                                                                    \
-  do {                                                                                    \
-    if constexpr (window_comes_here<T>(D))                                                \
-      if (a.local.window) return fwd_launch<T, D, true, true>(a, o, lse, st);             \
-    return a.causal ? fwd_launch<T, D, true, false>(a, o, lse, st) : fwd_launch<T, D, false, false>(a, o, lse, st); \
-  } while (0)
-#define BM_CALL(D) if (a.dtype == BM_DTYPE_BF16) BM_MASKS(bf16_t, D); else BM_MASKS(float, D)
+#define BM_CALL(D)                                                                             \
+  if (a.dtype == BM_DTYPE_BF16)                                                                \
+    return a.causal ? fwd_launch<bf16_t, D, true>(a, o, lse, st) : fwd_launch<bf16_t, D, false>(a, o, lse, st); \
+  else                                                                                         \
+    return a.causal ? fwd_launch<float, D, true>(a, o, lse, st) : fwd_launch<float, D, false>(a, o, lse, st)
   BM_DH_SWITCH(BM_CALL)
 #undef BM_CALL
-#undef BM_MASKS
   return BM_OK;
 }
 
@@ -443,17 +423,15 @@ bm_status attention_backward_generic(const AttnArgs& a, const void* o, const voi
                                      const float* lse, void* dq, void* dk, void* dv, int ldd,
                                      float* delta, hipStream_t st) {
   if (a.T == 0 && a.kv_T() == 0) return BM_OK;
-#define BM_MASKS(T, D)                                                                                             \
-  do {                                                                                                             \
-    if constexpr (window_comes_here<T>(D))                                                                         \
-      if (a.local.window) return bwd_launch<T, D, true, true>(a, o, d_o, lse, dq, dk, dv, ldd, delta, st);         \
-    return a.causal ? bwd_launch<T, D, true, false>(a, o, d_o, lse, dq, dk, dv, ldd, delta, st)                    \
-                    : bwd_launch<T, D, false, false>(a, o, d_o, lse, dq, dk, dv, ldd, delta, st);                  \
-  } while (0)
-#define BM_CALL(D) if (a.dtype == BM_DTYPE_BF16) BM_MASKS(bf16_t, D); else BM_MASKS(float, D)
+#define BM_CALL(D)                                                                             \
+  if (a.dtype == BM_DTYPE_BF16)                                                                \
+    return a.causal ? bwd_launch<bf16_t, D, true>(a, o, d_o, lse, dq, dk, dv, ldd, delta, st)  \
+                    : bwd_launch<bf16_t, D, false>(a, o, d_o, lse, dq, dk, dv, ldd, delta, st); \
+  else                                                                                         \
+    return a.causal ? bwd_launch<float, D, true>(a, o, d_o, lse, dq, dk, dv, ldd, delta, st)   \
+                    : bwd_launch<float, D, false>(a, o, d_o, lse, dq, dk, dv, ldd, delta, st)
   BM_DH_SWITCH(BM_CALL)
 #undef BM_CALL
-#undef BM_MASKS
   return BM_OK;
 }
 

@@ -1,4 +1,4 @@
-// Attention with a sliding window and first tokens that stay visible: entry points, argument checks, the choice between the
+// Attention with a sliding window and first tokens that stay visible: entry points, argument checks, the choice between
 // matrix-core kernels and those in plain fp32 arithmetic, and few queries in the latter.
 #include "attn_window.h"
 #include "../../include/bigmac_window_attention.h"
@@ -7,9 +7,11 @@
 
 namespace bm {
 
-bool attention_mfma_supported(const AttnArgs& a);
 size_t window_backward_mfma_scratch_bytes(int window, int sinks, int Hq, int Hkv, int dh, int S, int Tq, int Tk);
 bm_status window_forward_mfma(const AttnArgs& a, void* o, float* lse, hipStream_t st);
+bm_status window_forward_plain(const AttnArgs& a, void* o, float* lse, hipStream_t st);
+bm_status window_backward_plain(const AttnArgs& a, const void* o, const void* d_o, const float* lse, void* dq, void* dk, void* dv, int ld_dq,
+                                float* delta, hipStream_t st);
 bm_status window_tokens_mfma(const AttnArgs& a, const TokenSplit& split, void* o, float* lse, hipStream_t st);
 bm_status window_backward_mfma(const AttnArgs& a, const void* o, const void* d_o, const float* lse, void* dq, void* dk,
                                void* dv, int ld_dq, void* scratch, hipStream_t st);
@@ -349,7 +351,9 @@ bm_status window_tokens(const AttnArgs& a, void* scratch, void* o, float* lse, h
   return BM_OK;
 }
 
-constexpr int MAX_ROWS = 1 << 27;        // offsets of rows stay far from 2^31
+constexpr int MAX_ROWS = 1 << 26;        // offsets of rows stay far from 2^31
+
+constexpr int MAX_LD = 1 << 24;          // offsets in a tile of 128 rows stay below 2^32 bytes
 
 bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -383,8 +387,8 @@ bm_status check_args(int dtype, int window, int sinks, int Hq, int Hkv, int dh, 
                      AttnArgs* a, double* pairs) {
   BM_RETURN_IF(check_sizes(dtype, window, sinks, Hq, Hkv, dh, S));
   const int vec = dtype == BM_DTYPE_BF16 ? 8 : 4;
-  BM_ARG_CHECK(ld_q >= (long)Hq * dh && ld_q % vec == 0, "window attention: query row stride %d", ld_q);
-  BM_ARG_CHECK(ld_kv >= (long)Hkv * dh && ld_kv % vec == 0, "window attention: key/value row stride %d", ld_kv);
+  BM_ARG_CHECK(ld_q >= (long)Hq * dh && ld_q % vec == 0 && ld_q < MAX_LD, "window attention: query row stride %d", ld_q);
+  BM_ARG_CHECK(ld_kv >= (long)Hkv * dh && ld_kv % vec == 0 && ld_kv < MAX_LD, "window attention: key/value row stride %d", ld_kv);
   BM_ARG_CHECK(c.cu_q_dev && c.cu_q_host, "window attention: NULL offsets");
   const bool own = c.k_begin_dev || c.k_end_dev || c.k_begin_host || c.k_end_host;
   BM_ARG_CHECK(!own || (c.k_begin_dev && c.k_end_dev && c.k_begin_host && c.k_end_host),
@@ -403,8 +407,8 @@ bm_status check_args(int dtype, int window, int sinks, int Hq, int Hkv, int dh, 
     *pairs += pairs_of(lq, lk, window, sinks);
   }
   // grids stay below 2^32 threads
-  BM_ARG_CHECK((long)c.cu_q_host[S] * Hq < (1L << 27) && (long)rows * Hkv < (1L << 27) && (long)S * Hq < (1L << 23),
-               "window attention: %d sequences, %d queries of %d heads and %d keys of %d (rows x heads below 2^27, sequences x heads below 2^23)",
+  BM_ARG_CHECK((long)c.cu_q_host[S] * Hq < (1L << 26) && (long)rows * Hkv < (1L << 26) && (long)S * Hq < (1L << 22),
+               "window attention: %d sequences, %d queries of %d heads and %d keys of %d (rows x heads below 2^26, sequences x heads below 2^22)",
                S, c.cu_q_host[S], Hq, rows, Hkv);
   a->dtype = dtype; a->causal = 1; a->Hq = Hq; a->Hkv = Hkv; a->dh = dh;
   a->ld_qkv = ld_q; a->cu_dev = c.cu_q_dev; a->cu_host = c.cu_q_host; a->S = S; a->T = c.cu_q_host[S]; a->max_seqlen = max_q;
@@ -456,7 +460,7 @@ extern "C" bm_status bm_window_attention_forward(int32_t dtype, int32_t window, 
   ProfScope prof(PROF_ATTN_FWD, 4.0 * dh * Hq * pairs, st);
   if (a.max_seqlen * (long)(Hq / Hkv) <= TOKEN_ROWS) return window_tokens(a, scratch, o, lse, st);
   if (mfma_head(dtype, dh)) return window_forward_mfma(a, o, lse, st);
-  return attention_forward_generic(a, o, lse, st);
+  return window_forward_plain(a, o, lse, st);
 }
 
 extern "C" size_t bm_window_attention_backward_scratch_bytes(int32_t dtype, int32_t window, int32_t sinks, int32_t Hq,
@@ -491,5 +495,5 @@ extern "C" bm_status bm_window_attention_backward(int32_t dtype, int32_t window,
   hipStream_t st = (hipStream_t)hip_stream;
   ProfScope prof(PROF_ATTN_BWD, 10.0 * dh * Hq * pairs, st);
   if (mfma_head(dtype, dh)) return window_backward_mfma(a, o, d_o, lse, dq, dk, dv, ld_dq, scratch, st);
-  return attention_backward_generic(a, o, d_o, lse, dq, dk, dv, ld_dq, (float*)scratch, st);
+  return window_backward_plain(a, o, d_o, lse, dq, dk, dv, ld_dq, (float*)scratch, st);
 }
