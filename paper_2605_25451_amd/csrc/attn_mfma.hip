@@ -470,14 +470,33 @@ __global__ __launch_bounds__(256, 2) void fa_fwd_kernel(
       }
     }
     // mask: keys past the sequence end, and keys after the query under a causal mask
+    if constexpr (WINDOW && MASKED) {
+      // (element (b, r): key key0 + half * 4 + e; most tiles that need a test need one of the two)
+      const int first_at = off + q0 + wave_u * 32, ahead = off + qpos - key0 - half * 4;
+      if (key0 + FK - 1 > first_at)
+#pragma unroll
+        for (int b = 0; b < FK / 32; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sacc[b][r] = b * 32 + (r >> 2) * 8 + (r & 3) > ahead ? -INFINITY : sacc[b][r];
+      if (first_at + 31 - key0 >= w.window && key0 + FK > w.sinks) {
+        const int behind = ahead - w.window, sinks = w.sinks - key0 - half * 4;
+#pragma unroll
+        for (int b = 0; b < FK / 32; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int e = b * 32 + (r >> 2) * 8 + (r & 3);
+            sacc[b][r] = e <= behind && e >= sinks ? -INFINITY : sacc[b][r];
+          }
+      }
+    }
 #pragma unroll
     for (int b = 0; b < FK / 32; ++b) {
       float mx = -INFINITY;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        if (MASKED) {
+        if (MASKED && !WINDOW) {
           const int key = key0 + b * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
-          if (WINDOW ? hidden(w, key, off + qpos) : key >= Lk || (CAUSAL && key > qpos)) sacc[b][r] = -INFINITY;
+          if (key >= Lk || (CAUSAL && key > qpos)) sacc[b][r] = -INFINITY;
         }
         mx = fmaxf(mx, sacc[b][r]);
       }
@@ -921,7 +940,7 @@ __device__ inline bool find_part(const FirstKeys& f, const int32_t* __restrict__
   return false;
 }
 // Where a workgroup of dK/dV works with it: a tile of KEYS keys, or a part of the first one, and the query rows that it walks
-struct KeyTile { int seq, kt, part, hk_gs, qlo, qhi; };
+struct KeyTile { int seq, kt, part, hk_gs, qlo, qhi, from; };      // from: the first key that is not the parts'
 template <int KEYS>
 __device__ inline bool find_key_tile(const FirstKeys& f, const SeqOrder& ord, const int32_t* __restrict__ cu,
                                      const int32_t* __restrict__ cuq, int S, int heads, int block, KeyTile* t) {
@@ -940,9 +959,10 @@ __device__ inline bool find_key_tile(const FirstKeys& f, const SeqOrder& ord, co
   t->kt = n - 1 - t->kt;
   t->part = -1;
   const int L = f.mask.key_end[t->seq] - cu[t->seq], Lq = cuq[t->seq + 1] - cuq[t->seq], off = L - Lq;
-  const bool seen_by_all = t->kt == 0 && f.mask.sinks > 0;
-  if (seen_by_all && f.parts(Lq) > 0) return false;
-  t->qlo = max(0, t->kt * KEYS - off);
+  const bool in_parts = t->kt == 0 && f.parts(Lq) > 0, seen_by_all = t->kt == 0 && f.mask.sinks > 0 && !in_parts;
+  t->from = in_parts ? BK_KEYS : 0;
+  if (in_parts && (KEYS == BK_KEYS || L <= BK_KEYS)) return false;
+  t->qlo = max(0, t->kt * KEYS + t->from - off);
   t->qhi = seen_by_all ? Lq : min(Lq, min((t->kt + 1) * KEYS, L) - 1 - off + f.mask.window);
   return true;
 }
@@ -1474,14 +1494,14 @@ __device__ inline int fresh_lane() {
 }
 
 constexpr int DKDV_WIDE_LDS_BYTES = WideTile::RING * WideTile::BYTES + 2 * 4 * 4096;
-template <bool CAUSAL>
+template <bool CAUSAL, bool WINDOW = false>
 __device__ inline void dkdv_wide_tile(
     unsigned char* lds, int block, const bf16_t* __restrict__ q, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v, int ld,
     int ldk, const bf16_t* __restrict__ d_o, int ldo, const float* __restrict__ lse,
     const float* __restrict__ delta, const int32_t* __restrict__ cuq, const int32_t* __restrict__ cu,
     int S, bf16_t* __restrict__ dk, bf16_t* __restrict__ dv, int ldd, int Tq, int Ttot, int Hkv, int group,
     float scale, float scale_log2, int gsplit,
-    float* __restrict__ part /* [gsplit][2][Ttot][Hkv*DH] fp32 when gsplit > 1 */, SeqOrder ord) {
+    float* __restrict__ part /* [gsplit][2][Ttot][Hkv*DH] fp32 when gsplit > 1 */, SeqOrder ord, const FirstKeys& first = {}) {
   constexpr int DH = 128, KS = 8, NB = 4, KB = 2;
   using W = WideTile;
   using RT = RunTile<DH>;
@@ -1489,27 +1509,39 @@ __device__ inline void dkdv_wide_tile(
   unsigned char* const tiles = lds;
   unsigned char* const Pbuf = lds + W::RING * W::BYTES;  // [parity][pair][key block, half k-step][lane]
   int seq, kt, nkt, tile_id, hk, hk_gs;
-  tile_and_head(Hkv * gsplit, &tile_id, &hk_gs, block);
+  KeyTile where;                                       // sliding window
+  if constexpr (WINDOW) {
+    if (!find_key_tile<WIDE_KEYS>(first, ord, cu, cuq, S, Hkv * gsplit, block, &where)) return;
+    hk_gs = where.hk_gs; seq = where.seq; kt = where.kt;
+    where.qlo = __builtin_amdgcn_readfirstlane(where.qlo);
+    where.qhi = __builtin_amdgcn_readfirstlane(where.qhi);
+  } else {
+    tile_and_head(Hkv * gsplit, &tile_id, &hk_gs, block);
+  }
   hk = hk_gs / gsplit;
   const int gs = hk_gs % gsplit;
   const int gpart = group / gsplit;
-  if (!find_tile(cu, ord, S, WIDE_KEYS, tile_id, &seq, &kt, &nkt)) return;
-  kt = nkt - 1 - kt;                                   // early key tiles see the most queries
-  const int lo = cu[seq], L = cu[seq + 1] - lo;
+  if constexpr (!WINDOW) {
+    if (!find_tile(cu, ord, S, WIDE_KEYS, tile_id, &seq, &kt, &nkt)) return;
+    kt = nkt - 1 - kt;                                   // early key tiles see the most queries
+  }
+  const int lo = cu[seq], L = (WINDOW ? first.mask.key_end[seq] : cu[seq + 1]) - lo;
   const int loq = cuq[seq], Lq = cuq[seq + 1] - loq;
   const int kb0 = kt * WIDE_KEYS;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int pair = wave & 3;                            // wavefronts w and w+4 share a SIMD
   const int key0 = kb0 + pair * 64;                     // the pair's first key
-  const int qstart = CAUSAL ? kb0 : 0;
-  const int nqt = Lq > qstart ? (Lq - qstart + W::ROWS - 1) / W::ROWS : 0;   // no query: dk = dv = 0
+  const int off = WINDOW ? L - Lq : 0, qstart = WINDOW ? where.qlo : CAUSAL ? kb0 : 0, qend = WINDOW ? where.qhi : Lq;
+  const int nqt = qend > qstart ? (qend - qstart + W::ROWS - 1) / W::ROWS : 0;   // no query: dk = dv = 0
   const int iters = nqt * gpart;
   const int head0 = hk * group + gs * gpart;
   // A pair needs the mask tests where its keys are cut by the sequence end, on the last query tile when that is
   // cut, and up to its last key under a causal mask; it sits out the query tiles before its first key,
   // and all of them if it lies past the sequence.
   const bool keys_cut = key0 + 64 > L;
-  const int skip = key0 >= L ? nqt : CAUSAL ? min(nqt, (key0 - qstart) / W::ROWS) : 0;
+  // (WINDOW: and those behind the window of its last key, if its keys are no first tokens)
+  const int skip = key0 >= L || (WINDOW && key0 < where.from) ? nqt : CAUSAL ? min(nqt, (WINDOW ? max(0, key0 - off - qstart) : key0 - qstart) / W::ROWS) : 0;
+  const int stop = WINDOW && key0 >= first.mask.sinks ? max(skip, min(nqt, (key0 + 63 - off + first.mask.window - qstart + W::ROWS - 1) / W::ROWS)) : nqt;
   const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char*)tiles;
   constexpr int LOADS = 3;
 
@@ -1624,17 +1656,20 @@ __device__ inline void dkdv_wide_tile(
       if constexpr (ROLE == 0) {
         x[0] = x[1] = f32x16{};
         scores(n, x);
-        if (keys_cut || q0 + W::ROWS > Lq || (CAUSAL && q0 < key0 + 63)) {
+        if (WINDOW ? keys_cut || q0 + W::ROWS > qend || !all_visible(first.mask, key0, 64, off + q0, W::ROWS)
+                   : keys_cut || q0 + W::ROWS > Lq || (CAUSAL && q0 < key0 + 63)) {
           asm volatile("");                                 // keeps the tests out of the steps that need none
           const int l = fresh_lane(), h4 = (l >> 5) * 4, ki = key0 + (l & 31);
-          const int q_left = Lq - q0 - h4, k_left = L - ki, ahead = ki - q0 - h4;
+          const int q_left = qend - q0 - h4, k_left = L - ki, ahead = ki - off - q0 - h4;
+          const int behind = ahead + (WINDOW ? first.mask.window : 0), sinks = WINDOW ? first.mask.sinks - ki : 0;
 #pragma unroll
           for (int g = 0; g < 4; ++g)
 #pragma unroll
             for (int b = 0; b < KB; ++b)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                if (q_left <= g * 8 + e || k_left <= b * 32 || (CAUSAL && ahead > g * 8 + e - b * 32))
+                if (q_left <= g * 8 + e || k_left <= b * 32 || (CAUSAL && ahead > g * 8 + e - b * 32) ||
+                    (WINDOW && behind <= g * 8 + e - b * 32 && sinks <= b * 32))
                   x[b][g * 4 + e] = -INFINITY;              // P = 0
         }
         const unsigned char* stats = tile_of(n) + STATS_AT + (fresh_lane() >> 5) * 16;
@@ -1653,7 +1688,8 @@ __device__ inline void dkdv_wide_tile(
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             op[b][t] = acc_to_operand(x[b], t);
-            *reinterpret_cast<bf16x8*>(my_p + (b * 2 + t) * 1024) = op[b][t];
+            if constexpr (WINDOW) *reinterpret_cast<f16x8*>(my_p + (b * 2 + t) * 1024) = handed_p(x[b], t);
+            else *reinterpret_cast<bf16x8*>(my_p + (b * 2 + t) * 1024) = op[b][t];
           }
         hand_over(n);
       } else {
@@ -1684,7 +1720,7 @@ __device__ inline void dkdv_wide_tile(
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[b][t * 8 + e] *= (float)op[b][t][e];
+            for (int e = 0; e < 8; ++e) x[b][t * 8 + e] *= WINDOW ? (float)__builtin_bit_cast(f16x8, op[b][t])[e] : (float)op[b][t][e];
             op[b][t] = acc_to_operand(x[b], t);
           }
       }
@@ -1698,15 +1734,18 @@ __device__ inline void dkdv_wide_tile(
     barrier();
     for (int n = 0; n < iters;) {
       for (int t = 0; t < skip; ++t, ++n) { hand_over(n); fetch(); }
-      for (int t = skip; t < nqt; ++t, ++n) step(n, qstart + t * W::ROWS);
+      for (int t = skip; t < stop; ++t, ++n) step(n, qstart + t * W::ROWS);
+      if constexpr (WINDOW)
+        for (int t = stop; t < nqt; ++t, ++n) { hand_over(n); fetch(); }
     }
 
-    const float out_scale = ROLE == 0 ? 1.0f : scale;     // dV as it is, dK times the softmax scale
+    // dV as it is, dK times the softmax scale
+    const float out_scale = ROLE == 0 ? 1.0f : WINDOW ? scale * (1.0f / HANDED_SCALE) : scale;
     const int l = fresh_lane();
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
       const int key = key0 + b * 32 + (l & 31);
-      if (key >= L) continue;
+      if (key >= L || (WINDOW && key < where.from)) continue;
       const size_t row = (size_t)(lo + key);
 #pragma unroll
       for (int j = 0; j < NB; ++j)
@@ -2349,14 +2388,19 @@ __global__ __launch_bounds__(256, 2) void fa_window_bwd_kernel(WindowBwdArgs a, 
   }
 }
 
-template <int DH>
+template <int DH, bool WIDE>
 __global__ __launch_bounds__(512, 2) void fa_window_bwd512_kernel(WindowBwdArgs a, SeqOrder ord_kv, SeqOrder ord_q, FirstKeys first) {
-  constexpr int KV = dkdv_pair_lds_bytes<DH>(), Q = DH == 128 ? DQ_ALT_LDS_BYTES : 2 * dq_lds_bytes<DH>();
+  constexpr int PAIR = dkdv_pair_lds_bytes<DH>(), KV = WIDE && DKDV_WIDE_LDS_BYTES > PAIR ? DKDV_WIDE_LDS_BYTES : PAIR;
+  constexpr int Q = DH == 128 ? DQ_ALT_LDS_BYTES : 2 * dq_lds_bytes<DH>();
   __shared__ __attribute__((aligned(1024))) unsigned char lds[KV > Q ? KV : Q];
   const int Hq = a.Hkv * a.group;
-  if ((int)blockIdx.x < a.kv_wgs) {
+  if ((int)blockIdx.x < (WIDE ? first.wgs : a.kv_wgs)) {
     dkdv_pair_tile<DH, true, true>(lds, blockIdx.x, a.q, a.k, a.v, a.ld, a.ldk, a.d_o, a.ldo, a.lse, a.delta, a.cuq, a.cuk, a.S, a.dk, a.dv,
                                    a.ldd_kv, a.Tq, a.Tk, a.Hkv, a.group, a.scale, a.scale_log2, a.gsplit, a.part, ord_kv, first);
+  } else if (WIDE && (int)blockIdx.x < a.kv_wgs) {
+    if constexpr (WIDE)
+      dkdv_wide_tile<true, true>(lds, blockIdx.x, a.q, a.k, a.v, a.ld, a.ldk, a.d_o, a.ldo, a.lse, a.delta, a.cuq, a.cuk, a.S, a.dk, a.dv,
+                                 a.ldd_kv, a.Tq, a.Tk, a.Hkv, a.group, a.scale, a.scale_log2, a.gsplit, a.part, ord_kv, first);
   } else if constexpr (DH == 128) {
     dq_alt_tile<true, true>(lds, blockIdx.x - a.kv_wgs, a.q, a.k, a.v, a.ld, a.ldk, a.d_o, a.ldo, a.lse, a.delta, a.cuq, a.cuk, a.S, a.dq,
                             a.ldd, a.Tq, Hq, a.group, a.scale, a.scale_log2, ord_q, first.mask);
@@ -2650,6 +2694,17 @@ WindowBwd window_bwd(int window, int sinks, int Hq, int Hkv, int dh, int S, int 
   return w;
 }
 
+// The wide dK/dV kernel (head size 128) or the one with 128 keys per workgroup?  dQ fills what either leaves of the chip, so the wide one needs no
+// whole rounds, but sequences that 256-key tiles cut about as well, and enough workgroups.  Whole backward, us, narrow -> wide, 32 / 8 heads: 8192
+// tokens, window 2048 1055 -> 950, 1024 658 -> 610, 256 488 -> 458; 24 documents 338 -> 310; 4096 386 -> 343; 32768, window 4096, 6500 -> 5757; 16 / 16
+// heads, 2048 tokens (128 workgroups) 115 -> 109; but 2 documents in 777 (128 of 32 / 8, 64 of 16 / 16 heads) 64 -> 76, 56 -> 62; 8 / 1 heads, 2048 (64)
+// 106 -> 118.
+bool window_wide(const AttnArgs& a, int gsplit) {
+  const int tw = count_tiles(a.kv_cu_host(), a.key_end_host, a.S, WIDE_KEYS), tn = count_tiles(a.kv_cu_host(), a.key_end_host, a.S, BK_KEYS);
+  const long wgs = (long)tw * a.Hkv * gsplit;
+  return tw * 8L <= tn * 5L && (wgs >= NUM_CU || (wgs >= NUM_CU / 2 && tw >= 4 * a.S));
+}
+
 template <int DH>
 bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, const float* lse, void* dq, void* dk, void* dv,
                             int ldd, float* delta, hipStream_t st) {
@@ -2676,11 +2731,14 @@ bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, c
     hipLaunchKernelGGL((fa_delta_kernel<DH>), dim3(cdiv((long)a.T * a.Hq * DeltaLanes<DH>::N, 256)), dim3(256), 0, st,
                        (const bf16_t*)o, (const bf16_t*)d_o, ldo, delta, a.T, a.Hq);
   const int query_rows = DH == 128 ? AQ : FQ, heads_per_wg = DH == 72 ? 2 : 1;
+  bool wide = false;
+  if constexpr (DH == 128) wide = window_wide(a, wb.gsplit);
+  const int key_rows = wide ? WIDE_KEYS : BK_KEYS;
   const int ktiles = count_tiles(a.kv_cu_host(), a.key_end_host, a.S, BK_KEYS), qtiles = count_tiles(a.cu_host, a.S, query_rows);
-  const int kv_wgs = first.wgs + ktiles * a.Hkv * wb.gsplit, q_wgs = qtiles * cdiv(a.Hq, heads_per_wg);
+  const int kv_wgs = first.wgs + (wide ? count_tiles(a.kv_cu_host(), a.key_end_host, a.S, WIDE_KEYS) : ktiles) * a.Hkv * wb.gsplit, q_wgs = qtiles * cdiv(a.Hq, heads_per_wg);
   // (head size 72: as in bwd_plan)
   const bool together = DH != 72 || kv_wgs + q_wgs <= NUM_CU * 3 / 2 || (kv_wgs > NUM_CU && kv_wgs + q_wgs <= 2 * NUM_CU);
-  const SeqOrder ord_kv = make_seq_order(a.kv_cu_host(), a.cu_host, a.S, BK_KEYS, false, a.key_end_host);
+  const SeqOrder ord_kv = make_seq_order(a.kv_cu_host(), a.cu_host, a.S, key_rows, false, a.key_end_host);
   const SeqOrder ord_q = make_seq_order(a.cu_host, a.cu_host, a.S, query_rows, false);
   const WindowBwdArgs w{(const bf16_t*)a.q, (const bf16_t*)a.k, (const bf16_t*)a.v, (const bf16_t*)d_o, lse, delta, a.cu_dev, a.kv_cu_dev(),
                         (bf16_t*)dq, (bf16_t*)dk, (bf16_t*)dv, part, a.ld_qkv, a.kv_ld(), ldo, ldd, a.ld_dkv, a.S, a.T, Tk, a.Hkv, group,
@@ -2688,16 +2746,22 @@ bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, c
   const int wgs = kv_wgs + (together ? q_wgs : 0);
   if (wgs > 0) {
     if constexpr (DH <= 64) hipLaunchKernelGGL(fa_window_bwd_kernel<DH>, dim3(wgs), dim3(256), 0, st, w, ord_kv, ord_q, first);
-    else hipLaunchKernelGGL(fa_window_bwd512_kernel<DH>, dim3(wgs), dim3(512), 0, st, w, ord_kv, ord_q, first);
+    else {
+      auto kern = fa_window_bwd512_kernel<DH, false>;
+      if constexpr (DH == 128) if (wide) kern = fa_window_bwd512_kernel<DH, true>;
+      hipLaunchKernelGGL(kern, dim3(wgs), dim3(512), 0, st, w, ord_kv, ord_q, first);
+    }
   }
   if constexpr (DH == 72)
     if (!together && qtiles > 0)
       hipLaunchKernelGGL((fa_window_dq_kernel<DH>), dim3(qtiles * a.Hq), dim3(256), 0, st, w, ord_q, a.local);
   const int all_tiles = wb.gsplit > 1;
-  if (kv_wgs > 0 && (all_tiles || parts > 0))
+  if (kv_wgs > 0 && (all_tiles || parts > 0)) {
+    const SeqOrder ord = wide ? make_seq_order(a.kv_cu_host(), a.cu_host, a.S, BK_KEYS, false, a.key_end_host) : ord_kv;
     hipLaunchKernelGGL(fa_window_reduce_kernel, dim3(all_tiles ? ktiles : in_parts, a.Hkv, BK_KEYS / 16), dim3(256), 0, st, part,
                        wb.gsplit, a.cu_dev, a.kv_cu_dev(), a.S, Tk, a.Hkv, a.dh, (bf16_t*)dk, (bf16_t*)dv, a.ld_dkv, all_tiles,
-                       ord_kv, first);
+                       ord, first);
+  }
   BM_CHECK_LAUNCH("fa_window_bwd");
   return BM_OK;
 }

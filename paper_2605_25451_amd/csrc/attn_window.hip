@@ -218,48 +218,58 @@ __global__ __launch_bounds__(256) void window_map_kernel(const int32_t* __restri
   for (int i = 0; i < mine; ++i) t.map[3 * S + 1 + at[0] + i] = s;
 }
 
-// o and lse from the parts of a sequence, in part order: four threads share a column, each a quarter of the parts.
-// grid: x sequences of more than one part, y kv heads, z rows.
-constexpr int JOIN_COLS = 128;
+// o and lse from the parts of a sequence: 32 threads share a row, four columns each, and take every eighth part in order; the eight are
+// joined in order.  grid: x sequences of more than one part, y kv heads, z rows.
 template <typename T>
-__global__ __launch_bounds__(4 * JOIN_COLS) void window_join_kernel(const int32_t* __restrict__ cu, int S, T* __restrict__ o, int ldo,
-                                                                    float* __restrict__ lse, int Ttot, int Hkv, int group, int dh,
-                                                                    TokenSplit split) {
-  __shared__ float tops[4], sums[4], vals[3][JOIN_COLS];
+__global__ __launch_bounds__(256) void window_join_kernel(const int32_t* __restrict__ cu, int S, T* __restrict__ o, int ldo,
+                                                          float* __restrict__ lse, int Ttot, int Hkv, int group, int dh, TokenSplit split) {
+  __shared__ float tops[8], sums[8];
+  __shared__ float4 vals[8][32];
   const int hk = blockIdx.y, row = blockIdx.z;
   const TokenPart p = split_sequence(split, S, blockIdx.x);
   const int lo = cu[p.seq], rows = (cu[p.seq + 1] - lo) * group, n = p.parts;
   if (row >= rows) return;
-  const int c = threadIdx.x % JOIN_COLS, quarter = threadIdx.x / JOIN_COLS, share = (n + 3) / 4;
-  const int i0 = quarter * share, i1 = min(n, i0 + share);
+  const int c = threadIdx.x % 32, eighth = threadIdx.x / 32, col = min(c * 4, dh - 4);
   const size_t step = (size_t)Hkv * split.rows, at = ((size_t)p.place * Hkv + hk) * split.rows + row;
-  float top = NO_MAX;
-#pragma unroll 8
-  for (int i = i0; i < i1; ++i) top = fmaxf(top, split.stats[(at + i * step) * 2]);
-  if (c == 0) tops[quarter] = top;
-  float sum = 0.f, val = 0.f;
-#pragma unroll 8
-  for (int i = i0; i < i1; ++i) {
-    const float f = exp2f(split.stats[(at + i * step) * 2] - top);
-    sum = fmaf(f, split.stats[(at + i * step) * 2 + 1], sum);
-    val = fmaf(f, split.sums[(at + i * step) * dh + min(c, dh - 1)], val);
+  float top = NO_MAX, sum = 0.f;
+  float4 val = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = eighth; i < n; i += 8) {
+    const float2 s = *reinterpret_cast<const float2*>(split.stats + (at + i * step) * 2);
+    const float4 x = *reinterpret_cast<const float4*>(split.sums + (at + i * step) * dh + col);
+    const float m = fmaxf(top, s.x), old = exp2f(top - m), f = exp2f(s.x - m);
+    top = m;
+    sum = sum * old + f * s.y;
+    val.x = val.x * old + f * x.x;
+    val.y = val.y * old + f * x.y;
+    val.z = val.z * old + f * x.z;
+    val.w = val.w * old + f * x.w;
   }
-  if (c == 0) sums[quarter] = sum;
-  if (quarter > 0) vals[quarter - 1][c] = val;
+  if (c == 0) { tops[eighth] = top; sums[eighth] = sum; }
+  vals[eighth][c] = val;
   __syncthreads();
-  if (quarter > 0 || c >= dh) return;
-  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-  float f = exp2f(tops[0] - top);
-  sum = f * sums[0];
-  val *= f;
+  if (eighth > 0 || c * 4 >= dh) return;
+  top = NO_MAX;
 #pragma unroll
-  for (int x = 1; x < 4; ++x) {
-    f = exp2f(tops[x] - top);
+  for (int x = 0; x < 8; ++x) top = fmaxf(top, tops[x]);
+  sum = 0.f;
+  val = float4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int x = 0; x < 8; ++x) {
+    const float f = exp2f(tops[x] - top);
+    const float4 y = vals[x][c];
     sum = fmaf(f, sums[x], sum);
-    val = fmaf(f, vals[x - 1][c], val);
+    val.x = fmaf(f, y.x, val.x);
+    val.y = fmaf(f, y.y, val.y);
+    val.z = fmaf(f, y.z, val.z);
+    val.w = fmaf(f, y.w, val.w);
   }
   const int t = lo + row / group, h = hk * group + row % group;
-  o[(size_t)t * ldo + h * dh + c] = Elt<T>::from_f(val / sum);
+  T* out = o + (size_t)t * ldo + h * dh + c * 4;
+  out[0] = Elt<T>::from_f(val.x / sum);
+  out[1] = Elt<T>::from_f(val.y / sum);
+  out[2] = Elt<T>::from_f(val.z / sum);
+  out[3] = Elt<T>::from_f(val.w / sum);
   if (c == 0) lse[(size_t)h * Ttot + t] = (top + log2f(sum)) * LN2;
 }
 
@@ -340,7 +350,7 @@ bm_status window_tokens(const AttnArgs& a, void* scratch, void* o, float* lse, h
     BM_CHECK_LAUNCH("window_token");
   }
   if (joins > 0) {
-    const dim3 grid(joins, a.Hkv, t.rows), block(4 * JOIN_COLS);
+    const dim3 grid(joins, a.Hkv, t.rows), block(256);
 #define BM_L(TT)                                                                                                           \
   hipLaunchKernelGGL(window_join_kernel<TT>, grid, block, 0, st, a.cu_dev, a.S, (TT*)o, a.Hq * a.dh, lse, a.T, a.Hkv, a.Hq / a.Hkv, \
                      a.dh, t)
