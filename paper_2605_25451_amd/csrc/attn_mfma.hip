@@ -2440,7 +2440,9 @@ __device__ inline bool find_split(const FirstKeys& f, const int32_t* __restrict_
   return false;
 }
 // dk, dv of the key tiles that were left in fp32 -- parts of the first keys, q-head parts of any -- summed in order and
-// rounded once.  grid: x the key tiles (all of them, or with one q-head part the first ones that are in parts), y kv heads, z 16 rows.
+// rounded once.  grid: x the key tiles (all of them, or with one q-head part the first ones that are in parts), y kv heads, z few rows, so
+// that a thread has one column to sum (up to hundreds of partials, eight in flight).
+constexpr int REDUCE_ROWS = 4;
 __global__ __launch_bounds__(256) void fa_window_reduce_kernel(
     const float* __restrict__ part, int gsplit, const int32_t* __restrict__ cuq, const int32_t* __restrict__ cuk, int S, int Ttot,
     int Hkv, int dh, bf16_t* __restrict__ dk, bf16_t* __restrict__ dv, int ldd, int all_tiles, SeqOrder ord, FirstKeys first) {
@@ -2477,16 +2479,16 @@ __global__ __launch_bounds__(256) void fa_window_reduce_kernel(
     row_stride = (size_t)Hkv * dh;
     src = part + (size_t)(lo + kt * BK_KEYS) * row_stride + hk * dh;
   }
-  const int row0 = blockIdx.z * 16, rows = min(16, L - kt * BK_KEYS - row0), quads = dh / 4;
+  const int row0 = blockIdx.z * REDUCE_ROWS, rows = min(REDUCE_ROWS, L - kt * BK_KEYS - row0), quads = dh / 4;
   for (int i = threadIdx.x; i < 2 * rows * quads; i += 256) {
     const int c = i % quads * 4, r = i / quads % rows, which = i / quads / rows;
     const float* p = src + which * which_stride + (size_t)(row0 + r) * row_stride + c;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < n; ++j)
-      for (int g = 0; g < gsplit; ++g) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(p + j * step_part + g * step_gs);
-        s[0] += v[0]; s[1] += v[1]; s[2] += v[2]; s[3] += v[3];
-      }
+#pragma unroll 8
+    for (int j = 0; j < n * gsplit; ++j) {                 // parts in order, q-head parts within them
+      const f32x4 v = *reinterpret_cast<const f32x4*>(p + (j / gsplit) * step_part + (j % gsplit) * step_gs);
+      s[0] += v[0]; s[1] += v[1]; s[2] += v[2]; s[3] += v[3];
+    }
     const bf16x4 w = {(bf16_t)s[0], (bf16_t)s[1], (bf16_t)s[2], (bf16_t)s[3]};
     *reinterpret_cast<bf16x4*>((which == 0 ? dk : dv) + (size_t)(lo + kt * BK_KEYS + row0 + r) * ldd + hk * dh + c) = w;
   }
@@ -2758,7 +2760,7 @@ bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, c
   const int all_tiles = wb.gsplit > 1;
   if (kv_wgs > 0 && (all_tiles || parts > 0)) {
     const SeqOrder ord = wide ? make_seq_order(a.kv_cu_host(), a.cu_host, a.S, BK_KEYS, false, a.key_end_host) : ord_kv;
-    hipLaunchKernelGGL(fa_window_reduce_kernel, dim3(all_tiles ? ktiles : in_parts, a.Hkv, BK_KEYS / 16), dim3(256), 0, st, part,
+    hipLaunchKernelGGL(fa_window_reduce_kernel, dim3(all_tiles ? ktiles : in_parts, a.Hkv, BK_KEYS / REDUCE_ROWS), dim3(256), 0, st, part,
                        wb.gsplit, a.cu_dev, a.kv_cu_dev(), a.S, Tk, a.Hkv, a.dh, (bf16_t*)dk, (bf16_t*)dv, a.ld_dkv, all_tiles,
                        ord, first);
   }
