@@ -79,8 +79,9 @@ bm_status bm_qk_rotary_backward(const bm_qk_rotary_desc* desc, int32_t T, const 
  *   sinks            0..BM_WINDOW_MAX_SINKS
  *   q         dev    rows of ld_q elements, Hq heads of dh, sequences one behind the other by cu_q [S+1]
  *   k, v      dev    rows of ld_kv elements, Hkv heads; sequence s holds rows k_begin[s] .. k_end[s]-1.  The four
- *                    arrays are NULL where keys have the queries' packing; sequences do not overlap, but rows may lie
- *                    between them (slots of a cache), which are neither read nor written
+ *                    arrays are NULL where keys have the queries' packing.  Rows may lie between the sequences (slots of a
+ *                    cache), which are neither read nor written.  The forward pass takes sequences in any order, and ones that
+ *                    share rows (a common beginning); the backward pass takes them one behind the other
  *   cu_q, k_begin, k_end are given twice, in device and in host memory, with the same values
  *   o, d_o    dev    [Tq, Hq*dh], lse dev [Hq, Tq] fp32, Tq = cu_q[S]
  * S < 65536, Hq < 65536, Tq x Hq and Tk x Hkv below 2^26, S x Hq below 2^22, row strides below 2^24.  Lq <= Lk for every sequence; Lq = 0 is allowed (its
@@ -103,7 +104,8 @@ bm_status bm_window_attention_forward(int32_t dtype, int32_t window, int32_t sin
                                       void* o, float* lse, void* scratch, size_t scratch_bytes, void* hip_stream);
 
 /* The scratch is that of exactly these sizes.  Gradients from d_o and the forward's q, k, v, o and lse: dq in rows of ld_dq elements, dk and dv (rows k_begin ..
- * k_end-1 of every sequence) in rows of ld_dkv; overwritten, and apart from the inputs. */
+ * k_end-1 of every sequence) in rows of ld_dkv; overwritten.  Gradients that lie over an input are refused; columns of the same
+ * rows beside it are not. */
 size_t    bm_window_attention_backward_scratch_bytes(int32_t dtype, int32_t window, int32_t sinks, int32_t Hq,
                                                      int32_t Hkv, int32_t dh, int32_t S, int32_t Tq, int32_t Tk);
 bm_status bm_window_attention_backward(int32_t dtype, int32_t window, int32_t sinks, int32_t Hq, int32_t Hkv, int32_t dh,

@@ -428,6 +428,17 @@ bm_status check_args(int dtype, int window, int sinks, int Hq, int Hkv, int dh, 
   return BM_OK;
 }
 
+// Do rows of `heads` heads at p and at x share an element?  Equal strides: their columns may lie side by side.
+bool share(const void* p, int rows_p, long ld_p, long width_p, const void* x, int rows_x, long ld_x, long width_x, int size) {
+  if (rows_p == 0 || rows_x == 0) return false;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(x);
+  const uintptr_t a_end = a + ((rows_p - 1) * ld_p + width_p) * size, b_end = b + ((rows_x - 1) * ld_x + width_x) * size;
+  if (a >= b_end || b >= a_end) return false;
+  if (ld_p != ld_x) return true;
+  const uintptr_t row = (uintptr_t)ld_p * size, ahead = a >= b ? (a - b) % row : (row - (b - a) % row) % row;   // of a's columns against b's
+  return ahead < (uintptr_t)width_x * size || row - ahead < (uintptr_t)width_p * size;
+}
+
 bm_status check_scratch(const void* scratch, size_t bytes, size_t need) {
   BM_ARG_CHECK(al16(scratch), "window attention: misaligned scratch");
   if (need > 0 && (!scratch || bytes < need)) {
@@ -499,6 +510,20 @@ extern "C" bm_status bm_window_attention_backward(int32_t dtype, int32_t window,
   BM_ARG_CHECK(k && v && dk && dv && (a.T == 0 || (q && o && d_o && lse && dq)), "window attention: NULL pointer");
   BM_ARG_CHECK(al16(q) && al16(k) && al16(v) && al16(o) && al16(d_o) && al16(lse) && al16(dq) && al16(dk) && al16(dv),
                "window attention: misaligned pointer");
+  // every key row has one owner, and no tile may read what another one has overwritten
+  for (int s = 1, end = a.key_end_host[0]; s < S; ++s) {
+    if (a.key_end_host[s] == a.cu_k_host[s]) continue;
+    BM_ARG_CHECK(a.cu_k_host[s] >= end, "window attention: keys of sequence %d do not lie behind those in front of it", s);
+    end = a.key_end_host[s];
+  }
+  const int size = dtype == BM_DTYPE_BF16 ? 2 : 4;
+  const long wq = (long)Hq * dh, wk = (long)Hkv * dh;
+  const struct { const void* p; int rows; long ld, width; } in[] = {{q, a.T, ld_q, wq}, {o, a.T, wq, wq}, {d_o, a.T, wq, wq}, {k, a.Tk, ld_kv, wk},
+                                                                    {v, a.Tk, ld_kv, wk}},
+      out[] = {{dq, a.T, ld_dq, wq}, {dk, a.Tk, ld_dkv, wk}, {dv, a.Tk, ld_dkv, wk}};
+  for (const auto& x : in)
+    for (const auto& y : out)
+      BM_ARG_CHECK(!share(x.p, x.rows, x.ld, x.width, y.p, y.rows, y.ld, y.width, size), "window attention: a gradient lies over an input");
   BM_RETURN_IF(check_scratch(scratch, scratch_bytes,
                              bm_window_attention_backward_scratch_bytes(dtype, window, sinks, Hq, Hkv, dh, S, a.T, a.Tk)));
   a.q = q; a.k = k; a.v = v; a.ld_dkv = ld_dkv;

@@ -443,6 +443,43 @@ def test_keys_that_no_query_sees_are_not_read(window, sinks, dtype, dh, seqs):
     assert torch.equal(o[:x.Tq], x.o[:x.Tq]) and torch.equal(lse[:4 * x.Tq], x.lse[:4 * x.Tq])
 
 
+@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("bf16", 128), ("fp32", 32)])
+@pytest.mark.parametrize("queries", [(1, 2), (1, 90)])
+def test_sequences_that_share_keys_in_any_order(dtype, dh, queries):
+    """A common beginning, as several answers to one question have it, and a slot in front of the others."""
+    x = Window(dtype, 8, 2, dh, [(queries[0], 300), (queries[1], 320), (1, 100)], 80, 5, seed=10, gap=3)
+    x.begin[1], x.end[1] = x.begin[0], x.begin[0] + 320
+    x.begin[0], x.end[0], x.begin[2], x.end[2] = x.begin[2], x.end[2], x.begin[0], x.end[0]
+    x.seqs = [(q, int(e - b)) for (q, _), b, e in zip(x.seqs, x.begin, x.end)]
+    x.inside[:] = False
+    for b, e in zip(x.begin, x.end):
+        x.inside[b:e] = True
+    x.check_forward(*x.forward())
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("bf16", 72), ("fp32", 64)])
+@pytest.mark.parametrize("queries", [(1, 1), (2, 130)])
+def test_keys_far_into_a_cache(dtype, dh, queries):
+    """Rows whose offsets pass 2^32 bytes; the rest of the cache holds NaN."""
+    import torch
+    Hq, Hkv, lens, window, sinks, ld = 8, 2, (700, 333), 150, 3, 1024
+    rows = (1 << 33) // (ld * (2 if dtype == "bf16" else 4)) // 2
+    near = Window(dtype, Hq, Hkv, dh, list(zip(queries, lens)), window, sinks, seed=11, gap=1)
+    o, lse = near.forward()
+    near.check_forward(o, lse)
+    begin = np.array([rows - 1100, rows - 350], np.int32)
+    end = (begin + lens).astype(np.int32)
+    big = [torch.full((rows, ld), float("nan"), device="cuda", dtype=torch_of(dtype)) for _ in range(2)]
+    for b, nb, n in zip(begin, near.begin, lens):
+        for t, src in zip(big, (near.k, near.v)):
+            t[b:b + n, :Hkv * dh] = dev(src[nb:nb + n].reshape(n, -1), dtype)
+    n = bm.window_attention_scratch_bytes(near.code, window, sinks, Hq, Hkv, dh, 2, near.Tq, int(end[1]))
+    o2, lse2 = torch.empty_like(o[:near.Tq]), torch.empty(Hq * near.Tq, device="cuda")
+    bm.window_attention_forward(near.code, window, sinks, Hq, Hkv, dh, near.rows(near.q), Hq * dh, big[0], big[1], ld, dev(near.cu), near.cu, dev(begin),
+                                dev(end), begin, end, 2, o2, lse2, near.scratch(n), n)
+    assert torch.equal(o2, o[:near.Tq]) and torch.equal(lse2, lse[:Hq * near.Tq])
+
+
 @pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("bf16", 128), ("fp32", 64)])
 def test_window_replays_from_a_graph_and_repeats(dtype, dh):
     """The same bits again, from a graph with eager work between the replays, and on another stream."""

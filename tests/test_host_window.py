@@ -4,7 +4,7 @@ import pytest
 
 from paper_2605_25451_amd import binding as bm
 
-A = [4096 * (i + 1) for i in range(16)]                      # addresses that are never followed
+A = [(i + 1) << 20 for i in range(16)]                      # addresses that are never followed
 DESC = dict(dtype=0, n_q_heads=4, n_kv_heads=2, head_dim=16, pairs=[2, 3, 3], base=10000.0, own_frequencies=False, norm=True, eps=1e-6)
 
 
@@ -97,6 +97,21 @@ def test_window_forward_refusals(bad):
                                               dict(dv=A[12] + 2), dict(ld_dq=254), dict(ld_dkv=64), dict(ld_dkv=132)])
 def test_window_backward_refusals(bad):
     refused(bm.BM_ERR_INVALID_ARG, bm.window_attention_backward, *{**SIZES, **GRAD, **bad}.values())
+
+
+@pytest.mark.parametrize("bad", [dict(k_begin_host=[0, 2], k_end_host=[3, 16]), dict(k_begin_host=[10, 0], k_end_host=[16, 3]), dict(dq=A[0]),
+                                 dict(dk=A[1]), dict(dv=A[1] + 128), dict(dk=A[2] - 256 * 8), dict(dq=A[9]), dict(dq=A[6]), dict(dq=A[0] + 16),
+                                 dict(dq=A[0], ld_dq=264), dict(dk=A[2] - 64 * 2, ld_kv=256, ld_dkv=256)])
+def test_window_gradients_with_owners(bad):
+    """A key row of two sequences, and gradients over an input."""
+    refused(bm.BM_ERR_INVALID_ARG, bm.window_attention_backward, *{**SIZES, **GRAD, **bad}.values())
+
+
+@pytest.mark.parametrize("side", [dict(dk=A[1] + 256, dv=A[1] + 512), dict(dq=A[0] + 512, ld_q=1024, ld_dq=1024), dict(k_begin_host=[5, 10], k_end_host=[10, 16], cu_q_host=[0, 3, 5])])
+def test_window_gradients_beside_inputs(side):
+    """Columns of the same rows: nothing but the missing workspace is refused."""
+    call = {**SIZES, **GRAD, "ld_kv": 512, "ld_dkv": 512, **side, "scratch": None}
+    refused(bm.BM_ERR_WORKSPACE_TOO_SMALL, bm.window_attention_backward, *call.values())
 
 
 @pytest.mark.parametrize("fn,call", [(bm.window_attention_forward, CALL), (bm.window_attention_backward, GRAD)])
