@@ -507,6 +507,65 @@ def test_window_replays_from_a_graph_and_repeats(dtype, dh):
             assert torch.equal(got[:x.Tq], ref[:x.Tq])
 
 
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("bf16", 64), ("fp32", 64)])
+@pytest.mark.parametrize("S", [3, 70])
+def test_tokens_replay_from_graphs_that_run_at_the_same_time(S, dtype, dh):
+    """Two graphs with workspaces of their own, replayed side by side, lists that grow by nothing; then once more in eager mode."""
+    import torch
+    xs = [Window(dtype, 8, 2, dh, [(1 + i % 2, 40 + (i * 211 + 97 * j) % 1900) for i in range(S)], 900, 5, seed=12 + j, gap=1) for j in range(2)]
+    want = [tuple(t.clone() for t in x.forward()) for x in xs]
+    for x in xs:
+        x.check_forward(x.o, x.lse)
+    streams, graphs = [torch.cuda.Stream() for _ in xs], [torch.cuda.CUDAGraph() for _ in xs]
+    for x, st, g in zip(xs, streams, graphs):
+        st.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(g, stream=st):
+            x.fwd()
+    for _ in range(3):
+        for x in xs:
+            x.o[:x.Tq], x.lse[:8 * x.Tq] = 7.0, 7.0
+            x.fwd_work.fill_(255)
+        torch.cuda.synchronize()
+        for st, g in zip(streams, graphs):
+            with torch.cuda.stream(st):
+                g.replay()
+        torch.cuda.synchronize()
+        for x, (o, lse) in zip(xs, want):
+            assert torch.equal(x.o[:x.Tq], o[:x.Tq]) and torch.equal(x.lse[:8 * x.Tq], lse[:8 * x.Tq])
+    xs[0].fwd()
+    assert torch.equal(xs[0].o[:xs[0].Tq], want[0][0][:xs[0].Tq])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("norm", [False, True])
+def test_rotary_replays_from_a_graph(norm, dtype):
+    import torch
+    r = Rotary(dtype, norm, 700, 6, 2, 64, [8, 12, 12], False, seed=13)
+    x, dz, pos, gains = r.rows(r.x), r.rows(r.dz), dev(r.pos), r.gains()
+    z, dx, dg = torch.zeros_like(x), torch.zeros_like(x), [torch.zeros(64, device="cuda") for _ in range(2)]
+    n = bm.qk_rotary_backward_scratch_bytes(r.desc, 700)
+    work = torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
+    raw = r.halves(x) if norm else (None, None)
+
+    def both():
+        bm.qk_rotary_forward(r.desc, 700, *r.halves(x), r.ld, pos, *gains, *r.halves(z), r.ld)
+        bm.qk_rotary_backward(r.desc, 700, *raw, r.ld, pos, *gains, *r.halves(dz), r.ld, *r.halves(dx), r.ld, *(dg if norm else (None, None)), work, n)
+    both()
+    want = [t.clone() for t in (z, dx, *dg)]
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        both()
+    for _ in range(3):
+        for t in (z, dx, *dg):
+            t.zero_()
+        work.fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((z, dx, *dg), want))
+
+
 # ---- one after another, as a model uses them -------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", DTYPES)
