@@ -2531,7 +2531,8 @@ __global__ __launch_bounds__(256, 2) void fa_window_token_kernel(
   static_assert(RING * 2 * TILE * 2 >= 32 * OS * 4, "a wavefront's sums take its tiles' place");
   __shared__ __attribute__((aligned(1024))) bf16_t ring[4 * RING * 2 * TILE];
   __shared__ float stats[4][32][2];
-  const int hk = blockIdx.x % Hkv, slot = blockIdx.x / Hkv;
+  int hk;
+  const int slot = token_slot(split, Hkv, blockIdx.x, &hk);
   TokenPart where;
   if (!find_token_part(split, S, slot, &where)) return;
   const int seq = where.seq, nparts = where.parts;
@@ -2666,7 +2667,7 @@ __global__ __launch_bounds__(256, 2) void fa_window_token_kernel(
 
 template <int DH>
 bm_status window_token_launch(const AttnArgs& a, const TokenSplit& split, void* o, float* lse, hipStream_t st) {
-  hipLaunchKernelGGL((fa_window_token_kernel<DH>), dim3(split.wgs), dim3(256), 0, st, (const bf16_t*)a.q, (const bf16_t*)a.k,
+  hipLaunchKernelGGL((fa_window_token_kernel<DH>), dim3(token_grid(split, a.Hkv)), dim3(256), 0, st, (const bf16_t*)a.q, (const bf16_t*)a.k,
                      (const bf16_t*)a.v, a.ld_qkv, a.kv_ld(), a.cu_dev, a.kv_cu_dev(), a.S, (bf16_t*)o, a.Hq * a.dh, lse, a.T, a.Hkv,
                      a.Hq / a.Hkv, LOG2E / sqrtf((float)a.dh), a.local, split);
   BM_CHECK_LAUNCH("fa_window_token");

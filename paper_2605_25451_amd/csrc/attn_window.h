@@ -37,7 +37,7 @@ constexpr int TOKEN_KEYS = 32;       // keys of a tile
 constexpr int TOKEN_ROWS = 32;       // queries x heads of a group, at most
 constexpr int TOKEN_TABLE = 64;
 struct TokenSplit {
-  int per, rows, wgs;                // rows: of the sequence with most queries
+  int per, rows, wgs, same_xcd;      // rows: of the sequence with most queries
   float *sums, *stats;
   int n;                             // sequences whose parts stand below (0: more than the table holds, see map)
   // written by window_map_kernel: [S+1] first part and [S] first place of a sequence, [S] those of more than one part, [parts] the sequence
@@ -47,6 +47,13 @@ struct TokenSplit {
     return Lq > 0 ? (KeyWalk<TOKEN_KEYS>(w, Lk - Lq, 0, Lq, Lk).n + per - 1) / per : 0;
   }
 };
+// which part and kv head a workgroup takes (they go round-robin over the 8 XCDs), and how many there are
+__device__ inline int token_slot(const TokenSplit& t, int Hkv, int block, int* hk) {
+  const int id = t.same_xcd ? block >> 3 : block;
+  *hk = id % Hkv;
+  return t.same_xcd ? id / Hkv * 8 + (block & 7) : id / Hkv;
+}
+inline int token_grid(const TokenSplit& t, int Hkv) { return t.same_xcd ? cdiv(t.wgs, 8 * Hkv) * 8 * Hkv : t.wgs; }
 struct TokenPart { int seq, part, parts, place; };
 // sums of v over the lanes up to this one
 __device__ inline int scan_lanes(int v) {
@@ -72,6 +79,7 @@ __device__ inline bool find_token_part(const TokenSplit& t, int S, int id, Token
     if (past == 0) return false;
     *p = table_entry(__builtin_ctzll(past), mine, upto, places);
   } else {
+    if (id >= t.map[S]) return false;
     const int seq = t.map[3 * S + 1 + id], before = t.map[seq];
     *p = TokenPart{seq, before, t.map[seq + 1] - before, t.map[S + 1 + seq]};
   }
