@@ -2687,9 +2687,12 @@ WindowBwd window_bwd(int window, int sinks, int Hq, int Hkv, int dh, int S, int 
   // us, for 1024 -> 512 -> 256: 32 / 8 heads of 128, 8192 tokens, window 2048 1104 -> 1041 -> 1041, 256 650 -> 489 -> 489, 4096 448 -> 379 -> 347;
   // 32 / 8 of 64, 4096 207 -> 190 -> 239, 2048 94 -> 94 -> 129; 8 / 1 of 128, 32768, window 4096, 1705 -> 1733 -> 2463.
   w.gsplit = dkdv_group_split(2 * tiles, Hkv, Hq / Hkv);
-  // parts of the first keys about as long as the tiles of other keys
+  // Parts of the first keys about as long as the tiles of other keys, and of 512 rows or, where the longest workgroup decides, 192 at least.  us, 512 ->
+  // 192: 780 tokens, window 1, 16 / 16 heads of 64 42 -> 29, of 72 44 -> 30, 5 / 1 of 128 53 -> 37; 2048, window 256, 8 / 2 of 64 52 -> 44; 777, window 131,
+  // 16 / 16 of 64 34 -> 33; but 780 of 32 / 8 of 128 58 -> 64, 8192 of 5 / 1 142 -> 176.
   const int rows = (int)align_up(window < 4096 ? window : 4096, BK_Q);
-  w.part_rows = rows < 512 ? 512 : rows;
+  const int least = (long)Tq * Hq <= 20480 ? 192 : 512;
+  w.part_rows = rows < least ? least : rows;
   w.parts = sinks > 0 ? 2L * Tq / w.part_rows : 0;         // a sequence that is split has more rows than one part
   w.delta = align_up((size_t)Hq * Tq, 64);
   w.split = w.gsplit > 1 ? (size_t)w.gsplit * 2 * Tk * Hkv * dh : 0;

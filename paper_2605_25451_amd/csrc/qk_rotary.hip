@@ -219,13 +219,125 @@ __global__ __launch_bounds__(256) void qk_rotary_norm_bwd_kernel(RotaryArgs a, R
   }
 }
 
+// Heads of 32, 64 or 128 bytes, whose halves are less than a cache line: a lane holds one 16-byte run of the head, so that the lanes of a head
+// read it at once, and gets the other element of each pair from its mirror among them (lane c of the first half and LP - 1 - c hold the
+// same pairs).  16351 tokens, 12 + 12 heads of 64, bf16: 27.4 -> 22.7 us, with the norm 27.7 -> 24.7, its gradient 43.7 -> 40.4.
+template <int LP>
+__device__ inline float mirrored(float v) {
+  constexpr int CTRL = LP == 2 ? 0xB1 : LP == 4 ? 0x1B : 0x141;            // swaps in pairs, reversals of four and of eight lanes
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+
+template <typename T, int VEC, int LP, bool NORM, bool NT>
+__global__ __launch_bounds__(256) void qk_rotary_small_fwd_kernel(RotaryArgs a, Rotation rot, float sign) {
+  constexpr int DH = LP * VEC, HALF = DH / 2, U = 8;                       // heads in flight
+  const long gid = (long)blockIdx.x * 256 + threadIdx.x;
+  const long tok = gid / LP;
+  const int c = threadIdx.x % LP, upper = c >= LP / 2, i0 = (upper ? LP - 1 - c : c) * VEC, at = upper * HALF + i0;
+  const bool live = tok < a.T;
+  const int t = (int)min(tok, (long)a.T - 1);
+  const int side = (int)blockIdx.y < a.groups_q ? 0 : 1;
+  const int first = ((int)blockIdx.y - (side ? a.groups_q : 0)) * a.per[side], last = min(a.heads[side], first + a.per[side]);
+  float cs[VEC], sn[VEC], g[VEC];
+  cos_sin<VEC>(rot, a.positions, a.T, t, i0, upper ? sign : -sign, cs, sn);
+  if (NORM) load_vec<VEC>((const T*)a.gain[side] + at, g);
+  const T* in = (const T*)a.in[side] + (size_t)t * a.ld_in + at;
+  T* out = (T*)a.out[side] + (size_t)t * a.ld_out + at;
+  for (int h0 = first; h0 < last; h0 += U) {
+    float x[U][VEC];
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_vec<VEC, NT>(in + (size_t)min(h0 + u, last - 1) * DH, x[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (NORM) {
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) ss += x[u][e] * x[u][e];
+        const float r = rsqrtf(lanes_sum<LP>(ss) / (float)DH + a.eps);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[u][e] *= r * g[e];
+      }
+      float z[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) z[e] = x[u][e] * cs[e] + mirrored<LP>(x[u][e]) * sn[e];
+      if (live && h0 + u < last) store_vec<VEC, NT>(out + (size_t)(h0 + u) * DH, z);
+    }
+  }
+}
+
+template <typename T, int VEC, int LP, bool NT>
+__global__ __launch_bounds__(256) void qk_rotary_small_norm_bwd_kernel(RotaryArgs a, Rotation rot) {
+  constexpr int GROUPS = 256 / LP, DH = LP * VEC, HALF = DH / 2, U = 4;
+  __shared__ float sums[GROUPS][DH + 1];
+  const int c = threadIdx.x % LP, grp = threadIdx.x / LP, upper = c >= LP / 2, i0 = (upper ? LP - 1 - c : c) * VEC, at = upper * HALF + i0;
+  const int side = (int)blockIdx.y < a.groups_q ? 0 : 1;
+  const int walk = (int)blockIdx.y - (side ? a.groups_q : 0);
+  const int first = walk * a.per[side], last = min(a.heads[side], first + a.per[side]);
+  float g[VEC], dg[VEC];
+  load_vec<VEC>((const T*)a.gain[side] + at, g);
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) dg[e] = 0.f;
+  // (every lane of a wavefront makes the same number of trips: the sums go over lanes)
+  for (long base = (long)blockIdx.x * GROUPS; base < a.T; base += (long)gridDim.x * GROUPS) {
+    const long tok = base + grp;
+    const bool live = tok < a.T;
+    const int t = (int)min(tok, (long)a.T - 1);
+    float cs[VEC], sn[VEC];
+    cos_sin<VEC>(rot, a.positions, a.T, t, i0, upper ? -1.f : 1.f, cs, sn);
+    const T* in = (const T*)a.in[side] + (size_t)t * a.ld_in + at;
+    const T* raw = (const T*)a.x[side] + (size_t)t * a.ld_x + at;
+    T* out = (T*)a.out[side] + (size_t)t * a.ld_out + at;
+    for (int h0 = first; h0 < last; h0 += U) {
+      float d[U][VEC], x[U][VEC];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const size_t head = (size_t)min(h0 + u, last - 1) * DH;
+        load_vec<VEC, NT>(in + head, d[u]);
+        load_vec<VEC, NT>(raw + head, x[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float ss = 0.f, dot = 0.f, p[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          p[e] = d[u][e] * cs[e] + mirrored<LP>(d[u][e]) * sn[e];
+          ss += x[u][e] * x[u][e];
+          dot += p[e] * g[e] * x[u][e];
+        }
+        ss = lanes_sum<LP>(ss);
+        dot = lanes_sum<LP>(dot);
+        const float r = rsqrtf(ss * (1.0f / DH) + a.eps), k = dot * r * (1.0f / DH);      // k: mean(e n)
+        if (live && h0 + u < last) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            const float n = x[u][e] * r;
+            dg[e] += p[e] * n;
+            p[e] = r * (p[e] * g[e] - n * k);
+          }
+          store_vec<VEC, NT>(out + (size_t)(h0 + u) * DH, p);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) sums[grp][at + e] = dg[e];
+  __syncthreads();
+  if ((int)threadIdx.x < DH) {
+    float s = 0.f;
+    for (int i = 0; i < GROUPS; ++i) s += sums[i][threadIdx.x];
+    a.part[side][((size_t)walk * gridDim.x + blockIdx.x) * DH + threadIdx.x] = s;
+  }
+}
+
 // Lanes of a token and elements of a lane
-struct Lanes { int vec, chunks, pow2; };
+struct Lanes { int vec, chunks, pow2; bool small; };      // small: a lane for every 16 bytes of a head; otherwise for 16 (8) bytes of both halves
 Lanes lanes_of(const bm_qk_rotary_desc& d) {
   Lanes l;
   const int half = d.head_dim / 2;
-  l.vec = d.dtype == BM_DTYPE_BF16 && half % 8 == 0 ? 8 : 4;
-  l.chunks = half / l.vec;
+  const int bytes = d.head_dim * (int)elt_size(d.dtype);
+  l.small = bytes == 32 || bytes == 64 || bytes == 128;
+  l.vec = d.dtype == BM_DTYPE_BF16 && (half % 8 == 0 || l.small) ? 8 : 4;
+  l.chunks = l.small ? bytes / 16 : half / l.vec;
   l.pow2 = 1;
   while (l.pow2 < l.chunks) l.pow2 *= 2;
   return l;
@@ -320,18 +432,29 @@ Rotation rotation(const bm_qk_rotary_desc& d) {
   return r;
 }
 
-// Do rows go past the caches?  Whole 16-byte accesses of more than the L2s hold together (32 MB): 32 + 8 heads of 128, us, through them
+// Do rows go past the caches?  Accesses of whole 128-byte lines, of more than the L2s hold together (32 MB): 32 + 8 heads of 128, us, through them
 // -> past: 8192 tokens with the norm 41.7 -> 37.3, gradient 59.4 -> 54.8; 32768 tokens 146 -> 137, gradient 230 -> 222.  Fewer tokens are
-// read again while they are still there (2048: 12.6 -> 13.4); accesses of 8 bytes are slower (16 + 16 heads of 72, 2601 tokens, 11.6 -> 14.2).
+// read again while they are still there (2048: 12.6 -> 13.4); parts of lines are slower (fp32, 16 + 16 heads of 72, 8192 tokens, 41 -> 52).
 bool past_caches(const bm_qk_rotary_desc& d, const Lanes& l, int T) {
   const double bytes = (double)T * (d.n_q_heads + d.n_kv_heads) * d.head_dim * elt_size(d.dtype);
-  return l.vec * elt_size(d.dtype) == 16 && bytes > 32e6;
+  const int run = (l.small ? d.head_dim : d.head_dim / 2) * (int)elt_size(d.dtype);
+  return run % 128 == 0 && bytes > 32e6;
 }
 
 template <typename T, int VEC, bool NT>
 void launch_fwd(const RotaryArgs& a, const Rotation& r, const Lanes& l, bool norm, float sign, int groups, hipStream_t st) {
   const int lanes = norm ? l.pow2 : l.chunks;
   const dim3 grid(cdiv((long)a.T * lanes, 256), groups), block(256);
+  if (l.small) {
+#define BM_S(LP)                                                                                                        \
+  if (norm) hipLaunchKernelGGL((qk_rotary_small_fwd_kernel<T, VEC, LP, true, NT>), grid, block, 0, st, a, r, sign);      \
+  else hipLaunchKernelGGL((qk_rotary_small_fwd_kernel<T, VEC, LP, false, NT>), grid, block, 0, st, a, r, sign)
+    if constexpr (sizeof(T) * VEC == 16) {
+      switch (l.chunks) { case 2: BM_S(2); break; case 4: BM_S(4); break; default: BM_S(8); }
+    }
+#undef BM_S
+    return;
+  }
 #define BM_L(LP) hipLaunchKernelGGL((qk_rotary_fwd_kernel<T, VEC, LP, NT>), grid, block, 0, st, a, r, sign)
   if (!norm) BM_L(0);
   else switch (l.pow2) {
@@ -344,6 +467,14 @@ void launch_fwd(const RotaryArgs& a, const Rotation& r, const Lanes& l, bool nor
 template <typename T, int VEC, bool NT>
 void launch_bwd(const RotaryArgs& a, const Rotation& r, const Lanes& l, const BwdGrid& g, hipStream_t st) {
   const dim3 grid(g.x, g.y), block(256);
+  if (l.small) {
+#define BM_S(LP) hipLaunchKernelGGL((qk_rotary_small_norm_bwd_kernel<T, VEC, LP, NT>), grid, block, 0, st, a, r)
+    if constexpr (sizeof(T) * VEC == 16) {
+      switch (l.chunks) { case 2: BM_S(2); break; case 4: BM_S(4); break; default: BM_S(8); }
+    }
+#undef BM_S
+    return;
+  }
 #define BM_L(LP) hipLaunchKernelGGL((qk_rotary_norm_bwd_kernel<T, VEC, LP, NT>), grid, block, 0, st, a, r)
   switch (l.pow2) {
     case 1: BM_L(1); break; case 2: BM_L(2); break; case 4: BM_L(4); break;
