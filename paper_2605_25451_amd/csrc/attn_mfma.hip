@@ -1165,8 +1165,17 @@ __device__ inline void dkdv_tile(unsigned char* lds, int block, const bf16_t* __
     const bool all_masked = kb0 + BK_KEYS > L;
     const int n_front = CAUSAL ? min(nqt, (wave * 32 + 32 + BK_Q - 1) / BK_Q) : 0;
     const int n_whole = max(n_front, (Lq - qstart) % BK_Q ? nqt - 1 : nqt);
+    // a tile whose queries see none of this wavefront's keys: most of those behind the window of the first keys
+    auto idle = [&](int it) {
+      const int par = it & 1;
+      if (tid < BK_Q) { Lbuf[par * BK_Q + tid] = st_l * LOG2E; Dlbuf[par * BK_Q + tid] = st_d; }
+      wait_async_tiles();
+      __syncthreads();
+      if (it + 1 < iters) fetch(it + 1, 1 - par);
+    };
     for (int it = 0, t = 0; it < iters; ++it, t = (t + 1 == nqt ? 0 : t + 1)) {
       const int q0 = qstart + t * BK_Q;
+      if (WINDOW && none_visible(first.mask, kb0 + wave_u * 32, 32, off + q0, BK_Q)) { idle(it); continue; }
       const bool masked = WINDOW ? all_masked || q0 + BK_Q > qend || !all_visible(first.mask, kb0 + wave_u * 32, 32, off + q0, BK_Q)
                                  : all_masked || t < n_front || t >= n_whole;
       if (it & 1) { if (masked) step(it, std::true_type{}, P1{}); else step(it, std::false_type{}, P1{}); }
@@ -1431,10 +1440,21 @@ __device__ inline void dkdv_pair_tile(
     const bool all_masked = kb0 + BK_KEYS > L;
     const int n_front = CAUSAL ? min(nqt, (kb * 32 + 32 + BK_Q - 1) / BK_Q) : 0;
     const int n_whole = max(n_front, (Lq - qstart) % BK_Q ? nqt - 1 : nqt);
-    for (int it = 0, t = 0; it < iters; ++it, t = (t + 1 == nqt ? 0 : t + 1))
+    // a tile whose queries see none of this pair's keys: most of those behind the window of the first keys
+    auto idle = [&](int it) {
+      const int par = it & 1;
+      if (tid < BK_Q) { Lbuf[par * BK_Q + tid] = st_l * LOG2E; Dlbuf[par * BK_Q + tid] = st_d; }
+      wait_async_tiles();
+      __syncthreads();
+      if (it + 1 < iters) fetch(it + 1, 1 - par);
+      __syncthreads();
+    };
+    for (int it = 0, t = 0; it < iters; ++it, t = (t + 1 == nqt ? 0 : t + 1)) {
+      if (WINDOW && none_visible(first.mask, kb0 + wave_r * 32, 32, off + qstart + t * BK_Q, BK_Q)) { idle(it); continue; }
       step_of(it, WINDOW ? all_masked || qstart + (t + 1) * BK_Q > qend ||
                                !all_visible(first.mask, kb0 + wave_r * 32, 32, off + qstart + t * BK_Q, BK_Q)
                          : all_masked || t < n_front || t >= n_whole);
+    }
   }
   // dV as it is, dK times the softmax scale
   const float out_scale = role == 0 ? 1.0f : WINDOW ? scale * (1.0f / HANDED_SCALE) : scale;
@@ -1867,8 +1887,7 @@ __device__ inline void dq_tile(unsigned char* lds, int tid, int tile_id, int hq,
       tile.issue(kbase + next, ldk, Lk - nt * FKD, Kbuf + (1 - PAR) * TILE, wave_u);
       tile.issue(vbase + next, ldk, Lk - nt * FKD, Vbuf + (1 - PAR) * TILE, wave_u);
     }
-    const int key0 = walk.tile(kt) * FKD;
-    if (WINDOW && MASKED && none_visible(w, key0, FKD, off + q0 + wave_u * 32, 32)) return;
+    const int key0 = walk.tile(kt) * FKD, ahead = off + qpos - key0 - half * 4, sinks = WINDOW ? w.sinks - key0 - half * 4 : 0;
     // S^T = K Q^T and dP^T = V dO^T of BP 32-key blocks are issued before any softmax arithmetic,
     // so that one block's MFMAs run under the other's vector work; at head size 128 that is one
     // block at a time (two sets of accumulators do not fit next to two resident wavefronts).
@@ -1905,8 +1924,8 @@ __device__ inline void dq_tile(unsigned char* lds, int tid, int tile_id, int hq,
         for (int r = 0; r < 16; ++r) {
           float p = __builtin_amdgcn_exp2f(fmaf(sacc[bi][r], scale_log2, -my_lse));
           if (MASKED) {
-            const int key = key0 + b * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
-            if (WINDOW ? hidden(w, key, off + qpos) : key >= Lk || (CAUSAL && key > qpos)) p = 0.f;
+            const int e = b * 32 + (r >> 2) * 8 + (r & 3), key = key0 + half * 4 + e;
+            if (WINDOW ? e > ahead || (e <= ahead - w.window && e >= sinks) : key >= Lk || (CAUSAL && key > qpos)) p = 0.f;
           }
           dpacc[bi][r] = FOLD_DELTA ? p * dpacc[bi][r] : p * (dpacc[bi][r] - my_delta);
         }
@@ -1936,7 +1955,19 @@ __device__ inline void dq_tile(unsigned char* lds, int tid, int tile_id, int hq,
   n_plain = min(n_plain, nkt);
   using P0 = std::integral_constant<int, 0>;
   using P1 = std::integral_constant<int, 1>;
+  // a tile that none of this wavefront's queries see (left inside the step, this cost 44 registers at head size 128)
+  auto idle = [&](int kt) {
+    wait_async_tiles();
+    __syncthreads();
+    if (kt + 1 < nkt) {
+      const int nt = walk.tile(kt + 1);
+      const size_t next = (size_t)nt * FKD * ldk;
+      tile.issue(kbase + next, ldk, Lk - nt * FKD, Kbuf + (1 - (kt & 1)) * TILE, wave_u);
+      tile.issue(vbase + next, ldk, Lk - nt * FKD, Vbuf + (1 - (kt & 1)) * TILE, wave_u);
+    }
+  };
   for (int kt = 0; kt < nkt; ++kt) {
+    if (WINDOW && none_visible(w, walk.tile(kt) * FKD, FKD, off + q0 + wave_u * 32, 32)) { idle(kt); continue; }
     const bool plain = WINDOW ? all_visible(w, walk.tile(kt) * FKD, FKD, off + q0 + wave_u * 32, 32) : kt < n_plain;
     if (kt & 1) { if (plain) step(kt, std::false_type{}, P1{}); else step(kt, std::true_type{}, P1{}); }
     else { if (plain) step(kt, std::false_type{}, P0{}); else step(kt, std::true_type{}, P0{}); }
@@ -2361,9 +2392,9 @@ bm_status bwd_launch(const AttnArgs& a, const void* o, const void* d_o, const fl
 // sliding window: the kernels above with WINDOW, and what joins the parts of first keys
 // =============================================================================
 // The backward pass in one grid: the parts of first keys, the other key tiles, then dQ, which fills what they leave (as in
-// fa_bwd_joint_kernel and fa_bwd_joint512_kernel); at head size 72 dQ of 128 rows on its own where that is ahead, two workgroups to a CU.
-// At head size 128 dQ takes 256 rows and turns for any length: the 128-row tile, with the window's bounds, holds more than 256 registers
-// (dQ of 8192 queries, window 2048, 809 -> about 380 us; the whole pass of 777 queries, window 131, 73 -> 64).
+// fa_bwd_joint_kernel and fa_bwd_joint512_kernel; head size 72, 16 heads, dQ of 128 rows apart -> here: 8192 tokens 280 -> 275 us, 4096 178 -> 160,
+// 777 59 -> 38, 32768 2765 -> 2796).  At head size 128 dQ takes 256 rows and turns for any length: 128 rows of two heads are behind by 0 to
+// 6 % (8192 tokens, 32 / 8 heads, window 256 435 -> 455, 2048 957 -> 972).
 struct WindowBwdArgs {
   const bf16_t *q, *k, *v, *d_o;
   const float *lse, *delta;
@@ -2412,15 +2443,6 @@ __global__ __launch_bounds__(512, 2) void fa_window_bwd512_kernel(WindowBwdArgs 
                             a.ldk, a.d_o, a.ldo, a.lse, a.delta, a.cuq, a.cuk, a.S, a.dq, a.ldd, a.Tq, a.group, a.scale, a.scale_log2,
                             ord_q, first.mask);
   }
-}
-
-template <int DH>
-__global__ __launch_bounds__(256, 2) void fa_window_dq_kernel(WindowBwdArgs a, SeqOrder ord, LocalMask w) {
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[dq_lds_bytes<DH>()];
-  int tile, head;
-  tile_and_head(a.Hkv * a.group, &tile, &head, blockIdx.x);
-  dq_tile<DH, true, true>(lds, threadIdx.x, tile, head, true, a.q, a.k, a.v, a.ld, a.ldk, a.d_o, a.ldo, a.lse, a.delta, a.cuq, a.cuk, a.S,
-                          a.dq, a.ldd, a.Tq, a.group, a.scale, a.scale_log2, ord, w);
 }
 
 // the sequence that is the id-th of those whose first keys are in parts
@@ -2742,14 +2764,12 @@ bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, c
   const int key_rows = wide ? WIDE_KEYS : BK_KEYS;
   const int ktiles = count_tiles(a.kv_cu_host(), a.key_end_host, a.S, BK_KEYS), qtiles = count_tiles(a.cu_host, a.S, query_rows);
   const int kv_wgs = first.wgs + (wide ? count_tiles(a.kv_cu_host(), a.key_end_host, a.S, WIDE_KEYS) : ktiles) * a.Hkv * wb.gsplit, q_wgs = qtiles * cdiv(a.Hq, heads_per_wg);
-  // (head size 72: as in bwd_plan)
-  const bool together = DH != 72 || kv_wgs + q_wgs <= NUM_CU * 3 / 2 || (kv_wgs > NUM_CU && kv_wgs + q_wgs <= 2 * NUM_CU);
   const SeqOrder ord_kv = make_seq_order(a.kv_cu_host(), a.cu_host, a.S, key_rows, false, a.key_end_host);
   const SeqOrder ord_q = make_seq_order(a.cu_host, a.cu_host, a.S, query_rows, false);
   const WindowBwdArgs w{(const bf16_t*)a.q, (const bf16_t*)a.k, (const bf16_t*)a.v, (const bf16_t*)d_o, lse, delta, a.cu_dev, a.kv_cu_dev(),
                         (bf16_t*)dq, (bf16_t*)dk, (bf16_t*)dv, part, a.ld_qkv, a.kv_ld(), ldo, ldd, a.ld_dkv, a.S, a.T, Tk, a.Hkv, group,
                         wb.gsplit, kv_wgs, scale, sl2};
-  const int wgs = kv_wgs + (together ? q_wgs : 0);
+  const int wgs = kv_wgs + q_wgs;
   if (wgs > 0) {
     if constexpr (DH <= 64) hipLaunchKernelGGL(fa_window_bwd_kernel<DH>, dim3(wgs), dim3(256), 0, st, w, ord_kv, ord_q, first);
     else {
@@ -2758,9 +2778,6 @@ bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, c
       hipLaunchKernelGGL(kern, dim3(wgs), dim3(512), 0, st, w, ord_kv, ord_q, first);
     }
   }
-  if constexpr (DH == 72)
-    if (!together && qtiles > 0)
-      hipLaunchKernelGGL((fa_window_dq_kernel<DH>), dim3(qtiles * a.Hq), dim3(256), 0, st, w, ord_q, a.local);
   const int all_tiles = wb.gsplit > 1;
   if (kv_wgs > 0 && (all_tiles || parts > 0)) {
     const SeqOrder ord = wide ? make_seq_order(a.kv_cu_host(), a.cu_host, a.S, BK_KEYS, false, a.key_end_host) : ord_kv;
