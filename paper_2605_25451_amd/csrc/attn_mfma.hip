@@ -907,12 +907,12 @@ constexpr int WIDE_KEYS = 256;  // keys per workgroup of the wide dK/dV kernel
 constexpr int BK_KEYS = 128;   // keys per workgroup in the dK/dV kernel (32 per wavefront)
 constexpr int BK_Q = 64;       // query rows per step
 
-// Sliding window: the first 128 keys of a sequence hold its first tokens, which all of its queries see.  Where that is more
-// than `rows` query rows, their tile is split into parts of so many, which leave fp32 partials,
-// [part][kv head x split][dK, dV][128][DH].
+// Sliding window: the first tokens of a sequence, which all of its queries see, are among its first `keys` keys (32 or 128).  Where that
+// is more than `rows` query rows, these keys are split into parts of so many, which leave fp32 partials,
+// [part][kv head x split][dK, dV][keys][DH].
 struct FirstKeys {
   LocalMask mask = {0, 0, nullptr};
-  int rows = 0, wgs = 0;              // query rows of a part; workgroups of the parts, in front of the key tiles'
+  int keys = 0, rows = 0, wgs = 0;    // query rows of a part; workgroups of the parts, in front of the key tiles'
   float* out = nullptr;
   SeqOrder ord = {};                  // the parts of the sequences, in pack order
   __host__ __device__ inline int parts(int Lq) const { return mask.sinks > 0 && Lq > rows ? (Lq + rows - 1) / rows : 0; }
@@ -950,6 +950,7 @@ __device__ inline bool find_key_tile(const FirstKeys& f, const SeqOrder& ord, co
     if (!find_part(f, cuq, S, tile_id, &t->seq, &n)) return false;
     t->kt = 0;
     t->part = tile_id;
+    t->from = 0;
     t->qlo = n * f.rows;
     t->qhi = min(cuq[t->seq + 1] - cuq[t->seq], t->qlo + f.rows);
     return true;
@@ -960,8 +961,8 @@ __device__ inline bool find_key_tile(const FirstKeys& f, const SeqOrder& ord, co
   t->part = -1;
   const int L = f.mask.key_end[t->seq] - cu[t->seq], Lq = cuq[t->seq + 1] - cuq[t->seq], off = L - Lq;
   const bool in_parts = t->kt == 0 && f.parts(Lq) > 0, seen_by_all = t->kt == 0 && f.mask.sinks > 0 && !in_parts;
-  t->from = in_parts ? BK_KEYS : 0;
-  if (in_parts && (KEYS == BK_KEYS || L <= BK_KEYS)) return false;
+  t->from = in_parts ? f.keys : 0;
+  if (in_parts && (KEYS <= f.keys || L <= f.keys)) return false;
   t->qlo = max(0, t->kt * KEYS + t->from - off);
   t->qhi = seen_by_all ? Lq : min(Lq, min((t->kt + 1) * KEYS, L) - 1 - off + f.mask.window);
   return true;
@@ -1175,7 +1176,7 @@ __device__ inline void dkdv_tile(unsigned char* lds, int block, const bf16_t* __
     };
     for (int it = 0, t = 0; it < iters; ++it, t = (t + 1 == nqt ? 0 : t + 1)) {
       const int q0 = qstart + t * BK_Q;
-      if (WINDOW && none_visible(first.mask, kb0 + wave_u * 32, 32, off + q0, BK_Q)) { idle(it); continue; }
+      if (WINDOW && (kb0 + wave_u * 32 < where.from || none_visible(first.mask, kb0 + wave_u * 32, 32, off + q0, BK_Q))) { idle(it); continue; }
       const bool masked = WINDOW ? all_masked || q0 + BK_Q > qend || !all_visible(first.mask, kb0 + wave_u * 32, 32, off + q0, BK_Q)
                                  : all_masked || t < n_front || t >= n_whole;
       if (it & 1) { if (masked) step(it, std::true_type{}, P1{}); else step(it, std::false_type{}, P1{}); }
@@ -1183,6 +1184,7 @@ __device__ inline void dkdv_tile(unsigned char* lds, int block, const bf16_t* __
     }
   }
   const bool leaves_part = WINDOW && where.part >= 0;
+  if (WINDOW && kpos < where.from) return;
   if (kpos < L && (gsplit > 1 || leaves_part)) {
     const size_t plane = (size_t)Ttot * Hkv * DH;
     float* pk = part + ((size_t)gs * 2 + 0) * plane + (size_t)(lo + kpos) * (Hkv * DH) + hk * DH;
@@ -1450,7 +1452,7 @@ __device__ inline void dkdv_pair_tile(
       __syncthreads();
     };
     for (int it = 0, t = 0; it < iters; ++it, t = (t + 1 == nqt ? 0 : t + 1)) {
-      if (WINDOW && none_visible(first.mask, kb0 + wave_r * 32, 32, off + qstart + t * BK_Q, BK_Q)) { idle(it); continue; }
+      if (WINDOW && (kb0 + wave_r * 32 < where.from || none_visible(first.mask, kb0 + wave_r * 32, 32, off + qstart + t * BK_Q, BK_Q))) { idle(it); continue; }
       step_of(it, WINDOW ? all_masked || qstart + (t + 1) * BK_Q > qend ||
                                !all_visible(first.mask, kb0 + wave_r * 32, 32, off + qstart + t * BK_Q, BK_Q)
                          : all_masked || t < n_front || t >= n_whole);
@@ -1459,6 +1461,7 @@ __device__ inline void dkdv_pair_tile(
   // dV as it is, dK times the softmax scale
   const float out_scale = role == 0 ? 1.0f : WINDOW ? scale * (1.0f / HANDED_SCALE) : scale;
   const bool leaves_part = WINDOW && where.part >= 0;
+  if (WINDOW && kpos < where.from) return;
   if (kpos < L && (gsplit > 1 || leaves_part)) {
     const size_t plane = (size_t)Ttot * Hkv * DH;
     float* pp = part + ((size_t)gs * 2 + (role == 0 ? 1 : 0)) * plane + (size_t)(lo + kpos) * (Hkv * DH) + hk * DH;
@@ -1560,7 +1563,7 @@ __device__ inline void dkdv_wide_tile(
   // and all of them if it lies past the sequence.
   const bool keys_cut = key0 + 64 > L;
   // (WINDOW: and those behind the window of its last key, if its keys are no first tokens)
-  const int skip = key0 >= L || (WINDOW && key0 < where.from) ? nqt : CAUSAL ? min(nqt, (WINDOW ? max(0, key0 - off - qstart) : key0 - qstart) / W::ROWS) : 0;
+  const int skip = key0 >= L || (WINDOW && key0 + 64 <= where.from) ? nqt : CAUSAL ? min(nqt, (WINDOW ? max(0, key0 - off - qstart) : key0 - qstart) / W::ROWS) : 0;
   const int stop = WINDOW && key0 >= first.mask.sinks ? max(skip, min(nqt, (key0 + 63 - off + first.mask.window - qstart + W::ROWS - 1) / W::ROWS)) : nqt;
   const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char*)tiles;
   constexpr int LOADS = 3;
@@ -2404,11 +2407,125 @@ struct WindowBwdArgs {
   int ld, ldk, ldo, ldd, ldd_kv, S, Tq, Tk, Hkv, group, gsplit, kv_wgs;      // kv_wgs: the parts' among them
   float scale, scale_log2;
 };
+// A part of 32 first keys: every wavefront walks 32-query tiles of its own (heads of the group, then rows) through its own piece of LDS,
+// without a barrier, with both accumulators in registers; K and V are read from LDS by all, the sums meet there at the end, in pairs.
+// Bound by latency, which the wavefronts hide from one another.
+template <int DH, int W> constexpr int first_keys_lds_bytes() { return (2 + 2 * W) * 32 * HeadDim<DH>::DHL * 2 + W * 64 * 4; }
+template <int DH, int W>
+__device__ inline void first_keys_part(unsigned char* lds, int block, const WindowBwdArgs& a, const FirstKeys& f) {
+  constexpr int DHL = HeadDim<DH>::DHL, KS = HeadDim<DH>::KS, NB = HeadDim<DH>::NB, TILE = 32 * DHL;
+  using Tile = TileAsync<32, DH, 64>;
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  bf16_t* const Ks = reinterpret_cast<bf16_t*>(lds);
+  bf16_t* const Vs = Ks + TILE;
+  bf16_t* const Qs = Ks + (2 + 2 * wave) * TILE;
+  bf16_t* const Ds = Qs + TILE;
+  float* const stats = reinterpret_cast<float*>(Ks + (2 + 2 * W) * TILE) + wave * 64;
+  int part_id, hk_gs, seq, n;
+  tile_and_head(a.Hkv * a.gsplit, &part_id, &hk_gs, block);
+  if (!find_part(f, a.cuq, a.S, part_id, &seq, &n)) return;
+  const int hk = hk_gs / a.gsplit, gpart = a.group / a.gsplit, head0 = hk * a.group + hk_gs % a.gsplit * gpart;
+  const int lo = a.cuk[seq], L = f.mask.key_end[seq] - lo, loq = a.cuq[seq], Lq = a.cuq[seq + 1] - loq, off = L - Lq;
+  const int qlo = n * f.rows, qhi = min(Lq, qlo + f.rows), nqt = (qhi - qlo + 31) / 32, iters = nqt * gpart, kpos = lane & 31;
+  Tile tq, td;
+  tq.init(a.ld, lane);
+  td.init(a.ldo, lane);
+  Tile::zero_padding(Qs, lane);
+  Tile::zero_padding(Ds, lane);
+  if (wave < 2) {
+    Tile tk;
+    tk.init(a.ldk, lane);
+    Tile::zero_padding(wave == 0 ? Ks : Vs, lane);
+    tk.issue((wave == 0 ? a.k : a.v) + (size_t)lo * a.ldk + hk * DH, a.ldk, L, wave == 0 ? Ks : Vs, 0);
+  }
+  f32x16 dk[NB], dv[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) dk[j] = dv[j] = f32x16{};
+  wait_async_tiles();
+  __syncthreads();                                         // K and V
+  for (int it = wave; it < iters; it += W) {
+    const int hq = head0 + it / nqt, q0 = qlo + it % nqt * 32;
+    tq.issue(a.q + (size_t)(loq + q0) * a.ld + hq * DH, a.ld, Lq - q0, Qs, 0);
+    td.issue(a.d_o + (size_t)(loq + q0) * a.ldo + hq * DH, a.ldo, Lq - q0, Ds, 0);
+    const float x = (half ? a.delta : a.lse)[(size_t)hq * a.Tq + loq + min(q0 + kpos, Lq - 1)];
+    stats[lane] = half ? x : x * LOG2E;                    // lse in base 2, then delta
+    wait_async_tiles();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (a wavefront's own rows: no barrier)
+    __builtin_amdgcn_wave_barrier();
+    f32x16 s = {}, dp = {};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DHL>(Qs, 0, ks, lane), frag_rows<DHL>(Ks, 0, ks, lane), s, 0, 0, 0);
+      dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DHL>(Ds, 0, ks, lane), frag_rows<DHL>(Vs, 0, ks, lane), dp, 0, 0, 0);
+    }
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 l4 = *reinterpret_cast<const f32x4*>(stats + g * 8 + half * 4), d4 = *reinterpret_cast<const f32x4*>(stats + 32 + g * 8 + half * 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = g * 4 + e, qi = q0 + g * 8 + half * 4 + e;
+        const float p = qi >= qhi || hidden(f.mask, kpos, off + qi) ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2, -l4[e]));
+        s[r] = p;
+        dp[r] = p * (dp[r] - d4[e]);
+      }
+    }
+    const bf16x8 p0 = acc_to_operand(s, 0), p1 = acc_to_operand(s, 1), s0 = acc_to_operand(dp, 0), s1 = acc_to_operand(dp, 1);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      dv[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DHL>(Ds, j * 32, 0, lane), p0, dv[j], 0, 0, 0);
+      dv[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DHL>(Ds, j * 32, 16, lane), p1, dv[j], 0, 0, 0);
+      dk[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DHL>(Qs, j * 32, 0, lane), s0, dk[j], 0, 0, 0);
+      dk[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DHL>(Qs, j * 32, 16, lane), s1, dk[j], 0, 0, 0);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // Q, dO and the statistics have been read
+  }
+  // a wavefront's 2 NB x 16 sums a lane take the place of its partner's tiles
+  float* const sums = reinterpret_cast<float*>(Ks + 2 * TILE);
+  auto meet = [&](float* at, bool give) {
+#pragma unroll
+    for (int j = 0; j < 2 * NB; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        f32x16& acc = j < NB ? dk[j] : dv[j - NB];
+        f32x4* const to = reinterpret_cast<f32x4*>(at + (j * 4 + g) * 256 + lane * 4);
+        if (give) {
+          *to = f32x4{acc[g * 4], acc[g * 4 + 1], acc[g * 4 + 2], acc[g * 4 + 3]};
+        } else {
+          const f32x4 x = *to;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[g * 4 + e] += x[e];
+        }
+      }
+  };
+#pragma unroll
+  for (int h = W / 2; h > 0; h /= 2) {
+    __syncthreads();                                       // tiles and earlier sums have been read
+    if (wave >= h && wave < 2 * h) meet(sums + (wave - h) * 2 * TILE, true);
+    __syncthreads();
+    if (wave < h) meet(sums + wave * 2 * TILE, false);
+  }
+  if (wave != 0) return;
+  float* const pk = f.out + (((size_t)part_id * (a.Hkv * a.gsplit) + hk_gs) * 2 * 32 + kpos) * DH;
+#pragma unroll
+  for (int j = 0; j < 2 * NB; ++j)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int c = (j < NB ? j : j - NB) * 32 + g * 8 + half * 4;
+      const f32x16& acc = j < NB ? dk[j] : dv[j - NB];
+      const float m = j < NB ? a.scale : 1.0f;
+      if (DH % 32 == 0 || c < DH)
+        *reinterpret_cast<f32x4*>(pk + (j < NB ? 0 : 32 * DH) + c) = f32x4{acc[g * 4] * m, acc[g * 4 + 1] * m, acc[g * 4 + 2] * m, acc[g * 4 + 3] * m};
+    }
+}
+
 template <int DH>
 __global__ __launch_bounds__(256, 2) void fa_window_bwd_kernel(WindowBwdArgs a, SeqOrder ord_kv, SeqOrder ord_q, FirstKeys first) {
-  constexpr int LDS = dkdv_lds_bytes<DH>() > dq_lds_bytes<DH>() ? dkdv_lds_bytes<DH>() : dq_lds_bytes<DH>();
+  constexpr int TILES = dkdv_lds_bytes<DH>() > dq_lds_bytes<DH>() ? dkdv_lds_bytes<DH>() : dq_lds_bytes<DH>();
+  constexpr int LDS = first_keys_lds_bytes<DH, 4>() > TILES ? first_keys_lds_bytes<DH, 4>() : TILES;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS];
-  if ((int)blockIdx.x < a.kv_wgs) {
+  if (first.keys == 32 && (int)blockIdx.x < first.wgs) {
+    first_keys_part<DH, 4>(lds, blockIdx.x, a, first);
+  } else if ((int)blockIdx.x < a.kv_wgs) {
     dkdv_tile<DH, true, true>(lds, blockIdx.x, a.q, a.k, a.v, a.ld, a.ldk, a.d_o, a.ldo, a.lse, a.delta, a.cuq, a.cuk, a.S, a.dk, a.dv,
                               a.ldd_kv, a.Tq, a.Tk, a.Hkv, a.group, a.scale, a.scale_log2, a.gsplit, a.part, ord_kv, first);
   } else {
@@ -2423,9 +2540,12 @@ template <int DH, bool WIDE>
 __global__ __launch_bounds__(512, 2) void fa_window_bwd512_kernel(WindowBwdArgs a, SeqOrder ord_kv, SeqOrder ord_q, FirstKeys first) {
   constexpr int PAIR = dkdv_pair_lds_bytes<DH>(), KV = WIDE && DKDV_WIDE_LDS_BYTES > PAIR ? DKDV_WIDE_LDS_BYTES : PAIR;
   constexpr int Q = DH == 128 ? DQ_ALT_LDS_BYTES : 2 * dq_lds_bytes<DH>();
-  __shared__ __attribute__((aligned(1024))) unsigned char lds[KV > Q ? KV : Q];
+  constexpr int TILES = KV > Q ? KV : Q, LDS = first_keys_lds_bytes<DH, 8>() > TILES ? first_keys_lds_bytes<DH, 8>() : TILES;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS];
   const int Hq = a.Hkv * a.group;
-  if ((int)blockIdx.x < (WIDE ? first.wgs : a.kv_wgs)) {
+  if (first.keys == 32 && (int)blockIdx.x < first.wgs) {
+    first_keys_part<DH, 8>(lds, blockIdx.x, a, first);
+  } else if ((int)blockIdx.x < (WIDE ? first.wgs : a.kv_wgs)) {
     dkdv_pair_tile<DH, true, true>(lds, blockIdx.x, a.q, a.k, a.v, a.ld, a.ldk, a.d_o, a.ldo, a.lse, a.delta, a.cuq, a.cuk, a.S, a.dk, a.dv,
                                    a.ldd_kv, a.Tq, a.Tk, a.Hkv, a.group, a.scale, a.scale_log2, a.gsplit, a.part, ord_kv, first);
   } else if (WIDE && (int)blockIdx.x < a.kv_wgs) {
@@ -2476,7 +2596,8 @@ __global__ __launch_bounds__(256) void fa_window_reduce_kernel(
   } else if (!find_split(first, cuq, S, blockIdx.x, &seq)) {
     return;
   }
-  const int parts = kt == 0 ? first.parts(cuq[seq + 1] - cuq[seq]) : 0;
+  const int row0 = blockIdx.z * REDUCE_ROWS, parts = kt == 0 && row0 < first.keys ? first.parts(cuq[seq + 1] - cuq[seq]) : 0;
+  if (!all_tiles && parts == 0) return;
   const int lo = cuk[seq], L = first.mask.key_end[seq] - lo, hk = blockIdx.y;
   const float* src;
   size_t step_gs, step_part, row_stride, which_stride;
@@ -2489,7 +2610,7 @@ __global__ __launch_bounds__(256) void fa_window_reduce_kernel(
     if (mine) atomicAdd(&before, mine);                    // (whole numbers: any order)
     __syncthreads();
     n = parts;
-    which_stride = (size_t)BK_KEYS * dh;
+    which_stride = (size_t)first.keys * dh;
     step_gs = 2 * which_stride;
     step_part = step_gs * Hkv * gsplit;
     row_stride = dh;
@@ -2501,7 +2622,7 @@ __global__ __launch_bounds__(256) void fa_window_reduce_kernel(
     row_stride = (size_t)Hkv * dh;
     src = part + (size_t)(lo + kt * BK_KEYS) * row_stride + hk * dh;
   }
-  const int row0 = blockIdx.z * REDUCE_ROWS, rows = min(REDUCE_ROWS, L - kt * BK_KEYS - row0), quads = dh / 4;
+  const int rows = min(REDUCE_ROWS, L - kt * BK_KEYS - row0), quads = dh / 4;
   for (int i = threadIdx.x; i < 2 * rows * quads; i += 256) {
     const int c = i % quads * 4, r = i / quads % rows, which = i / quads / rows;
     const float* p = src + which * which_stride + (size_t)(row0 + r) * row_stride + c;
@@ -2698,7 +2819,7 @@ bm_status window_token_launch(const AttnArgs& a, const TokenSplit& split, void* 
 
 // What the backward pass of a window takes as workspace, by sizes that do not depend on single lengths
 struct WindowBwd {
-  int gsplit, part_rows;
+  int gsplit, keys, part_rows;
   long parts;                          // at most
   size_t delta, split, first;          // floats of the three pieces
 };
@@ -2709,16 +2830,24 @@ WindowBwd window_bwd(int window, int sinks, int Hq, int Hkv, int dh, int S, int 
   // us, for 1024 -> 512 -> 256: 32 / 8 heads of 128, 8192 tokens, window 2048 1104 -> 1041 -> 1041, 256 650 -> 489 -> 489, 4096 448 -> 379 -> 347;
   // 32 / 8 of 64, 4096 207 -> 190 -> 239, 2048 94 -> 94 -> 129; 8 / 1 of 128, 32768, window 4096, 1705 -> 1733 -> 2463.
   w.gsplit = dkdv_group_split(2 * tiles, Hkv, Hq / Hkv);
-  // Parts of the first keys about as long as the tiles of other keys, and of 512 rows or, where the longest workgroup decides, 192 at least.  us, 512 ->
-  // 192: 780 tokens, window 1, 16 / 16 heads of 64 42 -> 29, of 72 44 -> 30, 5 / 1 of 128 53 -> 37; 2048, window 256, 8 / 2 of 64 52 -> 44; 777, window 131,
-  // 16 / 16 of 64 34 -> 33; but 780 of 32 / 8 of 128 58 -> 64, 8192 of 5 / 1 142 -> 176.
-  const int rows = (int)align_up(window < 4096 ? window : 4096, BK_Q);
-  const int least = (long)Tq * Hq <= 20480 ? 192 : 512;
-  w.part_rows = rows < least ? least : rows;
+  // Up to 32 first tokens: the 128-key tile would compute four times what they need.  us, parts of 128 keys -> of 32, 32 / 8 heads of 128, 4 first tokens:
+  // 8192 tokens, window 1024 677 -> 615, 256 436 -> 400, 64 340 -> 306; 2048, 128 149 -> 125; 16 / 16 heads of 64, 8192, 256 124 -> 113.
+  w.keys = sinks <= 32 ? 32 : BK_KEYS;
+  // Rows of a part: short where the longest workgroup decides, long where partials cost more.  us, 256 -> 512 -> 1024 rows for 32 keys: 439 tokens, window 16,
+  // 32 / 8 heads of 128 41 -> 50 -> 50, 16 / 16 of 64 25 -> 31 -> 31; 4096, 256, 16 / 16 of 128 132 -> 126 -> 131; 8192, 1024 374 -> 363 -> 339, 24 documents
+  // 239 -> 218 -> 205.  Of 128 keys, as long as the tiles of other keys; 192 -> 512: 780 tokens, window 1, 16 / 16 heads of 64 29 -> 42; 8192, 256, 5 / 1 of 128
+  // 176 -> 142.
+  const bool few = (long)Tq * Hq <= 20480;
+  if (w.keys == 32) {
+    w.part_rows = few ? 256 : Tq < 6144 ? 512 : 1024;
+  } else {
+    const int rows = (int)align_up(window < 4096 ? window : 4096, BK_Q), least = few ? 192 : 512;
+    w.part_rows = rows < least ? least : rows;
+  }
   w.parts = sinks > 0 ? 2L * Tq / w.part_rows : 0;         // a sequence that is split has more rows than one part
   w.delta = align_up((size_t)Hq * Tq, 64);
   w.split = w.gsplit > 1 ? (size_t)w.gsplit * 2 * Tk * Hkv * dh : 0;
-  w.first = (size_t)w.parts * Hkv * w.gsplit * 2 * BK_KEYS * dh;
+  w.first = (size_t)w.parts * Hkv * w.gsplit * 2 * w.keys * dh;
   return w;
 }
 
@@ -2742,6 +2871,7 @@ bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, c
   float* part = delta + wb.delta;
   FirstKeys first;
   first.mask = a.local;
+  first.keys = wb.keys;
   first.rows = wb.part_rows;
   first.out = part + wb.split;
   long parts = 0;
