@@ -415,12 +415,14 @@ Rotation rotation(const bm_qk_rotary_desc& d) {
   const int half = d.head_dim / 2;
   const double turn = 6.283185307179586476925286766559, log_base = std::log((double)d.base);
   int first = 0;
+  double fine[8], fine_step = NAN;                         // base^-(j) by eights and ones: two roundings more
   for (int a = 0; a < BM_ROTARY_MAX_AXES; ++a) {
-    const int n = a < d.n_axes ? d.pairs[a] : 0;
+    const int n = a < d.n_axes ? d.pairs[a] : 0, j0 = d.own_frequencies ? 0 : first;
     const double step = d.own_frequencies ? -log_base / std::max(n, 1) : -log_base / half;
-    const int j0 = d.own_frequencies ? 0 : first;
-    double fine[8];                                        // base^-(j) by eights and ones: two roundings more
-    for (int j = 0; j < std::min(n, 8); ++j) fine[j] = std::exp(step * j);
+    if (step != fine_step) {
+      fine_step = step;
+      for (int j = 0; j < 8; ++j) fine[j] = std::exp(step * j);
+    }
     for (int j = 0; j < n; j += 8) {
       const double coarse = std::exp(step * (j0 + j)) / turn;
       for (int e = j; e < std::min(n, j + 8); ++e) r.turns[first + e] = coarse * fine[e - j];
