@@ -2660,7 +2660,8 @@ bm_status window_fwd_launch(const AttnArgs& a, void* o, float* lse, hipStream_t 
 // 32 columns of S^T, so K and V are read once for the whole group.  Each wavefront streams its own tiles of 32 keys through places of
 // its own in LDS, without a barrier: the next tile's K follows as soon as this one's is in registers, its V behind the products with
 // V.  The four meet in LDS at the end, the parts of a sequence in window_join_kernel.
-// Bound by reading K and V.
+// Bound by reading K and V: 64 sequences of up to 4096 visible keys, 8 kv heads of 128, 171 us, 5.1 TB/s; 1000 of 1024 5.8 (places for two tiles in a
+// workgroup that has a CU alone: 186 us; 59 sequences of 300, 16 heads of 64, 42 instead of 15).
 template <int DH> constexpr int token_ring() { return DH == 64 ? 2 : 1; }
 template <int DH>
 __global__ __launch_bounds__(256, 2) void fa_window_token_kernel(
@@ -2852,14 +2853,14 @@ WindowBwd window_bwd(int window, int sinks, int Hq, int Hkv, int dh, int S, int 
 }
 
 // The wide dK/dV kernel (head size 128) or the one with 128 keys per workgroup?  dQ fills what either leaves of the chip, so the wide one needs no
-// whole rounds, but sequences that 256-key tiles cut about as well, and enough workgroups.  Whole backward, us, narrow -> wide, 32 / 8 heads: 8192
-// tokens, window 2048 1055 -> 950, 1024 658 -> 610, 256 488 -> 458; 24 documents 338 -> 310; 4096 386 -> 343; 32768, window 4096, 6500 -> 5757; 16 / 16
-// heads, 2048 tokens (128 workgroups) 115 -> 109; but 2 documents in 777 (128 of 32 / 8, 64 of 16 / 16 heads) 64 -> 76, 56 -> 62; 8 / 1 heads, 2048 (64)
-// 106 -> 118.
+// whole rounds, but windows longer than its tile, sequences that 256-key tiles cut about as well, and enough workgroups.  Whole backward, us, narrow ->
+// wide, 32 / 8 heads: 8192 tokens, window 2048 1055 -> 950, 1024 658 -> 610, but 256 379 -> 399, 64 286 -> 306; 24 documents, 1024, 338 -> 310; 4096 386 ->
+// 343; 32768, window 4096, 6500 -> 5757; 16 / 16 heads, 2048 tokens (128 workgroups) 115 -> 109; but 2 documents in 777 (128 of 32 / 8, 64 of 16 / 16 heads)
+// 64 -> 76, 56 -> 62; 8 / 1 heads, 2048 (64) 106 -> 118.
 bool window_wide(const AttnArgs& a, int gsplit) {
   const int tw = count_tiles(a.kv_cu_host(), a.key_end_host, a.S, WIDE_KEYS), tn = count_tiles(a.kv_cu_host(), a.key_end_host, a.S, BK_KEYS);
   const long wgs = (long)tw * a.Hkv * gsplit;
-  return tw * 8L <= tn * 5L && (wgs >= NUM_CU || (wgs >= NUM_CU / 2 && tw >= 4 * a.S));
+  return a.local.window >= 512 && tw * 8L <= tn * 5L && (wgs >= NUM_CU || (wgs >= NUM_CU / 2 && tw >= 4 * a.S));
 }
 
 template <int DH>
