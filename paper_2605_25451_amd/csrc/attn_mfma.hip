@@ -129,7 +129,7 @@ __device__ inline const bf16_t* scalar_ptr(const void* p) {
 // s ^ tile_swizzle(row).  Padding slots (head sizes that are no multiple of 32) are never written
 // by a load: zero() clears them once.  The loads are asynchronous: wait for vmcnt(0), then a
 // workgroup barrier, before any wavefront reads the tile.
-template <int ROWS, int DH, int NT>
+template <int ROWS, int DH, int NT, bool STREAM = false>
 struct TileAsync {
   static constexpr int DHL = HeadDim<DH>::DHL;
   static constexpr int CPR = DHL / 8;
@@ -158,13 +158,18 @@ struct TileAsync {
       goff[i] = (uint32_t)row * (uint32_t)ld * 2u + (uint32_t)c * 16u;
     }
   }
+  // STREAM: past the caches, for data that no other workgroup reads.
   // One 16-byte load per lane straight into LDS.  Written as inline assembly so that the compiler does
   // not see an LDS write in flight: it would otherwise make every LDS read that follows wait for
   // vmcnt(0) and the tile would no longer stream in behind the arithmetic.  The caller orders the
   // reads of a tile after wait_async_tiles() and a barrier.
   static __device__ inline void load16(const void* base, uint32_t voff, uint32_t lds_addr) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                 :: "s"(lds_addr), "v"(voff), "s"(base) : "memory", "m0");
+    if constexpr (STREAM)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
+                   :: "s"(lds_addr), "v"(voff), "s"(base) : "memory", "m0");
+    else
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                   :: "s"(lds_addr), "v"(voff), "s"(base) : "memory", "m0");
   }
   // base: first row of the tile (wave-uniform); rows_left: valid rows from there (>= 1), rows beyond
   // them are clamped to the last valid one (their results are masked or unused); wave: wave-uniform
@@ -2660,17 +2665,17 @@ bm_status window_fwd_launch(const AttnArgs& a, void* o, float* lse, hipStream_t 
 // 32 columns of S^T, so K and V are read once for the whole group.  Each wavefront streams its own tiles of 32 keys through places of
 // its own in LDS, without a barrier: the next tile's K follows as soon as this one's is in registers, its V behind the products with
 // V.  The four meet in LDS at the end, the parts of a sequence in window_join_kernel.
-// Bound by reading K and V: 64 sequences of up to 4096 visible keys, 8 kv heads of 128, 171 us, 5.1 TB/s; 1000 of 1024 5.8 (places for two tiles in a
+// Bound by reading K and V: 64 sequences of up to 4096 visible keys, 8 kv heads of 128, 153 us, 5.75 TB/s; 1000 of 1024 6.4 (places for two tiles in a
 // workgroup that has a CU alone: 186 us; 59 sequences of 300, 16 heads of 64, 42 instead of 15).
 template <int DH> constexpr int token_ring() { return DH == 64 ? 2 : 1; }
-template <int DH>
+template <int DH, bool STREAM>
 __global__ __launch_bounds__(256, 2) void fa_window_token_kernel(
     const bf16_t* __restrict__ q, const bf16_t* __restrict__ k, const bf16_t* __restrict__ v, int ld, int ldk,
     const int32_t* __restrict__ cu, const int32_t* __restrict__ cuk, int S, bf16_t* __restrict__ o, int ldo,
     float* __restrict__ lse, int Ttot, int Hkv, int group, float scale_log2, LocalMask w, TokenSplit split) {
   constexpr int DHL = HeadDim<DH>::DHL, KS = HeadDim<DH>::KS, NB = HeadDim<DH>::NB, TILE = TOKEN_KEYS * DHL;
   constexpr int RING = token_ring<DH>(), OS = DH == 128 ? DH : DH + 4;       // OS: row stride of what a wavefront leaves
-  using Tile = TileAsync<TOKEN_KEYS, DH, 64>;
+  using Tile = TileAsync<TOKEN_KEYS, DH, 64, STREAM>;
   constexpr int CH = Tile::CH;                             // loads of a tile of K or V
   static_assert(RING * 2 * TILE * 2 >= 32 * OS * 4, "a wavefront's sums take its tiles' place");
   __shared__ __attribute__((aligned(1024))) bf16_t ring[4 * RING * 2 * TILE];
@@ -2811,7 +2816,7 @@ __global__ __launch_bounds__(256, 2) void fa_window_token_kernel(
 
 template <int DH>
 bm_status window_token_launch(const AttnArgs& a, const TokenSplit& split, void* o, float* lse, hipStream_t st) {
-  hipLaunchKernelGGL((fa_window_token_kernel<DH>), dim3(token_grid(split, a.Hkv)), dim3(256), 0, st, (const bf16_t*)a.q, (const bf16_t*)a.k,
+  hipLaunchKernelGGL((split.stream ? fa_window_token_kernel<DH, true> : fa_window_token_kernel<DH, false>), dim3(token_grid(split, a.Hkv)), dim3(256), 0, st, (const bf16_t*)a.q, (const bf16_t*)a.k,
                      (const bf16_t*)a.v, a.ld_qkv, a.kv_ld(), a.cu_dev, a.kv_cu_dev(), a.S, (bf16_t*)o, a.Hq * a.dh, lse, a.T, a.Hkv,
                      a.Hq / a.Hkv, LOG2E / sqrtf((float)a.dh), a.local, split);
   BM_CHECK_LAUNCH("fa_window_token");

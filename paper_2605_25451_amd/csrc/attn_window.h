@@ -37,7 +37,7 @@ constexpr int TOKEN_KEYS = 32;       // keys of a tile
 constexpr int TOKEN_ROWS = 32;       // queries x heads of a group, at most
 constexpr int TOKEN_TABLE = 64;
 struct TokenSplit {
-  int per, rows, wgs, same_xcd;      // rows: of the sequence with most queries
+  int per, rows, wgs, same_xcd, stream;       // rows: of the sequence with most queries
   float *sums, *stats;
   int n;                             // sequences whose parts stand below (0: more than the table holds, see map)
   // written by window_map_kernel: [S+1] first part and [S] first place of a sequence, [S] those of more than one part, [parts] the sequence

@@ -33,7 +33,16 @@ template <int P> __device__ inline float lanes_sum(float v) {      // over the l
 //   values: the lanes of a row hold 16 bytes of it each, the weights come back from LDS
 // Bound by reading K and V up to four rows.
 constexpr int RB = 4;
-template <typename T, int DH>
+template <bool STREAM, typename T>
+__device__ inline void read16(const T* p, float (&x)[Elt<T>::VEC]) {
+  using Raw = unsigned int __attribute__((ext_vector_type(4)));
+  struct alignas(16) Run { T v[Elt<T>::VEC]; };
+  const Raw* from = reinterpret_cast<const Raw*>(p);
+  const Run run = __builtin_bit_cast(Run, STREAM ? __builtin_nontemporal_load(from) : *from);
+#pragma unroll
+  for (int e = 0; e < Elt<T>::VEC; ++e) x[e] = Elt<T>::to_f(run.v[e]);
+}
+template <typename T, int DH, bool STREAM>
 __global__ __launch_bounds__(256) void window_token_kernel(
     const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, int ld, int ldk, const int32_t* __restrict__ cu,
     const int32_t* __restrict__ cuk, int S, T* __restrict__ o, int ldo, float* __restrict__ lse, int Ttot, int Hkv, int group,
@@ -93,7 +102,7 @@ __global__ __launch_bounds__(256) void window_token_kernel(
 #pragma unroll
       for (int n = 0; n < CL; ++n) {
         float x[VEC];
-        load16(row + min(j + 8 * n, CH - 1) * VEC, x);
+        read16<STREAM>(row + min(j + 8 * n, CH - 1) * VEC, x);
 #pragma unroll
         for (int r = 0; r < RB; ++r)
 #pragma unroll
@@ -130,7 +139,7 @@ __global__ __launch_bounds__(256) void window_token_kernel(
     for (int i = 0; i < 64 / KV; ++i) {
       const int n = i * KV + vg;
       float x[VEC];
-      load16(vb + (size_t)min(seen_row(w, begin, key_of(n)), Lk - 1) * ldk + min(vc, CH - 1) * VEC, x);
+      read16<STREAM>(vb + (size_t)min(seen_row(w, begin, key_of(n)), Lk - 1) * ldk + min(vc, CH - 1) * VEC, x);
       const float4 f = *reinterpret_cast<const float4*>(weight[wave][n]);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
@@ -276,7 +285,7 @@ __global__ __launch_bounds__(256) void window_join_kernel(const int32_t* __restr
 
 template <typename T, int DH>
 void token_launch(const AttnArgs& a, const TokenSplit& split, void* o, float* lse, hipStream_t st) {
-  hipLaunchKernelGGL((window_token_kernel<T, DH>), dim3(token_grid(split, a.Hkv), cdiv(split.rows, RB)), dim3(256), 0, st, (const T*)a.q,
+  hipLaunchKernelGGL((split.stream ? window_token_kernel<T, DH, true> : window_token_kernel<T, DH, false>), dim3(token_grid(split, a.Hkv), cdiv(split.rows, RB)), dim3(256), 0, st, (const T*)a.q,
                      (const T*)a.k, (const T*)a.v, a.ld_qkv, a.kv_ld(), a.cu_dev, a.kv_cu_dev(), a.S, (T*)o, a.Hq * a.dh, lse, a.T,
                      a.Hkv, a.Hq / a.Hkv, LOG2E / sqrtf((float)a.dh), a.local, split);
 }
@@ -320,6 +329,10 @@ bm_status window_tokens(const AttnArgs& a, void* scratch, void* o, float* lse, h
     joins += n > 1;
   }
   t.wgs = (int)(parts * a.Hkv);
+  // Keys and values past the caches, where they are more than the L2s hold and read by one workgroup each.  us, through them -> past: 64 sequences of up to 4096
+  // (883 MB) 171 -> 153, 256 of 1024 172 -> 151, 1000 of 1024 518 -> 467, 4 of 4096 (67 MB) 22.2 -> 21.4; but 55 of 300 (39 MB) 12.6 -> 13.1, 59 of 300, 16 heads
+  // of 64 (43 MB) 14.9 -> 15.2; fp32, 16 of 2000 46 -> 42.
+  t.stream = (mfma_head(a.dtype, a.dh) || t.rows <= RB) && (double)tiles * TOKEN_KEYS * a.Hkv * a.dh * 2 * elt_size(a.dtype) > 60e6;
   // The kv heads of a part on one XCD, where a row of a head is no whole cache lines or the chip is full many times: us, 20 sequences of 2000, 16
   // heads of 72, 44.5 -> 35.9; 1000 of 1024, 8 kv heads of 128, 541 -> 517, 256 174 -> 172.5; but one of 8192 13.8 -> 14.5, 16 101 -> 104.
   t.same_xcd = a.dh * elt_size(a.dtype) % 128 != 0 || t.wgs >= 8 * NUM_CU;
