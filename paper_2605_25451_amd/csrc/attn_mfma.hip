@@ -944,6 +944,12 @@ __device__ inline bool find_part(const FirstKeys& f, const int32_t* __restrict__
   }
   return false;
 }
+// The queries that see a key, as a range of elements counted from row `base`: from .. from + n - 1; rows from `qend` on do not take part
+struct SeenBy { int from; uint32_t n; };
+__device__ inline SeenBy seen_by(const LocalMask& w, int key, int L, int off, int base, int qend) {
+  const int from = key - off - base, to = min(qend - base, key >= w.sinks ? from + w.window : qend - base);
+  return SeenBy{from, key < L ? (uint32_t)max(0, to - from) : 0u};
+}
 // Where a workgroup of dK/dV works with it: a tile of KEYS keys, or a part of the first one, and the query rows that it walks
 struct KeyTile { int seq, kt, part, hk_gs, qlo, qhi, from; };      // from: the first key that is not the parts'
 template <int KEYS>
@@ -1075,6 +1081,8 @@ __device__ inline void dkdv_tile(unsigned char* lds, int block, const bf16_t* __
     __syncthreads();      // tile `it` is there for everyone, and everyone is done with tile it-1
     if (it + 1 < iters) fetch(it + 1, 1 - PAR);
     const int q0 = qstart + (it % nqt) * BK_Q;
+    SeenBy seen = {0, 0};
+    if constexpr (WINDOW && MASKED) seen = seen_by(first.mask, kpos, L, off, q0 + half * 4, qend);
     // S = Q K^T and dP = dO V^T for both 32-query blocks first, then per block the
     // softmax arithmetic (under the other block's MFMAs) followed by its dV / dK MFMAs.
     f32x16 sacc[BK_Q / 32], dpacc[BK_Q / 32];
@@ -1126,9 +1134,10 @@ __device__ inline void dkdv_tile(unsigned char* lds, int block, const bf16_t* __
         for (int e = 0; e < 4; ++e) {
           const int r = g * 4 + e;
           float p = __builtin_amdgcn_exp2f(fmaf(sacc[qb][r], scale_log2, -l4[e]));
-          if (MASKED) {
+          if (WINDOW && MASKED) p = (uint32_t)(qb * 32 + g * 8 + e - seen.from) < seen.n ? p : 0.f;
+          if (!WINDOW && MASKED) {
             const int qi = q0 + qoff + e;
-            if (qi >= qend || kpos >= L || (WINDOW ? hidden(first.mask, kpos, off + qi) : CAUSAL && kpos > qi)) p = 0.f;
+            if (qi >= qend || kpos >= L || (CAUSAL && kpos > qi)) p = 0.f;
           }
           sacc[qb][r] = p;
           dpacc[qb][r] = FOLD_DELTA ? p * dpacc[qb][r] : p * (dpacc[qb][r] - d4[e]);
@@ -1369,6 +1378,8 @@ __device__ inline void dkdv_pair_tile(
     }
     bf16x8 op[NQB][2];                                  // B operands of phase 2: P (role 0) or dS (role 1)
     if (role == 0) {
+      SeenBy seen = {0, 0};
+      if constexpr (WINDOW && MASKED) seen = seen_by(first.mask, kpos, L, off, q0 + half * 4, qend);
 #pragma unroll
       for (int qb = 0; qb < NQB; ++qb) {
 #pragma unroll
@@ -1379,9 +1390,10 @@ __device__ inline void dkdv_pair_tile(
           for (int e = 0; e < 4; ++e) {
             const int r = g * 4 + e;
             float p = __builtin_amdgcn_exp2f(fmaf(xacc[qb][r], scale_log2, -l4[e]));
-            if (MASKED) {
+            if (WINDOW && MASKED) p = (uint32_t)(qb * 32 + g * 8 + e - seen.from) < seen.n ? p : 0.f;
+            if (!WINDOW && MASKED) {
               const int qi = q0 + qoff + e;
-              if (qi >= qend || kpos >= L || (WINDOW ? hidden(first.mask, kpos, off + qi) : CAUSAL && kpos > qi)) p = 0.f;
+              if (qi >= qend || kpos >= L || (CAUSAL && kpos > qi)) p = 0.f;
             }
             xacc[qb][r] = p;
           }
@@ -2457,6 +2469,7 @@ __device__ inline void first_keys_part(unsigned char* lds, int block, const Wind
     wait_async_tiles();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (a wavefront's own rows: no barrier)
     __builtin_amdgcn_wave_barrier();
+    const SeenBy seen = seen_by(f.mask, kpos, L, off, q0 + half * 4, qhi);
     f32x16 s = {}, dp = {};
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
@@ -2468,8 +2481,8 @@ __device__ inline void first_keys_part(unsigned char* lds, int block, const Wind
       const f32x4 l4 = *reinterpret_cast<const f32x4*>(stats + g * 8 + half * 4), d4 = *reinterpret_cast<const f32x4*>(stats + 32 + g * 8 + half * 4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int r = g * 4 + e, qi = q0 + g * 8 + half * 4 + e;
-        const float p = qi >= qhi || hidden(f.mask, kpos, off + qi) ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2, -l4[e]));
+        const int r = g * 4 + e;
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2, -l4[e])), p = (uint32_t)(g * 8 + e - seen.from) < seen.n ? x : 0.f;
         s[r] = p;
         dp[r] = p * (dp[r] - d4[e]);
       }
@@ -2568,6 +2581,15 @@ __global__ __launch_bounds__(512, 2) void fa_window_bwd512_kernel(WindowBwdArgs 
                             a.ldk, a.d_o, a.ldo, a.lse, a.delta, a.cuq, a.cuk, a.S, a.dq, a.ldd, a.Tq, a.group, a.scale, a.scale_log2,
                             ord_q, first.mask);
   }
+}
+
+template <int DH>
+__global__ __launch_bounds__(256, 2) void fa_window_dq_kernel(WindowBwdArgs a, SeqOrder ord, LocalMask w) {
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[dq_lds_bytes<DH>()];
+  int tile, head;
+  tile_and_head(a.Hkv * a.group, &tile, &head, blockIdx.x);
+  dq_tile<DH, true, true>(lds, threadIdx.x, tile, head, true, a.q, a.k, a.v, a.ld, a.ldk, a.d_o, a.ldo, a.lse, a.delta, a.cuq, a.cuk, a.S,
+                          a.dq, a.ldd, a.Tq, a.group, a.scale, a.scale_log2, ord, w);
 }
 
 // the sequence that is the id-th of those whose first keys are in parts
@@ -2894,7 +2916,10 @@ bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, c
   if (a.T > 0)
     hipLaunchKernelGGL((fa_delta_kernel<DH>), dim3(cdiv((long)a.T * a.Hq * DeltaLanes<DH>::N, 256)), dim3(256), 0, st,
                        (const bf16_t*)o, (const bf16_t*)d_o, ldo, delta, a.T, a.Hq);
-  const int query_rows = DH == 128 ? AQ : FQ, heads_per_wg = DH == 72 ? 2 : 1;
+  // dQ of narrow windows apart, in tiles of 128 rows and two workgroups to a CU, where there are enough of them: us, together -> apart, 8192 tokens, 32 / 8
+  // heads, window 64 288 -> 275, 256 381 -> 370, 512 485 -> 482; 16 / 16 heads 185 -> 172, 225 -> 217; but 2048 tokens, 16 / 16 heads, 64 (256) 62 -> 66.
+  const bool apart = DH == 128 && a.local.window < 512 && count_tiles(a.cu_host, a.S, FQ) * a.Hq >= 2 * NUM_CU;
+  const int query_rows = DH == 128 && !apart ? AQ : FQ, heads_per_wg = DH == 72 ? 2 : 1;
   bool wide = false;
   if constexpr (DH == 128) wide = window_wide(a, wb.gsplit);
   const int key_rows = wide ? WIDE_KEYS : BK_KEYS;
@@ -2905,7 +2930,7 @@ bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, c
   const WindowBwdArgs w{(const bf16_t*)a.q, (const bf16_t*)a.k, (const bf16_t*)a.v, (const bf16_t*)d_o, lse, delta, a.cu_dev, a.kv_cu_dev(),
                         (bf16_t*)dq, (bf16_t*)dk, (bf16_t*)dv, part, a.ld_qkv, a.kv_ld(), ldo, ldd, a.ld_dkv, a.S, a.T, Tk, a.Hkv, group,
                         wb.gsplit, kv_wgs, scale, sl2};
-  const int wgs = kv_wgs + q_wgs;
+  const int wgs = kv_wgs + (apart ? 0 : q_wgs);
   if (wgs > 0) {
     if constexpr (DH <= 64) hipLaunchKernelGGL(fa_window_bwd_kernel<DH>, dim3(wgs), dim3(256), 0, st, w, ord_kv, ord_q, first);
     else {
@@ -2914,6 +2939,8 @@ bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, c
       hipLaunchKernelGGL(kern, dim3(wgs), dim3(512), 0, st, w, ord_kv, ord_q, first);
     }
   }
+  if constexpr (DH == 128)
+    if (apart && q_wgs > 0) hipLaunchKernelGGL((fa_window_dq_kernel<DH>), dim3(q_wgs), dim3(256), 0, st, w, ord_q, a.local);
   const int all_tiles = wb.gsplit > 1;
   if (kv_wgs > 0 && (all_tiles || parts > 0)) {
     const SeqOrder ord = wide ? make_seq_order(a.kv_cu_host(), a.cu_host, a.S, BK_KEYS, false, a.key_end_host) : ord_kv;
