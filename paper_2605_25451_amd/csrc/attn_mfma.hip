@@ -343,6 +343,26 @@ __device__ inline bool all_visible(const LocalMask& w, int key0, int n, int a, i
 __device__ inline bool none_visible(const LocalMask& w, int key0, int n, int a, int m) {
   return key0 > a + m - 1 || (a - (key0 + n - 1) >= w.window && key0 >= w.sinks);
 }
+// Scores of NB blocks of 32 keys from key0 on that the query at `ahead` behind key0 + half * 4 does not see become -inf; first_at: the first of the
+// wavefront's 32 queries.  Most tiles that need a test need one of the two.
+template <int NB>
+__device__ inline void hide_scores(const LocalMask& w, int key0, int first_at, int ahead, int half4, f32x16 (&s)[NB]) {
+  if (key0 + NB * 32 - 1 > first_at)
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[b][r] = b * 32 + (r >> 2) * 8 + (r & 3) > ahead ? -INFINITY : s[b][r];
+  if (first_at + 31 - key0 >= w.window && key0 + NB * 32 > w.sinks) {
+    const int behind = ahead - w.window, sinks = w.sinks - key0 - half4;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int e = b * 32 + (r >> 2) * 8 + (r & 3);
+        s[b][r] = e <= behind && e >= sinks ? -INFINITY : s[b][r];
+      }
+  }
+}
 // Linear workgroup id -> (tile id, head).  Heads vary fastest, and since workgroup
 // ids go round-robin over the 8 XCDs, head index i lands on XCD i%8: give XCD x
 // the consecutive heads x*(H/8).., so every tile of one head -- and the q heads of
@@ -475,25 +495,7 @@ __global__ __launch_bounds__(256, 2) void fa_fwd_kernel(
       }
     }
     // mask: keys past the sequence end, and keys after the query under a causal mask
-    if constexpr (WINDOW && MASKED) {
-      // (element (b, r): key key0 + half * 4 + e; most tiles that need a test need one of the two)
-      const int first_at = off + q0 + wave_u * 32, ahead = off + qpos - key0 - half * 4;
-      if (key0 + FK - 1 > first_at)
-#pragma unroll
-        for (int b = 0; b < FK / 32; ++b)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) sacc[b][r] = b * 32 + (r >> 2) * 8 + (r & 3) > ahead ? -INFINITY : sacc[b][r];
-      if (first_at + 31 - key0 >= w.window && key0 + FK > w.sinks) {
-        const int behind = ahead - w.window, sinks = w.sinks - key0 - half * 4;
-#pragma unroll
-        for (int b = 0; b < FK / 32; ++b)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int e = b * 32 + (r >> 2) * 8 + (r & 3);
-            sacc[b][r] = e <= behind && e >= sinks ? -INFINITY : sacc[b][r];
-          }
-      }
-    }
+    if constexpr (WINDOW && MASKED) hide_scores<FK / 32>(w, key0, off + q0 + wave_u * 32, off + qpos - key0 - half * 4, half * 4, sacc);
 #pragma unroll
     for (int b = 0; b < FK / 32; ++b) {
       float mx = -INFINITY;
@@ -1907,7 +1909,7 @@ __device__ inline void dq_tile(unsigned char* lds, int tid, int tile_id, int hq,
       tile.issue(kbase + next, ldk, Lk - nt * FKD, Kbuf + (1 - PAR) * TILE, wave_u);
       tile.issue(vbase + next, ldk, Lk - nt * FKD, Vbuf + (1 - PAR) * TILE, wave_u);
     }
-    const int key0 = walk.tile(kt) * FKD, ahead = off + qpos - key0 - half * 4, sinks = WINDOW ? w.sinks - key0 - half * 4 : 0;
+    const int key0 = walk.tile(kt) * FKD;
     // S^T = K Q^T and dP^T = V dO^T of BP 32-key blocks are issued before any softmax arithmetic,
     // so that one block's MFMAs run under the other's vector work; at head size 128 that is one
     // block at a time (two sets of accumulators do not fit next to two resident wavefronts).
@@ -1937,15 +1939,19 @@ __device__ inline void dq_tile(unsigned char* lds, int tid, int tile_id, int hq,
           __builtin_amdgcn_sched_barrier(0);
         }
       }
+      if constexpr (WINDOW && MASKED) {
+        const int first_key = key0 + b0 * 32;
+        hide_scores<BP>(w, first_key, off + q0 + wave_u * 32, off + qpos - first_key - half * 4, half * 4, sacc);
+      }
 #pragma unroll
       for (int bi = 0; bi < BP; ++bi) {
         const int b = b0 + bi;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           float p = __builtin_amdgcn_exp2f(fmaf(sacc[bi][r], scale_log2, -my_lse));
-          if (MASKED) {
-            const int e = b * 32 + (r >> 2) * 8 + (r & 3), key = key0 + half * 4 + e;
-            if (WINDOW ? e > ahead || (e <= ahead - w.window && e >= sinks) : key >= Lk || (CAUSAL && key > qpos)) p = 0.f;
+          if (MASKED && !WINDOW) {
+            const int key = key0 + b * 32 + (r >> 2) * 8 + half * 4 + (r & 3);
+            if (key >= Lk || (CAUSAL && key > qpos)) p = 0.f;
           }
           dpacc[bi][r] = FOLD_DELTA ? p * dpacc[bi][r] : p * (dpacc[bi][r] - my_delta);
         }
@@ -2165,16 +2171,21 @@ __device__ inline void dq_alt_tile(
   };
   auto softmax = [&](int t) {
     const int key0 = walk.tile(t) * FK;
-    if (WINDOW ? !all_visible(w, key0, FK, off + qfirst, 32) : t >= plain) {
+    if constexpr (WINDOW) {
+      if (!all_visible(w, key0, FK, off + qfirst, 32)) {
+        asm volatile("");                                  // keeps the tests out of the tiles that need none
+        const int h4 = (fresh_lane() >> 5) * 4;
+        hide_scores<KBL>(w, key0, off + qfirst, off + qfirst + (fresh_lane() & 31) - key0 - h4, h4, sacc);
+      }
+    } else if (t >= plain) {
       asm volatile("");                                    // keeps the tests out of the tiles that need none
-      const int h4 = (fresh_lane() >> 5) * 4, left = Lk - key0 - h4, ahead = off + qfirst + (fresh_lane() & 31) - key0 - h4;
-      const int behind = ahead - (WINDOW ? w.window : 0), sinks = WINDOW ? w.sinks - key0 - h4 : 0;
+      const int h4 = (fresh_lane() >> 5) * 4, left = Lk - key0 - h4, ahead = qfirst + (fresh_lane() & 31) - key0 - h4;
 #pragma unroll
       for (int b = 0; b < KBL; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int e = b * 32 + (r >> 2) * 8 + (r & 3);
-          if (WINDOW ? e > ahead || (e <= behind && e >= sinks) : e >= left || (CAUSAL && e > ahead)) sacc[b][r] = -INFINITY;   // P = 0
+          if (e >= left || (CAUSAL && e > ahead)) sacc[b][r] = -INFINITY;   // P = 0
         }
     }
 #pragma unroll
