@@ -1702,17 +1702,25 @@ __device__ inline void dkdv_wide_tile(
                    : keys_cut || q0 + W::ROWS > Lq || (CAUSAL && q0 < key0 + 63)) {
           asm volatile("");                                 // keeps the tests out of the steps that need none
           const int l = fresh_lane(), h4 = (l >> 5) * 4, ki = key0 + (l & 31);
-          const int q_left = qend - q0 - h4, k_left = L - ki, ahead = ki - off - q0 - h4;
-          const int behind = ahead + (WINDOW ? first.mask.window : 0), sinks = WINDOW ? first.mask.sinks - ki : 0;
+          if constexpr (WINDOW) {
 #pragma unroll
-          for (int g = 0; g < 4; ++g)
+            for (int b = 0; b < KB; ++b) {
+              const SeenBy seen = seen_by(first.mask, ki + b * 32, L, off, q0 + h4, qend);
 #pragma unroll
-            for (int b = 0; b < KB; ++b)
+              for (int r = 0; r < 16; ++r)
+                x[b][r] = (uint32_t)((r >> 2) * 8 + (r & 3) - seen.from) < seen.n ? x[b][r] : -INFINITY;      // P = 0
+            }
+          } else {
+            const int q_left = Lq - q0 - h4, k_left = L - ki, ahead = ki - q0 - h4;
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (q_left <= g * 8 + e || k_left <= b * 32 || (CAUSAL && ahead > g * 8 + e - b * 32) ||
-                    (WINDOW && behind <= g * 8 + e - b * 32 && sinks <= b * 32))
-                  x[b][g * 4 + e] = -INFINITY;              // P = 0
+            for (int g = 0; g < 4; ++g)
+#pragma unroll
+              for (int b = 0; b < KB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (q_left <= g * 8 + e || k_left <= b * 32 || (CAUSAL && ahead > g * 8 + e - b * 32))
+                    x[b][g * 4 + e] = -INFINITY;            // P = 0
+          }
         }
         const unsigned char* stats = tile_of(n) + STATS_AT + (fresh_lane() >> 5) * 16;
 #pragma unroll
@@ -2424,8 +2432,8 @@ bm_status bwd_launch(const AttnArgs& a, const void* o, const void* d_o, const fl
 // =============================================================================
 // The backward pass in one grid: the parts of first keys, the other key tiles, then dQ, which fills what they leave (as in
 // fa_bwd_joint_kernel and fa_bwd_joint512_kernel; head size 72, 16 heads, dQ of 128 rows apart -> here: 8192 tokens 280 -> 275 us, 4096 178 -> 160,
-// 777 59 -> 38, 32768 2765 -> 2796).  At head size 128 dQ takes 256 rows and turns for any length: 128 rows of two heads are behind by 0 to
-// 6 % (8192 tokens, 32 / 8 heads, window 256 435 -> 455, 2048 957 -> 972).
+// 777 59 -> 38, 32768 2765 -> 2796).  At head size 128 dQ takes 256 rows and turns: 128 rows of two heads side by side are behind by 0 to 6 %
+// (8192 tokens, 32 / 8 heads, window 256 435 -> 455, 2048 957 -> 972, before tests of a tile's front and back came apart).
 struct WindowBwdArgs {
   const bf16_t *q, *k, *v, *d_o;
   const float *lse, *delta;
@@ -2891,14 +2899,14 @@ WindowBwd window_bwd(int window, int sinks, int Hq, int Hkv, int dh, int S, int 
 }
 
 // The wide dK/dV kernel (head size 128) or the one with 128 keys per workgroup?  dQ fills what either leaves of the chip, so the wide one needs no
-// whole rounds, but windows longer than its tile, sequences that 256-key tiles cut about as well, and enough workgroups.  Whole backward, us, narrow ->
-// wide, 32 / 8 heads: 8192 tokens, window 2048 1055 -> 950, 1024 658 -> 610, but 256 379 -> 399, 64 286 -> 306; 24 documents, 1024, 338 -> 310; 4096 386 ->
-// 343; 32768, window 4096, 6500 -> 5757; 16 / 16 heads, 2048 tokens (128 workgroups) 115 -> 109; but 2 documents in 777 (128 of 32 / 8, 64 of 16 / 16 heads)
-// 64 -> 76, 56 -> 62; 8 / 1 heads, 2048 (64) 106 -> 118.
+// whole rounds, but windows as long as its tile, sequences that 256-key tiles cut about as well, and enough workgroups.  Whole backward, us, narrow ->
+// wide, 32 / 8 heads: 8192 tokens, window 2048 943 -> 881, 1024 592 -> 552, 256 312 -> 306, but 64 229 -> 242; 24 documents, 1024, 275 -> 261; 16 / 16 heads,
+// 8192, 256 196 -> 188, 2048 tokens (128 workgroups), 1024, 101 -> 95; but 2 documents in 777 (128 of 32 / 8, 64 of 16 / 16 heads) 53 -> 60, 38 -> 47; 5 / 1
+// heads, 2048 (40) 39 -> 48.
 bool window_wide(const AttnArgs& a, int gsplit) {
   const int tw = count_tiles(a.kv_cu_host(), a.key_end_host, a.S, WIDE_KEYS), tn = count_tiles(a.kv_cu_host(), a.key_end_host, a.S, BK_KEYS);
   const long wgs = (long)tw * a.Hkv * gsplit;
-  return a.local.window >= 512 && tw * 8L <= tn * 5L && (wgs >= NUM_CU || (wgs >= NUM_CU / 2 && tw >= 4 * a.S));
+  return a.local.window >= 256 && tw * 8L <= tn * 5L && (wgs >= NUM_CU || (wgs >= NUM_CU / 2 && tw >= 4 * a.S));
 }
 
 template <int DH>
@@ -2928,8 +2936,9 @@ bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, c
     hipLaunchKernelGGL((fa_delta_kernel<DH>), dim3(cdiv((long)a.T * a.Hq * DeltaLanes<DH>::N, 256)), dim3(256), 0, st,
                        (const bf16_t*)o, (const bf16_t*)d_o, ldo, delta, a.T, a.Hq);
   // dQ of narrow windows apart, in tiles of 128 rows and two workgroups to a CU, where there are enough of them: us, together -> apart, 8192 tokens, 32 / 8
-  // heads, window 64 288 -> 275, 256 381 -> 370, 512 485 -> 482; 16 / 16 heads 185 -> 172, 225 -> 217; but 2048 tokens, 16 / 16 heads, 64 (256) 62 -> 66.
-  const bool apart = DH == 128 && a.local.window < 512 && count_tiles(a.cu_host, a.S, FQ) * a.Hq >= 2 * NUM_CU;
+  // heads, window 16 210 -> 175, 64 229 -> 224, 128 262 -> 263, 256 313 -> 318; 16 / 16 heads 143 -> 129, 152 -> 146, 172 -> 169, 196 -> 199; but 2048 tokens, 16 / 16
+  // heads, 64 (256) 53 -> 59.
+  const bool apart = DH == 128 && a.local.window <= 64 && count_tiles(a.cu_host, a.S, FQ) * a.Hq >= 2 * NUM_CU;
   const int query_rows = DH == 128 && !apart ? AQ : FQ, heads_per_wg = DH == 72 ? 2 : 1;
   bool wide = false;
   if constexpr (DH == 128) wide = window_wide(a, wb.gsplit);
