@@ -412,10 +412,13 @@ def test_window_of_many_sequences(dtype, dh, sinks):
 
 @pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("bf16", 64)])
 @pytest.mark.parametrize("sinks", [0, 5, 90])
-@pytest.mark.parametrize("heads,seqs", [((16, 16), [(2100, 2100)]), ((16, 8), [(2200, 2300)]), ((12, 6), [(1500, 1500), (40, 900), (700, 1111)])], ids=str)
-def test_window_of_long_sequences(heads, seqs, sinks, dtype, dh):
-    """Packs that fill the chip: 256 keys to a workgroup of dK/dV at head size 128, q heads of a group in parts, first keys in parts of 512 rows."""
-    x = Window(dtype, *heads, dh, seqs, 530 if heads[0] > 12 else 60, sinks, seed=14, gap=2 if seqs[0][0] != seqs[0][1] else None)
+@pytest.mark.parametrize("heads,seqs,window", [((16, 16), [(2100, 2100)], 530), ((16, 8), [(2200, 2300)], 530),
+                                               ((12, 6), [(1500, 1500), (40, 900), (700, 1111)], 300),
+                                               ((12, 6), [(1500, 1500), (40, 900), (700, 1111)], 60)], ids=str)
+def test_window_of_long_sequences(heads, seqs, window, sinks, dtype, dh):
+    """Packs that fill the chip: 256 keys to a workgroup of dK/dV at head size 128, dQ of a narrow window in a launch of its own, q heads of a group in
+    parts, first keys in parts of 512 rows."""
+    x = Window(dtype, *heads, dh, seqs, window, sinks, seed=14, gap=2 if seqs[0][0] != seqs[0][1] else None)
     x.check_forward(*x.forward())
     x.check_backward(*x.backward())
 
