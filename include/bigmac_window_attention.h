@@ -84,8 +84,10 @@ bm_status bm_qk_rotary_backward(const bm_qk_rotary_desc* desc, int32_t T, const 
  *                    share rows (a common beginning); the backward pass takes them one behind the other
  *   cu_q, k_begin, k_end are given twice, in device and in host memory, with the same values
  *   o, d_o    dev    [Tq, Hq*dh], lse dev [Hq, Tq] fp32, Tq = cu_q[S]
- * S < 65536, Hq < 65536, Tq x Hq and Tk x Hkv below 2^26, S x Hq below 2^22, row strides below 2^24.  Lq <= Lk for every sequence; Lq = 0 is allowed (its
- * dk, dv are 0), and so is Lk = 0 with it.
+ * S < 65536, Hq < 65536, Tq x Hq and Tk x Hkv below 2^26, S x Hq below 2^22, row strides below 2^24.  The backward
+ * pass in bf16 at head size 128 refuses packs that come to 2^23 workgroups, one for each 128 keys and each 256 queries
+ * of a head, which takes S x Hq of 2^21 and more.  Lq <= Lk for every sequence; Lq = 0 is allowed (its dk, dv are 0), and
+ * so is Lk = 0 with it.
  * The forward pass does not read keys and values that no query of the call sees: they may be anything.  A key or value that some
  * queries see and others do not has weight 0 for the latter and is finite, in the backward pass all of them are.
  * dh is 8, 16, 32, 64, 72 or 128; q head a uses kv head a / (Hq/Hkv).  bf16 with head sizes 64, 72 and 128 runs on the

@@ -2932,9 +2932,6 @@ bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, c
   first.ord = make_seq_order(a.cu_host, a.cu_host, a.S, wb.part_rows, false);
   for (int i = 0; i < first.ord.n && i < a.S; ++i)
     first.ord.w[i] = (uint32_t)first.parts(a.cu_host[i + 1] - a.cu_host[i]) << 8 | (uint32_t)i;
-  if (a.T > 0)
-    hipLaunchKernelGGL((fa_delta_kernel<DH>), dim3(cdiv((long)a.T * a.Hq * DeltaLanes<DH>::N, 256)), dim3(256), 0, st,
-                       (const bf16_t*)o, (const bf16_t*)d_o, ldo, delta, a.T, a.Hq);
   // dQ of narrow windows apart, in tiles of 128 rows and two workgroups to a CU, where there are enough of them: us, together -> apart, 8192 tokens, 32 / 8
   // heads, window 16 210 -> 175, 64 229 -> 224, 128 262 -> 263, 256 313 -> 318; 16 / 16 heads 143 -> 129, 152 -> 146, 172 -> 169, 196 -> 199; but 2048 tokens, 16 / 16
   // heads, 64 (256) 53 -> 59.
@@ -2951,6 +2948,11 @@ bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, c
                         (bf16_t*)dq, (bf16_t*)dk, (bf16_t*)dv, part, a.ld_qkv, a.kv_ld(), ldo, ldd, a.ld_dkv, a.S, a.T, Tk, a.Hkv, group,
                         wb.gsplit, kv_wgs, scale, sl2};
   const int wgs = kv_wgs + (apart ? 0 : q_wgs);
+  // Workgroups of 512 threads for both kinds of tiles: at head size 128 tens of thousands of sequences of many heads come to more.
+  BM_ARG_CHECK((long)wgs * (DH <= 64 ? 256 : 512) < (1L << 32), "window attention: the gradients' %d workgroups are past a grid of 2^32 threads", wgs);
+  if (a.T > 0)
+    hipLaunchKernelGGL((fa_delta_kernel<DH>), dim3(cdiv((long)a.T * a.Hq * DeltaLanes<DH>::N, 256)), dim3(256), 0, st,
+                       (const bf16_t*)o, (const bf16_t*)d_o, ldo, delta, a.T, a.Hq);
   if (wgs > 0) {
     if constexpr (DH <= 64) hipLaunchKernelGGL(fa_window_bwd_kernel<DH>, dim3(wgs), dim3(256), 0, st, w, ord_kv, ord_q, first);
     else {

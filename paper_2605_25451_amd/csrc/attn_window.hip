@@ -433,7 +433,7 @@ bm_status check_args(int dtype, int window, int sinks, int Hq, int Hkv, int dh, 
     rows = std::max(rows, ke[s]);
     *pairs += pairs_of(lq, lk, window, sinks);
   }
-  // grids stay below 2^32 threads
+  // grids stay below 2^32 threads, but for the gradients' at head size 128, which look at theirs before they launch anything
   BM_ARG_CHECK((long)c.cu_q_host[S] * Hq < (1L << 26) && (long)rows * Hkv < (1L << 26) && (long)S * Hq < (1L << 22),
                "window attention: %d sequences, %d queries of %d heads and %d keys of %d (rows x heads below 2^26, sequences x heads below 2^22)",
                S, c.cu_q_host[S], Hq, rows, Hkv);
