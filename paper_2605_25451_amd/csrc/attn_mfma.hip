@@ -1250,15 +1250,16 @@ __device__ inline void dkdv_tile(unsigned char* lds, int block, const bf16_t* __
 // two are resident per SIMD and one's vector work runs under the other's MFMAs.  P travels as
 // bf16 in the operand layout: role 0 feeds exactly these values to its own MFMAs, and role 1
 // owns the same (key, query) elements in the same lanes, so the exchange is lane-private.
-// (sliding windows: dS from P in fp16 times 2^15, 2^-12 off down to probabilities of 2^-29, instead of from what bf16 leaves; dK carries
-// the factor to the end.)
-using f16x8 = __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16;
+// (sliding windows: dS from P in fp16 times 2^15, 2^-12 off down to probabilities of 2^-29 and 0 below 2^-40, instead of from what bf16
+// leaves; dK carries the factor to the end.  No probability is above 1: what rounds there -- at scores of 2^22 and more the roundings of a score and of its
+// row's lse are whole powers of e -- is 1, since from 2 on fp16 would make it infinite.)
+using f16x8 = _Float16 __attribute__((ext_vector_type(8)));
 constexpr float HANDED_SCALE = 32768.f;
 __device__ inline f16x8 handed_p(const f32x16& p, int t) {
   f16x8 r;
 #pragma unroll
   for (int e = 0; e < 8; ++e) r[e] = (_Float16)(p[t * 8 + e] * HANDED_SCALE);
-  return r;
+  return __builtin_elementwise_min(r, (f16x8)(_Float16)HANDED_SCALE);
 }
 template <int DH> constexpr int dkdv_pair_lds_bytes() { return 4 * BK_Q * HeadDim<DH>::DHL * 2 + 4 * (BK_Q / 32) * 2 * 64 * 16 + 4 * BK_Q * 4; }
 template <int DH, bool CAUSAL, bool WINDOW = false>
@@ -2503,7 +2504,7 @@ __device__ inline void first_keys_part(unsigned char* lds, int block, const Wind
         const int r = g * 4 + e;
         const float x = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2, -l4[e])), p = (uint32_t)(g * 8 + e - seen.from) < seen.n ? x : 0.f;
         s[r] = p;
-        dp[r] = p * (dp[r] - d4[e]);
+        dp[r] = fminf(p, 1.0f) * (dp[r] - d4[e]);          // (no probability is above 1, see handed_p)
       }
     }
     const bf16x8 p0 = acc_to_operand(s, 0), p1 = acc_to_operand(s, 1), s0 = acc_to_operand(dp, 0), s1 = acc_to_operand(dp, 1);
