@@ -119,6 +119,16 @@ bm_status bm_window_attention_backward(int32_t dtype, int32_t window, int32_t si
                                        void* dq, int32_t ld_dq, void* dk, void* dv, int32_t ld_dkv, void* scratch,
                                        size_t scratch_bytes, void* hip_stream);
 
+/* What such calls launch (host only, nothing is launched).
+ *   forward [4]   host  0: tiles in fp32 arithmetic, 1: tiles on the matrix cores, 2: few queries, their keys in parts;
+ *                       of 2, else 0: workgroups, 1 if keys and values go past the caches, 1 if the kv heads of a part
+ *                       share an XCD
+ *   backward [4]  host  keys of a workgroup of dK/dV, rows of one of dQ, launches of both (1 or 2), workgroups for parts
+ *                       of first tokens' keys; 0 in fp32 arithmetic */
+bm_status bm_probe_window_plan(int32_t dtype, int32_t window, int32_t sinks, int32_t Hq, int32_t Hkv, int32_t dh,
+                               const int32_t* cu_q_host, const int32_t* k_begin_host, const int32_t* k_end_host, int32_t S,
+                               int32_t* forward, int32_t* backward);
+
 #ifdef __cplusplus
 }
 #endif

@@ -258,8 +258,9 @@ def lib() -> C.CDLL:
         l.bm_window_attention_forward.argtypes = [i32] * 6 + [vp, i32, vp, vp, i32] + [vp] * 6 + [i32, vp, vp, vp, sz, vp]
         l.bm_window_attention_backward.argtypes = ([i32] * 6 + [vp, i32, vp, vp, i32, vp, vp, vp] + [vp] * 6 +
                                                    [i32, vp, i32, vp, vp, i32, vp, sz, vp])
+        l.bm_probe_window_plan.argtypes = [i32] * 6 + [vp] * 3 + [i32, vp, vp]
         for name in ("bm_qk_rotary_forward", "bm_qk_rotary_backward", "bm_window_attention_forward",
-                     "bm_window_attention_backward"):
+                     "bm_window_attention_backward", "bm_probe_window_plan"):
             getattr(l, name).restype = i32
         for name in ("bm_embedding_forward", "bm_embedding_backward", "bm_cross_entropy", "bm_orthogonalize"):
             getattr(l, name).restype = C.c_int
@@ -667,6 +668,15 @@ def probe_attention_plan(mask, Hq, Hkv, dh, cu_q_host, cu_k_host=None):
 def probe_attention_backward_plan(mask, Hq, Hkv, dh, cu_q_host, cu_k_host=None):
     """(launches of dK/dV and dQ, workgroups of dK/dV, workgroups of dQ)."""
     return _probe_attention(lib().bm_probe_attention_backward_plan, mask, Hq, Hkv, dh, cu_q_host, cu_k_host)
+
+
+def probe_window_plan(dtype, window, sinks, Hq, Hkv, dh, cu_q_host, k_begin_host=None, k_end_host=None):
+    """Of attention with a sliding window: (kind, workgroups, past the caches, kv heads on one XCD) of the forward pass and
+    (keys of a workgroup, rows of a workgroup, launches, workgroups for first tokens) of the backward pass."""
+    kept, (cq, kb, ke) = _host_offsets(cu_q_host, k_begin_host, k_end_host)
+    out = [(C.c_int32 * 4)() for _ in range(2)]
+    _check(lib().bm_probe_window_plan(dtype, window, sinks, Hq, Hkv, dh, cq, kb, ke, len(kept[0]) - 1, *out))
+    return tuple(map(tuple, out))
 
 
 def probe_block_backward_plan(desc: BlockDesc, T, S):

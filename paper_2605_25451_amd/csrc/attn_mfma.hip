@@ -2910,45 +2910,64 @@ bool window_wide(const AttnArgs& a, int gsplit) {
   return a.local.window >= 256 && tw * 8L <= tn * 5L && (wgs >= NUM_CU || (wgs >= NUM_CU / 2 && tw >= 4 * a.S));
 }
 
+// What a backward pass launches
+struct WindowBwdPlan {
+  WindowBwd sizes;
+  bool apart, wide;                    // dQ in a launch of its own, 256 keys a workgroup of dK/dV
+  int query_rows, key_rows, key_tiles, part_wgs, kv_wgs, q_wgs, split_seqs;      // key_tiles: of 128; kv_wgs: the parts' among them; split_seqs: in parts
+  int wgs() const { return kv_wgs + (apart ? 0 : q_wgs); }                       // of the grid that holds dK/dV
+};
+template <int DH>
+WindowBwdPlan window_bwd_plan(const AttnArgs& a) {
+  WindowBwdPlan p;
+  p.sizes = window_bwd(a.local.window, a.local.sinks, a.Hq, a.Hkv, a.dh, a.S, a.T, a.kv_T());
+  FirstKeys first;
+  first.mask = a.local;
+  first.rows = p.sizes.part_rows;
+  long parts = 0;
+  p.split_seqs = 0;
+  for (int s = 0; s < a.S; ++s) {
+    const int n = first.parts(a.cu_host[s + 1] - a.cu_host[s]);
+    parts += n;
+    p.split_seqs += n > 0;
+  }
+  // dQ of narrow windows apart, in tiles of 128 rows and two workgroups to a CU, where there are enough of them: us, together -> apart, 8192 tokens, 32 / 8
+  // heads, window 16 210 -> 175, 64 229 -> 224, 128 262 -> 263, 256 313 -> 318; 16 / 16 heads 143 -> 129, 152 -> 146, 172 -> 169, 196 -> 199; but 2048 tokens, 16 / 16
+  // heads, 64 (256) 53 -> 59.
+  p.apart = DH == 128 && a.local.window <= 64 && count_tiles(a.cu_host, a.S, FQ) * a.Hq >= 2 * NUM_CU;
+  p.query_rows = DH == 128 && !p.apart ? AQ : FQ;
+  p.wide = DH == 128 && window_wide(a, p.sizes.gsplit);
+  p.key_rows = p.wide ? WIDE_KEYS : BK_KEYS;
+  p.key_tiles = count_tiles(a.kv_cu_host(), a.key_end_host, a.S, BK_KEYS);
+  p.part_wgs = (int)parts * a.Hkv * p.sizes.gsplit;
+  p.kv_wgs = p.part_wgs + (p.wide ? count_tiles(a.kv_cu_host(), a.key_end_host, a.S, WIDE_KEYS) : p.key_tiles) * a.Hkv * p.sizes.gsplit;
+  p.q_wgs = count_tiles(a.cu_host, a.S, p.query_rows) * cdiv(a.Hq, DH == 72 ? 2 : 1);
+  return p;
+}
+
 template <int DH>
 bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, const float* lse, void* dq, void* dk, void* dv,
                             int ldd, float* delta, hipStream_t st) {
   const int ldo = a.Hq * a.dh, Tk = a.kv_T(), group = a.Hq / a.Hkv;
   const float scale = 1.0f / sqrtf((float)a.dh), sl2 = scale * LOG2E;
-  const WindowBwd wb = window_bwd(a.local.window, a.local.sinks, a.Hq, a.Hkv, a.dh, a.S, a.T, Tk);
+  const WindowBwdPlan p = window_bwd_plan<DH>(a);
+  const WindowBwd& wb = p.sizes;
   float* part = delta + wb.delta;
   FirstKeys first;
   first.mask = a.local;
   first.keys = wb.keys;
   first.rows = wb.part_rows;
+  first.wgs = p.part_wgs;
   first.out = part + wb.split;
-  long parts = 0;
-  int in_parts = 0;
-  for (int s = 0; s < a.S; ++s) {
-    const int n = first.parts(a.cu_host[s + 1] - a.cu_host[s]);
-    parts += n;
-    in_parts += n > 0;
-  }
-  first.wgs = (int)parts * a.Hkv * wb.gsplit;
   first.ord = make_seq_order(a.cu_host, a.cu_host, a.S, wb.part_rows, false);
   for (int i = 0; i < first.ord.n && i < a.S; ++i)
     first.ord.w[i] = (uint32_t)first.parts(a.cu_host[i + 1] - a.cu_host[i]) << 8 | (uint32_t)i;
-  // dQ of narrow windows apart, in tiles of 128 rows and two workgroups to a CU, where there are enough of them: us, together -> apart, 8192 tokens, 32 / 8
-  // heads, window 16 210 -> 175, 64 229 -> 224, 128 262 -> 263, 256 313 -> 318; 16 / 16 heads 143 -> 129, 152 -> 146, 172 -> 169, 196 -> 199; but 2048 tokens, 16 / 16
-  // heads, 64 (256) 53 -> 59.
-  const bool apart = DH == 128 && a.local.window <= 64 && count_tiles(a.cu_host, a.S, FQ) * a.Hq >= 2 * NUM_CU;
-  const int query_rows = DH == 128 && !apart ? AQ : FQ, heads_per_wg = DH == 72 ? 2 : 1;
-  bool wide = false;
-  if constexpr (DH == 128) wide = window_wide(a, wb.gsplit);
-  const int key_rows = wide ? WIDE_KEYS : BK_KEYS;
-  const int ktiles = count_tiles(a.kv_cu_host(), a.key_end_host, a.S, BK_KEYS), qtiles = count_tiles(a.cu_host, a.S, query_rows);
-  const int kv_wgs = first.wgs + (wide ? count_tiles(a.kv_cu_host(), a.key_end_host, a.S, WIDE_KEYS) : ktiles) * a.Hkv * wb.gsplit, q_wgs = qtiles * cdiv(a.Hq, heads_per_wg);
-  const SeqOrder ord_kv = make_seq_order(a.kv_cu_host(), a.cu_host, a.S, key_rows, false, a.key_end_host);
-  const SeqOrder ord_q = make_seq_order(a.cu_host, a.cu_host, a.S, query_rows, false);
+  const SeqOrder ord_kv = make_seq_order(a.kv_cu_host(), a.cu_host, a.S, p.key_rows, false, a.key_end_host);
+  const SeqOrder ord_q = make_seq_order(a.cu_host, a.cu_host, a.S, p.query_rows, false);
   const WindowBwdArgs w{(const bf16_t*)a.q, (const bf16_t*)a.k, (const bf16_t*)a.v, (const bf16_t*)d_o, lse, delta, a.cu_dev, a.kv_cu_dev(),
                         (bf16_t*)dq, (bf16_t*)dk, (bf16_t*)dv, part, a.ld_qkv, a.kv_ld(), ldo, ldd, a.ld_dkv, a.S, a.T, Tk, a.Hkv, group,
-                        wb.gsplit, kv_wgs, scale, sl2};
-  const int wgs = kv_wgs + (apart ? 0 : q_wgs);
+                        wb.gsplit, p.kv_wgs, scale, sl2};
+  const int wgs = p.wgs();
   // Workgroups of 512 threads for both kinds of tiles: at head size 128 tens of thousands of sequences of many heads come to more.
   BM_ARG_CHECK((long)wgs * (DH <= 64 ? 256 : 512) < (1L << 32), "window attention: the gradients' %d workgroups are past a grid of 2^32 threads", wgs);
   if (a.T > 0)
@@ -2958,16 +2977,16 @@ bm_status window_bwd_launch(const AttnArgs& a, const void* o, const void* d_o, c
     if constexpr (DH <= 64) hipLaunchKernelGGL(fa_window_bwd_kernel<DH>, dim3(wgs), dim3(256), 0, st, w, ord_kv, ord_q, first);
     else {
       auto kern = fa_window_bwd512_kernel<DH, false>;
-      if constexpr (DH == 128) if (wide) kern = fa_window_bwd512_kernel<DH, true>;
+      if constexpr (DH == 128) if (p.wide) kern = fa_window_bwd512_kernel<DH, true>;
       hipLaunchKernelGGL(kern, dim3(wgs), dim3(512), 0, st, w, ord_kv, ord_q, first);
     }
   }
   if constexpr (DH == 128)
-    if (apart && q_wgs > 0) hipLaunchKernelGGL((fa_window_dq_kernel<DH>), dim3(q_wgs), dim3(256), 0, st, w, ord_q, a.local);
+    if (p.apart && p.q_wgs > 0) hipLaunchKernelGGL((fa_window_dq_kernel<DH>), dim3(p.q_wgs), dim3(256), 0, st, w, ord_q, a.local);
   const int all_tiles = wb.gsplit > 1;
-  if (kv_wgs > 0 && (all_tiles || parts > 0)) {
-    const SeqOrder ord = wide ? make_seq_order(a.kv_cu_host(), a.cu_host, a.S, BK_KEYS, false, a.key_end_host) : ord_kv;
-    hipLaunchKernelGGL(fa_window_reduce_kernel, dim3(all_tiles ? ktiles : in_parts, a.Hkv, BK_KEYS / REDUCE_ROWS), dim3(256), 0, st, part,
+  if (p.kv_wgs > 0 && (all_tiles || p.part_wgs > 0)) {
+    const SeqOrder ord = p.wide ? make_seq_order(a.kv_cu_host(), a.cu_host, a.S, BK_KEYS, false, a.key_end_host) : ord_kv;
+    hipLaunchKernelGGL(fa_window_reduce_kernel, dim3(all_tiles ? p.key_tiles : p.split_seqs, a.Hkv, BK_KEYS / REDUCE_ROWS), dim3(256), 0, st, part,
                        wb.gsplit, a.cu_dev, a.kv_cu_dev(), a.S, Tk, a.Hkv, a.dh, (bf16_t*)dk, (bf16_t*)dv, a.ld_dkv, all_tiles,
                        ord, first);
   }
@@ -2999,6 +3018,15 @@ bm_status window_backward_mfma(const AttnArgs& a, const void* o, const void* d_o
   if (a.dh == 128) return window_bwd_launch<128>(a, o, d_o, lse, dq, dk, dv, ld_dq, (float*)scratch, st);
   if (a.dh == 72) return window_bwd_launch<72>(a, o, d_o, lse, dq, dk, dv, ld_dq, (float*)scratch, st);
   return window_bwd_launch<64>(a, o, d_o, lse, dq, dk, dv, ld_dq, (float*)scratch, st);
+}
+
+// keys of a workgroup of dK/dV, rows of one of dQ, launches of both, parts of first keys (times their heads)
+void window_backward_mfma_plan(const AttnArgs& a, int32_t* out) {
+  const WindowBwdPlan p = a.dh == 128 ? window_bwd_plan<128>(a) : a.dh == 72 ? window_bwd_plan<72>(a) : window_bwd_plan<64>(a);
+  out[0] = p.key_rows;
+  out[1] = p.query_rows;
+  out[2] = p.apart ? 2 : 1;
+  out[3] = p.part_wgs;
 }
 
 bool attention_mfma_supported(const AttnArgs& a) {

@@ -15,6 +15,7 @@ bm_status window_backward_plain(const AttnArgs& a, const void* o, const void* d_
 bm_status window_tokens_mfma(const AttnArgs& a, const TokenSplit& split, void* o, float* lse, hipStream_t st);
 bm_status window_backward_mfma(const AttnArgs& a, const void* o, const void* d_o, const float* lse, void* dq, void* dk,
                                void* dv, int ld_dq, void* scratch, hipStream_t st);
+void window_backward_mfma_plan(const AttnArgs& a, int32_t* out);
 
 namespace {
 
@@ -306,7 +307,10 @@ int token_rows(int Hq, int Hkv, int Tq) {
 }
 size_t token_map_ints(int S) { return S > TOKEN_TABLE ? 4 * (size_t)S + 1 + TOKEN_WGS : 0; }
 
-bm_status window_tokens(const AttnArgs& a, void* scratch, void* o, float* lse, hipStream_t st) {
+bool few_queries(const AttnArgs& a) { return a.max_seqlen * (long)(a.Hq / a.Hkv) <= TOKEN_ROWS; }
+
+struct TokenPlan { TokenSplit split; long places; int joins; };    // joins: sequences of more than one part
+TokenPlan token_plan(const AttnArgs& a) {
   TokenSplit t{};
   const int32_t *cq = a.cu_host, *kb = a.cu_k_host, *ke = a.key_end_host;
   long tiles = 0, whole = 0;
@@ -319,7 +323,7 @@ bm_status window_tokens(const AttnArgs& a, void* scratch, void* o, float* lse, h
   t.per = std::max(whole * a.Hkv >= NUM_CU ? 2 * TOKEN_TILES : TOKEN_TILES, cdiv(tiles * a.Hkv, TOKEN_WGS));
   t.rows = a.max_seqlen * (a.Hq / a.Hkv);
   long parts = 0, places = 0;
-  int joins = 0;                     // sequences of more than one part
+  int joins = 0;
   t.n = a.S <= TOKEN_TABLE ? a.S : 0;
   for (int s = 0; s < a.S; ++s) {
     const int n = t.count(a.local, cq[s + 1] - cq[s], ke[s] - kb[s]);
@@ -336,9 +340,15 @@ bm_status window_tokens(const AttnArgs& a, void* scratch, void* o, float* lse, h
   // The kv heads of a part on one XCD, where a row of a head is no whole cache lines or the chip is full many times: us, 20 sequences of 2000, 16
   // heads of 72, 44.5 -> 35.9; 1000 of 1024, 8 kv heads of 128, 541 -> 517, 256 174 -> 172.5; but one of 8192 13.8 -> 14.5, 16 101 -> 104.
   t.same_xcd = a.dh * elt_size(a.dtype) % 128 != 0 || t.wgs >= 8 * NUM_CU;
+  return TokenPlan{t, places, joins};
+}
+
+bm_status window_tokens(const AttnArgs& a, void* scratch, void* o, float* lse, hipStream_t st) {
+  const TokenPlan plan = token_plan(a);
+  TokenSplit t = plan.split;
   t.sums = (float*)scratch;
-  t.stats = t.sums + (size_t)places * a.Hkv * t.rows * a.dh;
-  t.map = (int32_t*)(t.stats + (size_t)places * a.Hkv * t.rows * 2);
+  t.stats = t.sums + (size_t)plan.places * a.Hkv * t.rows * a.dh;
+  t.map = (int32_t*)(t.stats + (size_t)plan.places * a.Hkv * t.rows * 2);
   if (!t.n) {
     hipLaunchKernelGGL(window_map_kernel, dim3(cdiv(a.S, 256)), dim3(256), 0, st, a.cu_dev, a.kv_cu_dev(), a.S, a.local, t);
     BM_CHECK_LAUNCH("window_map");
@@ -366,8 +376,8 @@ bm_status window_tokens(const AttnArgs& a, void* scratch, void* o, float* lse, h
 #undef BM_HEAD
     BM_CHECK_LAUNCH("window_token");
   }
-  if (joins > 0) {
-    const dim3 grid(joins, a.Hkv, t.rows), block(256);
+  if (plan.joins > 0) {
+    const dim3 grid(plan.joins, a.Hkv, t.rows), block(256);
 #define BM_L(TT)                                                                                                           \
   hipLaunchKernelGGL(window_join_kernel<TT>, grid, block, 0, st, a.cu_dev, a.S, (TT*)o, a.Hq * a.dh, lse, a.T, a.Hkv, a.Hq / a.Hkv, \
                      a.dh, t)
@@ -496,7 +506,7 @@ extern "C" bm_status bm_window_attention_forward(int32_t dtype, int32_t window, 
   a.q = q; a.k = k; a.v = v;
   hipStream_t st = (hipStream_t)hip_stream;
   ProfScope prof(PROF_ATTN_FWD, 4.0 * dh * Hq * pairs, st);
-  if (a.max_seqlen * (long)(Hq / Hkv) <= TOKEN_ROWS) return window_tokens(a, scratch, o, lse, st);
+  if (few_queries(a)) return window_tokens(a, scratch, o, lse, st);
   if (mfma_head(dtype, dh)) return window_forward_mfma(a, o, lse, st);
   return window_forward_plain(a, o, lse, st);
 }
@@ -548,4 +558,25 @@ extern "C" bm_status bm_window_attention_backward(int32_t dtype, int32_t window,
   ProfScope prof(PROF_ATTN_BWD, 10.0 * dh * Hq * pairs, st);
   if (mfma_head(dtype, dh)) return window_backward_mfma(a, o, d_o, lse, dq, dk, dv, ld_dq, scratch, st);
   return window_backward_plain(a, o, d_o, lse, dq, dk, dv, ld_dq, (float*)scratch, st);
+}
+
+extern "C" bm_status bm_probe_window_plan(int32_t dtype, int32_t window, int32_t sinks, int32_t Hq, int32_t Hkv, int32_t dh,
+                                          const int32_t* cu_q_host, const int32_t* k_begin_host, const int32_t* k_end_host, int32_t S,
+                                          int32_t* forward, int32_t* backward) {
+  BM_ARG_CHECK(forward && backward, "window plan: NULL pointer");
+  AttnArgs a{};
+  double pairs = 0;
+  // (the device's copies are not looked at)
+  const Sequences c{cu_q_host, cu_q_host, k_begin_host, k_end_host, k_begin_host, k_end_host};
+  BM_RETURN_IF(check_args(dtype, window, sinks, Hq, Hkv, dh, Hq * dh, Hkv * dh, c, S, &a, &pairs));
+  for (int i = 0; i < 4; ++i) forward[i] = backward[i] = 0;
+  forward[0] = few_queries(a) ? 2 : mfma_head(dtype, dh) ? 1 : 0;
+  if (forward[0] == 2) {
+    const TokenSplit t = token_plan(a).split;
+    forward[1] = t.wgs;
+    forward[2] = t.stream;
+    forward[3] = t.same_xcd;
+  }
+  if (mfma_head(dtype, dh)) window_backward_mfma_plan(a, backward);
+  return BM_OK;
 }
