@@ -4,6 +4,7 @@
 #include "../../include/bigmac_window_attention.h"
 
 #include <algorithm>
+#include <vector>
 
 namespace bm {
 
@@ -309,6 +310,29 @@ size_t token_map_ints(int S) { return S > TOKEN_TABLE ? 4 * (size_t)S + 1 + TOKE
 
 bool few_queries(const AttnArgs& a) { return a.max_seqlen * (long)(a.Hq / a.Hkv) <= TOKEN_ROWS; }
 
+// Has every one of the Tk key rows one sequence at most?  Lists that are not in order are sorted, us: 256 sequences 3, 1000 16, 4000 220, which their kernels (151,
+// 467, 522) cover; longer ones count as shared.
+constexpr int SORTED_SEQS = 4096;
+bool owned_rows(const int32_t* begin, const int32_t* end, int S, int Tk) {
+  long rows = 0;
+  bool in_order = true;
+  for (int s = 0, last = 0; s < S; ++s) {
+    if (end[s] == begin[s]) continue;
+    rows += end[s] - begin[s];
+    in_order = in_order && begin[s] >= last;
+    last = end[s];
+  }
+  if (in_order || rows > Tk || S > SORTED_SEQS) return in_order;
+  std::vector<uint64_t> spans;
+  spans.reserve(S);
+  for (int s = 0; s < S; ++s)
+    if (end[s] > begin[s]) spans.push_back((uint64_t)begin[s] << 32 | (uint32_t)end[s]);
+  std::sort(spans.begin(), spans.end());
+  for (size_t i = 1; i < spans.size(); ++i)
+    if ((spans[i] >> 32) < (uint32_t)spans[i - 1]) return false;
+  return true;
+}
+
 struct TokenPlan { TokenSplit split; long places; int joins; };    // joins: sequences of more than one part
 TokenPlan token_plan(const AttnArgs& a) {
   TokenSplit t{};
@@ -335,8 +359,10 @@ TokenPlan token_plan(const AttnArgs& a) {
   t.wgs = (int)(parts * a.Hkv);
   // Keys and values past the caches, where they are more than the L2s hold and read by one workgroup each.  us, through them -> past: 64 sequences of up to 4096
   // (883 MB) 171 -> 153, 256 of 1024 172 -> 151, 1000 of 1024 518 -> 467, 4 of 4096 (67 MB) 22.2 -> 21.4; but 55 of 300 (39 MB) 12.6 -> 13.1, 59 of 300, 16 heads
-  // of 64 (43 MB) 14.9 -> 15.2; fp32, 16 of 2000 46 -> 42.
-  t.stream = (mfma_head(a.dtype, a.dh) || t.rows <= RB) && (double)tiles * TOKEN_KEYS * a.Hkv * a.dh * 2 * elt_size(a.dtype) > 60e6;
+  // of 64 (43 MB) 14.9 -> 15.2; fp32, 16 of 2000 46 -> 42.  Sequences that share rows find them in the caches: 256 that share 2048 keys 106 -> 222, 16
+  // prompts of 4096 with 4 answers each 69 -> 107, 8 that share 32768 67 -> 121.
+  t.stream = (mfma_head(a.dtype, a.dh) || t.rows <= RB) && (double)tiles * TOKEN_KEYS * a.Hkv * a.dh * 2 * elt_size(a.dtype) > 60e6 &&
+             owned_rows(kb, ke, a.S, a.Tk);
   // The kv heads of a part on one XCD, where a row of a head is no whole cache lines or the chip is full many times: us, 20 sequences of 2000, 16
   // heads of 72, 44.5 -> 35.9; 1000 of 1024, 8 kv heads of 128, 541 -> 517, 256 174 -> 172.5; but one of 8192 13.8 -> 14.5, 16 101 -> 104.
   t.same_xcd = a.dh * elt_size(a.dtype) % 128 != 0 || t.wgs >= 8 * NUM_CU;

@@ -34,6 +34,28 @@ def test_parts_of_few_queries():
     assert plan([4096] * 8, window=1 << 20, dtype=1, dh=64, queries=[2] * 8)[0][2] == 0      # 8 rows: read by two workgroups
 
 
+def streamed(spans, **kw):
+    """Single queries behind keys begin .. end; none where there are no keys."""
+    args = dict(dtype=0, window=1 << 20, sinks=0, Hq=32, Hkv=8, dh=128, **kw)
+    begin, end = np.array(spans, np.int32).T
+    return bm.probe_window_plan(*args.values(), np.concatenate([[0], np.cumsum(end > begin)]), begin, end)[0][2]
+
+
+def test_keys_of_several_sequences_stay_in_the_caches():
+    slots = [(i * 5000, i * 5000 + 4096) for i in range(64)]
+    rng = np.random.default_rng(1)
+    assert streamed(slots) == streamed(slots[::-1]) == streamed([slots[i] for i in rng.permutation(64)]) == 1
+    assert streamed([(7, 7)] + slots + [(0, 0)]) == 1                                # sequences of no keys own nothing
+    assert streamed([(0, 4096)] * 64) == 0
+    answers = [slots[i // 4] for i in range(64)]                                     # four answers to a question each
+    assert streamed(answers) == streamed([answers[i] for i in rng.permutation(64)]) == 0
+    assert streamed(slots[:-1] + [(10 * 5000 + 100, 10 * 5000 + 4000)]) == streamed(slots[1:] + [(0, 5001)]) == 0
+    many = [(i * 300, i * 300 + 256) for i in range(4000)]
+    many = [many[i] for i in rng.permutation(4000)]
+    assert streamed(many) == 1 and streamed(many[:-1] + many[:1]) == 0
+    assert streamed(many[:-1] + [(many[0][0] + 255, many[0][0] + 300)]) == 0
+
+
 @pytest.mark.parametrize("args,want", [
     (dict(lens=[8192], window=2048, sinks=64), (256, 256, 1, 8 * 4)),                # first keys in parts of 2048 rows
     (dict(lens=[8192], window=64), (128, 128, 2, 0)), (dict(lens=[8192], window=65), (128, 256, 1, 0)),
