@@ -37,7 +37,8 @@ extern "C" {
  * The first pairs[0] pairs belong to axis 0, the next pairs[1] to axis 1, and so on; together they are
  * head_dim / 2 (an axis may have none; an axis whose positions are all 0 leaves its pairs as they are).
  * With one axis of head_dim / 2 pairs and positions that count up in every sequence this is the rotation
- * that a block with rope = 1 makes.  Angles are formed and reduced in fp64, so far positions lose nothing. */
+ * that a block with rope = 1 makes.  Angles are formed and reduced in fp64, off by at most 2^-50 of the position
+ * for bases of 1 and more: 2^-24 at position 2^26.  Squares are summed in fp32. */
 #define BM_ROTARY_MAX_AXES 4
 typedef struct {
   int32_t dtype, n_q_heads, n_kv_heads, head_dim;  /* head_dim: a multiple of 8 up to 256; one of the head counts may be 0 */
@@ -79,23 +80,28 @@ bm_status bm_qk_rotary_backward(const bm_qk_rotary_desc* desc, int32_t T, const 
  *   sinks            0..BM_WINDOW_MAX_SINKS
  *   q         dev    rows of ld_q elements, Hq heads of dh, sequences one behind the other by cu_q [S+1]
  *   k, v      dev    rows of ld_kv elements, Hkv heads; sequence s holds rows k_begin[s] .. k_end[s]-1.  The four
- *                    arrays are NULL where keys have the queries' packing.  Rows may lie between the sequences (slots of a
- *                    cache), which are neither read nor written.  The forward pass takes sequences in any order, and ones that
- *                    share rows (a common beginning); the backward pass takes them one behind the other
+ *                    arrays are NULL where keys have the queries' packing.  Rows may lie between the sequences
+ *                    (slots of a cache), which are neither read nor written.  The forward pass takes sequences in
+ *                    any order, and ones that share rows (a common beginning); the backward pass takes them one
+ *                    behind the other
  *   cu_q, k_begin, k_end are given twice, in device and in host memory, with the same values
  *   o, d_o    dev    [Tq, Hq*dh], lse dev [Hq, Tq] fp32, Tq = cu_q[S]
- * S < 65536, Hq < 65536, Tq x Hq and Tk x Hkv below 2^26, S x Hq below 2^22, row strides below 2^24.  The backward
- * pass in bf16 at head size 128 refuses packs that come to 2^23 workgroups, one for each 128 keys and each 256 queries
- * of a head, which takes S x Hq of 2^21 and more.  Lq <= Lk for every sequence; Lq = 0 is allowed (its dk, dv are 0), and
- * so is Lk = 0 with it.
- * The forward pass does not read keys and values that no query of the call sees: they may be anything.  A key or value that some
- * queries see and others do not has weight 0 for the latter and is finite, in the backward pass all of them are.
- * dh is 8, 16, 32, 64, 72 or 128; q head a uses kv head a / (Hq/Hkv).  bf16 with head sizes 64, 72 and 128 runs on the
- * matrix cores, in which probabilities are rounded to bf16; everything else is fp32 arithmetic.
- * Few queries behind long key lists are split over the keys; the parts are joined in a fixed order. */
+ * Limits: S < 65536, Hq < 65536, Tq x Hq and Tk x Hkv below 2^26, S x Hq below 2^22, row strides below 2^24.
+ * The backward pass in bf16 at head size 128 refuses packs that come to 2^23 workgroups, one for each 128 keys and
+ * each 256 queries of a head, which takes S x Hq of 2^21 and more.
+ * Lq <= Lk for every sequence; Lq = 0 is allowed (its dk, dv are 0), and so is Lk = 0 with it.
+ * The forward pass does not read keys and values that no query of the call sees: they may be anything.  A key or
+ * value that some queries see and others do not has weight 0 for the latter and is finite, in the backward pass all
+ * of them are.
+ * dh is 8, 16, 32, 64, 72 or 128; q head a uses kv head a / (Hq/Hkv).  bf16 with head sizes 64, 72 and 128 runs on
+ * the matrix cores: probabilities, and dS in the backward pass, are rounded to bf16 before the products that they
+ * enter.  Everything else is fp32 arithmetic.
+ * Where every sequence of a call has Lq x (Hq/Hkv) <= 32, the keys are split over the chip and the parts joined in a
+ * fixed order.  One sequence with more sends all of the call through tiles of 128 queries (16 in fp32 arithmetic), in
+ * which a workgroup walks all the keys that its queries see: chunks of queries and single ones take separate calls. */
 #define BM_WINDOW_MAX_SINKS 128
-/* Tq = cu_q[S], Tk = the largest k_end.  0 for sizes that are refused.  A size that is enough for S sequences and Tq queries
- * is enough for fewer of either, whatever their lengths. */
+/* Tq = cu_q[S], Tk = the largest k_end.  0 for sizes that are refused.  A size that is enough for S sequences and Tq
+ * queries is enough for fewer of either, whatever their lengths. */
 size_t    bm_window_attention_scratch_bytes(int32_t dtype, int32_t window, int32_t sinks, int32_t Hq, int32_t Hkv,
                                             int32_t dh, int32_t S, int32_t Tq, int32_t Tk);
 bm_status bm_window_attention_forward(int32_t dtype, int32_t window, int32_t sinks, int32_t Hq, int32_t Hkv, int32_t dh,
@@ -105,9 +111,10 @@ bm_status bm_window_attention_forward(int32_t dtype, int32_t window, int32_t sin
                                       const int32_t* k_begin_host, const int32_t* k_end_host, int32_t S,
                                       void* o, float* lse, void* scratch, size_t scratch_bytes, void* hip_stream);
 
-/* The scratch is that of exactly these sizes.  Gradients from d_o and the forward's q, k, v, o and lse: dq in rows of ld_dq elements, dk and dv (rows k_begin ..
- * k_end-1 of every sequence) in rows of ld_dkv; overwritten.  Gradients that lie over an input are refused; columns of the same
- * rows beside it are not. */
+/* The scratch is that of exactly these sizes.  Gradients from d_o and the forward's q, k, v, o and lse, which belong
+ * together: an lse below that of these q and k makes probabilities above 1, which are held to 1 in some sums and not
+ * in others.  dq in rows of ld_dq elements, dk and dv (rows k_begin .. k_end-1 of every sequence) in rows of ld_dkv;
+ * overwritten.  Gradients that lie over an input are refused; columns of the same rows beside it are not. */
 size_t    bm_window_attention_backward_scratch_bytes(int32_t dtype, int32_t window, int32_t sinks, int32_t Hq,
                                                      int32_t Hkv, int32_t dh, int32_t S, int32_t Tq, int32_t Tk);
 bm_status bm_window_attention_backward(int32_t dtype, int32_t window, int32_t sinks, int32_t Hq, int32_t Hkv, int32_t dh,

@@ -1583,8 +1583,12 @@ __device__ inline void dkdv_wide_tile(
   // and all of them if it lies past the sequence.
   const bool keys_cut = key0 + 64 > L;
   // (WINDOW: and those behind the window of its last key, if its keys are no first tokens)
-  const int skip = key0 >= L || (WINDOW && key0 + 64 <= where.from) ? nqt : CAUSAL ? min(nqt, (WINDOW ? max(0, key0 - off - qstart) : key0 - qstart) / W::ROWS) : 0;
-  const int stop = WINDOW && key0 >= first.mask.sinks ? max(skip, min(nqt, (key0 + 63 - off + first.mask.window - qstart + W::ROWS - 1) / W::ROWS)) : nqt;
+  const int skip = key0 >= L || (WINDOW && key0 + 64 <= where.from) ? nqt
+                   : CAUSAL ? min(nqt, (WINDOW ? max(0, key0 - off - qstart) : key0 - qstart) / W::ROWS)
+                            : 0;
+  const int stop = WINDOW && key0 >= first.mask.sinks
+                       ? max(skip, min(nqt, (key0 + 63 - off + first.mask.window - qstart + W::ROWS - 1) / W::ROWS))
+                       : nqt;
   const uint32_t lds0 = (uint32_t)(size_t)(__attribute__((address_space(3))) unsigned char*)tiles;
   constexpr int LOADS = 3;
 
@@ -2858,8 +2862,9 @@ __global__ __launch_bounds__(256, 2) void fa_window_token_kernel(
 
 template <int DH>
 bm_status window_token_launch(const AttnArgs& a, const TokenSplit& split, void* o, float* lse, hipStream_t st) {
-  hipLaunchKernelGGL((split.stream ? fa_window_token_kernel<DH, true> : fa_window_token_kernel<DH, false>), dim3(token_grid(split, a.Hkv)), dim3(256), 0, st, (const bf16_t*)a.q, (const bf16_t*)a.k,
-                     (const bf16_t*)a.v, a.ld_qkv, a.kv_ld(), a.cu_dev, a.kv_cu_dev(), a.S, (bf16_t*)o, a.Hq * a.dh, lse, a.T, a.Hkv,
+  auto kern = split.stream ? fa_window_token_kernel<DH, true> : fa_window_token_kernel<DH, false>;
+  hipLaunchKernelGGL(kern, dim3(token_grid(split, a.Hkv)), dim3(256), 0, st, (const bf16_t*)a.q, (const bf16_t*)a.k, (const bf16_t*)a.v, a.ld_qkv,
+                     a.kv_ld(), a.cu_dev, a.kv_cu_dev(), a.S, (bf16_t*)o, a.Hq * a.dh, lse, a.T, a.Hkv,
                      a.Hq / a.Hkv, LOG2E / sqrtf((float)a.dh), a.local, split);
   BM_CHECK_LAUNCH("fa_window_token");
   return BM_OK;
@@ -2875,16 +2880,16 @@ WindowBwd window_bwd(int window, int sinks, int Hq, int Hkv, int dh, int S, int 
   WindowBwd w;
   const int tiles = cdiv(Tk, BK_KEYS) > S ? cdiv(Tk, BK_KEYS) : S;
   // as without a window, but for 512 workgroups: dQ follows in the same grid, and the tiles of a window are short for the fp32 partials.
-  // us, for 1024 -> 512 -> 256: 32 / 8 heads of 128, 8192 tokens, window 2048 1104 -> 1041 -> 1041, 256 650 -> 489 -> 489, 4096 448 -> 379 -> 347;
-  // 32 / 8 of 64, 4096 207 -> 190 -> 239, 2048 94 -> 94 -> 129; 8 / 1 of 128, 32768, window 4096, 1705 -> 1733 -> 2463.
+  // us, for 1024 -> 512 -> 256, 4 first tokens: 32 / 8 heads of 128, 8192 tokens, window 2048 940 -> 882 -> 881, 256 378 -> 304 -> 303; 4096, 1024, 348 -> 306
+  // -> 298; 32 / 8 of 64, 4096, 1024, 184 -> 174 -> 156, 2048 90 all three; 8 / 1 of 128, 32768, window 4096, 1827 -> 1771 -> 1937.
   w.gsplit = dkdv_group_split(2 * tiles, Hkv, Hq / Hkv);
   // Up to 32 first tokens: the 128-key tile would compute four times what they need.  us, parts of 128 keys -> of 32, 32 / 8 heads of 128, 4 first tokens:
-  // 8192 tokens, window 1024 677 -> 615, 256 436 -> 400, 64 340 -> 306; 2048, 128 149 -> 125; 16 / 16 heads of 64, 8192, 256 124 -> 113.
+  // 8192 tokens, window 2048 903 -> 882, 1024 587 -> 557, 256 340 -> 304, 64 234 -> 222; 2048, 128 115 -> 104; 16 / 16 heads of 64, 8192, 256 101 -> 92.
   w.keys = sinks <= 32 ? 32 : BK_KEYS;
   // Rows of a part: short where the longest workgroup decides, long where partials cost more.  us, 256 -> 512 -> 1024 rows for 32 keys: 439 tokens, window 16,
-  // 32 / 8 heads of 128 41 -> 50 -> 50, 16 / 16 of 64 25 -> 31 -> 31; 4096, 256, 16 / 16 of 128 132 -> 126 -> 131; 8192, 1024 374 -> 363 -> 339, 24 documents
-  // 239 -> 218 -> 205.  Of 128 keys, as long as the tiles of other keys; 192 -> 512: 780 tokens, window 1, 16 / 16 heads of 64 29 -> 42; 8192, 256, 5 / 1 of 128
-  // 176 -> 142.
+  // 32 / 8 heads of 128 37.5 -> 42 -> 42, 16 / 16 of 64 23.5 all three; 4096, 256, 16 / 16 of 128 109 -> 103 -> 107; 32 / 8 of 128, 8192, 1024 595 -> 552 -> 557, 256
+  // 317 -> 310 -> 304, 24 documents, 1024, 286 -> 272 -> 262.  Of 128 keys, as long as the tiles of other keys; 192 -> 512: 780 tokens, window 1, 16 / 16 heads of
+  // 64 24 -> 28; 8192, 256, 5 / 1 of 128 150 -> 118.
   const bool few = (long)Tq * Hq <= 20480;
   if (w.keys == 32) {
     w.part_rows = few ? 256 : Tq < 6144 ? 512 : 1024;
@@ -2932,8 +2937,8 @@ WindowBwdPlan window_bwd_plan(const AttnArgs& a) {
     p.split_seqs += n > 0;
   }
   // dQ of narrow windows apart, in tiles of 128 rows and two workgroups to a CU, where there are enough of them: us, together -> apart, 8192 tokens, 32 / 8
-  // heads, window 16 210 -> 175, 64 229 -> 224, 128 262 -> 263, 256 313 -> 318; 16 / 16 heads 143 -> 129, 152 -> 146, 172 -> 169, 196 -> 199; but 2048 tokens, 16 / 16
-  // heads, 64 (256) 53 -> 59.
+  // heads, 4 first tokens: window 16 230 -> 217, 64 226 -> 222, 128 259 -> 261, 256 303 -> 313; 16 / 16 heads 149 -> 139, 148 -> 142, 168 -> 164, 184 -> 186; but 2048
+  // tokens, 16 / 16 heads, 64 (256 of them) 52 -> 57.  Without first tokens 208 -> 177, 203 -> 180, 229 -> 207, 277 -> 257.
   p.apart = DH == 128 && a.local.window <= 64 && count_tiles(a.cu_host, a.S, FQ) * a.Hq >= 2 * NUM_CU;
   p.query_rows = DH == 128 && !p.apart ? AQ : FQ;
   p.wide = DH == 128 && window_wide(a, p.sizes.gsplit);

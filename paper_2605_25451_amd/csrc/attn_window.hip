@@ -287,8 +287,9 @@ __global__ __launch_bounds__(256) void window_join_kernel(const int32_t* __restr
 
 template <typename T, int DH>
 void token_launch(const AttnArgs& a, const TokenSplit& split, void* o, float* lse, hipStream_t st) {
-  hipLaunchKernelGGL((split.stream ? window_token_kernel<T, DH, true> : window_token_kernel<T, DH, false>), dim3(token_grid(split, a.Hkv), cdiv(split.rows, RB)), dim3(256), 0, st, (const T*)a.q,
-                     (const T*)a.k, (const T*)a.v, a.ld_qkv, a.kv_ld(), a.cu_dev, a.kv_cu_dev(), a.S, (T*)o, a.Hq * a.dh, lse, a.T,
+  auto kern = split.stream ? window_token_kernel<T, DH, true> : window_token_kernel<T, DH, false>;
+  hipLaunchKernelGGL(kern, dim3(token_grid(split, a.Hkv), cdiv(split.rows, RB)), dim3(256), 0, st, (const T*)a.q, (const T*)a.k,
+                     (const T*)a.v, a.ld_qkv, a.kv_ld(), a.cu_dev, a.kv_cu_dev(), a.S, (T*)o, a.Hq * a.dh, lse, a.T,
                      a.Hkv, a.Hq / a.Hkv, LOG2E / sqrtf((float)a.dh), a.local, split);
 }
 
