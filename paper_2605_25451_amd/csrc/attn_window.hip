@@ -4,7 +4,6 @@
 #include "../../include/bigmac_window_attention.h"
 
 #include <algorithm>
-#include <vector>
 
 namespace bm {
 
@@ -324,12 +323,12 @@ bool owned_rows(const int32_t* begin, const int32_t* end, int S, int Tk) {
     last = end[s];
   }
   if (in_order || rows > Tk || S > SORTED_SEQS) return in_order;
-  std::vector<uint64_t> spans;
-  spans.reserve(S);
+  uint64_t spans[SORTED_SEQS];
+  int n = 0;
   for (int s = 0; s < S; ++s)
-    if (end[s] > begin[s]) spans.push_back((uint64_t)begin[s] << 32 | (uint32_t)end[s]);
-  std::sort(spans.begin(), spans.end());
-  for (size_t i = 1; i < spans.size(); ++i)
+    if (end[s] > begin[s]) spans[n++] = (uint64_t)begin[s] << 32 | (uint32_t)end[s];
+  std::sort(spans, spans + n);
+  for (int i = 1; i < n; ++i)
     if ((spans[i] >> 32) < (uint32_t)spans[i - 1]) return false;
   return true;
 }
